@@ -346,6 +346,176 @@ int tlf_attn_decode(const tlf_attn_args* a, void* scratch, size_t scratch_bytes,
  * has no counterpart of this entry point. */
 int tlf_attn_decode_static(const tlf_attn_args* a, void* stream);
 
+/* ---- operators on a caller's paged caches and logits --------------------- */
+
+/* What a serving program does around a model's layers when it keeps its own caches: turn the queries and keys of new
+ * tokens and put keys and values into their pages (tlf_rope_append), attend from a chunk of new tokens of every
+ * sequence to its cache (tlf_attn_chunk), cut caches to a budget of entries (tlf_cache_evict) and draw the next tokens
+ * (tlf_sample). The paper has no counterpart of these entry points.
+ *
+ * Conventions: all buffers are device pointers owned by the caller. The calls launch on `stream` (a cudaStream_t) and
+ * return without synchronising; they allocate nothing, can be captured into a CUDA graph, and any number of them may be
+ * in flight as long as those that overlap share no scratch and no output. A refused call (INVALID_ARG, CUDA, with the
+ * message in tlf_last_error(NULL) on the calling thread) has launched nothing unless the code is CUDA. What only the
+ * device can see (a page id, an offset or a position out of range, a bounded wait that ran out) sets a bit of *err and
+ * is skipped, never followed: bit 1 = a bounded wait expired, bit 2 = a bad index. *err is OR-ed into; err = NULL drops
+ * the report, not the check. */
+
+/* A batch of chunks: row b has the new tokens cu_tokens[b] .. cu_tokens[b+1]-1 of the batch (none is allowed) and a
+ * cache of lens[b] entries that ends with them: its i-th new token is entry lens[b] - (new tokens of b) + i. Entry e sits
+ * in page page_table[b * max_pages + e / 64] at offset e % 64; pages are laid out
+ * [n_pages][n_layers][2 (K, V)][n_kv_heads][64][head_dim] in the dtype, as everywhere in this library. Any number of
+ * query heads per kv head up to 64. */
+typedef struct tlf_chunk {
+  int32_t n;            /* rows (sequences), 1..1024 */
+  int32_t n_tokens;     /* new tokens of all rows; 0 is allowed */
+  int32_t max_chunk;    /* an upper bound of the new tokens of a row (more sets err bit 2 and is cut); 0 = n_tokens */
+  int32_t n_heads;      /* Hq */
+  int32_t n_kv_heads;   /* Hkv, divides Hq */
+  int32_t head_dim;     /* 16, 32, 64 or 128 (bf16: 32, 64 or 128) */
+  int32_t n_layers;     /* layers stored per page */
+  int32_t layer;        /* the layer that the call reads or writes */
+  int32_t page_size;    /* 64 */
+  int32_t dtype;        /* tlf_dtype of the pool, q, k, v and out */
+  int32_t max_pages;    /* entries per page-table row */
+  int32_t reserved0;    /* must be 0 */
+  int64_t n_pages;      /* pages in the pool */
+  void* pool;           /* KV pages, 16-byte aligned */
+  const int32_t* page_table; /* [n][max_pages] */
+  const int32_t* cu_tokens;  /* [n + 1], not decreasing, within 0..n_tokens */
+  const int32_t* lens;       /* [n], 0..max_pages * 64 */
+  uint32_t* err;        /* optional device word */
+} tlf_chunk;
+
+/* Rotary tables. For pair k of rot_dim / 2 and position p: (cos, sin) of p * f_k times `magnitude`, computed in 64 bits,
+ * stored as float32 [max_pos][rot_dim / 2][2]. f_k = base^(-2k / rot_dim), changed for contexts longer than the ones
+ * trained on (`original_len` positions) by a factor:
+ *   NONE    f_k
+ *   LINEAR  f_k / factor (positions interpolated)
+ *   NTK     f_k with base * factor^(rot_dim / (rot_dim - 2)) (rot_dim > 2): the lowest frequency is divided by the
+ *           factor, the highest keeps its value
+ *   RAMP    f_k (1 - r) / factor + f_k r by the turns n_k = original_len f_k / (2 pi) that a pair makes over the trained
+ *           context: r = clamp((n_k - low_turns) / (high_turns - low_turns), 0, 1). Pairs that turn often keep their
+ *           frequency, pairs that turn less than low_turns are interpolated. */
+enum tlf_rope_scaling { TLF_ROPE_NONE = 0, TLF_ROPE_LINEAR = 1, TLF_ROPE_NTK = 2, TLF_ROPE_RAMP = 3 };
+typedef struct tlf_rope_config {
+  int32_t rot_dim;      /* even, 2..256: dims of a head that are rotated */
+  int32_t scaling;      /* tlf_rope_scaling */
+  double base;          /* 10000 */
+  double factor;        /* >= 1 (ignored by NONE) */
+  double original_len;  /* RAMP: trained context */
+  double low_turns;     /* RAMP: 1 is usual */
+  double high_turns;    /* RAMP: 32 is usual, > low_turns */
+  double magnitude;     /* factor of cos and sin; 1 leaves lengths as they are */
+} tlf_rope_config;
+int tlf_rope_table(const tlf_rope_config* cfg, int32_t max_pos, float* table, void* stream);
+
+/* Rotary positions and cache append. Token t of the batch is turned by positions[t] (an entry's position and its place in
+ * the cache need not agree: a loop's cache holds the tokens that ran the loop): the first rot_dim dims of every q and k
+ * head in pairs (x_a, x_b) -> (x_a cos - x_b sin, x_b cos + x_a sin), a = k, b = k + rot_dim / 2 (HALF) or a = 2k,
+ * b = 2k + 1 (INTERLEAVED); the others are copied. The turned k and v go to the token's entry of the given layer, the
+ * turned q to q_out. The arithmetic is float32, rounded once to the dtype. A token whose position is out of range gets a
+ * zero query and no entry, one without an entry (lens[b] smaller than its new tokens, a bad page) only its query. */
+enum tlf_rope_layout { TLF_ROPE_HALF = 0, TLF_ROPE_INTERLEAVED = 1 };
+typedef struct tlf_rope_args {
+  const void* q;        /* token t's heads [Hq][head_dim] at q + t * q_stride elements; likewise k, v with Hkv heads */
+  const void* k;
+  const void* v;
+  int64_t q_stride, k_stride, v_stride; /* in elements */
+  const int32_t* positions; /* [n_tokens] */
+  const float* table;   /* [max_pos][rot_dim / 2][2] */
+  int32_t max_pos;
+  int32_t rot_dim;      /* even, 2..head_dim */
+  int32_t layout;       /* tlf_rope_layout */
+  int32_t q_f32;        /* 1: q_out in float32 (what tlf_attn_decode takes), 0: in the dtype */
+  void* q_out;          /* [n_tokens][Hq][head_dim] */
+  int32_t* entry_pos;   /* optional [n_pages][64]: position of the entry */
+  float* entry_weight;  /* optional [n_pages][64]: set to 0 for the entry (see tlf_attn_chunk) */
+} tlf_rope_args;
+int tlf_rope_append(const tlf_chunk* c, const tlf_rope_args* a, void* stream);
+
+/* Attention of a chunk of new tokens over a paged cache. Query t at entry E(t) of row b sees the entries e <= E(t) of the
+ * row (the cache before the chunk, and the chunk causally): with s_e = scale q_t,h . k_e,
+ *   lse[t][h] = log sum_e exp(s_e),   out[t][h] = sum_e exp(s_e - lse[t][h]) v_e
+ * for kv head h / (Hq / Hkv). A query that sees nothing (E(t) < 0, because lens[b] is smaller than its new tokens) gets
+ * zeros and lse = -inf; what it may not see does not reach it, whatever it holds. Softmax statistics and sums are float32;
+ * with bf16 the probabilities are rounded to bf16 for the product with v.
+ * With weight_out the call also keeps account of what was looked at: for every entry e < lens[b] of every row
+ *   weight_out[page][offset] = weight_in[page][offset] + sum over queries t that see e and heads h of exp(s_e - lse[t][h])
+ * (weight_in NULL counts as zeros, and may be weight_out itself). Rows must not share pages then. */
+typedef struct tlf_attn_chunk_args {
+  const void* q;        /* [n_tokens][Hq][head_dim], rows q_stride elements apart, turned already */
+  int64_t q_stride;     /* in elements; 0 = Hq * head_dim */
+  void* out;            /* [n_tokens][Hq][head_dim], rows out_stride elements apart */
+  int64_t out_stride;   /* in elements; 0 = Hq * head_dim */
+  float* lse;           /* optional [n_tokens][Hq] */
+  const float* weight_in; /* optional [n_pages][64] */
+  float* weight_out;    /* optional [n_pages][64] */
+  float scale;          /* 0 = 1 / sqrt(head_dim) */
+  int32_t reserved0;    /* must be 0 */
+} tlf_attn_chunk_args;
+/* Scratch bytes of the call on the current device; 0 for arguments that the call refuses. */
+size_t tlf_attn_chunk_scratch_bytes(const tlf_chunk* c, const tlf_attn_chunk_args* a);
+int tlf_attn_chunk(const tlf_chunk* c, const tlf_attn_chunk_args* a, void* scratch, size_t scratch_bytes, void* stream);
+
+/* Cut every row's cache to at most `budget` entries, in all layers and heads at once. The entries that stay are the
+ * `budget` first ones by: protected entries (position < n_first, or position >= next_pos[b] - n_recent), then higher
+ * weight, then lower entry index; a NaN weighs less than anything. A row of at most `budget` entries keeps them all.
+ * Entries beyond the budget that stay move into the places below it that become free, both in order, so most entries keep
+ * their place and the others' order is not kept: attention does not depend on it, positions and weights move along. Pages
+ * past the first ceil(lens_out / 64) of a row hold nothing any more and may be given to other rows.
+ * pos_out and weight_out get the entries below lens_out[b] only; they and lens_out may be the inputs' own buffers. Rows
+ * must not share pages. */
+typedef struct tlf_evict_args {
+  int32_t n;            /* rows, 1..1024 */
+  int32_t n_kv_heads, head_dim, n_layers;
+  int32_t page_size;    /* 64 */
+  int32_t dtype;        /* tlf_dtype */
+  int32_t max_pages;
+  int32_t budget;       /* >= 1, n_first + n_recent <= budget */
+  int32_t n_first;      /* >= 0 */
+  int32_t n_recent;     /* >= 0 */
+  int64_t n_pages;
+  void* pool;
+  const int32_t* page_table; /* [n][max_pages] */
+  const int32_t* lens;       /* [n] */
+  const int32_t* next_pos;   /* [n]: position of the row's next token */
+  const int32_t* pos_in;     /* [n_pages][64] */
+  int32_t* pos_out;
+  const float* weight_in;    /* [n_pages][64] */
+  float* weight_out;
+  int32_t* lens_out;         /* [n] */
+  uint32_t* err;        /* optional */
+} tlf_evict_args;
+size_t tlf_cache_evict_scratch_bytes(const tlf_evict_args* a);
+int tlf_cache_evict(const tlf_evict_args* a, void* scratch, size_t scratch_bytes, void* stream);
+
+/* The next token of every row. With l the row's logits (NaN and -inf: a token that cannot be drawn; +inf counts as the
+ * largest float), M their maximum and T = temperature (1 where it is <= 0): z_i = (l_i - M) / T, w_i = exp(z_i). The
+ * tokens are ordered by l, ties by lower index; of that order are kept
+ *   top-k   the first top_k (<= 0: all); only the first where temperature <= 0 (greedy);
+ *   top-p   of those, each whose predecessors weigh less than top_p of the top-k tokens' weight (>= 1: all);
+ *   min-p   of those, each with w_i >= min_p;
+ * the first is always kept. The token is the kept one with the largest z_i - log(-log u_i) (ties: the lower index), u_i its
+ * random number: for u uniform in (0, 1) that draws token i with probability w_i / (sum of the kept w). NaN counts as 0.
+ * logprob is z_i - log sum_j w_j over the whole row. A row in which no token can be drawn gets token -1 and logprob -inf.
+ * Same inputs give the same tokens: sums that decide are taken in a fixed order or in fixed point. */
+typedef struct tlf_sample_args {
+  int32_t n;            /* rows, 1..65535 */
+  int32_t vocab;        /* 1..2^22 */
+  const float* logits;  /* [n][vocab], rows logits_stride elements apart */
+  int64_t logits_stride;
+  const float* noise;   /* [n][vocab], rows noise_stride elements apart */
+  int64_t noise_stride;
+  const float* temperature; /* [n] or NULL = 1 */
+  const int32_t* top_k;     /* [n] or NULL = all */
+  const float* top_p;       /* [n] or NULL = 1 */
+  const float* min_p;       /* [n] or NULL = 0 */
+  int32_t* tokens;      /* [n] */
+  float* logprobs;      /* [n] or NULL */
+} tlf_sample_args;
+int tlf_sample(const tlf_sample_args* a, void* stream);
+
 /* ---- inspection ---------------------------------------------------------- */
 
 /* Number of live sequences and free pages. */

@@ -1,0 +1,58 @@
+// The work split of the chunk attention (k_chunk.cu), on the host and on the device.
+#pragma once
+
+namespace tlf {
+
+// A row's queries are cut into tiles of qt, its cache into blocks of bk entries (both powers of two). Tile t of a row of ql
+// new tokens behind s0 = len - ql old entries sees the first nb(t) blocks; an item is a tile of one kv head. All items'
+// blocks lie in one flat order (row, head, tile, block), of which every CTA takes an equal share: it streams the same number
+// of blocks whatever the lengths, and items that it shares with other CTAs are joined afterwards. nb is at least 1, so that
+// queries that see nothing are answered too. The sums over tiles are closed forms: no list of items is ever written.
+struct ChunkSplit {
+  int qt_log, bk_log;
+
+  __host__ __device__ int tiles(int ql) const { return (ql + (1 << qt_log) - 1) >> qt_log; }
+  __host__ __device__ int blocks(int s0, int ql, int t) const {
+    const long long q = ((long long)t + 1) << qt_log;
+    const long long keys = s0 + (q < ql ? q : (long long)ql);
+    return keys <= 0 ? 1 : (int)((keys + (1 << bk_log) - 1) >> bk_log);
+  }
+  // sum over u = 1 .. n of ceil(u / 2^r)
+  __host__ __device__ static long long ceil_sum(long long n, int r) {
+    const long long q = n >> r, rem = n & ((1LL << r) - 1);
+    return ((q * (q + 1) / 2) << r) + rem * (q + 1);
+  }
+  // blocks of the row's first t tiles (of one head); only its last tile may be cut short, so tiles before it are whole
+  __host__ __device__ long long before(int s0, int ql, int t) const {
+    const int nt = tiles(ql), whole = t < nt ? t : nt - 1;
+    if (t <= 0 || nt <= 0) return 0;
+    long long sum;
+    if (qt_log >= bk_log) {  // nb(i) = max(1, c + (i + 1) m)
+      const int ml = qt_log - bk_log;
+      const long long m = 1LL << ml, c = -((-(long long)s0) >> bk_log);
+      long long k0 = c >= 1 ? 0 : ((1 - c + m - 1) >> ml) - 1;  // tiles with c + (i + 1) m < 1
+      if (k0 < 0) k0 = 0;
+      if (k0 > whole) k0 = whole;
+      sum = k0 + (whole - k0) * c + ((long long)whole * (whole + 1) / 2 - k0 * (k0 + 1) / 2) * m;
+    } else {  // nb(i) = max(1, ceil((a + i + 1) / r))
+      const int rl = bk_log - qt_log;
+      const long long a = -((-(long long)s0) >> qt_log);
+      long long k0 = a >= 0 ? 0 : -a;
+      if (k0 > whole) k0 = whole;
+      sum = k0 + ceil_sum(a + whole > 0 ? a + whole : 0, rl) - ceil_sum(a + k0 > 0 ? a + k0 : 0, rl);
+    }
+    return t < nt ? sum : sum + blocks(s0, ql, nt - 1);
+  }
+  // the tile that holds block `at` (counted from the row's first) of the row's head
+  __host__ __device__ int tile_of(int s0, int ql, long long at) const {
+    int lo = 0, hi = tiles(ql);  // before(lo) <= at < before(hi)
+    while (hi - lo > 1) {
+      const int mid = lo + (hi - lo) / 2;
+      if (before(s0, ql, mid) <= at) lo = mid;
+      else hi = mid;
+    }
+    return lo;
+  }
+};
+
+}  // namespace tlf

@@ -26,6 +26,8 @@ DTYPE = {"f32": 0, "bf16": 1}
 EXIT = {"argmax": 0, "survival": 1}
 GEMM = {"auto": 0, "simt": 1}
 ABLATION = {"none": 0, "no_gather": 1, "dense_cache": 2}
+ROPE_SCALING = {"none": 0, "linear": 1, "ntk": 2, "ramp": 3}
+ROPE_LAYOUT = {"half": 0, "interleaved": 1}
 
 
 class TlfConfig(C.Structure):
@@ -52,6 +54,42 @@ class TlfAttnArgs(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n", "n_heads", "n_kv_heads", "head_dim", "n_layers", "layer",
                                          "page_size", "dtype", "max_pages", "reserved0")] + [
         ("n_pages", C.c_int64)] + [(n, C.c_void_p) for n in ("q", "pool", "page_table", "lens", "out", "err")]
+
+
+class TlfChunk(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n", "n_tokens", "max_chunk", "n_heads", "n_kv_heads", "head_dim", "n_layers",
+                                         "layer", "page_size", "dtype", "max_pages", "reserved0")] + [
+        ("n_pages", C.c_int64)] + [(n, C.c_void_p) for n in ("pool", "page_table", "cu_tokens", "lens", "err")]
+
+
+class TlfRopeConfig(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("scaling", C.c_int32)] + [
+        (n, C.c_double) for n in ("base", "factor", "original_len", "low_turns", "high_turns", "magnitude")]
+
+
+class TlfRopeArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v")] + [
+        (n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride")] + [("positions", C.c_void_p), ("table", C.c_void_p)] + [
+        (n, C.c_int32) for n in ("max_pos", "rot_dim", "layout", "q_f32")] + [
+        (n, C.c_void_p) for n in ("q_out", "entry_pos", "entry_weight")]
+
+
+class TlfAttnChunkArgs(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_stride", C.c_int64), ("out", C.c_void_p), ("out_stride", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("lse", "weight_in", "weight_out")] + [("scale", C.c_float), ("reserved0", C.c_int32)]
+
+
+class TlfEvictArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n", "n_kv_heads", "head_dim", "n_layers", "page_size", "dtype", "max_pages",
+                                         "budget", "n_first", "n_recent")] + [("n_pages", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("pool", "page_table", "lens", "next_pos", "pos_in", "pos_out", "weight_in", "weight_out",
+                                  "lens_out", "err")]
+
+
+class TlfSampleArgs(C.Structure):
+    _fields_ = [("n", C.c_int32), ("vocab", C.c_int32), ("logits", C.c_void_p), ("logits_stride", C.c_int64),
+                ("noise", C.c_void_p), ("noise_stride", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p", "tokens", "logprobs")]
 
 
 class TlfError(RuntimeError):
@@ -87,6 +125,13 @@ _SIGS = {
     "tlf_attn_decode_scratch_bytes": (C.c_size_t, [C.POINTER(TlfAttnArgs)]),
     "tlf_attn_decode": (C.c_int, [C.POINTER(TlfAttnArgs), _P, C.c_size_t, _P]),
     "tlf_attn_decode_static": (C.c_int, [C.POINTER(TlfAttnArgs), _P]),
+    "tlf_rope_table": (C.c_int, [C.POINTER(TlfRopeConfig), C.c_int32, _P, _P]),
+    "tlf_rope_append": (C.c_int, [C.POINTER(TlfChunk), C.POINTER(TlfRopeArgs), _P]),
+    "tlf_attn_chunk_scratch_bytes": (C.c_size_t, [C.POINTER(TlfChunk), C.POINTER(TlfAttnChunkArgs)]),
+    "tlf_attn_chunk": (C.c_int, [C.POINTER(TlfChunk), C.POINTER(TlfAttnChunkArgs), _P, C.c_size_t, _P]),
+    "tlf_cache_evict_scratch_bytes": (C.c_size_t, [C.POINTER(TlfEvictArgs)]),
+    "tlf_cache_evict": (C.c_int, [C.POINTER(TlfEvictArgs), _P, C.c_size_t, _P]),
+    "tlf_sample": (C.c_int, [C.POINTER(TlfSampleArgs), _P]),
 }
 
 
@@ -248,6 +293,184 @@ def tlf_attn_decode(a: TlfAttnArgs, scratch, scratch_bytes: int, stream=None):
 def tlf_attn_decode_static(a: TlfAttnArgs, stream=None):
     """tlf_attn_decode without caller scratch: uses the library's built-in 4 MiB device array."""
     _check(load_library().tlf_attn_decode_static(C.byref(a), _stream(stream)), None)
+
+
+# Operators on a caller's paged caches and logits. The builders take torch CUDA tensors, read shapes, types and strides off
+# them, and keep them alive with the arguments; a program makes the arguments once for its buffers and calls with them.
+
+def _torch_dtype(t) -> int:
+    name = str(t.dtype)
+    if name == "torch.float32":
+        return DTYPE["f32"]
+    if name in ("torch.bfloat16", "torch.int16", "torch.uint16"):  # bfloat16, or its bits
+        return DTYPE["bf16"]
+    raise ValueError(f"{name}: float32 or bfloat16 is wanted")
+
+
+def _dense(what: str, t, dtype: Optional[str], *shape):
+    """A contiguous tensor of the given type and shape (None: any extent), or None."""
+    if t is None:
+        return None
+    if not t.is_contiguous() or (dtype and str(t.dtype) != "torch." + dtype) or len(t.shape) != len(shape) or any(
+            w is not None and w != h for w, h in zip(shape, t.shape)):
+        raise ValueError(f"{what}: a contiguous {dtype or ''} tensor of shape {shape} is wanted, got {str(t.dtype)} "
+                         f"{tuple(t.shape)}")
+    return t
+
+
+def _heads(what: str, t, dtype: int, rows: int, heads: int, hd: int) -> int:
+    """Elements between the rows of a tensor of shape [rows or more, heads, hd] or [rows or more, heads * hd]."""
+    if _torch_dtype(t) != dtype or tuple(t.shape[1:]) not in ((heads, hd), (heads * hd,)) or t.shape[0] < rows or \
+            t.stride(-1) != 1 or (t.dim() == 3 and t.stride(1) != hd):
+        raise ValueError(f"{what}: {rows} rows of {heads} heads of {hd} in the pool's type are wanted, each row contiguous, got "
+                         f"{str(t.dtype)} {tuple(t.shape)} with strides {t.stride()}")
+    return t.stride(0)
+
+
+def chunk_args(pool, page_table, cu_tokens, lens, n_heads: int, n_tokens: int, layer: int = 0, max_chunk: int = 0,
+               err=None) -> TlfChunk:
+    """A batch of chunks over a paged cache: pool [pages, layers, 2, kv heads, 64, head_dim], page_table [n, most pages]
+    int32, cu_tokens [n + 1] int32, lens [n] int32 (with the new tokens)."""
+    if len(pool.shape) != 6 or pool.shape[2] != 2:
+        raise ValueError(f"pool: [pages, layers, 2, kv heads, 64, head_dim] is wanted, got {tuple(pool.shape)}")
+    _dense("pool", pool, None, *pool.shape)
+    n = page_table.shape[0]
+    _dense("page_table", page_table, "int32", n, None)
+    _dense("cu_tokens", cu_tokens, "int32", n + 1)
+    _dense("lens", lens, "int32", n)
+    c = TlfChunk(n=n, n_tokens=n_tokens, max_chunk=max_chunk, n_heads=n_heads, n_kv_heads=pool.shape[3],
+                 head_dim=pool.shape[5], n_layers=pool.shape[1], layer=layer, page_size=pool.shape[4],
+                 dtype=_torch_dtype(pool), max_pages=page_table.shape[1], n_pages=pool.shape[0], pool=_addr(pool),
+                 page_table=_addr(page_table), cu_tokens=_addr(cu_tokens), lens=_addr(lens), err=_addr(err))
+    c.kept = (pool, page_table, cu_tokens, lens, err)
+    return c
+
+
+def rope_config(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_len: float = 0.0,
+                low_turns: float = 1.0, high_turns: float = 32.0, magnitude: float = 1.0) -> TlfRopeConfig:
+    return TlfRopeConfig(rot_dim=rot_dim, scaling=ROPE_SCALING[scaling], base=base, factor=factor,
+                         original_len=original_len, low_turns=low_turns, high_turns=high_turns, magnitude=magnitude)
+
+
+def tlf_rope_table(cfg: TlfRopeConfig, max_pos: int, table, stream=None):
+    """Fills table, a float32 tensor [max_pos, rot_dim / 2, 2]."""
+    _dense("table", table, "float32", max_pos, cfg.rot_dim // 2, 2)
+    _check(load_library().tlf_rope_table(C.byref(cfg), max_pos, _addr(table), _stream(stream)), None)
+
+
+def rope_args(q, k, v, positions, table, q_out, layout: str = "half", entry_pos=None, entry_weight=None) -> TlfRopeArgs:
+    """q, k, v: [tokens, heads, head_dim] or [tokens, heads * head_dim], for example three parts of one projection's output;
+    table [max_pos, rot_dim / 2, 2]; q_out [tokens, heads, head_dim] in the pool's type or in float32."""
+    T, hq, hd = q_out.shape
+    _dense("table", table, "float32", None, None, 2)
+    _dense("positions", positions, "int32", None)
+    _dense("q_out", q_out, None, T, hq, hd)
+    _dense("entry_pos", entry_pos, "int32", None, 64)
+    _dense("entry_weight", entry_weight, "float32", None, 64)
+    dt = _torch_dtype(q)
+    kh = k.shape[1] if k.dim() == 3 else k.shape[1] // hd
+    a = TlfRopeArgs(q=_addr(q), k=_addr(k), v=_addr(v), q_stride=_heads("q", q, dt, 0, hq, hd),
+                    k_stride=_heads("k", k, dt, 0, kh, hd), v_stride=_heads("v", v, dt, 0, kh, hd),
+                    positions=_addr(positions), table=_addr(table), max_pos=table.shape[0], rot_dim=2 * table.shape[1],
+                    layout=ROPE_LAYOUT[layout], q_f32=int(_torch_dtype(q_out) == DTYPE["f32"] != dt), q_out=_addr(q_out),
+                    entry_pos=_addr(entry_pos), entry_weight=_addr(entry_weight))
+    a.kept = (q, k, v, positions, table, q_out, entry_pos, entry_weight)
+    a.fits = (min(x.shape[0] for x in (q, k, v, positions, q_out)), hq, kh, hd, dt, [
+        t.shape[0] for t in (entry_pos, entry_weight) if t is not None])
+    return a
+
+
+def _pair(c: TlfChunk, a):
+    """The arguments' tensors are large enough for the batch (looked at once for a pair of them)."""
+    if getattr(a, "batch", None) is c:
+        return
+    rows, hq, kh, hd, dt, pages = a.fits
+    if rows < c.n_tokens or hq != c.n_heads or (kh and kh != c.n_kv_heads) or hd != c.head_dim or dt != c.dtype or any(
+            p != c.n_pages for p in pages):
+        raise ValueError(f"the arguments are for {rows} tokens of {hq} heads of {hd} and caches of {pages} pages, the batch has "
+                         f"{c.n_tokens} tokens of {c.n_heads} heads of {c.head_dim} and {c.n_pages} pages")
+    a.batch = c
+
+
+def tlf_rope_append(c: TlfChunk, a: TlfRopeArgs, stream=None):
+    _pair(c, a)
+    _check(load_library().tlf_rope_append(C.byref(c), C.byref(a), _stream(stream)), None)
+
+
+def attn_chunk_args(q, out, lse=None, weight_in=None, weight_out=None, scale: float = 0.0) -> TlfAttnChunkArgs:
+    """q, out: [tokens, heads, head_dim], rows any stride apart; lse [tokens, heads] float32; weights [pages, 64] float32."""
+    _, hq, hd = q.shape
+    _dense("lse", lse, "float32", None, hq)
+    _dense("weight_in", weight_in, "float32", None, 64)
+    _dense("weight_out", weight_out, "float32", None, 64)
+    dt = _torch_dtype(q)
+    a = TlfAttnChunkArgs(q=_addr(q), q_stride=_heads("q", q, dt, 0, hq, hd), out=_addr(out),
+                         out_stride=_heads("out", out, dt, q.shape[0], hq, hd), lse=_addr(lse), weight_in=_addr(weight_in),
+                         weight_out=_addr(weight_out), scale=scale)
+    a.kept = (q, out, lse, weight_in, weight_out)
+    a.fits = (min(x.shape[0] for x in (q, out, lse) if x is not None), hq, 0, hd, dt,
+              [t.shape[0] for t in (weight_in, weight_out) if t is not None])
+    return a
+
+
+def tlf_attn_chunk_scratch_bytes(c: TlfChunk, a: TlfAttnChunkArgs) -> int:
+    return load_library().tlf_attn_chunk_scratch_bytes(C.byref(c), C.byref(a))
+
+
+def tlf_attn_chunk(c: TlfChunk, a: TlfAttnChunkArgs, scratch, scratch_bytes: int, stream=None):
+    _pair(c, a)
+    _check(load_library().tlf_attn_chunk(C.byref(c), C.byref(a), _addr(scratch), scratch_bytes, _stream(stream)), None)
+
+
+def evict_args(pool, page_table, lens, next_pos, pos_in, pos_out, weight_in, weight_out, lens_out, budget: int,
+               n_first: int = 0, n_recent: int = 0, err=None) -> TlfEvictArgs:
+    """Shapes as in chunk_args; pos [pages, 64] int32, weight [pages, 64] float32."""
+    if len(pool.shape) != 6 or pool.shape[2] != 2:
+        raise ValueError(f"pool: [pages, layers, 2, kv heads, 64, head_dim] is wanted, got {tuple(pool.shape)}")
+    _dense("pool", pool, None, *pool.shape)
+    n, pages = page_table.shape[0], pool.shape[0]
+    _dense("page_table", page_table, "int32", n, None)
+    for what, t in (("lens", lens), ("next_pos", next_pos), ("lens_out", lens_out)):
+        _dense(what, t, "int32", n)
+    for what, t, dt in (("pos_in", pos_in, "int32"), ("pos_out", pos_out, "int32"), ("weight_in", weight_in, "float32"),
+                        ("weight_out", weight_out, "float32")):
+        _dense(what, t, dt, pages, 64)
+    a = TlfEvictArgs(n=n, n_kv_heads=pool.shape[3], head_dim=pool.shape[5], n_layers=pool.shape[1], page_size=pool.shape[4],
+                     dtype=_torch_dtype(pool), max_pages=page_table.shape[1], budget=budget, n_first=n_first,
+                     n_recent=n_recent, n_pages=pages, pool=_addr(pool), page_table=_addr(page_table), lens=_addr(lens),
+                     next_pos=_addr(next_pos), pos_in=_addr(pos_in), pos_out=_addr(pos_out), weight_in=_addr(weight_in),
+                     weight_out=_addr(weight_out), lens_out=_addr(lens_out), err=_addr(err))
+    a.kept = (pool, page_table, lens, next_pos, pos_in, pos_out, weight_in, weight_out, lens_out, err)
+    return a
+
+
+def tlf_cache_evict_scratch_bytes(a: TlfEvictArgs) -> int:
+    return load_library().tlf_cache_evict_scratch_bytes(C.byref(a))
+
+
+def tlf_cache_evict(a: TlfEvictArgs, scratch, scratch_bytes: int, stream=None):
+    _check(load_library().tlf_cache_evict(C.byref(a), _addr(scratch), scratch_bytes, _stream(stream)), None)
+
+
+def sample_args(logits, noise, tokens, logprobs=None, temperature=None, top_k=None, top_p=None, min_p=None) -> TlfSampleArgs:
+    """logits, noise: float32 [rows, vocab], rows any stride apart; tokens int32 [rows]; logprobs and the parameters [rows]."""
+    n, V = logits.shape
+    for what, t in (("logits", logits), ("noise", noise)):
+        if str(t.dtype) != "torch.float32" or tuple(t.shape) != (n, V) or t.stride(1) != 1:
+            raise ValueError(f"{what}: float32 [{n}, {V}] with contiguous rows is wanted, got {str(t.dtype)} {tuple(t.shape)}")
+    _dense("tokens", tokens, "int32", n)
+    for what, t, dt in (("logprobs", logprobs, "float32"), ("temperature", temperature, "float32"), ("top_k", top_k, "int32"),
+                        ("top_p", top_p, "float32"), ("min_p", min_p, "float32")):
+        _dense(what, t, dt, n)
+    a = TlfSampleArgs(n=n, vocab=V, logits=_addr(logits), logits_stride=logits.stride(0), noise=_addr(noise),
+                      noise_stride=noise.stride(0), temperature=_addr(temperature), top_k=_addr(top_k), top_p=_addr(top_p),
+                      min_p=_addr(min_p), tokens=_addr(tokens), logprobs=_addr(logprobs))
+    a.kept = (logits, noise, tokens, logprobs, temperature, top_k, top_p, min_p)
+    return a
+
+
+def tlf_sample(a: TlfSampleArgs, stream=None):
+    _check(load_library().tlf_sample(C.byref(a), _stream(stream)), None)
 
 
 # ----------------------------------------------------------------------------
