@@ -57,6 +57,13 @@ __device__ __forceinline__ int chunk_page(const int* table, int max_pages, long 
   return -1;
 }
 
+// 2^x with the hardware approximation (relative error about 2^-22).
+__device__ __forceinline__ float ex2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 template <typename T>
 __device__ __forceinline__ T block_sum(T v, T* red) {  // every thread gets the sum; red: 33 values; fixed order
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;

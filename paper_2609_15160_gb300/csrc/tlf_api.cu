@@ -23,6 +23,7 @@
 #include <cudaTypedefs.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -293,14 +294,16 @@ extern "C" const char* tlf_last_error(const tlf_ctx* ctx) {
 // ----------------------------------------------------------------------------
 // creation
 // ----------------------------------------------------------------------------
-static PFN_cuTensorMapEncodeTiled_v12000 get_encode_fn() {
-  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+PFN_cuTensorMapEncodeTiled_v12000 tlf::tensor_map_encoder() {
+  static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> found{nullptr};
+  PFN_cuTensorMapEncodeTiled_v12000 fn = found.load(std::memory_order_acquire);
   if (!fn) {
     cudaDriverEntryPointQueryResult q;
     void* p = nullptr;
     if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
         q == cudaDriverEntryPointSuccess)
       fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+    found.store(fn, std::memory_order_release);
   }
   return fn;
 }
@@ -308,7 +311,7 @@ static PFN_cuTensorMapEncodeTiled_v12000 get_encode_fn() {
 // 2-D bf16 tensor map over a row-major [rows][cols] matrix with row stride ld
 // elements; box = 64 columns x box_rows rows, 128-byte swizzle, zero fill.
 static bool make_map(CUtensorMap* m, const void* base, int rows, int cols, int ld, int box_rows) {
-  auto fn = get_encode_fn();
+  auto fn = tensor_map_encoder();
   if (!fn) return false;
   cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
@@ -324,7 +327,7 @@ static bool make_map(CUtensorMap* m, const void* base, int rows, int cols, int l
 // J * 2 * Hkv * page_size rows of a page, pages}, box {64, 64, 1}, 128-byte swizzle (a page keeps
 // its own coordinate, so coordinates stay within int32 for any pool size).
 static bool make_pool_map(CUtensorMap* m, const void* base, const ModelDims& md) {
-  auto fn = get_encode_fn();
+  auto fn = tensor_map_encoder();
   if (!fn) return false;
   cuuint64_t dims[3] = {(cuuint64_t)md.hd, (cuuint64_t)md.J * 2 * md.Hkv * md.page_size, (cuuint64_t)md.n_pages};
   cuuint64_t strides[2] = {(cuuint64_t)md.hd * 2, (cuuint64_t)md.page_elems * 2};
@@ -339,7 +342,7 @@ static bool make_pool_map(CUtensorMap* m, const void* base, const ModelDims& md)
 // 3-D bf16 tensor map over the prefill q planes ([2 C rows][Hq][hd]): box = 64 elements x the G query heads of a kv
 // head x 128 / G rows, i.e. one column of a 128-row query tile (row = query * G + head).
 static bool make_q_map(CUtensorMap* m, const void* base, const ModelDims& md, int rows) {
-  auto fn = get_encode_fn();
+  auto fn = tensor_map_encoder();
   if (!fn) return false;
   const cuuint32_t G = (cuuint32_t)(md.Hq / md.Hkv);
   cuuint64_t dims[3] = {(cuuint64_t)md.hd, (cuuint64_t)md.Hq, (cuuint64_t)rows};
@@ -443,7 +446,7 @@ static int create_impl(tlf_ctx* ctx, const tlf_weights* w) {
   CK(ctx, cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev));
   if (major != 10) return fail(ctx, TLF_ERR_CUDA, "libtlf is built for sm_103a; device is sm_%d%d", major, minor);
   ctx->use_tc = (c.dtype == TLF_DTYPE_BF16 && c.gemm_impl == TLF_GEMM_AUTO);
-  if (ctx->use_tc && !get_encode_fn()) return fail(ctx, TLF_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable");
+  if (ctx->use_tc && !tensor_map_encoder()) return fail(ctx, TLF_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable");
   {
     int nt = ((c.max_batch + 15) / 16) * 16, b = 16;
     while (b < nt) b <<= 1;

@@ -8,6 +8,7 @@
 #pragma once
 
 #include <cuda.h>
+#include <cudaTypedefs.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -710,6 +711,8 @@ AttnOpLayout attn_op_layout(const tlf_attn_args* a, int num_sms);
 const char* attn_op_validate(const tlf_attn_args* a);
 cudaError_t attn_op_run(const tlf_attn_args* a, uint8_t* scratch, const AttnOpLayout& L, cudaStream_t st);
 int current_num_sms();
+// The driver's cuTensorMapEncodeTiled (NULL: unavailable).
+PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder();
 
 // Record a message for tlf_last_error(NULL) on this thread; returns code.
 int set_thread_error(int code, const char* msg);
