@@ -6,6 +6,7 @@
 // O = sum 2^(s - m) v, all in float32. An item inside one CTA's share is written out; the parts of a shared one go to the
 // scratch, and k_chunk_join adds them: M = max m_c, O = sum 2^(m_c - M) O_c / sum 2^(m_c - M) l_c.
 //
+// k_chunk_pair   bfloat16, more rows: tcgen05 on pairs of 128-row tiles.
 // k_chunk_mma    bfloat16, up to 64 query rows a tile: tensor cores through mma.sync.
 // k_chunk_simt   float32: tiles in shared memory, products on the CUDA cores.
 // k_chunk_weigh  with weights: adds up exp(s - lse) of every entry over the queries that see it.
@@ -710,6 +711,455 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
 }
 
 // ----------------------------------------------------------------------------
+// Tensor cores, many rows: tcgen05 (bfloat16, head_dim 64 and 128)
+// ----------------------------------------------------------------------------
+// One CTA an SM. An item is two tiles of 128 MMA rows (row = query * G + head) that share every block of 128 keys (two
+// pages), so that the tensor cores work on one tile while the other tile's softmax runs:
+//   warps 0-3, 4-7  softmax of tile 0 and 1, one thread a row: S from tensor memory, mask, running maximum (refreshed lazily)
+//                   and sum in float32, P in bf16 back to tensor memory, where it is the A operand of P V; at the end O out;
+//   warp 8          producer: q of both tiles, then K and V of every block, through tensor maps;
+//   warp 9          issues S = Q K^T and O += P V (V taken as an MN-major operand).
+// In an item's last block the softmax warps of the last queries zero V behind them (P = 0 does not cancel an infinity).
+// Tensor memory: S of both tiles (128 columns each) and O of both. At head_dim 128 that is all 512 columns, so P overwrites
+// its S; one thread's MMAs run in order, so the next S of a tile may be issued right behind the P V that reads P. At head_dim
+// 64 P has columns of its own and the next S is issued as soon as the softmax has read the one before.
+constexpr int PAIR_THREADS = 320;
+
+template <int HD>
+struct PairShape {
+  static constexpr int ATOMS = HD / 64, COL = 128 * 128, T_BYTES = ATOMS * COL;  // a tile of 128 rows
+  static constexpr int NST = HD == 128 ? 4 : 8;  // K, V ring
+  static constexpr int OFF_KV = 2 * T_BYTES, OFF_BAR = OFF_KV + NST * T_BYTES, NBAR = 2 * NST + 2 + 8 + 2;
+  static constexpr int OFF_INT = OFF_BAR + NBAR * 8, OFF_BASE = OFF_INT + 48;
+  static int bytes(int n) { return std::max(OFF_BASE + (n + 1) * 8 + 1024, tmem_min_smem(512)); }
+  static constexpr bool SEP_P = HD == 64;
+  static constexpr uint32_t SCOL = 0, OCOL = 256, PCOL = SEP_P ? 384 : 0, P_STEP = SEP_P ? 64 : 128;
+};
+
+// D(tmem) (+)= A(tmem) * B(smem desc)
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t at, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(at), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_put_16(uint32_t taddr, const uint32_t* r) {  // completes at the next wait::st
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
+__device__ __forceinline__ void tmem_st_wait_done() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+template <int HD>
+__global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int g_log, const __grid_constant__ CUtensorMap q_map,
+                                                                const __grid_constant__ CUtensorMap pool_map) {
+  using Sh = PairShape<HD>;
+  constexpr int NST = Sh::NST;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ long long s_red[33];
+  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sm + Sh::OFF_BAR);
+  volatile int* s_flag = reinterpret_cast<volatile int*>(sm + Sh::OFF_INT);  // [8] of a block: its pages that are not there
+  volatile int* abort_flag = s_flag + 8;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + Sh::OFF_INT) + 9;
+  long long* s_base = reinterpret_cast<long long*>(sm + Sh::OFF_BASE);
+  auto bar = [&](int i) { return smem_u32(&bars[i]); };
+  auto kv_full = [&](unsigned i) { return bar(i % NST); };
+  auto kv_empty = [&](unsigned i) { return bar(NST + i % NST); };
+  auto q_full = [&](int x) { return bar(2 * NST + x); };
+  auto s_full = [&](int x) { return bar(2 * NST + 2 + x); };  // S of tile x written
+  auto s_read = [&](int x) { return bar(2 * NST + 4 + x); };  // ... read by its softmax (SEP_P)
+  auto p_full = [&](int x) { return bar(2 * NST + 6 + x); };  // P of tile x written
+  auto o_done = [&](int x) { return bar(2 * NST + 8 + x); };  // its P V product done
+  const uint32_t q_free = bar(2 * NST + 10), v_tail = bar(2 * NST + 11);
+  const ChunkDev& c = a.c;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < NST; ++i) {
+      mbar_init(bar(i), 1);
+      mbar_init(bar(NST + i), 1);
+    }
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(q_full(x), 1);
+      mbar_init(s_full(x), 1);
+      mbar_init(s_read(x), 4);
+      mbar_init(p_full(x), 4);
+      mbar_init(o_done(x), 1);
+    }
+    mbar_init(q_free, 1);
+    mbar_init(v_tail, 4);
+    *abort_flag = 0;
+    fence_barrier_init();
+    prefetch_tensormap(&q_map);
+    prefetch_tensormap(&pool_map);
+  }
+  if (warp == 9) {
+    tmem_alloc(smem_u32(tmem_slot), 512);
+    tmem_relinquish();
+  }
+  pdl_wait();
+  chunk_plan(c, a.sp, s_base, s_red);
+  tc_fence_before();
+  __syncthreads();  // barriers initialised, tensor memory allocated
+  tc_fence_after();
+  pdl_trigger();  // not before: a dependent CTA on this SM could take the columns that warp 9 still waits for
+  const uint32_t tmem = *tmem_slot;
+  const long long all = s_base[c.n], per = chunk_share(a, all);
+  long long pos = blockIdx.x * per;
+  const long long end = pos + per < all ? pos + per : all;
+  const int qt_log = a.sp.qt_log, QT = 1 << (qt_log - 1);  // queries of a tile
+  // a bounded wait; once any role has given up, the others skip their waits and wind down
+  auto wait = [&](uint32_t b, uint32_t parity) {
+    if (*abort_flag) return false;
+    if (mbar_wait(b, parity & 1u, a.werr)) return true;
+    *abort_flag = 1;
+    return false;
+  };
+  // this CTA's part of the item at `pos`: blocks kb0 .. kb1 - 1, of which tile x has the first e[x]
+  struct Seg {
+    ChunkItem it;
+    int kb0, kb1, nq[2], e[2], token0, see0;
+  };
+  auto segment = [&](long long at) {
+    Seg s;
+    s.it = chunk_item(c, a.sp, s_base, at);
+    s.kb0 = (int)(at - s.it.first);
+    s.kb1 = (int)(end - s.it.first < s.it.nb ? end - s.it.first : s.it.nb);
+    const int q0 = s.it.t << qt_log, left = s.it.ql - q0;
+    s.token0 = s.it.t0 + q0;
+    s.see0 = s.it.s0 + q0;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      s.nq[x] = max(0, min(QT, left - x * QT));
+      const int last = s.see0 + x * QT + s.nq[x] - 1;  // entry of the tile's last query
+      const int nb = s.nq[x] > 0 ? (last < 0 ? 1 : last / 128 + 1) : 0;
+      s.e[x] = max(0, min(s.kb1, nb) - s.kb0);
+    }
+    return s;
+  };
+
+  if (warp == 8) {
+    // ---------------- producer ----------------
+    unsigned ring = 0, blk = 0, segs = 0;
+    while (pos < end) {
+      const Seg s = segment(pos);
+      const int E = s.kb1 - s.kb0;
+      bool ok = true;
+      if (lane == 0) {
+        ok = segs == 0 || wait(q_free, segs - 1);
+        for (int x = 0; x < 2; ++x) {
+          if (!ok || s.e[x] == 0) continue;
+          mbar_arrive_expect_tx(q_full(x), Sh::T_BYTES);
+#pragma unroll
+          for (int k = 0; k < Sh::ATOMS; ++k)
+            tma_load_3d(smem_u32(sm + x * Sh::T_BYTES + k * Sh::COL), &q_map, k * 64, s.it.h << g_log, s.token0 + x * QT, q_full(x));
+        }
+      }
+      const int rowK = (c.layer * 2 * c.Hkv + s.it.h) * 64, rowV = rowK + c.Hkv * 64;
+      const int last_page = (s.it.len - 1) / 64;
+      for (int g0 = 0; g0 < E; g0 += 16) {
+        // the pages of 16 blocks, one a lane; a block past the last page loads that one twice, one that is not there page 0
+        int mine = 0, bad = 0;
+        if (g0 + lane / 2 < E) {
+          const int p = min(2 * (s.kb0 + g0) + lane, max(last_page, 0));
+          mine = s.it.len > 0 ? chunk_page(c.page_table, c.max_pages, c.n_pages, s.it.b, p, c.err) : -1;
+          bad = mine < 0;
+          mine = max(mine, 0);
+        }
+        const unsigned bads = __ballot_sync(0xffffffffu, bad);
+        for (int i = 0; i < min(16, E - g0); ++i, ++blk, ring += 2) {
+          const int pg[2] = {__shfl_sync(0xffffffffu, mine, 2 * i), __shfl_sync(0xffffffffu, mine, 2 * i + 1)};
+          if (lane == 0 && ok) {
+            s_flag[blk & 7] = (bads >> (2 * i)) & 3;
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+              const unsigned r = ring + kv;
+              if (r >= NST && !wait(kv_empty(r), r / NST - 1)) {
+                ok = false;
+                break;
+              }
+              mbar_arrive_expect_tx(kv_full(r), Sh::T_BYTES);
+              const uint32_t dst = smem_u32(sm + Sh::OFF_KV + (r % NST) * Sh::T_BYTES);
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int k = 0; k < Sh::ATOMS; ++k)
+                  tma_load_3d(dst + k * Sh::COL + h * (Sh::COL / 2), &pool_map, k * 64, kv ? rowV : rowK, pg[h], kv_full(r));
+            }
+          }
+          __syncwarp();
+        }
+      }
+      ++segs;
+      pos = s.it.first + s.kb1;
+    }
+  } else if (warp == 9) {
+    // ---------------- MMA issuer ----------------
+    if (lane == 0) {
+      constexpr uint32_t IDS = idesc_bf16_f32(128, 128), IDO = idesc_bf16_f32_bmn(128, HD);
+      constexpr uint64_t T_E = Sh::T_BYTES >> 4, COL_E = Sh::COL >> 4, V16_E = 2048 >> 4;
+      const uint64_t dq = smem_desc_sw128(smem_u32(sm)), dk = smem_desc_sw128(smem_u32(sm + Sh::OFF_KV));
+      const uint64_t dv = smem_desc_sw128_mn(smem_u32(sm + Sh::OFF_KV), Sh::COL);
+      unsigned ring = 0, ns[2] = {0, 0}, np[2] = {0, 0}, nqf[2] = {0, 0}, tails = 0;
+      auto issue_s = [&](int x, unsigned r) {
+        const uint64_t kd = dk + (uint64_t)(r % NST) * T_E, qd = dq + (uint64_t)x * T_E;
+#pragma unroll
+        for (int kc = 0; kc < Sh::ATOMS; ++kc)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)  // K = 16 an MMA: +32 bytes (encoded +2) inside the atom column
+            tc_mma_f16(tmem + Sh::SCOL + 128u * x, qd + kc * COL_E + 2 * k, kd + kc * COL_E + 2 * k, IDS, (kc | k) ? 1u : 0u);
+        tc_commit(s_full(x));
+        ++ns[x];
+      };
+      auto issue_pv = [&](int x, unsigned r, bool first) {
+        const uint64_t vd = dv + (uint64_t)(r % NST) * T_E;
+        const uint32_t d = tmem + Sh::OCOL + (uint32_t)(HD * x), pa = tmem + Sh::PCOL + Sh::P_STEP * (uint32_t)x;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)  // K = 16 keys an MMA: 8 columns of P, +2048 bytes (16 rows) of V
+          mma_ts(d, pa + 8u * k, vd + V16_E * k, IDO, !first || k > 0 ? 1u : 0u);
+        tc_commit(o_done(x));
+        ++np[x];
+      };
+      bool ok = true;
+      while (pos < end && ok) {
+        const Seg s = segment(pos);
+        const int E = s.kb1 - s.kb0;
+        auto full = [&](int i, int kv) { return wait(kv_full(ring + 2 * i + kv), (ring + 2 * i + kv) / NST); };
+        ok = full(0, 0);
+        for (int x = 0; x < 2 && ok; ++x)
+          if (s.e[x] > 0) {
+            ok = wait(q_full(x), nqf[x]++) && (!Sh::SEP_P || ns[x] == 0 || wait(s_read(x), ns[x] - 1));
+            if (!ok) break;
+            tc_fence_after();
+            issue_s(x, ring);
+          }
+        if (!ok) break;
+        tc_commit(kv_empty(ring));
+        if (E == 1) tc_commit(q_free);
+        for (int i = 0; i < E && ok; ++i) {
+          const bool next = i + 1 < E;
+          const unsigned kn = ring + 2 * (i + 1), v = ring + 2 * i + 1;
+          if (Sh::SEP_P && next) {
+            // both next S products first: each waits only for the softmax to have read the S before
+            ok = full(i + 1, 0);
+            for (int x = 0; x < 2 && ok; ++x)
+              if (i + 1 < s.e[x]) {
+                ok = wait(s_read(x), ns[x] - 1);
+                if (!ok) break;
+                tc_fence_after();
+                issue_s(x, kn);
+              }
+            if (!ok) break;
+            tc_commit(kv_empty(kn));
+            if (i + 2 == E) tc_commit(q_free);
+          }
+          ok = full(i, 1) && (s.kb0 + i + 1 < s.it.nb || wait(v_tail, tails++));
+          for (int x = 0; x < 2 && ok; ++x) {
+            if (i < s.e[x]) {
+              ok = wait(p_full(x), np[x]);
+              if (!ok) break;
+              tc_fence_after();
+              issue_pv(x, v, i == 0);
+            }
+            if (!Sh::SEP_P && i + 1 < s.e[x]) {
+              ok = full(i + 1, 0);
+              if (!ok) break;
+              tc_fence_after();
+              issue_s(x, kn);
+            }
+          }
+          if (!ok) break;
+          tc_commit(kv_empty(v));
+          if (!Sh::SEP_P && next) {
+            tc_commit(kv_empty(kn));
+            if (i + 2 == E) tc_commit(q_free);
+          }
+        }
+        ring += 2 * E;
+        pos = s.it.first + s.kb1;
+      }
+    }
+    __syncwarp();
+  } else {
+    // ---------------- softmax: thread = MMA row = TMEM lane ----------------
+    const int x = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
+    const uint32_t lane_off = (uint32_t)(quad * 32) << 16;
+    const uint32_t t_s = tmem + lane_off + Sh::SCOL + 128u * (uint32_t)x;
+    const uint32_t t_p = tmem + lane_off + Sh::PCOL + Sh::P_STEP * (uint32_t)x;
+    const uint32_t t_o = tmem + lane_off + Sh::OCOL + (uint32_t)(HD * x);
+    const int qi = row >> g_log, g = row & ((1 << g_log) - 1);
+    const float scale = a.scale, grow_by = 8.f / scale;
+    unsigned n = 0, blk = 0;  // blocks of this tile, and of the CTA (block i of the CTA: K, V in ring places 2 i, 2 i + 1)
+    bool ok = true;
+    // waits taken by the whole warp: the TMEM accesses after them are warp-collective
+    auto wait_w = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, wait(b, parity)); };
+    while (pos < end && ok) {
+      const Seg s = segment(pos);
+      const bool row_ok = qi < s.nq[x];
+      const int see = row_ok ? s.see0 + x * QT + qi : -1;  // a row past the tile's queries sees nothing
+      float m_run = -INFINITY, l_run = 0.f;                // m in units of the raw scores
+      for (int i = 0; i < s.e[x]; ++i, ++n) {
+        if (!wait_w(s_full(x), n)) { ok = false; break; }
+        tc_fence_after();
+        if (s.kb0 + i + 1 == s.it.nb && x == (s.nq[1] > 0)) {
+          // V's barrier is in this use's phase: the stage's use before was read by a P V before this S, and this one's use
+          // ends with a P V that waits for v_tail
+          const unsigned r = 2 * (blk + i) + 1;
+          if (s.see0 + s.nq[0] + s.nq[1] <= (s.it.nb - 1) * 128 + row && wait(kv_full(r), r / NST)) {
+            uint8_t* v = sm + Sh::OFF_KV + (r % NST) * Sh::T_BYTES + row * 128;  // (a row keeps its place in the swizzle)
+#pragma unroll
+            for (int k = 0; k < 8 * Sh::ATOMS; ++k)
+              *reinterpret_cast<uint4*>(v + (k / 8) * Sh::COL + (k % 8) * 16) = make_uint4(0, 0, 0, 0);
+            fence_proxy_async_smem();
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(v_tail);
+        }
+        uint32_t su[128];
+#pragma unroll
+        for (int k = 0; k < 128; k += 32) tmem_ld_32_issue(t_s + (uint32_t)k, su + k);
+        tmem_ld_wait();
+        if (Sh::SEP_P) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(s_read(x));
+        }
+        const int vis = see - (s.kb0 + i) * 128;  // columns 0..vis are visible
+        const int flag = s_flag[(blk + i) & 7];
+        float pm4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        if (__any_sync(0xffffffffu, vis < 127)) {
+#pragma unroll
+          for (int k = 0; k < 128; ++k)
+            if (k > vis) su[k] = 0xff800000u;  // -inf
+        }
+        if (flag) {
+#pragma unroll
+          for (int k = 0; k < 128; ++k)
+            if (flag >> (k / 64) & 1) su[k] = 0xff800000u;
+        }
+#pragma unroll
+        for (int k = 0; k < 128; ++k) pm4[k & 3] = fmaxf(pm4[k & 3], __uint_as_float(su[k]));
+        const float pm = fmaxf(fmaxf(pm4[0], pm4[1]), fmaxf(pm4[2], pm4[3]));
+        // O is rescaled only when a row's maximum grows by more than 8 in base 2, after the P V before has landed
+        const bool grow = pm > m_run + grow_by;
+        const float cr = grow ? exp2f((m_run - pm) * scale) : 1.f;  // 0 when m_run was -inf
+        if (i > 0 && (Sh::SEP_P || __any_sync(0xffffffffu, grow))) {
+          if (!wait_w(o_done(x), n - 1)) { ok = false; break; }  // (with its own columns, P is free too)
+          tc_fence_after();
+          if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+            for (int c0 = 0; c0 < HD; c0 += 16) {
+              float o[16];
+              tmem_ld_16(t_o + (uint32_t)c0, o);
+#pragma unroll
+              for (int k = 0; k < 16; ++k) o[k] *= cr;
+              tmem_st_16(t_o + (uint32_t)c0, o);
+            }
+          }
+        }
+        if (grow) {
+          l_run *= cr;
+          m_run = pm;
+        }
+        const float mref = m_run == -INFINITY ? 0.f : m_run * scale;  // no visible key so far: any finite value
+        float ps4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c0 = 0; c0 < 128; c0 += 32) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int k = 0; k < 32; k += 2) {
+            const float p0 = ex2_fast(fmaf(__uint_as_float(su[c0 + k]), scale, -mref));
+            const float p1 = ex2_fast(fmaf(__uint_as_float(su[c0 + k + 1]), scale, -mref));
+            ps4[(k >> 1) & 3] += p0 + p1;
+            pk[k / 2] = pack_bf16(p0, p1);
+          }
+          tmem_put_16(t_p + (uint32_t)(c0 / 2), pk);
+        }
+        l_run += (ps4[0] + ps4[1]) + (ps4[2] + ps4[3]);
+        tmem_st_wait_done();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full(x));
+      }
+      // the last P V, then the row out: O / l, or its part
+      const bool whole = s.kb0 == 0 && s.kb1 == s.it.nb;
+      const long long token = s.token0 + x * QT + qi;
+      const int head = (s.it.h << g_log) + g;
+      const size_t part = ((size_t)(2 * blockIdx.x + (s.kb0 == 0)) * a.rows + x * 128 + row);
+      bf16* orow = static_cast<bf16*>(a.out) + token * a.os + (long long)head * HD;
+      const bool wide = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && a.os % 8 == 0;
+      bool bad = false;
+      if (ok && s.e[x] > 0) {
+        if (!wait_w(o_done(x), n - 1)) break;
+        tc_fence_after();
+        const float inv = whole ? (l_run != 0.f ? 1.f / l_run : 0.f) : 1.f;
+#pragma unroll
+        for (int c0 = 0; c0 < HD; c0 += 32) {
+          float o[32];
+          tmem_ld_32(t_o + (uint32_t)c0, o);
+#pragma unroll
+          for (int k = 0; k < 32; ++k) bad |= !(fabsf(o[k]) < INFINITY);
+          if (!row_ok) continue;
+          if (!whole) {
+#pragma unroll
+            for (int k = 0; k < 32; k += 4)
+              *reinterpret_cast<float4*>(a.part_o + part * HD + c0 + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+          } else if (wide) {
+#pragma unroll
+            for (int k = 0; k < 32; k += 8)
+              *reinterpret_cast<uint4*>(orow + c0 + k) =
+                  make_uint4(pack_bf16(o[k] * inv, o[k + 1] * inv), pack_bf16(o[k + 2] * inv, o[k + 3] * inv),
+                             pack_bf16(o[k + 4] * inv, o[k + 5] * inv), pack_bf16(o[k + 6] * inv, o[k + 7] * inv));
+          } else {
+#pragma unroll
+            for (int k = 0; k < 32; ++k) orow[c0 + k] = from_f32<bf16>(o[k] * inv);
+          }
+        }
+        tc_fence_before();
+      } else if (row_ok && !whole) {  // the tile has no block here: an empty part
+        for (int k = 0; k < HD; ++k) a.part_o[part * HD + k] = 0.f;
+      }
+      if (row_ok) {
+        if (!whole) a.part_ml[part] = make_float2(m_run == -INFINITY ? -INFINITY : m_run * scale, l_run);
+        else if (a.lse) a.lse[token * c.Hq + head] = l_run != 0.f ? (m_run * scale + log2f(l_run)) * LN2 : -INFINITY;
+      }
+      // rows that a 0 x infinity of a key which only others see has spoilt: again, over what they see
+      unsigned again = __ballot_sync(0xffffffffu, bad && row_ok && s.nq[0] + s.nq[1] > 1);
+      while (again) {
+        const int src = __ffs(again) - 1;
+        again &= again - 1;
+        const long long tk = __shfl_sync(0xffffffffu, token, src);
+        const int hh = __shfl_sync(0xffffffffu, head, src), see_r = __shfl_sync(0xffffffffu, see, src);
+        const size_t pt = __shfl_sync(0xffffffffu, (unsigned long long)part, src);
+        float mm, ll, oo[HD / 32];
+        chunk_redo<HD>(a, s.it.b, s.it.h, tk, hh, s.kb0 * 128, min(s.kb1 * 128, see_r + 1), mm, ll, oo);
+        const float inv = ll != 0.f ? 1.f / ll : 0.f;
+#pragma unroll
+        for (int k = 0; k < HD / 32; ++k) {
+          if (whole) static_cast<bf16*>(a.out)[tk * a.os + (long long)hh * HD + lane + 32 * k] = from_f32<bf16>(oo[k] * inv);
+          else a.part_o[pt * HD + lane + 32 * k] = oo[k];
+        }
+        if (lane == 0) {
+          if (!whole) a.part_ml[pt] = make_float2(mm, ll);
+          else if (a.lse) a.lse[tk * c.Hq + hh] = ll != 0.f ? (mm + log2f(ll)) * LN2 : -INFINITY;
+        }
+        __syncwarp();
+      }
+      blk += s.kb1 - s.kb0;
+      pos = s.it.first + s.kb1;
+    }
+  }
+  if (*abort_flag) drain_copies();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) tmem_dealloc(tmem, 512);
+}
+
+// ----------------------------------------------------------------------------
 // Weights
 // ----------------------------------------------------------------------------
 // An item is a page of a row, with all heads and all queries that see one of its entries; one writer an entry, and a fixed
@@ -793,7 +1243,8 @@ __global__ void __launch_bounds__(256) k_chunk_weigh(ChunkAttn a, const float* w
 // ----------------------------------------------------------------------------
 // Which kernel and split a call takes; a function of the arguments and the device alone.
 struct ChunkPath {
-  int rt;       // rows of a tile
+  bool pair;    // k_chunk_pair
+  int rt;       // rows of an item
   int ctas;
   size_t part_ml, lse, werr, total;  // scratch offsets (part_o at 0)
 };
@@ -809,8 +1260,10 @@ static ChunkPath chunk_path(const ChunkDev& c, int dtype, const tlf_attn_chunk_a
     p.rt = rows <= 16 ? 16 : 64;
     p.ctas = 2 * num_sms;
   } else {
-    p.rt = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
-    p.ctas = (c.hd == 128 ? 1 : 2) * num_sms;
+    const bool pow2 = (c.G & (c.G - 1)) == 0, q16 = reinterpret_cast<uintptr_t>(a.q) % 16 == 0 && a.q_stride % 8 == 0;
+    p.pair = rows > 64 && c.hd >= 64 && pow2 && q16;
+    p.rt = p.pair ? 256 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+    p.ctas = (c.hd == 128 || p.pair ? 1 : 2) * num_sms;
   }
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o = (o + bytes + 255) / 256 * 256; return at; };
@@ -843,6 +1296,25 @@ static bool pool_map(CUtensorMap* m, const ChunkDev& c) {
             c.hd == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+// 3-D map over q: {head_dim, Hq, tokens}, boxes of 64 elements x the heads of a kv head x 128 / G tokens, one column of a tile
+// of 128 rows; tokens past the last read as zeros.
+static bool q_map(CUtensorMap* m, const ChunkAttn& a) {
+  const auto fn = tensor_map_encoder();
+  if (!fn) return false;
+  cuuint64_t dims[3] = {(cuuint64_t)a.c.hd, (cuuint64_t)a.c.Hq, (cuuint64_t)a.c.T};
+  cuuint64_t strides[2] = {(cuuint64_t)a.c.hd * 2, (cuuint64_t)a.qs * 2};
+  cuuint32_t box[3] = {64, (cuuint32_t)a.c.G, (cuuint32_t)(128 / a.c.G)}, es[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.q), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+template <int HD>
+static cudaError_t pair_launch(const ChunkAttn& a, cudaStream_t st) {
+  CUtensorMap qm, pm;
+  if (!q_map(&qm, a) || !pool_map(&pm, a.c)) return cudaErrorInvalidValue;
+  using Sh = PairShape<HD>;
+  if (cudaError_t e = ensure_kernel_attrs(reinterpret_cast<const void*>(k_chunk_pair<HD>), Sh::bytes(SV_MAX_ROWS))) return e;
+  return launch_k(k_chunk_pair<HD>, dim3(a.ctas), dim3(PAIR_THREADS), Sh::bytes(a.c.n), st, a, pow2_log(a.c.G), qm, pm);
+}
 template <int HD, int MT>
 static cudaError_t mma_launch(const ChunkAttn& a, cudaStream_t st) {
   CUtensorMap map;
@@ -853,6 +1325,8 @@ static cudaError_t mma_launch(const ChunkAttn& a, cudaStream_t st) {
 }
 template <int HD>
 static cudaError_t mma_rows(const ChunkAttn& a, cudaStream_t st) {
+  if constexpr (HD >= 64)
+    if (a.rows == 256) return pair_launch<HD>(a, st);
   return a.rows == 16 ? mma_launch<HD, 1>(a, st) : a.rows == 32 ? mma_launch<HD, 2>(a, st) : mma_launch<HD, 4>(a, st);
 }
 template <int HD>
@@ -889,7 +1363,7 @@ cudaError_t launch_chunk_attn(const ChunkDev& c, int dtype, const tlf_attn_chunk
   char* s = static_cast<char*>(scratch);
   ChunkAttn a{};
   a.c = c;
-  a.sp = ChunkSplit{pow2_log(std::max(1, p.rt / c.G)), 6};
+  a.sp = ChunkSplit{pow2_log(std::max(1, p.rt / c.G)), p.pair ? 7 : 6};
   a.q = args.q;
   a.qs = args.q_stride ? args.q_stride : (long long)c.Hq * c.hd;
   a.out = args.out;

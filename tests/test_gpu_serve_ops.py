@@ -87,6 +87,9 @@ ATTEND = {
     "many-mha": ([0, 1, 500], [300, 127, 128], 2, 2, 64, "bf16"),
     "many-g5": ([17, 200], [140, 33], 5, 1, 64, "bf16"),
     "many-32": ([0, 99], [200, 70], 4, 2, 32, "bf16"),
+    "many-short": ([3], [66], 2, 2, 64, "bf16"),
+    "many-g16": ([40, 0], [9, 30], 32, 2, 128, "bf16"),
+    "many-far": ([3000], [70], 2, 1, 128, "bf16"),
     "one-row": ([4000], [40], 4, 1, 128, "bf16"),
     "f32-16": ([0, 1, 64, 90], [1, 5, 64, 3], 4, 4, 16, "f32"),
     "f32-64": ([0, 300], [70, 1], 4, 2, 64, "f32"),
