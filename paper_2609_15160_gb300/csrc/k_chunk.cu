@@ -9,7 +9,10 @@
 // k_chunk_pair   bfloat16, more rows: tcgen05 on pairs of 128-row tiles.
 // k_chunk_mma    bfloat16, up to 64 query rows a tile: tensor cores through mma.sync.
 // k_chunk_simt   float32: tiles in shared memory, products on the CUDA cores.
-// k_chunk_weigh  with weights: adds up exp(s - lse) of every entry over the queries that see it.
+// With weights, exp(s - lse) of every entry added up over the queries that see it:
+// k_weigh_tc            behind k_chunk_pair: S^T again on tcgen05, a thread a key;
+// k_chunk_weigh_scores  from the scores that k_chunk_mma leaves;
+// k_chunk_weigh         the rest, on the CUDA cores.
 #include <algorithm>
 #include <type_traits>
 
@@ -29,6 +32,7 @@ struct ChunkAttn {
   float scale;     // of the scores, times log2 e
   int ctas, rows;  // CTAs that share the blocks; rows of a part
   long long min_blocks;  // least share of a CTA
+  float* scores;   // k_chunk_mma: [T][Hq][max_pages * 64] scores that it leaves for the weights, or NULL
   uint32_t* werr;  // error word of the waits: the caller's, or one in the scratch
   float* part_o;   // [2 ctas][rows][hd]
   float2* part_ml; // [2 ctas][rows]
@@ -547,6 +551,17 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
             if (tail && key0 + i * 8 + (lane & 3) * 2 + (j & 1) > sees[j >> 1]) s[i][j] = -INFINITY;
             mx[j >> 1] = fmaxf(mx[j >> 1], s[i][j]);
           }
+        if (a.scores) {
+          const long long width = (long long)c.max_pages * 64;
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const int r = x ? r1 : r0;
+            if (r >= rows) continue;
+            float* to = a.scores + ((long long)(token0 + r / G) * c.Hq + it.h * G + r % G) * width + key0 + (lane & 3) * 2;
+#pragma unroll
+            for (int i = 0; i < NT; ++i) *reinterpret_cast<float2*>(to + i * 8) = make_float2(s[i][2 * x], s[i][2 * x + 1]);
+          }
+        }
         float cr[2] = {1.f, 1.f};
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -1162,6 +1177,31 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
 // ----------------------------------------------------------------------------
 // Weights
 // ----------------------------------------------------------------------------
+// base[b] = items (`entries` entries each) of the rows before b; returns how many there are. By the whole block.
+__device__ __forceinline__ long long weigh_items(const ChunkDev& c, int entries, long long* base, long long* red) {
+  long long carry = 0;
+  for (int b0 = 0; b0 < c.n; b0 += blockDim.x) {
+    const int b = b0 + threadIdx.x;
+    const long long items = b < c.n ? (chunk_row(c, b).len + entries - 1) / entries : 0;
+    long long total;
+    const long long at = carry + block_scan(items, red, &total);
+    if (b < c.n) base[b] = at;
+    carry += total;
+  }
+  if (threadIdx.x == 0) base[c.n] = carry;
+  __syncthreads();
+  return carry;
+}
+__device__ __forceinline__ int item_row(const long long* base, int n, long long item) {  // largest b with base[b] <= item
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (base[mid] <= item) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
 // An item is a page of a row, with all heads and all queries that see one of its entries; one writer an entry, and a fixed
 // order of the sums. Four threads a key, each with every fourth query row.
 template <typename T, int HD>
@@ -1177,23 +1217,9 @@ __global__ void __launch_bounds__(256) k_chunk_weigh(ChunkAttn a, const float* w
   __shared__ float s_sum[4][64];
   const ChunkDev& c = a.c;
   const int tid = threadIdx.x, key = tid & 63, part = tid >> 6, G = c.G;
-  long long carry = 0;
-  for (int b0 = 0; b0 < c.n; b0 += 256) {
-    const int b = b0 + tid;
-    long long total;
-    const long long pages = b < c.n ? (chunk_row(c, b).len + 63) / 64 : 0, at = carry + block_scan(pages, s_red, &total);
-    if (b < c.n) s_base[b] = at;
-    carry += total;
-  }
-  if (tid == 0) s_base[c.n] = carry;
-  __syncthreads();
-  for (long long item = blockIdx.x; item < carry; item += gridDim.x) {
-    int lo = 0, hi = c.n;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (s_base[mid] <= item) lo = mid;
-      else hi = mid;
-    }
+  const long long items = weigh_items(c, 64, s_base, s_red);
+  for (long long item = blockIdx.x; item < items; item += gridDim.x) {
+    const int lo = item_row(s_base, c.n, item);
     const int pg = (int)(item - s_base[lo]), page = chunk_page(c.page_table, c.max_pages, c.n_pages, lo, pg, c.err);
     if (page < 0) continue;
     const ChunkRow r = chunk_row(c, lo);
@@ -1238,6 +1264,352 @@ __global__ void __launch_bounds__(256) k_chunk_weigh(ChunkAttn a, const float* w
   pdl_trigger();
 }
 
+// The same from the scores that k_chunk_mma left: an item is 256 entries of a row; 64 threads x 4 entries, four groups of
+// threads that take every fourth (query, head). Reads 4 bytes a (query, head, entry) instead of K again.
+__global__ void __launch_bounds__(256) k_chunk_weigh_scores(ChunkAttn a, const float* w_in, float* w_out) {
+  pdl_wait();
+  extern __shared__ long long s_base[];
+  __shared__ long long s_red[33];
+  __shared__ float4 s_sum[4][64];
+  const ChunkDev& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 63, part = tid >> 6;
+  const long long items = weigh_items(c, 256, s_base, s_red), width = (long long)c.max_pages * 64;
+  for (long long item = blockIdx.x; item < items; item += gridDim.x) {
+    const int b = item_row(s_base, c.n, item);
+    const ChunkRow r = chunk_row(c, b);
+    const int e = (int)(item - s_base[b]) * 256 + lane * 4, s0 = r.len - r.ql;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (e < r.len) {
+      // query i sees entries up to s0 + i
+      const int i0 = max(0, e - s0), n = (r.ql - i0) * c.Hq;
+      for (int j = part; j < n; j += 4) {
+        const long long at = (long long)(r.t0 + i0) * c.Hq + j;
+        const float l = a.lse[at] * LOG2E;
+        const float4 s = *reinterpret_cast<const float4*>(a.scores + at * width + e);
+        const int see = s0 + i0 + j / c.Hq - e;
+        sum.x += exp2f(s.x - l);
+        if (see >= 1) sum.y += exp2f(s.y - l);
+        if (see >= 2) sum.z += exp2f(s.z - l);
+        if (see >= 3) sum.w += exp2f(s.w - l);
+      }
+    }
+    __syncthreads();
+    s_sum[part][lane] = sum;
+    __syncthreads();
+    if (part == 0 && e < r.len) {
+      const int page = chunk_page(c.page_table, c.max_pages, c.n_pages, b, e / 64, c.err);
+      if (page < 0) continue;
+      const float4 x = s_sum[1][lane], y = s_sum[2][lane], z = s_sum[3][lane];
+      const float add[4] = {(sum.x + x.x) + (y.x + z.x), (sum.y + x.y) + (y.y + z.y), (sum.z + x.z) + (y.z + z.z), (sum.w + x.w) + (y.w + z.w)};
+      const long long at = (long long)page * 64 + e % 64;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (e + k < r.len) w_out[at + k] = (w_in ? w_in[at + k] : 0.f) + add[k];
+    }
+  }
+  pdl_trigger();
+}
+
+// ----------------------------------------------------------------------------
+// Weights on tcgen05 (bfloat16, head_dim 64 and 128, many rows)
+// ----------------------------------------------------------------------------
+// S^T = K Q^T with the keys as MMA rows: a thread owns one key (TMEM lane) and adds exp(s - lse) over the columns, which are
+// query rows, so sums need no exchange between threads and no atomics. A CTA goes over its units of the flat order (row, block
+// of 256 keys, head, tile of 128 query rows); K of a (block, head) stays in shared memory while the tiles of q stream through.
+//   warps 0-3, 4-7  keys 0-127 and 128-255 of the block: S from tensor memory, sums, the block's sums out at its end;
+//   warp 8          producer (tensor maps);  warp 9  issues S^T into one of two pairs of TMEM buffers;
+//   warp 10         the tile's lse into shared memory.
+// A block inside one CTA's share is written out; parts of a shared one meet in k_weigh_join, in the CTAs' order.
+constexpr int WEIGH_THREADS = 352;
+struct WeighTc {
+  WeighSplit sp;
+  const float* w_in;
+  float* w_out;
+  float* part;  // [2 ctas][256]
+};
+template <int HD>
+struct WeighShape {
+  static constexpr int ATOMS = HD / 64, COL = 128 * 128, T_BYTES = ATOMS * COL;
+  static constexpr int NQ = HD == 128 ? 2 : 6;
+  static constexpr int OFF_Q = 4 * T_BYTES;  // K: two buffers of two tiles
+  static constexpr int OFF_LSE = OFF_Q + NQ * T_BYTES, OFF_BAR = OFF_LSE + 2 * 128 * 4, NBAR = 4 + 2 * NQ + 6;
+  static constexpr int OFF_INT = OFF_BAR + NBAR * 8, OFF_BASE = OFF_INT + 16;
+  static int bytes(int n) { return std::max(OFF_BASE + (n + 1) * 8 + 1024, tmem_min_smem(512)); }
+};
+
+__device__ __forceinline__ long long weigh_plan(const ChunkDev& c, const WeighSplit& sp, long long* base, long long* red) {
+  long long carry = 0;
+  for (int b0 = 0; b0 < c.n; b0 += blockDim.x) {
+    const int b = b0 + threadIdx.x;
+    long long u = 0;
+    if (b < c.n) {
+      const ChunkRow r = chunk_row(c, b);
+      u = sp.before(r.len - r.ql, r.ql, sp.blocks(r.len - r.ql, r.ql)) * c.Hkv;
+    }
+    long long total;
+    const long long at = carry + block_scan(u, red, &total);
+    if (b < c.n) base[b] = at;
+    carry += total;
+  }
+  if (threadIdx.x == 0) base[c.n] = carry;
+  __syncthreads();
+  return carry;
+}
+struct WeighBlock {
+  int b, kb, t0, s0, ql, len, first, vis;  // row, block; the row's tokens and entries; the block's first tile, tiles
+  long long begin;                         // its first unit in the flat order; it has vis * Hkv
+};
+__device__ __forceinline__ WeighBlock weigh_block(const ChunkDev& c, const WeighSplit& sp, const long long* base, long long pos) {
+  WeighBlock w;
+  w.b = item_row(base, c.n, pos);
+  const ChunkRow r = chunk_row(c, w.b);
+  w.t0 = r.t0;
+  w.ql = r.ql;
+  w.len = r.len;
+  w.s0 = r.len - r.ql;
+  w.kb = sp.block_of(w.s0, w.ql, c.Hkv, pos - base[w.b]);
+  w.first = sp.first(w.s0, w.kb);
+  w.vis = sp.tiles(w.ql) - w.first;
+  w.begin = base[w.b] + sp.before(w.s0, w.ql, w.kb) * c.Hkv;
+  return w;
+}
+
+template <int HD>
+__global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, WeighTc wt, int g_log, const __grid_constant__ CUtensorMap q_map,
+                                                               const __grid_constant__ CUtensorMap pool_map) {
+  using Sh = WeighShape<HD>;
+  constexpr int NQ = Sh::NQ;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ long long s_red[33];
+  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sm + Sh::OFF_BAR);
+  float* s_lse = reinterpret_cast<float*>(sm + Sh::OFF_LSE);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + Sh::OFF_INT);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + Sh::OFF_INT) + 1;
+  long long* s_base = reinterpret_cast<long long*>(sm + Sh::OFF_BASE);
+  auto bar = [&](int i) { return smem_u32(&bars[i]); };
+  auto k_full = [&](unsigned i) { return bar(i & 1); };
+  auto k_empty = [&](unsigned i) { return bar(2 + (i & 1)); };
+  auto q_full = [&](unsigned i) { return bar(4 + i % NQ); };
+  auto q_empty = [&](unsigned i) { return bar(4 + NQ + i % NQ); };
+  auto s_full = [&](unsigned i) { return bar(4 + 2 * NQ + (i & 1)); };
+  auto s_read = [&](unsigned i) { return bar(4 + 2 * NQ + 2 + (i & 1)); };
+  auto l_full = [&](unsigned i) { return bar(4 + 2 * NQ + 4 + (i & 1)); };
+  const ChunkDev& c = a.c;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < 4 + 2 * NQ; ++i) mbar_init(bar(i), 1);
+    for (unsigned i = 0; i < 2; ++i) {
+      mbar_init(s_full(i), 1);
+      mbar_init(s_read(i), 8);
+      mbar_init(l_full(i), 1);
+    }
+    *abort_flag = 0;
+    fence_barrier_init();
+    prefetch_tensormap(&q_map);
+    prefetch_tensormap(&pool_map);
+  }
+  if (warp == 9) {
+    tmem_alloc(smem_u32(tmem_slot), 512);
+    tmem_relinquish();
+  }
+  pdl_wait();
+  const long long all = weigh_plan(c, wt.sp, s_base, s_red);
+  tc_fence_before();
+  __syncthreads();  // barriers initialised, tensor memory allocated
+  tc_fence_after();
+  pdl_trigger();
+  const uint32_t tmem = *tmem_slot;
+  const long long per = chunk_share(a, all);
+  long long pos = blockIdx.x * per;
+  const long long end = pos + per < all ? pos + per : all;
+  const int QT = 1 << wt.sp.qt_log;
+  auto wait = [&](uint32_t b, uint32_t parity) {
+    if (*abort_flag) return false;
+    if (mbar_wait(b, parity & 1u, a.werr)) return true;
+    *abort_flag = 1;
+    return false;
+  };
+  // f(block, head, tile, unit's number in this CTA, first unit of its K here, last one) for this CTA's units; false ends it
+  auto each = [&](auto&& f, auto&& block_end) {
+    unsigned n = 0;
+    while (pos < end) {
+      const WeighBlock w = weigh_block(c, wt.sp, s_base, pos);
+      const long long stop = w.begin + (long long)w.vis * c.Hkv < end ? w.begin + (long long)w.vis * c.Hkv : end, start = pos;
+      int h = (int)((pos - w.begin) / w.vis), t = (int)((pos - w.begin) % w.vis);
+      for (bool k_new = true; pos < stop; ++pos, ++n) {
+        const bool k_last = t + 1 == w.vis || pos + 1 == stop;
+        if (!f(w, h, w.first + t, n, k_new, k_last)) return;
+        k_new = k_last;
+        if (++t == w.vis) t = 0, ++h;
+      }
+      if (!block_end(w, start, stop)) return;
+    }
+  };
+  auto no_end = [](const WeighBlock&, long long, long long) { return true; };
+
+  if (warp == 8) {
+    unsigned kl = 0;
+    each([&](const WeighBlock& w, int h, int t, unsigned n, bool k_new, bool) {
+      bool ok = true;
+      if (k_new) {
+        const int p = min(w.kb * 4 + (lane & 3), (w.len - 1) / 64);
+        int mine = chunk_page(c.page_table, c.max_pages, c.n_pages, w.b, p, lane < 4 ? c.err : nullptr);
+        mine = max(mine, 0);  // reported; what it adds goes nowhere
+        int pg[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pg[i] = __shfl_sync(0xffffffffu, mine, i);
+        if (lane == 0 && (kl < 2 || (ok = wait(k_empty(kl), kl / 2 - 1)))) {
+          mbar_arrive_expect_tx(k_full(kl), 2 * Sh::T_BYTES);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < Sh::ATOMS; ++k)
+              tma_load_3d(smem_u32(sm + ((kl & 1) * 2 + i / 2) * Sh::T_BYTES + k * Sh::COL + (i & 1) * (Sh::COL / 2)), &pool_map, k * 64,
+                          (c.layer * 2 * c.Hkv + h) * 64, pg[i], k_full(kl));
+        }
+        ++kl;
+      }
+      if (lane == 0 && ok && (n < NQ || (ok = wait(q_empty(n), n / NQ - 1)))) {
+        mbar_arrive_expect_tx(q_full(n), Sh::T_BYTES);
+#pragma unroll
+        for (int k = 0; k < Sh::ATOMS; ++k)
+          tma_load_3d(smem_u32(sm + Sh::OFF_Q + (n % NQ) * Sh::T_BYTES + k * Sh::COL), &q_map, k * 64, h << g_log, w.t0 + t * QT, q_full(n));
+      }
+      return (bool)__all_sync(0xffffffffu, ok);
+    }, no_end);
+  } else if (warp == 9) {
+    if (lane == 0) {
+      constexpr uint32_t IDS = idesc_bf16_f32(128, 128);
+      constexpr uint64_t T_E = Sh::T_BYTES >> 4, COL_E = Sh::COL >> 4;
+      const uint64_t dk = smem_desc_sw128(smem_u32(sm)), dq = smem_desc_sw128(smem_u32(sm + Sh::OFF_Q));
+      unsigned kl = 0;
+      each([&](const WeighBlock&, int, int, unsigned n, bool k_new, bool k_last) {
+        if (k_new && !wait(k_full(kl), kl / 2)) return false;
+        if (!wait(q_full(n), n / NQ) || (n >= 2 && !wait(s_read(n), n / 2 - 1))) return false;
+        tc_fence_after();
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int kc = 0; kc < Sh::ATOMS; ++kc)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              tc_mma_f16(tmem + (n & 1) * 256 + 128u * x, dk + ((kl & 1) * 2 + x) * T_E + kc * COL_E + 2 * k,
+                         dq + (n % NQ) * T_E + kc * COL_E + 2 * k, IDS, (kc | k) ? 1u : 0u);
+        tc_commit(s_full(n));
+        tc_commit(q_empty(n));
+        if (k_last) {
+          tc_commit(k_empty(kl));
+          ++kl;
+        }
+        return true;
+      }, no_end);
+    }
+    __syncwarp();
+  } else if (warp == 10) {
+    each([&](const WeighBlock& w, int h, int t, unsigned n, bool, bool) {
+      if (n >= 2 && !__all_sync(0xffffffffu, wait(s_read(n), n / 2 - 1))) return false;
+      const int cols = min(QT, w.ql - t * QT) << g_log;
+#pragma unroll
+      for (int j = lane; j < 128; j += 32) {
+        float l = 0.f;
+        if (j < cols) l = a.lse[(long long)(w.t0 + t * QT + (j >> g_log)) * c.Hq + (h << g_log) + (j & ((1 << g_log) - 1))] * LOG2E;
+        s_lse[(n & 1) * 128 + j] = l;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(l_full(n));
+      return true;
+    }, no_end);
+  } else {
+    const int x = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t t_s = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 128u * (uint32_t)x;
+    const float scale = a.scale;
+    float sum = 0.f;
+    each([&](const WeighBlock& w, int, int t, unsigned n, bool, bool) {
+      if (!__all_sync(0xffffffffu, wait(s_full(n), n / 2) && wait(l_full(n), n / 2))) return false;
+      tc_fence_after();
+      const int key = w.kb * 256 + x * 128 + row, cols = min(QT, w.ql - t * QT) << g_log;
+      // query i of the row sees the key when s0 + i >= key: columns from lo on
+      const long long lo = ((long long)key - w.s0 - (long long)t * QT) << g_log;
+      const bool cut = cols < 128 || __any_sync(0xffffffffu, lo > 0);
+      const float* l = s_lse + (n & 1) * 128;
+      float p4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+      for (int c0 = 0; c0 < cols; c0 += 64) {
+        uint32_t su[64];
+        tmem_ld_32_issue(t_s + (n & 1) * 256 + (uint32_t)c0, su);
+        tmem_ld_32_issue(t_s + (n & 1) * 256 + (uint32_t)c0 + 32, su + 32);
+        tmem_ld_wait();
+        if (!cut) {
+#pragma unroll
+          for (int j = 0; j < 64; j += 4) {
+            const float4 v = *reinterpret_cast<const float4*>(l + c0 + j);
+            p4[0] += ex2_fast(fmaf(__uint_as_float(su[j]), scale, -v.x));
+            p4[1] += ex2_fast(fmaf(__uint_as_float(su[j + 1]), scale, -v.y));
+            p4[2] += ex2_fast(fmaf(__uint_as_float(su[j + 2]), scale, -v.z));
+            p4[3] += ex2_fast(fmaf(__uint_as_float(su[j + 3]), scale, -v.w));
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 64; ++j)
+            if (c0 + j >= lo && c0 + j < cols) p4[j & 3] += ex2_fast(fmaf(__uint_as_float(su[j]), scale, -l[c0 + j]));
+        }
+      }
+      sum += (p4[0] + p4[1]) + (p4[2] + p4[3]);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(s_read(n));
+      return true;
+    }, [&](const WeighBlock& w, long long start, long long stop) {
+      const int key = w.kb * 256 + x * 128 + row;
+      if (start != w.begin || stop != w.begin + (long long)w.vis * c.Hkv) {
+        wt.part[(2 * blockIdx.x + (start == w.begin)) * 256 + x * 128 + row] = sum;
+      } else if (key < w.len) {
+        const int page = chunk_page(c.page_table, c.max_pages, c.n_pages, w.b, key / 64, nullptr);
+        const long long at = (long long)page * 64 + key % 64;
+        if (page >= 0) wt.w_out[at] = (wt.w_in ? wt.w_in[at] : 0.f) + sum;
+      }
+      sum = 0.f;
+      return true;
+    });
+  }
+  if (*abort_flag) drain_copies();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) tmem_dealloc(tmem, 512);
+}
+
+// Blocks that k_weigh_tc's CTAs share: the first CTA whose share starts inside one adds its parts (grid x < ctas - 1). The
+// other CTAs of the grid copy the weights of rows without new tokens.
+__global__ void __launch_bounds__(256) k_weigh_join(ChunkAttn a, WeighTc wt, int per_row) {
+  pdl_wait();
+  extern __shared__ long long s_base[];
+  __shared__ long long s_red[33];
+  const ChunkDev& c = a.c;
+  if ((int)blockIdx.x >= a.ctas - 1) {
+    const int i = blockIdx.x - (a.ctas - 1), b = i / per_row;
+    const ChunkRow r = chunk_row(c, b);
+    if (r.ql > 0) return;
+    for (int e = (i % per_row) * 256 + threadIdx.x; e < r.len; e += per_row * 256) {
+      const int page = chunk_page(c.page_table, c.max_pages, c.n_pages, b, e / 64, c.err);
+      const long long at = (long long)page * 64 + e % 64;
+      if (page >= 0) wt.w_out[at] = wt.w_in ? wt.w_in[at] : 0.f;
+    }
+    return;
+  }
+  const long long all = weigh_plan(c, wt.sp, s_base, s_red), per = chunk_share(a, all), pos = (blockIdx.x + 1) * per;
+  if (pos >= all) return;
+  const WeighBlock w = weigh_block(c, wt.sp, s_base, pos);
+  if (w.begin == pos || w.begin / per != blockIdx.x) return;
+  const int c0 = blockIdx.x, c1 = (int)((w.begin + (long long)w.vis * c.Hkv - 1) / per), key = w.kb * 256 + threadIdx.x;
+  float sum = wt.part[(2 * c0 + 1) * 256 + threadIdx.x];
+  for (int i = c0 + 1; i <= c1; ++i) sum += wt.part[2 * i * 256 + threadIdx.x];
+  if (key >= w.len) return;
+  const int page = chunk_page(c.page_table, c.max_pages, c.n_pages, w.b, key / 64, c.err);
+  const long long at = (long long)page * 64 + key % 64;
+  if (page >= 0) wt.w_out[at] = (wt.w_in ? wt.w_in[at] : 0.f) + sum;
+}
+
 // ----------------------------------------------------------------------------
 // Launches
 // ----------------------------------------------------------------------------
@@ -1246,7 +1618,8 @@ struct ChunkPath {
   bool pair;    // k_chunk_pair
   int rt;       // rows of an item
   int ctas;
-  size_t part_ml, lse, werr, total;  // scratch offsets (part_o at 0)
+  bool scores;  // k_chunk_mma leaves its scores for the weights
+  size_t part_ml, lse, werr, scores_at, total;  // scratch offsets (part_o at 0)
 };
 static int pow2_log(int x) {  // largest l with 2^l <= x
   int l = 0;
@@ -1271,6 +1644,11 @@ static ChunkPath chunk_path(const ChunkDev& c, int dtype, const tlf_attn_chunk_a
   p.part_ml = take((size_t)2 * p.ctas * p.rt * 8);
   p.lse = take(a.weight_out && !a.lse ? (size_t)c.T * c.Hq * 4 : 0);
   p.werr = take(4);
+  // 4 bytes a (query, head, entry): less than reading K again while G x new tokens is below head_dim / 2, and the same kernel
+  // then serves all rows; a bound on the scratch, which the host can only size by the longest row
+  const long long score_bytes = (long long)c.T * c.Hq * c.max_pages * 256;
+  p.scores = dtype == TLF_DTYPE_BF16 && a.weight_out && !p.pair && score_bytes <= (256LL << 20);
+  p.scores_at = take(p.scores ? (size_t)score_bytes : 0);
   p.total = o;
   return p;
 }
@@ -1315,6 +1693,19 @@ static cudaError_t pair_launch(const ChunkAttn& a, cudaStream_t st) {
   if (cudaError_t e = ensure_kernel_attrs(reinterpret_cast<const void*>(k_chunk_pair<HD>), Sh::bytes(SV_MAX_ROWS))) return e;
   return launch_k(k_chunk_pair<HD>, dim3(a.ctas), dim3(PAIR_THREADS), Sh::bytes(a.c.n), st, a, pow2_log(a.c.G), qm, pm);
 }
+// The weights behind k_chunk_pair; the parts lie where the attention's were (k_chunk_join has read them).
+template <int HD>
+static cudaError_t weigh_launch(const ChunkAttn& a, const tlf_attn_chunk_args& args, cudaStream_t st) {
+  CUtensorMap qm, pm;
+  if (!q_map(&qm, a) || !pool_map(&pm, a.c)) return cudaErrorInvalidValue;
+  using Sh = WeighShape<HD>;
+  if (cudaError_t e = ensure_kernel_attrs(reinterpret_cast<const void*>(k_weigh_tc<HD>), Sh::bytes(SV_MAX_ROWS))) return e;
+  const WeighTc w{WeighSplit{a.sp.qt_log - 1, 8}, args.weight_in, args.weight_out, a.part_o};
+  if (cudaError_t e = launch_k(k_weigh_tc<HD>, dim3(a.ctas), dim3(WEIGH_THREADS), Sh::bytes(a.c.n), st, a, w, pow2_log(a.c.G), qm, pm))
+    return e;
+  const int per_row = std::max(1, std::min(8, 1024 / a.c.n));
+  return launch_k(k_weigh_join, dim3(a.ctas - 1 + per_row * a.c.n), dim3(256), (a.c.n + 1) * 8, st, a, w, per_row);
+}
 template <int HD, int MT>
 static cudaError_t mma_launch(const ChunkAttn& a, cudaStream_t st) {
   CUtensorMap map;
@@ -1345,6 +1736,9 @@ static cudaError_t chunk_launch(const ChunkAttn& a, const tlf_attn_chunk_args& a
   if (cudaError_t j = launch_k(k_chunk_join<T>, dim3(a.ctas - 1, (a.rows + 7) / 8), dim3(256), base, st, a)) return j;
   if (!args.weight_out) return cudaSuccess;
   const dim3 grid(4 * num_sms);
+  if constexpr (std::is_same<T, bf16>::value)
+    if (a.rows == 256) return a.c.hd == 64 ? weigh_launch<64>(a, args, st) : weigh_launch<128>(a, args, st);
+  if (a.scores) return launch_k(k_chunk_weigh_scores, grid, dim3(256), base, st, a, args.weight_in, args.weight_out);
   switch (a.c.hd) {
     case 16: return launch_k(k_chunk_weigh<T, 16>, grid, dim3(256), base, st, a, args.weight_in, args.weight_out);
     case 32: return launch_k(k_chunk_weigh<T, 32>, grid, dim3(256), base, st, a, args.weight_in, args.weight_out);
@@ -1373,6 +1767,7 @@ cudaError_t launch_chunk_attn(const ChunkDev& c, int dtype, const tlf_attn_chunk
   a.ctas = p.ctas;
   a.rows = p.rt;
   a.min_blocks = 1;
+  a.scores = p.scores ? reinterpret_cast<float*>(s + p.scores_at) : nullptr;
   a.werr = c.err ? c.err : reinterpret_cast<uint32_t*>(s + p.werr);
   a.part_o = reinterpret_cast<float*>(s);
   a.part_ml = reinterpret_cast<float2*>(s + p.part_ml);

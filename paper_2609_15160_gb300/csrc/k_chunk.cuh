@@ -55,4 +55,39 @@ struct ChunkSplit {
   }
 };
 
+// The split of the tensor-core weights (k_weigh_tc): a row's cache in blocks of 2^bk_log entries, its queries in tiles of
+// 2^qt_log <= 2^bk_log. A unit is one tile that sees something of a block, for one kv head; the flat order is (row, block,
+// head, tile), shared out like the above. Tile t sees block kb when its last query sees the block's first entry:
+// t >= first(kb), the tile of query kb 2^bk_log - s0.
+struct WeighSplit {
+  int qt_log, bk_log;
+
+  __host__ __device__ int tiles(int ql) const { return (ql + (1 << qt_log) - 1) >> qt_log; }
+  __host__ __device__ int blocks(int s0, int ql) const {  // a row without new tokens has none
+    return ql > 0 && s0 + ql > 0 ? (s0 + ql + (1 << bk_log) - 1) >> bk_log : 0;
+  }
+  __host__ __device__ int first(int s0, int kb) const {
+    const long long t = ((long long)kb << (bk_log - qt_log)) + ((-(long long)s0) >> qt_log);
+    return t > 0 ? (int)t : 0;
+  }
+  // units of one head in the row's first n blocks
+  __host__ __device__ long long before(int s0, int ql, int n) const {
+    const int ml = bk_log - qt_log;
+    const long long a = -((-(long long)s0) >> qt_log);         // first(kb) = max(0, kb 2^ml - a)
+    long long k0 = a < 0 ? 0 : (a >> ml) + 1;                  // blocks with first = 0
+    if (k0 > n) k0 = n;
+    return (long long)n * tiles(ql) - ((((long long)n * (n - 1) - k0 * (k0 - 1)) / 2 << ml) - (n - k0) * a);
+  }
+  // the block that holds unit `at` of the row (all heads)
+  __host__ __device__ int block_of(int s0, int ql, int heads, long long at) const {
+    int lo = 0, hi = blocks(s0, ql);
+    while (hi - lo > 1) {
+      const int mid = lo + (hi - lo) / 2;
+      if (before(s0, ql, mid) * heads <= at) lo = mid;
+      else hi = mid;
+    }
+    return lo;
+  }
+};
+
 }  // namespace tlf

@@ -183,6 +183,22 @@ int main() {
         sum += want;
       }
     }
+  for (int it = 0; it < 6000; ++it) {
+    const tlf::WeighSplit s{1 + rand() % 7, 8};
+    const int ql = rand() % 700, any = it % 5 ? rand() % 1500 - 700 : rand() % 100000, s0 = any < -ql ? -ql : any, nb = s.blocks(s0, ql);
+    const int nt = (ql + (1 << s.qt_log) - 1) >> s.qt_log, heads = 1 + rand() % 8;
+    if (nb != (ql > 0 ? (s0 + ql + 255) / 256 : 0)) return 5;
+    long long sum = 0;
+    for (int kb = 0; kb <= nb; ++kb) {
+      if (s.before(s0, ql, kb) != sum) return 6;
+      if (kb == nb) break;
+      int first = 0;  // the first tile whose last query (whole tiles) sees entry 256 kb
+      while (s0 + ((first + 1) << s.qt_log) - 1 < 256 * kb) ++first;
+      if (s.first(s0, kb) != first || first >= nt) return 7;
+      if (s.block_of(s0, ql, heads, sum * heads) != kb || s.block_of(s0, ql, heads, (sum + nt - first) * heads - 1) != kb) return 8;
+      sum += nt - first;
+    }
+  }
   printf("ok\n");
   return 0;
 }
