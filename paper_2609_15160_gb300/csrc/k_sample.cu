@@ -5,12 +5,13 @@
 // a threshold key, or equal to it and early enough among the equal ones. Among the kept, argmax of z_i - log(-log u_i) draws i
 // with probability w_i / sum of the kept w: only kept tokens need their random number, and no sum decides between two of them.
 //
-// Three passes over the row (the second and third find it in L2): maximum; sum of w; candidates. Candidates are a superset of
-// the kept tokens that is small for the usual limits: with top-k <= 1024 the tokens not below the k-th largest of the
-// threads' maxima, with top-p those that weigh at least (1 - top_p) sum / V (all lighter ones together weigh less than
-// 1 - top_p of the sum), with min-p those not below it. The threshold is then a radix select over the candidates' keys: by
-// count for top-k, by weight for top-p. Weights are added in 2^-40 fixed point, so the order of the atomics does not matter.
-// Where the candidates are too many for the list (flat logits), the same steps run over the whole row.
+// Passes over the row (all but the first find it in L2): the maximum; the sum of w, with a histogram of the tokens over bins
+// of z of width 1/16; the candidates. Candidates are the bins that top-k or top-p can reach: by count for top-k, and for top-p
+// by the least that the bins' tokens can weigh. They are few for the usual limits and go to a list in shared memory, where a
+// radix select over the keys finds the threshold: by count for top-k, by weight for top-p. Weights are then added in 2^-40
+// fixed point, so the order of the atomics does not matter. When top-p alone leaves too many candidates (flat logits), the
+// bins' weights are added up in a pass of their own, which leaves the one bin with the threshold for the list; what lies above
+// it takes part in the draw at once. Where that is too much for the list too, the select goes over the whole row.
 #include "k_serve.cuh"
 
 namespace tlf {
@@ -47,27 +48,59 @@ __device__ __forceinline__ float sample_unkey(uint32_t k) {
 }
 __device__ __forceinline__ u64 sample_mass(float w) { return __float2ull_rn(w * 1099511627776.f); }  // w in 0..1
 
+constexpr int SM_BINS = 512;
+constexpr float SM_BIN = 16.f;  // bins per unit of z; the last bin holds the rest
+// Bin of a token, rounded to nearest: bin i holds z in -(i + 1/2) / 16 .. -(i - 1/2) / 16.
+__device__ __forceinline__ int sample_bin(float z) {
+  return (int)(__float_as_uint(fminf(z * -SM_BIN, (float)(SM_BINS - 1)) + 8388608.f) & 0x3ffu);
+}
+
+// f(logit, index) over the row, all threads taking part in every step; index -1: nothing.
+template <typename F>
+__device__ __forceinline__ void sample_pass(const float* row, int V, bool wide, F&& f) {
+  if (wide) {
+    for (int i0 = 0; i0 < V; i0 += 4 * SM_THREADS) {
+      const int i = i0 + 4 * threadIdx.x;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (i + 3 < V) v = *reinterpret_cast<const float4*>(row + i);
+      else if (i < V) v = make_float4(row[i], i + 1 < V ? row[i + 1] : 0.f, i + 2 < V ? row[i + 2] : 0.f, 0.f);
+      f(sample_logit(v.x), i < V ? i : -1);
+      f(sample_logit(v.y), i + 1 < V ? i + 1 : -1);
+      f(sample_logit(v.z), i + 2 < V ? i + 2 : -1);
+      f(sample_logit(v.w), i + 3 < V ? i + 3 : -1);
+    }
+  } else {
+    for (int i0 = 0; i0 < V; i0 += SM_THREADS) {
+      const int i = i0 + threadIdx.x;
+      f(i < V ? sample_logit(row[i]) : -INFINITY, i < V ? i : -1);
+    }
+  }
+}
+
 __global__ void __launch_bounds__(SM_THREADS) k_sample(SampleDev a) {
   pdl_wait();
   __shared__ uint32_t s_key[SM_LIST];
   __shared__ int s_idx[SM_LIST];
-  __shared__ u64 s_mass[256];
+  __shared__ unsigned s_bin[SM_BINS];
+  __shared__ u64 s_mass[SM_BINS];  // of a bin, or of a digit of the select
   __shared__ unsigned s_cnt[256];
   __shared__ float s_redf[33];
   __shared__ int s_redi[33];
   __shared__ u64 s_redl[33];
-  __shared__ int s_n;
-  __shared__ uint32_t s_prefix;
+  __shared__ int s_n, s_pick;
+  __shared__ uint32_t s_lo, s_hi, s_prefix;
   __shared__ unsigned s_need, s_hit;
   __shared__ u64 s_above;
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = a.V;
   const float* row = a.logits + b * a.ls;
+  const float* noise = a.noise + b * a.ns;
+  const bool wide = reinterpret_cast<uintptr_t>(row) % 16 == 0;
 
   float mx = -INFINITY;
-  for (int i = tid; i < V; i += SM_THREADS) mx = fmaxf(mx, sample_logit(row[i]));
-  const float mine = mx;  // this thread's largest
+  sample_pass(row, V, wide, [&](float l, int i) { mx = fmaxf(mx, i >= 0 ? l : -INFINITY); });
   mx = warp_max(mx);
   if (lane == 0) s_redf[warp] = mx;
+  if (tid < SM_BINS) s_bin[tid] = 0;
   if (tid == 0) s_n = 0;
   __syncthreads();
   mx = warp_max(s_redf[lane]);
@@ -82,84 +115,153 @@ __global__ void __launch_bounds__(SM_THREADS) k_sample(SampleDev a) {
   const float temp = a.temperature ? a.temperature[b] : 1.f;
   float min_p = a.min_p ? a.min_p[b] : 0.f;
   const double top_p = a.top_p && a.top_p[b] < 1.f ? (double)a.top_p[b] : 1.0;
-  const float T = temp > 0.f ? temp : 1.f;
+  const float T = temp > 0.f ? fmaxf(temp, 1.2e-38f) : 1.f, rT = 1.f / T;
   int k = a.top_k ? a.top_k[b] : 0;
   k = k <= 0 || k > V ? V : k;
   if (!(temp > 0.f) || top_p <= 0.0 || !(min_p <= 1.f)) {  // only the first token
     k = 1;
     min_p = 0.f;
   }
+  const bool by_k = k < V, by_p = top_p < 1.0 && k > 1;
+  // z as the definition has it, for what decides; times 1 / T for sums and bins
   auto z_of = [&](float l) { return (l - mx) / T; };
-  auto w_of = [&](float l) { return l > -INFINITY ? expf(z_of(l)) : 0.f; };
+  auto zq_of = [&](float l) { return l > -INFINITY ? fmaxf((l - mx) * rT, -INFINITY) : -INFINITY; };
+  auto mass_of = [&](uint32_t key) { return sample_mass(expf(z_of(sample_unkey(key)))); };
 
   float sum = 0.f;
-  u64 mass = 0;  // of all tokens; needed by top-p without top-k
-  for (int i = tid; i < V; i += SM_THREADS) {
-    const float w = w_of(sample_logit(row[i]));
-    sum += w;
-    mass += sample_mass(w);
+  if (by_k || by_p) {
+    sample_pass(row, V, wide, [&](float l, int i) {
+      const float z = i >= 0 ? zq_of(l) : -INFINITY;
+      sum += ex2_fast(z * 1.4426950408889634f);
+      const int bin = sample_bin(z);
+      if (bin < SM_BINS - 1) atomicAdd(&s_bin[bin], 1u);
+    });
+  } else {
+    sample_pass(row, V, wide, [&](float l, int i) { sum += i >= 0 ? ex2_fast(zq_of(l) * 1.4426950408889634f) : 0.f; });
   }
   sum = block_sum(sum, s_redf);
-  mass = block_sum(mass, s_redl);
 
-  // candidates: keys from `cand` on, z from `zc` on
-  const bool by_k = k < V, by_p = top_p < 1.0;
-  uint32_t cand = SAMPLE_NEVER + 1;
-  float zc = -INFINITY;
-  bool limited = false;
-  if (by_k && k <= SM_THREADS) {
-    // k-th largest of the threads' maxima, bit by bit: the largest x with at least k of them at or above it
-    const uint32_t own = sample_key(mine);
-    uint32_t x = 0;
-    for (int bit = 31; bit >= 0; --bit)
-      if (__syncthreads_count(own >= (x | 1u << bit)) >= k) x |= 1u << bit;
-    cand = max(cand, x);  // fewer than k threads with a token that can be drawn: all tokens
-    limited = true;
-  } else if (!by_k) {
-    // what the lighter tokens weigh together, each rounded up, stays below the part that top-p leaves out
-    const double light = by_p ? (1.0 - top_p) * (double)mass / V - 1.0 : 0.0;
-    if (light > 0.0) zc = logf((float)(light / 1099511627776.0)) - 1e-3f;
-    if (min_p > 0.f) zc = fmaxf(zc, logf(min_p) - 1e-3f);
-    limited = zc > -INFINITY;
-  }
-  bool list = limited;
-  if (limited) {
-    for (int i0 = 0; i0 < V; i0 += SM_THREADS) {
-      const int i = i0 + tid;
-      const float l = i < V ? sample_logit(row[i]) : -INFINITY;
-      const uint32_t key = sample_key(l);
-      const bool is = key >= cand && (zc == -INFINITY || z_of(l) >= zc);
-      const unsigned in = __ballot_sync(0xffffffffu, is);
-      if (in) {
+  // the draw: largest z - log(-log u), ties to the lower index
+  float best = -INFINITY;
+  int token = V;
+  auto race = [&](float l, int idx) {
+    const float z = z_of(l);
+    if (min_p > 0.f && l != mx && !(expf(z) >= min_p)) return;
+    float score = z - logf(-logf(noise[idx]));
+    if (!(score == score)) score = -INFINITY;
+    if (score > best || (score == best && idx < token)) {
+      best = score;
+      token = idx;
+    }
+  };
+  // the first bin (from the heaviest tokens on) at which `reached` holds for the values up to it; SM_BINS - 1 if none
+  auto first_bin = [&](auto value, auto reached) {
+    if (tid == 0) s_pick = SM_BINS - 1;
+    auto v = value(tid);  // one bin a thread; threads past the bins add nothing
+    decltype(v) before = block_scan(v, reinterpret_cast<decltype(v)*>(s_redl), (decltype(v)*)nullptr);
+    if (tid < SM_BINS - 1 && !reached(before) && reached(before + v)) s_pick = tid;
+    __syncthreads();
+    return s_pick;
+  };
+  // all tokens of bins first .. last into the list; tokens of bins before `first` take part in the draw
+  auto gather = [&](int first, int last) {
+    sample_pass(row, V, wide, [&](float l, int i) {
+      const int bin = i >= 0 && l > -INFINITY ? sample_bin(zq_of(l)) : SM_BINS;
+      if (bin < first) race(l, i);
+      const bool in = bin >= first && bin <= last;
+      const unsigned who = __ballot_sync(0xffffffffu, in);
+      if (who) {
         int at = 0;
-        if (lane == 0) at = atomicAdd(&s_n, __popc(in));
-        at = __shfl_sync(0xffffffffu, at, 0) + __popc(in & ((1u << lane) - 1u));
-        if (is && at < SM_LIST) {
-          s_key[at] = key;
+        if (lane == 0) at = atomicAdd(&s_n, __popc(who));
+        at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1u));
+        if (in && at < SM_LIST) {
+          s_key[at] = sample_key(l);
           s_idx[at] = i;
         }
       }
-    }
+    });
     __syncthreads();
-    list = s_n <= SM_LIST;
+  };
+
+  bool list = false;      // candidates are the list's (else the row's)
+  u64 heavier = 0;        // weight of tokens heavier than the list's, which have taken part in the draw already
+  if (by_k) {
+    const int bin = first_bin([&](int i) { return i < SM_BINS - 1 ? s_bin[i] : 0u; }, [&](unsigned n) { return n >= (unsigned)k; });
+    if (bin < SM_BINS - 1) {
+      gather(0, bin);
+      list = s_n <= SM_LIST;
+    }
+  } else if (by_p) {
+    // a token of bin i weighs at least exp(-(i + 1/2) / 16) (and a little: z is rounded)
+    const float want = (float)top_p * sum * 1.0001f;
+    const int bin = first_bin([&](int i) { return i < SM_BINS - 1 ? s_bin[i] * ex2_fast(-(i + 0.51f) * (1.4426950408889634f / SM_BIN)) : 0.f; },
+                              [&](float m) { return m >= want; });
+    if (bin < SM_BINS - 1) {
+      const int n = block_sum(tid <= bin ? (int)s_bin[tid] : 0, s_redi);
+      if (n <= SM_LIST) {
+        gather(0, bin);
+        list = true;
+      } else {
+        if (tid < SM_BINS) s_mass[tid] = 0;
+        __syncthreads();
+        unsigned* mass32 = reinterpret_cast<unsigned*>(s_mass);
+        sample_pass(row, V, wide, [&](float l, int i) {
+          const int at = i >= 0 && l > -INFINITY ? sample_bin(zq_of(l)) : SM_BINS;
+          if (at > bin) return;
+          const u64 m = mass_of(sample_key(l));
+          const unsigned lo = (unsigned)m, old = atomicAdd(&mass32[2 * at], lo), hi = (unsigned)(m >> 32) + (old + lo < old);
+          if (hi) atomicAdd(&mass32[2 * at + 1], hi);
+        });
+        __syncthreads();
+        const double target = top_p * (double)sample_mass(1.f) * (double)sum;
+        const int at = first_bin([&](int i) { return i <= bin ? s_mass[i] : 0ull; }, [&](u64 m) { return (double)m >= target; });
+        if (at <= bin && s_bin[at] <= SM_LIST) {
+          heavier = block_sum(tid < at ? s_mass[tid] : 0ull, s_redl);
+          gather(at, at);
+          list = true;
+        }
+      }
+    }
   }
   const int n = list ? s_n : V;
   auto key_at = [&](int i) { return list ? s_key[i] : sample_key(sample_logit(row[i])); };
-  auto mass_of = [&](uint32_t key) { return sample_mass(w_of(sample_unkey(key))); };
 
   // Kept: keys above thr, and the first `ties` of the `equal` tokens with key thr.
   uint32_t thr = SAMPLE_NEVER;
   unsigned ties = 0, equal = 0;
-  // Radix select over keys above `from` (a byte a level, from the largest bin on): the bin in which count or weight reaches
-  // what is wanted. By weight, `from` itself stands for `from_ties` tokens. False: not reached, all of them are kept.
+  // Radix select over the candidates' keys above `from`, eight bits of (key - smallest) a level, from the largest digit on: the
+  // key at which count or weight reaches what is wanted. By weight, `from` itself stands for `from_ties` tokens. False: not
+  // reached, all of them are kept.
   auto walk = [&](bool weigh, unsigned want, double target, uint32_t from, unsigned from_ties) {
     if (tid == 0) {
+      s_lo = 0xffffffffu;
+      s_hi = 0;
       s_prefix = 0;
       s_need = want;
       s_hit = 0;
-      s_above = 0;
+      s_above = weigh ? heavier : 0;
     }
-    for (int shift = 24; shift >= 0; shift -= 8) {
+    __syncthreads();
+    uint32_t lo = 0xffffffffu, hi = 0;
+    for (int i = tid; i < n; i += SM_THREADS) {
+      const uint32_t key = key_at(i);
+      if (key <= from && !(from_ties && key == from)) continue;
+      lo = min(lo, key);
+      hi = max(hi, key);
+    }
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    if (lane == 0) {
+      atomicMin(&s_lo, lo);
+      atomicMax(&s_hi, hi);
+    }
+    __syncthreads();
+    lo = s_lo;
+    hi = s_hi;
+    if (lo > hi) return false;
+    int up = 32 - __clz(hi - lo);  // bits that are not settled yet
+    do {
+      const int down = up > 8 ? up - 8 : 0, bits = up - down;
       if (tid < 256) {
         s_cnt[tid] = 0;
         s_mass[tid] = 0;
@@ -170,17 +272,18 @@ __global__ void __launch_bounds__(SM_THREADS) k_sample(SampleDev a) {
       const u64 above0 = s_above;
       for (int i = tid; i < n; i += SM_THREADS) {
         const uint32_t key = key_at(i);
-        if (key <= from || (shift < 24 && (key >> (shift + 8)) != prefix)) continue;
-        const unsigned bin = (key >> shift) & 255u;
-        atomicAdd(&s_cnt[bin], 1u);
-        if (weigh) atomicAdd(&s_mass[bin], mass_of(key));
+        if (key <= from || (u64)(key - lo) >> up != prefix) continue;
+        const unsigned digit = (key - lo) >> down & ((1u << bits) - 1u);
+        atomicAdd(&s_cnt[digit], 1u);
+        if (weigh) atomicAdd(&s_mass[digit], mass_of(key));
       }
-      if (weigh && tid == 0 && from_ties && (shift == 24 || (from >> (shift + 8)) == prefix)) {
-        atomicAdd(&s_cnt[(from >> shift) & 255u], from_ties);
-        atomicAdd(&s_mass[(from >> shift) & 255u], from_ties * mass_of(from));
+      if (weigh && tid == 0 && from_ties && (u64)(from - lo) >> up == prefix) {
+        const unsigned digit = (from - lo) >> down & ((1u << bits) - 1u);
+        atomicAdd(&s_cnt[digit], from_ties);
+        atomicAdd(&s_mass[digit], from_ties * mass_of(from));
       }
       __syncthreads();
-      if (warp == 0) {  // a lane has eight bins, from the largest
+      if (warp == 0) {  // a lane has eight digits, from the largest
         unsigned c[8], cs = 0;
         u64 m[8], ms = 0;
 #pragma unroll
@@ -197,25 +300,27 @@ __global__ void __launch_bounds__(SM_THREADS) k_sample(SampleDev a) {
           if (lane >= o) cb += cy, mb += my;
         }
         cb -= cs;
-        mb -= ms;
-        u64 above = above0 + mb;
+        u64 at = above0 + (mb - ms);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const bool hit = weigh ? (double)above < target && (double)(above + m[i]) >= target : cb < need && cb + c[i] >= need;
+          const bool hit = weigh ? (double)at < target && (double)(at + m[i]) >= target : cb < need && cb + c[i] >= need;
           if (hit) {
-            s_prefix = (prefix << 8) | (unsigned)(255 - 8 * lane - i);
+            s_prefix = (prefix << bits) | (unsigned)(255 - 8 * lane - i);
             s_need = need - cb;
-            s_above = above;
+            s_above = at;
             s_hit = c[i];
           }
           cb += c[i];
-          above += m[i];
+          at += m[i];
         }
       }
       __syncthreads();
-      if (!s_hit) break;
-    }
-    return s_hit != 0;
+      if (!s_hit) return false;
+      up = down;
+    } while (up > 0);
+    if (tid == 0) s_prefix += lo;
+    __syncthreads();
+    return true;
   };
   if (by_k && walk(false, (unsigned)k, 0.0, SAMPLE_NEVER, 0)) {
     thr = s_prefix;
@@ -223,17 +328,17 @@ __global__ void __launch_bounds__(SM_THREADS) k_sample(SampleDev a) {
     equal = s_hit;
   }
   __syncthreads();
-  if (by_p && k > 1) {
-    u64 kept = mass;
+  if (by_p) {
+    double target = top_p * (double)sample_mass(1.f) * (double)sum;
     if (by_k) {
-      kept = 0;
+      u64 kept = 0;
       for (int i = tid; i < n; i += SM_THREADS) {
         const uint32_t key = key_at(i);
         if (key > thr) kept += mass_of(key);
       }
       kept = block_sum(kept, s_redl) + ties * mass_of(thr);
+      target = top_p * (double)kept;
     }
-    const double target = top_p * (double)kept;
     const uint32_t from = thr;
     const unsigned from_ties = ties, from_equal = equal;
     if (walk(true, 0, target, from, from_ties)) {
@@ -258,23 +363,16 @@ __global__ void __launch_bounds__(SM_THREADS) k_sample(SampleDev a) {
     last = s_n;
   }
 
-  // the draw: largest z - log(-log u), ties to the lower index
-  float best = -INFINITY;
-  int token = V;
-  const float* noise = a.noise + b * a.ns;
-  for (int i = tid; i < n; i += SM_THREADS) {
-    const uint32_t key = key_at(i);
-    const int idx = list ? s_idx[i] : i;
-    if (key <= SAMPLE_NEVER || key < thr || (key == thr && idx > last)) continue;
-    const float z = z_of(sample_unkey(key));
-    if (min_p > 0.f && key != sample_key(mx) && !(expf(z) >= min_p)) continue;
-    const float u = noise[idx];
-    float score = z - logf(-logf(u));
-    if (!(score == score)) score = -INFINITY;
-    if (score > best || (score == best && idx < token)) {
-      best = score;
-      token = idx;
+  if (list) {
+    for (int i = tid; i < n; i += SM_THREADS) {
+      const uint32_t key = s_key[i];
+      if (key > thr || (key == thr && s_idx[i] <= last)) race(sample_unkey(key), s_idx[i]);
     }
+  } else {
+    sample_pass(row, V, wide, [&](float l, int i) {
+      const uint32_t key = sample_key(l);
+      if (i >= 0 && key > SAMPLE_NEVER && (key > thr || (key == thr && i <= last))) race(l, i);
+    });
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
