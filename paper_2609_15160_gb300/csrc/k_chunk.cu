@@ -97,8 +97,9 @@ __device__ __forceinline__ ChunkItem chunk_item(const ChunkDev& c, const ChunkSp
 // Joining the parts of shared items
 // ----------------------------------------------------------------------------
 // blockIdx.x + 1 = a CTA whose share starts inside an item; the first such CTA of an item joins it. CTA c's first item has
-// its part at 2c if it began in an earlier share, the part of an item that goes on past its share is at 2c + 1. A warp a row.
-template <typename T>
+// its part at 2c if it began in an earlier share, the part of an item that goes on past its share is at 2c + 1. A warp takes
+// a row at a time, VW dims a lane (hd = 32 VW, or 16 with VW = 1), and every eight-th row of a CTA's.
+template <typename T, int VW>
 __global__ void __launch_bounds__(256) k_chunk_join(ChunkAttn a) {
   pdl_wait();
   extern __shared__ long long s_base[];
@@ -108,40 +109,54 @@ __global__ void __launch_bounds__(256) k_chunk_join(ChunkAttn a) {
   if (pos >= all) return;
   const ChunkItem it = chunk_item(a.c, a.sp, s_base, pos);
   if (it.first == pos || it.first / per != blockIdx.x) return;
-  const int c0 = blockIdx.x, c1 = (int)((it.first + it.nb - 1) / per), parts = c1 - c0 + 1;
-  const int qt = 1 << a.sp.qt_log, rows = min(qt, it.ql - it.t * qt) * a.c.G, lane = threadIdx.x & 31, hd = a.c.hd;
-  const int row = blockIdx.y * 8 + (threadIdx.x >> 5);
-  if (row >= rows) return;
-  auto slot = [&](int i) { return (size_t)(i == 0 ? 2 * c0 + 1 : 2 * (c0 + i)) * a.rows + row; };
-  float m = -INFINITY;
-  for (int i = lane; i < parts; i += 32) m = fmaxf(m, a.part_ml[slot(i)].x);
-  m = warp_max(m);
-  float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int i0 = 0; i0 < parts; i0 += 32) {
-    float w = 0.f;
-    if (i0 + lane < parts) {
-      const float2 ml = a.part_ml[slot(i0 + lane)];
-      w = exp2f(ml.x - (m == -INFINITY ? 0.f : m));
-      l += w * ml.y;
-    }
-    const int n = min(32, parts - i0);
-    for (int i = 0; i < n; ++i) {
-      const float wi = __shfl_sync(0xffffffffu, w, i);
-      const float* p = a.part_o + slot(i0 + i) * hd;
-      if (wi != 0.f)
+  const int c0 = blockIdx.x, parts = (int)((it.first + it.nb - 1) / per) - c0 + 1;
+  const int qt = 1 << a.sp.qt_log, G = a.c.G, rows = min(qt, it.ql - it.t * qt) * G, lane = threadIdx.x & 31, hd = a.c.hd;
+  const bool mine = lane * VW < hd;
+  for (int row = blockIdx.y * 8 + (threadIdx.x >> 5); row < rows; row += gridDim.y * 8) {
+    auto slot = [&](int i) { return (size_t)(i == 0 ? 2 * c0 + 1 : 2 * (c0 + i)) * a.rows + row; };
+    float m = -INFINITY, l = 0.f, o[VW];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (lane + 32 * k < hd) o[k] += wi * p[lane + 32 * k];
+    for (int k = 0; k < VW; ++k) o[k] = 0.f;
+    auto add = [&](int i, float w) {
+      if (w == 0.f || !mine) return;
+      const float* p = a.part_o + slot(i) * hd + lane * VW;
+      float v[VW];
+      if (VW == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(p);
+      else if (VW == 2) *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(p);
+      else v[0] = *p;
+#pragma unroll
+      for (int k = 0; k < VW; ++k) o[k] += w * v[k];
+    };
+    if (parts == 2) {  // the usual case, without the exchange
+      const float2 x = a.part_ml[slot(0)], y = a.part_ml[slot(1)];
+      m = fmaxf(x.x, y.x);
+      const float ref = m == -INFINITY ? 0.f : m, wx = exp2f(x.x - ref), wy = exp2f(y.x - ref);
+      l = wx * x.y + wy * y.y;
+      add(0, wx);
+      add(1, wy);
+    } else {
+      for (int i = lane; i < parts; i += 32) m = fmaxf(m, a.part_ml[slot(i)].x);
+      m = warp_max(m);
+      const float ref = m == -INFINITY ? 0.f : m;
+      for (int i0 = 0; i0 < parts; i0 += 32) {
+        float w = 0.f;
+        if (i0 + lane < parts) {
+          const float2 ml = a.part_ml[slot(i0 + lane)];
+          w = exp2f(ml.x - ref);
+          l += w * ml.y;
+        }
+        for (int i = 0; i < min(32, parts - i0); ++i) add(i0 + i, __shfl_sync(0xffffffffu, w, i));
+      }
+      l = warp_sum(l);
     }
+    const int token = it.t0 + it.t * qt + row / G, head = it.h * G + row % G;
+    T* out = static_cast<T*>(a.out) + token * a.os + (long long)head * hd + lane * VW;
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+    if (mine)
+#pragma unroll
+      for (int k = 0; k < VW; ++k) out[k] = from_f32<T>(o[k] * inv);
+    if (lane == 0 && a.lse) a.lse[(long long)token * a.c.Hq + head] = l != 0.f ? (m + log2f(l)) * LN2 : -INFINITY;
   }
-  l = warp_sum(l);
-  const int token = it.t0 + it.t * qt + row / a.c.G, head = it.h * a.c.G + row % a.c.G;
-  T* out = static_cast<T*>(a.out) + token * a.os + (long long)head * hd;
-  const float inv = l != 0.f ? 1.f / l : 0.f;
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (lane + 32 * k < hd) out[lane + 32 * k] = from_f32<T>(o[k] * inv);
-  if (lane == 0 && a.lse) a.lse[(long long)token * a.c.Hq + head] = l != 0.f ? (m + log2f(l)) * LN2 : -INFINITY;
 }
 
 // ----------------------------------------------------------------------------
@@ -1733,7 +1748,11 @@ static cudaError_t chunk_launch(const ChunkAttn& a, const tlf_attn_chunk_args& a
     e = a.c.hd == 16 ? simt_rows<16>(a, st) : a.c.hd == 32 ? simt_rows<32>(a, st) : a.c.hd == 64 ? simt_rows<64>(a, st) : simt_rows<128>(a, st);
   if (e) return e;
   const int base = (a.c.n + 1) * 8;
-  if (cudaError_t j = launch_k(k_chunk_join<T>, dim3(a.ctas - 1, (a.rows + 7) / 8), dim3(256), base, st, a)) return j;
+  const dim3 jg(a.ctas - 1, a.rows == 256 ? 4 : (a.rows + 7) / 8);
+  e = a.c.hd == 128  ? launch_k(k_chunk_join<T, 4>, jg, dim3(256), base, st, a)
+      : a.c.hd == 64 ? launch_k(k_chunk_join<T, 2>, jg, dim3(256), base, st, a)
+                     : launch_k(k_chunk_join<T, 1>, jg, dim3(256), base, st, a);
+  if (e) return e;
   if (!args.weight_out) return cudaSuccess;
   const dim3 grid(4 * num_sms);
   if constexpr (std::is_same<T, bf16>::value)

@@ -3,6 +3,7 @@
 // Pair (x_a, x_b) of a head at position p becomes (x_a c - x_b s, x_b c + x_a s), (c, s) = table[p][pair]: what is
 // turned at position p and what is turned at p' then meet in q . k as a function of p - p'. The table is read, not computed:
 // a float32 angle p f_k loses log2(p f_k) bits of the turn, and a row of it is shared by every head of the token.
+#include <algorithm>
 #include <cmath>
 
 #include "k_serve.cuh"
@@ -46,7 +47,7 @@ cudaError_t launch_rope_scaled_table(const tlf_rope_config& cfg, int max_pos, fl
 }
 
 constexpr int ROPE_THREADS = 256;
-constexpr int ROPE_TOKENS = 8;  // most tokens of a CTA
+constexpr int ROPE_TOKENS = 4;  // most tokens of a CTA
 
 struct RopeDev {
   const void *q, *k, *v;
@@ -75,7 +76,7 @@ __device__ __forceinline__ void store16<bf16>(bf16* p, const float* x) {
 // rows that end at or before it), then all threads go over the tokens' units: VEC elements (16 bytes) of a head, or the two
 // groups of VEC that a rotation in halves pairs up. VEC = 1 takes what is not aligned to 16 bytes.
 template <typename T, typename QT, int VEC>
-__global__ void __launch_bounds__(ROPE_THREADS) k_rope_chunk(ChunkDev c, RopeDev a) {
+__global__ void __launch_bounds__(ROPE_THREADS, 4) k_rope_chunk(ChunkDev c, RopeDev a) {
   pdl_wait();
   __shared__ long long s_dst[ROPE_TOKENS];  // element offset of the token's K in head 0 of its page, -1: no entry
   __shared__ int s_pos[ROPE_TOKENS];        // -1: out of range
@@ -134,67 +135,99 @@ __global__ void __launch_bounds__(ROPE_THREADS) k_rope_chunk(ChunkDev c, RopeDev
       for (int i = 0; i < VEC; i += 16 / (int)sizeof(QT)) store16<QT>(p + i, x + i);
     }
   };
-  for (unsigned u = tid; u < nt * per; u += ROPE_THREADS) {
-    const unsigned j = u / per, w = u - j * per;
-    const long long t = first + (int)j, dst = s_dst[j];
-    const int pos = s_pos[j];
-    float x[VEC], y[VEC];
+  // A thread keeps its unit and goes over the tokens, U of them in flight; units that leave threads over get several threads,
+  // each with a share of the tokens.
+  constexpr int U = 2;
+  const unsigned shares = per >= ROPE_THREADS ? 1 : ROPE_THREADS / per;
+  const int share = shares == 1 ? 0 : tid / per;
+  if (share >= (int)shares) return;
+  for (unsigned w = shares == 1 ? tid : tid - share * per; w < per; w += shares == 1 ? ROPE_THREADS : per) {
     if (w >= qk) {  // v: copied
       const unsigned h = (w - qk) / vu, d = (w - qk - h * vu) * VEC;
-      if (dst < 0) continue;
-      load(static_cast<const T*>(a.v) + t * a.vs + h * hd + d, x);
-      store_t(pool + dst + (c.Hkv + h) * seg + d, x);
+      const T* src = static_cast<const T*>(a.v) + h * hd + d;
+      T* dst = pool + (c.Hkv + h) * seg + d;
+      for (int j0 = share * U; j0 < nt; j0 += shares * U) {
+        float x[U][VEC];
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+          if (j0 + i < nt) load(src + (long long)(first + j0 + i) * a.vs, x[i]);
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+          if (j0 + i < nt && s_dst[j0 + i] >= 0) store_t(dst + s_dst[j0 + i], x[i]);
+      }
       continue;
     }
     const unsigned h = w / hu, i = w - h * hu;
     const bool is_q = h < (unsigned)c.Hq;
-    if (!is_q && dst < 0) continue;
-    const T* src = is_q ? static_cast<const T*>(a.q) + t * a.qs + h * hd
-                        : static_cast<const T*>(a.k) + t * a.ks + (h - c.Hq) * hd;
-    T* kd = pool + dst + ((long long)h - c.Hq) * seg;  // used for k only
-    QT* qd = static_cast<QT*>(a.q_out) + (t * c.Hq + h) * hd;
+    const T* src = is_q ? static_cast<const T*>(a.q) + h * hd : static_cast<const T*>(a.k) + (h - c.Hq) * hd;
+    const long long step = is_q ? a.qs : a.ks;
+    T* kd = pool + ((long long)h - c.Hq) * seg;  // used for k only
+    QT* qd = static_cast<QT*>(a.q_out) + (long long)first * c.Hq * hd + h * hd;
+    // a unit is VEC dims at da; in halves (and element by element) also the VEC dims at db that they pair up with
+    const bool turned = i < ru, two = turned && (!a.interleaved || VEC == 1);
     unsigned da, db = 0;
-    bool two = false;
-    if (i >= ru) {  // behind the turned dims
+    if (!turned) {
       da = rot + (i - ru) * VEC;
-      load(src + da, x);
-    } else if (!a.interleaved || VEC == 1) {
-      const unsigned k = i * VEC;  // first pair
-      da = a.interleaved ? 2 * k : k;
-      db = a.interleaved ? 2 * k + 1 : k + rot / 2;
-      two = true;
-      load(src + da, x);
-      load(src + db, y);
-      const float2* cs = a.table + (long long)max(pos, 0) * (rot / 2) + k;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        const float2 f = cs[e];
-        const float xa = x[e], xb = y[e];
-        x[e] = xa * f.x - xb * f.y;
-        y[e] = xb * f.x + xa * f.y;
-      }
+    } else if (two) {
+      da = a.interleaved ? 2 * i : i * VEC;
+      db = a.interleaved ? 2 * i + 1 : i * VEC + rot / 2;
     } else {
       da = i * VEC;
-      load(src + da, x);
-      const float2* cs = a.table + (long long)max(pos, 0) * (rot / 2) + da / 2;
-#pragma unroll
-      for (int e = 0; e + 1 < VEC; e += 2) {
-        const float2 f = cs[e / 2];
-        const float xa = x[e], xb = x[e + 1];
-        x[e] = xa * f.x - xb * f.y;
-        x[e + 1] = xb * f.x + xa * f.y;
-      }
     }
-    if (is_q) {
-      if (pos < 0) {
+    const float2* cs0 = a.table + (two ? i * VEC : da / 2);
+    for (int j0 = share * U; j0 < nt; j0 += shares * U) {
+      float x[U][VEC], y[U][VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) x[e] = y[e] = 0.f;
+      for (int n = 0; n < U; ++n)
+        if (j0 + n < nt) {
+          load(src + (long long)(first + j0 + n) * step + da, x[n]);
+          if (two) load(src + (long long)(first + j0 + n) * step + db, y[n]);
+        }
+#pragma unroll
+      for (int n = 0; n < U; ++n) {
+        const int j = j0 + n;
+        if (j >= nt) break;
+        const int pos = s_pos[j];
+        const float2* cs = cs0 + (long long)max(pos, 0) * (rot / 2);
+        if (two) {
+#pragma unroll
+          for (int e = 0; e < VEC; e += VEC == 1 ? 1 : 2) {
+            float4 f;  // two pairs
+            if (VEC == 1) f = make_float4(cs->x, cs->y, 0.f, 0.f);
+            else f = __ldg(reinterpret_cast<const float4*>(cs + e));
+            const float xa = x[n][e], xb = y[n][e];
+            x[n][e] = xa * f.x - xb * f.y;
+            y[n][e] = xb * f.x + xa * f.y;
+            if (VEC > 1) {
+              const float va = x[n][e + (VEC > 1)], vb = y[n][e + (VEC > 1)];
+              x[n][e + (VEC > 1)] = va * f.z - vb * f.w;
+              y[n][e + (VEC > 1)] = vb * f.z + va * f.w;
+            }
+          }
+        } else if (turned) {
+#pragma unroll
+          for (int e = 0; e + 3 < VEC; e += 4) {
+            const float4 f = __ldg(reinterpret_cast<const float4*>(cs + e / 2));
+            float xa = x[n][e], xb = x[n][e + 1];
+            x[n][e] = xa * f.x - xb * f.y;
+            x[n][e + 1] = xb * f.x + xa * f.y;
+            xa = x[n][e + 2], xb = x[n][e + 3];
+            x[n][e + 2] = xa * f.z - xb * f.w;
+            x[n][e + 3] = xb * f.z + xa * f.w;
+          }
+        }
+        if (is_q) {
+          if (pos < 0) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) x[n][e] = y[n][e] = 0.f;
+          }
+          store_q(qd + (long long)j * c.Hq * hd + da, x[n]);
+          if (two) store_q(qd + (long long)j * c.Hq * hd + db, y[n]);
+        } else if (s_dst[j] >= 0) {
+          store_t(kd + s_dst[j] + da, x[n]);
+          if (two) store_t(kd + s_dst[j] + db, y[n]);
+        }
       }
-      store_q(qd + da, x);
-      if (two) store_q(qd + db, y);
-    } else {
-      store_t(kd + da, x);
-      if (two) store_t(kd + db, y);
     }
   }
   pdl_trigger();
@@ -212,10 +245,9 @@ cudaError_t launch_rope_chunk(const ChunkDev& c, int dtype, const tlf_rope_args&
   const auto al = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
   const bool wide = al(a.q) && al(a.k) && al(a.v) && al(a.q_out) && al(a.table) && a.q_stride % vec == 0 &&
                     a.k_stride % vec == 0 && a.v_stride % vec == 0 &&
-                    (d.interleaved ? a.rot_dim % vec == 0 : a.rot_dim / 2 % vec == 0);
-  const int units = (c.Hq + 2 * c.Hkv) * c.hd / (wide ? vec : 1);
-  // few tokens: one a CTA; many: about four units a thread
-  if (c.T > 1024) d.tokens = std::min(ROPE_TOKENS, std::max(1, 4 * ROPE_THREADS / units));
+                    (d.interleaved ? a.rot_dim % vec == 0 : a.rot_dim / 2 % vec == 0) && (a.rot_dim / 2) % 2 == 0;
+  // few tokens: one a CTA; many: up to eight, so that a thread has several in flight
+  d.tokens = std::min(ROPE_TOKENS, std::max(1, c.T / 608));
   if (dtype == TLF_DTYPE_BF16) {
     if (a.q_f32) return wide ? rope_launch<bf16, float, 8>(c, d, st) : rope_launch<bf16, float, 1>(c, d, st);
     return wide ? rope_launch<bf16, bf16, 8>(c, d, st) : rope_launch<bf16, bf16, 1>(c, d, st);
