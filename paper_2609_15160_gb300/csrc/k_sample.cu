@@ -8,13 +8,17 @@
 // Passes over the row (all but the first find it in L2): the maximum; the sum of w; the candidates. Candidates are tokens that
 // top-k or top-p can reach; they are few for the usual limits and go to a list in shared memory, where the threshold is found.
 //   top-k   tokens from the k-th largest of the threads' own maxima on (to the next 1/16 in z): at least k of them;
-//   top-p   tokens from the bin of z on (width 1/16) behind which the rest weighs at most 1 - top_p of the sum at the most;
-//           that takes a histogram of the tokens, in the pass of the sum.
+//   top-p   a histogram over bins of z of width 1/16 (taken in the pass of the sum) bounds the weight up to every bin from
+//           both sides: bins that surely stay, bins that surely do not, and a few between them, where the threshold lies and
+//           which alone take part in finding it. The ones that stay go to the list too, or, where they are too many, take
+//           part in the draw at once.
 // A short list is sorted by counting. A longer one takes a radix select over the keys: by count for top-k, by weight for top-p,
-// with weights in 2^-40 fixed point, so the order of the atomics does not matter. When top-p alone leaves too many candidates
-// (flat logits), the bins' weights are added up in a pass of their own, which leaves the one bin with the threshold for the
-// list; what lies above it takes part in the draw at once. Where that is too much for the list too, the select goes over the
-// whole row. A row is split over a cluster of up to eight CTAs while there are SMs left over.
+// with weights in 2^-40 fixed point, so the order of the atomics does not matter. Where the candidates are too many for the
+// list (logits that are nearly all alike), the select goes over the whole row. A row is split over a cluster of up to eight
+// CTAs while there are SMs left over. In the draw a token's -log(-log u) is first bounded by -log(1 - u), and only the few that
+// could beat the warp's best so far are computed.
+#include <type_traits>
+
 #include <cooperative_groups.h>
 
 #include "k_serve.cuh"
@@ -25,7 +29,7 @@ namespace tlf {
 
 constexpr int SM_THREADS = 512;
 constexpr int SM_LIST = 6144;
-constexpr int SM_SORT = 256;   // longest list that is sorted by counting
+constexpr int SM_SORT = 512;   // longest list that is sorted by counting
 constexpr int SM_CLUSTER = 8;  // most CTAs that share a row
 
 struct SampleDev {
@@ -59,28 +63,41 @@ __device__ __forceinline__ u64 sample_mass(float w) { return __float2ull_rn(w * 
 
 constexpr int SM_BINS = 512;
 constexpr float SM_BIN = 16.f;  // bins per unit of z; the last bin holds the rest
-// Bin of a token, rounded to nearest: bin i holds z in -(i + 1/2) / 16 .. -(i - 1/2) / 16.
-__device__ __forceinline__ int sample_bin(float z) {
-  return (int)(__float_as_uint(fminf(z * -SM_BIN, (float)(SM_BINS - 1)) + 8388608.f) & 0x3ffu);
+// Bin of a token with z2 = z log2 e, rounded to nearest: bin i holds z in -(i + 1/2) / 16 .. -(i - 1/2) / 16.
+__device__ __forceinline__ int sample_bin(float z2) {
+  return (int)(__float_as_uint(fminf(z2 * (-SM_BIN * 0.6931471805599453f), (float)(SM_BINS - 1)) + 8388608.f) & 0x3ffu);
 }
 
-// f(four logits, index of the first) over entries v0 .. v1 - 1 of the row (v0 a multiple of 4), all threads taking part in
-// every step; NaN (a token that cannot be drawn) past the end. U loads of a thread are in flight before the first is used.
+// f(16 logits, index of the first): the logits are four times four in a row, SM_STEP apart. Entries v0 .. v1 - 1 of the row (v0 a
+// multiple of 4), all threads taking part in every step; NaN (a token that cannot be drawn) past the end.
+constexpr int SM_STEP = 4 * SM_THREADS;
 template <typename F>
 __device__ __forceinline__ void sample_pass(const float* row, int v0, int v1, bool wide, F&& f) {
-  constexpr int U = 8;
   const float none = __int_as_float(0x7fffffff);
-  for (int i0 = v0; i0 < v1; i0 += 4 * U * SM_THREADS) {
-    float4 v[U];
+  int i = v0 + 4 * (int)threadIdx.x, left = v1 - v0;
+  float e[16];
+  if (wide)
+    for (; left >= 4 * SM_STEP; left -= 4 * SM_STEP, i += 4 * SM_STEP) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = i0 + 4 * (u * SM_THREADS + (int)threadIdx.x);
-      if (wide && i + 3 < v1) v[u] = __ldg(reinterpret_cast<const float4*>(row + i));
-      else v[u] = make_float4(i < v1 ? row[i] : none, i + 1 < v1 ? row[i + 1] : none, i + 2 < v1 ? row[i + 2] : none, i + 3 < v1 ? row[i + 3] : none);
+      for (int u = 0; u < 4; ++u) {
+        const float4 v = __ldg(reinterpret_cast<const float4*>(row + i + u * SM_STEP));
+        e[4 * u] = v.x, e[4 * u + 1] = v.y, e[4 * u + 2] = v.z, e[4 * u + 3] = v.w;
+      }
+      f(e, i);
     }
+  for (; left > 0; left -= 4 * SM_STEP, i += 4 * SM_STEP) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i0 + 4 * u * SM_THREADS < v1) f(v[u], i0 + 4 * (u * SM_THREADS + (int)threadIdx.x));
+    for (int u = 0; u < 4; ++u) {
+      const int at = i + u * SM_STEP;
+      if (wide && at + 3 < v1) {
+        const float4 v = __ldg(reinterpret_cast<const float4*>(row + at));
+        e[4 * u] = v.x, e[4 * u + 1] = v.y, e[4 * u + 2] = v.z, e[4 * u + 3] = v.w;
+      } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) e[4 * u + x] = at + x < v1 ? row[at + x] : none;
+      }
+    }
+    f(e, i);
   }
 }
 
@@ -105,7 +122,8 @@ struct SampleShared {
   u64 redl[33];
   float mx, sum, best[SM_CLUSTER];  // what this CTA found in its part; of all parts (at rank 0)
   int token[SM_CLUSTER];
-  int n, pick;
+  float heavy[SM_CLUSTER];
+  int n, n_sure, pick;
   uint32_t lo, hi, prefix;
   unsigned need, hit;
   u64 above;
@@ -124,17 +142,15 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
   constexpr float FMAX = 3.402823466e38f;
 
   float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-  sample_pass(row, v0, v1, wide, [&](float4 v, int) {
-    m4[0] = fmaxf(m4[0], v.x);
-    m4[1] = fmaxf(m4[1], v.y);
-    m4[2] = fmaxf(m4[2], v.z);
-    m4[3] = fmaxf(m4[3], v.w);
+  sample_pass(row, v0, v1, wide, [&](const float (&e)[16], int) {
+#pragma unroll
+    for (int x = 0; x < 16; ++x) m4[x & 3] = fmaxf(m4[x & 3], e[x]);
   });
   const float mine = fminf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), FMAX);  // this thread's largest
   float mx = warp_max(mine);
   if (lane == 0) S.redf[warp] = mx;
   for (int i = tid; i < SM_BINS; i += SM_THREADS) S.bin[i] = 0;
-  if (tid == 0) S.n = 0;
+  if (tid == 0) S.n = S.n_sure = 0;
   __syncthreads();
   mx = warp_max(S.redf[lane & (SM_THREADS / 32 - 1)]);
   if (cs > 1) {
@@ -163,33 +179,34 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
   }
   const bool by_k = k < V, by_p = top_p < 1.0 && k > 1;
   const bool by_max = by_k && k <= SM_THREADS * cs;  // the threads' maxima bound the top-k
-  // z as the definition has it, for what decides; times 1 / T for sums and bins (NaN, or 0 x infinity: far below)
+  // z as the definition has it, for what decides; z log2 e by a factor for sums and bins (NaN, or 0 x infinity: far below)
   auto z_of = [&](float l) { return (l - mx) / T; };
-  auto zq_of = [&](float raw) { return fminf(fmaxf((raw - mx) * rT, -1000.f), 0.f); };
+  const float r2 = rT * 1.4426950408889634f;
+  auto z2_of = [&](float raw) { return fminf(fmaxf((raw - mx) * r2, -1000.f), 0.f); };
   auto mass_of = [&](uint32_t key) { return sample_mass(expf(z_of(sample_unkey(key)))); };
-  // a logit that is not above any token of z >= zc, whatever the roundings
+  // a logit that no token of z >= zc is below, whatever the roundings
   auto cut_at = [&](float zc) { return fmaxf(mx + zc * T * 1.00001f - 1e-6f * fabsf(mx), -FMAX); };
 
   if (by_max && mine > -INFINITY) {
-    const int bin = sample_bin(zq_of(mine));
+    const int bin = sample_bin(z2_of(mine));
     if (bin < SM_BINS - 1) atomicAdd(&S.bin[bin], 1u);
   }
   float sum = 0.f;
   if (a.logprobs || by_p || (by_k && !by_max)) {
     float s4[4] = {0.f, 0.f, 0.f, 0.f};
-    const bool bins = !by_max && (by_k || by_p);
-    sample_pass(row, v0, v1, wide, [&](float4 v, int) {
-      const float z[4] = {zq_of(v.x), zq_of(v.y), zq_of(v.z), zq_of(v.w)};
+    auto add = [&](const float (&e)[16], auto bins) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s4[e] += ex2_fast(z[e] * 1.4426950408889634f);
-      if (bins) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int bin = sample_bin(z[e]);
+      for (int x = 0; x < 16; ++x) {
+        const float z2 = z2_of(e[x]);
+        s4[x & 3] += ex2_fast(z2);
+        if (bins) {
+          const int bin = sample_bin(z2);
           if (bin < SM_BINS - 1) atomicAdd(&S.bin[bin], 1u);
         }
       }
-    });
+    };
+    if (!by_max && (by_k || by_p)) sample_pass(row, v0, v1, wide, [&](const float (&e)[16], int) { add(e, std::true_type{}); });
+    else sample_pass(row, v0, v1, wide, [&](const float (&e)[16], int) { add(e, std::false_type{}); });
     sum = block_sum((s4[0] + s4[1]) + (s4[2] + s4[3]), S.redf);
   }
   if (cs > 1) {
@@ -211,15 +228,49 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
   // the draw: largest z - log(-log u), ties to the lower index
   float best = -INFINITY;
   int token = V;
-  auto race = [&](float l, int idx) {
+  auto race = [&](float l, float u, int idx) {
     const float z = z_of(l);
     if (min_p > 0.f && l != mx && !(expf(z) >= min_p)) return;
-    float score = z - logf(-logf(noise[idx]));
+    float score = z - logf(-logf(u));
     if (!(score == score)) score = -INFINITY;
     if (score > best || (score == best && idx < token)) {
       best = score;
       token = idx;
     }
+  };
+  // a token that -log u >= 1 - u lets beat `lim` (what is not a number may)
+  float lim = -INFINITY;  // best of the warp
+  auto may_win = [&](float raw, float u) { return !((raw - mx) * rT - 0.6931471805599453f * __log2f(1.f - u) + 1e-3f < lim); };
+  const bool wide_u = reinterpret_cast<uintptr_t>(noise) % 16 == 0;
+  // all tokens from `cut` on take part; returns their weight
+  auto race_pass = [&](float cut, auto weigh) {
+    float mass = 0.f;
+    sample_pass(row, v0, v1, wide, [&](const float (&e)[16], int i) {
+      float u[16];
+#pragma unroll
+      for (int x = 0; x < 16; x += 4) {
+        const int at = i + (x / 4) * SM_STEP;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (fmaxf(fmaxf(e[x], e[x + 1]), fmaxf(e[x + 2], e[x + 3])) >= cut) {
+          if (wide_u && at + 3 < V) v = __ldg(reinterpret_cast<const float4*>(noise + at));
+          else v = make_float4(noise[at], at + 1 < V ? noise[at + 1] : 0.f, at + 2 < V ? noise[at + 2] : 0.f, at + 3 < V ? noise[at + 3] : 0.f);
+        }
+        u[x] = v.x, u[x + 1] = v.y, u[x + 2] = v.z, u[x + 3] = v.w;
+      }
+      unsigned may = 0;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        if (e[x] >= cut && may_win(e[x], u[x])) may |= 1u << x;
+        if (weigh && e[x] >= cut) mass += ex2_fast(z2_of(e[x]));
+      }
+      if (__any_sync(0xffffffffu, may != 0)) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x)
+          if (may >> x & 1) race(sample_logit(e[x]), u[x], i + (x / 4) * SM_STEP + x % 4);
+        lim = warp_max(best);
+      }
+    });
+    return mass;
   };
   // the first bin (from the heaviest tokens on) at which `reached` holds for the values up to it; SM_BINS - 1 if none
   static_assert(SM_BINS == SM_THREADS, "a bin a thread");
@@ -232,92 +283,90 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
   };
   // tokens for which `in` holds into the list, which is rank 0's
   int* n_at = cs > 1 ? cl.map_shared_rank(&S.n, 0) : &S.n;
+  int* sure_at = cs > 1 ? cl.map_shared_rank(&S.n_sure, 0) : &S.n_sure;
   uint32_t* key_to = cs > 1 ? cl.map_shared_rank(S.key, 0) : S.key;
   int* idx_to = cs > 1 ? cl.map_shared_rank(S.idx, 0) : S.idx;
-  auto put = [&](float raw, int i, bool in) {
-    const unsigned who = __ballot_sync(0xffffffffu, in);
-    if (!who) return;
-    int at = 0;
-    if (lane == 0) at = atomicAdd(n_at, __popc(who));
-    at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1u));
-    if (in && at < SM_LIST) {
-      key_to[at] = sample_key(sample_logit(raw));
-      idx_to[at] = i;
-    }
-  };
-  auto gather = [&](float cut) {
-    sample_pass(row, v0, v1, wide, [&](float4 v, int i) {
-      const float e[4] = {v.x, v.y, v.z, v.w};
-      if (__any_sync(0xffffffffu, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)) >= cut)) {
+  // tokens from `cut` on into the list, those from `top` on (NaN: none) from its end down, or nowhere; the weight of the latter
+  auto gather = [&](float cut, float top, bool keep) {
+    float mass = 0.f;
+    sample_pass(row, v0, v1, wide, [&](const float (&e)[16], int i) {
+      unsigned in = 0, high = 0;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) put(e[x], i + x, e[x] >= cut);
+      for (int x = 0; x < 16; ++x) {
+        if (e[x] >= cut) in |= 1u << x;
+        if (e[x] >= top) high |= 1u << x;
+      }
+      if (!keep) in &= ~high, high = 0;
+      if (!__any_sync(0xffffffffu, in != 0)) return;
+      const int mine = __popc(in ^ high) | __popc(high) << 16;
+      int upto = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += y;
+      }
+      int front = 0, back = 0;
+      if (lane == 31) {
+        if (upto & 0xffff) front = atomicAdd(n_at, upto & 0xffff);
+        if (upto >> 16) back = atomicAdd(sure_at, upto >> 16);
+      }
+      front = __shfl_sync(0xffffffffu, front, 31) + ((upto - mine) & 0xffff);
+      back = SM_LIST - 1 - __shfl_sync(0xffffffffu, back, 31) - ((upto - mine) >> 16);
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        if (!(in >> x & 1)) continue;
+        const bool is_high = high >> x & 1;
+        if (is_high) mass += ex2_fast(z2_of(e[x]));
+        const int at = is_high ? back-- : front++;
+        if (at >= 0 && at < SM_LIST) {
+          key_to[at] = sample_key(sample_logit(e[x]));
+          idx_to[at] = i + (x >> 2) * SM_STEP + (x & 3);
+        }
       }
     });
+    return mass;
   };
 
+  const float none_f = __int_as_float(0x7fffffff);
   bool list = false;  // candidates are the list's (else the row's)
-  u64 heavier = 0;    // weight of tokens heavier than the list's, which have taken part in the draw already
+  float heavy = 0.f;  // weight of the tokens that stay for sure
   const double all_mass = (double)sample_mass(1.f) * (double)sum;
   if (by_k) {
     const int bin = first_bin(tid < SM_BINS - 1 ? S.tot[tid] : 0u, [&](unsigned n) { return n >= (unsigned)k; });
     if (bin < SM_BINS - 1 && (by_max || block_sum(tid <= bin ? (int)S.tot[tid] : 0, S.redi) <= SM_LIST)) {
-      gather(cut_at(-(bin + 0.51f) / SM_BIN));
+      gather(cut_at(-(bin + 0.51f) / SM_BIN), none_f, false);
       list = true;
     }
   } else if (by_p) {
-    // a token of bin i weighs at most exp(-(i - 1/2) / 16), and all of the last bin together next to nothing
-    const float most = S.tot[tid] * ex2_fast(-(tid - 0.51f) * (1.4426950408889634f / SM_BIN));
-    const float rest = (float)(1.0 - top_p) * sum * 0.999f, all = block_sum(most, S.redf);
-    const int bin = first_bin(most, [&](float m) { return all - m <= rest - 1e-6f * all; });
-    if (bin < SM_BINS - 1) {
-      if (block_sum(tid <= bin ? (int)S.tot[tid] : 0, S.redi) <= SM_LIST - SM_LIST / 32) {
-        gather(cut_at(-(bin + 0.51f) / SM_BIN));
-        list = true;
+    // a token of bin i weighs between exp(-(i + 1/2) / 16) and exp(-(i - 1/2) / 16) (and a little: z is rounded), all of the
+    // last bin together next to nothing
+    const bool some = tid < SM_BINS - 1;
+    const float at_least = some ? S.tot[tid] * ex2_fast(-(tid + 0.51f) * (1.4426950408889634f / SM_BIN)) : 0.f;
+    const float at_most = some ? S.tot[tid] * ex2_fast(-(tid - 0.51f) * (1.4426950408889634f / SM_BIN)) : 0.f;
+    float all_least, all_most;
+    const float lower = block_scan(at_least, S.redf, &all_least) + at_least;
+    const float upper = block_scan(at_most, S.redf, &all_most) + at_most;
+    const float goal = (float)top_p * sum, rest = (float)(1.0 - top_p) * sum, slip = 1e-5f * sum;
+    // bins up to `sure` stay whole; bins from `none` on do not
+    const int sure = __syncthreads_count(some && (upper < goal - slip || all_least - lower > rest + slip)) - 1;
+    const int none = __syncthreads_count(some && !(lower > goal + slip || all_most - upper < rest - slip)) + 1;
+    const int n_sure = block_sum(tid <= sure ? (int)S.tot[tid] : 0, S.redi);
+    const int n_between = block_sum(tid > sure && tid < none ? (int)S.tot[tid] : 0, S.redi);
+    if (none < SM_BINS && n_between <= SM_LIST) {
+      // from `top` on a token is in a sure bin; the rest of those counts as between
+      const float cut = cut_at(-(none - 0.49f) / SM_BIN);
+      const float top = sure < 0 ? none_f : mx - (sure + 0.49f) / SM_BIN * T * 0.99999f + 1e-6f * fabsf(mx);
+      if (n_sure + n_between <= SM_LIST - SM_LIST / 32) {
+        heavy = gather(cut, top, true);
       } else {
-        S.mass[tid] = 0;
-        __syncthreads();
-        sample_pass(row, v0, v1, wide, [&](float4 v, int) {
-          const float e[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const int at = sample_bin(zq_of(e[x]));
-            if (at <= bin) add_mass(&S.mass[at], mass_of(sample_key(sample_logit(e[x]))));
-          }
-        });
-        __syncthreads();
-        if (cs > 1) {
-          cl.sync();
-          u64 m = 0;
-          for (int r = 0; r < cs; ++r) m += cl.map_shared_rank(S.mass, r)[tid];
-          cl.sync();
-          S.mass[tid] = m;
-          __syncthreads();
-        }
-        const u64 target = (u64)ceil(top_p * all_mass);
-        const int at = first_bin(tid <= bin ? S.mass[tid] : 0ull, [&](u64 m) { return m >= target; });
-        if (at <= bin && S.tot[at] <= SM_LIST) {
-          heavier = block_sum(tid < at ? S.mass[tid] : 0ull, S.redl);
-          sample_pass(row, v0, v1, wide, [&](float4 v, int i) {
-            const float e[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const int bin_x = sample_bin(zq_of(e[x]));
-              if (bin_x < at) race(sample_logit(e[x]), i + x);
-              put(e[x], i + x, bin_x == at);
-            }
-          });
-          list = true;
-        }
+        heavy = race_pass(top, std::true_type{});
+        gather(cut, top, false);
       }
+      heavy = block_sum(heavy, S.redf);
+      list = true;
     }
   } else {  // no limit but min-p
-    const float cut = min_p > 0.f ? cut_at(logf(min_p) - 1e-3f) : -FMAX;
-    sample_pass(row, v0, v1, wide, [&](float4 v, int i) {
-      if (v.x >= cut) race(sample_logit(v.x), i);
-      if (v.y >= cut) race(sample_logit(v.y), i + 1);
-      if (v.z >= cut) race(sample_logit(v.z), i + 2);
-      if (v.w >= cut) race(sample_logit(v.w), i + 3);
-    });
+    race_pass(min_p > 0.f ? cut_at(logf(min_p) - 1e-3f) : -FMAX, std::false_type{});
   }
   auto race_warp = [&] {
 #pragma unroll
@@ -346,6 +395,7 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
     if (tid == 0) {
       cl.map_shared_rank(S.best, 0)[rank] = best;
       cl.map_shared_rank(S.token, 0)[rank] = token;
+      cl.map_shared_rank(S.heavy, 0)[rank] = heavy;
     }
     cl.sync();
     if (rank != 0) {
@@ -354,25 +404,46 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
     }
     best = tid < cs ? S.best[tid] : -INFINITY;
     token = tid < cs ? S.token[tid] : V;
+    heavy = 0.f;
+    for (int r = 0; r < cs; ++r) heavy += S.heavy[r];
   }
   __syncthreads();
-  if (list && S.n > SM_LIST) list = false;  // (the cut lets tokens below the bin in, by a rounding)
+  if (list && S.n + S.n_sure > SM_LIST) list = false;  // more tokens at the bound than the bins let expect
   const int n = list ? S.n : V;
-  if (!list && heavier) {  // taken back: the whole row draws again
-    heavier = 0;
-    best = -INFINITY;
-    token = V;
-  }
-
-  if (list && !heavier && n <= SM_SORT) {
+  const u64 heavier = list ? (u64)(heavy * 1099511627776.f) : 0;
+  // list entries that take part: noise of four in flight
+  auto race_list = [&](int first, int count, auto stays) {
+    for (int i0 = 0; i0 < count; i0 += 4 * SM_THREADS) {
+      float u[4];
+      bool on[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int i = i0 + x * SM_THREADS + tid;
+        on[x] = i < count && stays(S.key[first + i], S.idx[first + i]);
+        u[x] = on[x] ? noise[S.idx[first + i]] : 0.f;
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int i = i0 + x * SM_THREADS + tid;
+        if (on[x] && may_win(sample_unkey(S.key[first + i]), u[x])) race(sample_unkey(S.key[first + i]), u[x], S.idx[first + i]);
+        lim = fmaxf(lim, best);
+      }
+    }
+  };
+  if (list && S.n_sure) race_list(SM_LIST - S.n_sure, S.n_sure, [](uint32_t, int) { return true; });
+  if (list && n <= SM_SORT) {
     // sorted by (key, lower index): a token's place is the number of tokens before it
     if (tid < n) {
-      const uint32_t key = S.key[tid];
-      const int idx = S.idx[tid];
+      S.mass[tid] = (u64)S.key[tid] << 32 | (uint32_t)~S.idx[tid];
+    }
+    __syncthreads();
+    if (tid < n) {
+      const u64 key = S.mass[tid];
       int place = 0;
-      for (int i = 0; i < n; ++i) place += S.key[i] > key || (S.key[i] == key && S.idx[i] < idx);
-      S.skey[place] = key;
-      S.sidx[place] = idx;
+#pragma unroll 4
+      for (int i = 0; i < n; ++i) place += S.mass[i] > key;
+      S.skey[place] = S.key[tid];
+      S.sidx[place] = S.idx[tid];
     }
     __syncthreads();
     const bool in = tid < n && tid < k;
@@ -382,9 +453,9 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
       const u64 m = in ? mass_of(key) : 0;
       u64 total;
       const u64 before = block_scan(m, S.redl, &total);
-      stays = in && (tid == 0 || (double)before < top_p * (by_k ? (double)total : all_mass));
+      stays = in && ((tid == 0 && !heavier) || (double)(heavier + before) < top_p * (by_k ? (double)total : all_mass));
     }
-    if (stays) race(sample_unkey(key), S.sidx[tid]);
+    if (stays) race(sample_unkey(key), noise[S.sidx[tid]], S.sidx[tid]);
   } else if (by_k || by_p) {
     auto key_at = [&](int i) { return list ? S.key[i] : sample_key(sample_logit(row[i])); };
     // Kept: keys above thr, and the first `ties` of the `equal` tokens with key thr.
@@ -505,7 +576,7 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
       if (walk(true, 0, (u64)ceil(target), from, from_ties)) {
         thr = S.prefix;
         const double w = (double)mass_of(thr), left = target - (double)S.above;
-        ties = (unsigned)fmin((double)S.hit, fmax(1.0, ceil(left / w)));
+        ties = (unsigned)fmin((double)S.hit, fmax(heavier ? 0.0 : 1.0, ceil(left / w)));
         equal = thr == from ? from_equal : S.hit;
       }
       __syncthreads();
@@ -523,10 +594,13 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
       __syncthreads();
       last = S.pick;
     }
-    for (int i = tid; i < n; i += SM_THREADS) {
-      const uint32_t key = key_at(i);
-      const int idx = list ? S.idx[i] : i;
-      if (key > SAMPLE_NEVER && (key > thr || (key == thr && idx <= last))) race(sample_unkey(key), idx);
+    if (list) {
+      race_list(0, n, [&](uint32_t key, int idx) { return key > thr || (key == thr && idx <= last); });
+    } else {
+      for (int i = tid; i < V; i += SM_THREADS) {
+        const uint32_t key = key_at(i);
+        if (key > SAMPLE_NEVER && (key > thr || (key == thr && i <= last))) race(sample_unkey(key), noise[i], i);
+      }
     }
   }
   race_block();

@@ -131,7 +131,7 @@ inline cudaError_t launch_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 bloc
 
 // ---- launchers ----
 cudaError_t launch_rope_scaled_table(const tlf_rope_config& cfg, int max_pos, float* table, cudaStream_t st);
-cudaError_t launch_rope_chunk(const ChunkDev& c, int dtype, const tlf_rope_args& a, cudaStream_t st);
+cudaError_t launch_rope_chunk(const ChunkDev& c, int dtype, const tlf_rope_args& a, int num_sms, cudaStream_t st);
 
 // Attention of chunks: scratch (0 bytes: refused) and launch.
 size_t chunk_attn_scratch(const ChunkDev& c, int dtype, const tlf_attn_chunk_args& a, int num_sms);

@@ -160,7 +160,9 @@ extern "C" int tlf_rope_append(const tlf_chunk* c, const tlf_rope_args* a, void*
     if (const char* why = chunk_validate(c)) return refuse("tlf_rope_append", why);
     if (const char* why = rope_validate(c, a)) return refuse("tlf_rope_append", why);
     if (c->n_tokens == 0) return (int)TLF_OK;
-    return done(launch_rope_chunk(chunk_dev(c), c->dtype, *a, static_cast<cudaStream_t>(stream)));
+    const int sms = current_num_sms();
+    if (sms <= 0) return set_thread_error(TLF_ERR_CUDA, "no current CUDA device");
+    return done(launch_rope_chunk(chunk_dev(c), c->dtype, *a, sms, static_cast<cudaStream_t>(stream)));
   });
 }
 
