@@ -7,8 +7,8 @@
 //
 // Passes over the row (all but the first find it in L2): the maximum; the sum of w; the candidates. Candidates are tokens that
 // top-k or top-p can reach; they are few for the usual limits and go to a list in shared memory, where the threshold is found.
-//   top-k   tokens from the k-th largest of the threads' own maxima on (to the next 1/16 in z): at least k of them;
-//   top-p   a histogram over bins of z of width 1/16 (taken in the pass of the sum) bounds the weight up to every bin from
+//   top-k   tokens from the k-th largest of the threads' own maxima on (to the next 1/32 in z): at least k of them;
+//   top-p   a histogram over bins of z of width 1/32 (taken in the pass of the sum) bounds the weight up to every bin from
 //           both sides: bins that surely stay, bins that surely do not, and a few between them, where the threshold lies and
 //           which alone take part in finding it. The ones that stay go to the list too, or, where they are too many, take
 //           part in the draw at once.
@@ -61,11 +61,11 @@ __device__ __forceinline__ float sample_unkey(uint32_t k) {
 }
 __device__ __forceinline__ u64 sample_mass(float w) { return __float2ull_rn(w * 1099511627776.f); }  // w in 0..1
 
-constexpr int SM_BINS = 512;
-constexpr float SM_BIN = 16.f;  // bins per unit of z; the last bin holds the rest
-// Bin of a token with z2 = z log2 e, rounded to nearest: bin i holds z in -(i + 1/2) / 16 .. -(i - 1/2) / 16.
+constexpr int SM_BINS = 1024;   // two a thread
+constexpr float SM_BIN = 32.f;  // bins per unit of z; the last bin holds the rest
+// Bin of a token with z2 = z log2 e, rounded to nearest: bin i holds z in -(i + 1/2) / 32 .. -(i - 1/2) / 32.
 __device__ __forceinline__ int sample_bin(float z2) {
-  return (int)(__float_as_uint(fminf(z2 * (-SM_BIN * 0.6931471805599453f), (float)(SM_BINS - 1)) + 8388608.f) & 0x3ffu);
+  return (int)(__float_as_uint(fminf(z2 * (-SM_BIN * 0.6931471805599453f), (float)(SM_BINS - 1)) + 8388608.f) & 0x7ffu);
 }
 
 // f(16 logits, index of the first): the logits are four times four in a row, SM_STEP apart. Entries v0 .. v1 - 1 of the row (v0 a
@@ -111,7 +111,7 @@ __device__ __forceinline__ void add_mass(u64* at, u64 m) {
 struct SampleShared {
   uint32_t key[SM_LIST];
   int idx[SM_LIST];
-  u64 mass[SM_BINS];      // of a bin, or of a digit of the select
+  u64 mass[SM_SORT];      // of a digit of the select; of the list, sorted
   unsigned bin[SM_BINS];  // tokens of this CTA's part, or threads' maxima
   unsigned tot[SM_BINS];  // bin of the whole row
   unsigned cnt[256];
@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
       for (int x = 0; x < 16; x += 4) {
         const int at = i + (x / 4) * SM_STEP;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (fmaxf(fmaxf(e[x], e[x + 1]), fmaxf(e[x + 2], e[x + 3])) >= cut) {
+        if (cut <= -FMAX ? at < V : fmaxf(fmaxf(e[x], e[x + 1]), fmaxf(e[x + 2], e[x + 3])) >= cut) {
           if (wide_u && at + 3 < V) v = __ldg(reinterpret_cast<const float4*>(noise + at));
           else v = make_float4(noise[at], at + 1 < V ? noise[at + 1] : 0.f, at + 2 < V ? noise[at + 2] : 0.f, at + 3 < V ? noise[at + 3] : 0.f);
         }
@@ -272,16 +272,13 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
     });
     return mass;
   };
-  // the first bin (from the heaviest tokens on) at which `reached` holds for the values up to it; SM_BINS - 1 if none
-  static_assert(SM_BINS == SM_THREADS, "a bin a thread");
-  auto first_bin = [&](auto v, auto reached) {
-    if (tid == 0) S.pick = SM_BINS - 1;
-    decltype(v) before = block_scan(v, reinterpret_cast<decltype(v)*>(S.redl), (decltype(v)*)nullptr);
-    if (tid < SM_BINS - 1 && !reached(before) && reached(before + v)) S.pick = tid;
-    __syncthreads();
-    return S.pick;
+  static_assert(SM_BINS == 2 * SM_THREADS && SM_SORT <= SM_THREADS, "two bins a thread");
+  const int bin0 = 2 * tid, bin1 = bin0 + 1;
+  const unsigned tot0 = S.tot[bin0], tot1 = bin1 < SM_BINS - 1 ? S.tot[bin1] : 0u;
+  // tokens of bins first .. last
+  auto tokens_in = [&](int first, int last) {
+    return block_sum((bin0 >= first && bin0 <= last ? (int)tot0 : 0) + (bin1 >= first && bin1 <= last ? (int)tot1 : 0), S.redi);
   };
-  // tokens for which `in` holds into the list, which is rank 0's
   int* n_at = cs > 1 ? cl.map_shared_rank(&S.n, 0) : &S.n;
   int* sure_at = cs > 1 ? cl.map_shared_rank(&S.n_sure, 0) : &S.n_sure;
   uint32_t* key_to = cs > 1 ? cl.map_shared_rank(S.key, 0) : S.key;
@@ -332,27 +329,33 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
   float heavy = 0.f;  // weight of the tokens that stay for sure
   const double all_mass = (double)sample_mass(1.f) * (double)sum;
   if (by_k) {
-    const int bin = first_bin(tid < SM_BINS - 1 ? S.tot[tid] : 0u, [&](unsigned n) { return n >= (unsigned)k; });
-    if (bin < SM_BINS - 1 && (by_max || block_sum(tid <= bin ? (int)S.tot[tid] : 0, S.redi) <= SM_LIST)) {
+    // the first bin at which the count reaches k
+    if (tid == 0) S.pick = SM_BINS - 1;
+    const unsigned before = block_scan(tot0 + tot1, reinterpret_cast<unsigned*>(S.redi), (unsigned*)nullptr);
+    if (before < (unsigned)k && before + tot0 + tot1 >= (unsigned)k) S.pick = before + tot0 >= (unsigned)k ? bin0 : bin1;
+    __syncthreads();
+    const int bin = S.pick;
+    if (bin < SM_BINS - 1 && (by_max || tokens_in(0, bin) <= SM_LIST)) {
       gather(cut_at(-(bin + 0.51f) / SM_BIN), none_f, false);
       list = true;
     }
   } else if (by_p) {
-    // a token of bin i weighs between exp(-(i + 1/2) / 16) and exp(-(i - 1/2) / 16) (and a little: z is rounded), all of the
+    // a token of bin i weighs between exp(-(i + 1/2) / 32) and exp(-(i - 1/2) / 32) (and a little: z is rounded), all of the
     // last bin together next to nothing
-    const bool some = tid < SM_BINS - 1;
-    const float at_least = some ? S.tot[tid] * ex2_fast(-(tid + 0.51f) * (1.4426950408889634f / SM_BIN)) : 0.f;
-    const float at_most = some ? S.tot[tid] * ex2_fast(-(tid - 0.51f) * (1.4426950408889634f / SM_BIN)) : 0.f;
+    auto weight = [&](unsigned n, int bin, float off) { return n * ex2_fast(-(bin + off) * (1.4426950408889634f / SM_BIN)); };
+    const float least0 = weight(tot0, bin0, 0.52f), least1 = weight(tot1, bin1, 0.52f);
+    const float most0 = weight(tot0, bin0, -0.52f), most1 = weight(tot1, bin1, -0.52f);
     float all_least, all_most;
-    const float lower = block_scan(at_least, S.redf, &all_least) + at_least;
-    const float upper = block_scan(at_most, S.redf, &all_most) + at_most;
+    const float lower0 = block_scan(least0 + least1, S.redf, &all_least) + least0, lower1 = lower0 + least1;
+    const float upper0 = block_scan(most0 + most1, S.redf, &all_most) + most0, upper1 = upper0 + most1;
     const float goal = (float)top_p * sum, rest = (float)(1.0 - top_p) * sum, slip = 1e-5f * sum;
     // bins up to `sure` stay whole; bins from `none` on do not
-    const int sure = __syncthreads_count(some && (upper < goal - slip || all_least - lower > rest + slip)) - 1;
-    const int none = __syncthreads_count(some && !(lower > goal + slip || all_most - upper < rest - slip)) + 1;
-    const int n_sure = block_sum(tid <= sure ? (int)S.tot[tid] : 0, S.redi);
-    const int n_between = block_sum(tid > sure && tid < none ? (int)S.tot[tid] : 0, S.redi);
-    if (none < SM_BINS && n_between <= SM_LIST) {
+    auto stays = [&](float lower, float upper) { return upper < goal - slip || all_least - lower > rest + slip; };
+    auto open = [&](float lower, float upper) { return !(lower > goal + slip || all_most - upper < rest - slip); };
+    const int sure = block_sum((int)stays(lower0, upper0) + (int)(bin1 < SM_BINS - 1 && stays(lower1, upper1)), S.redi) - 1;
+    const int none = block_sum((int)open(lower0, upper0) + (int)(bin1 < SM_BINS - 1 && open(lower1, upper1)), S.redi) + 1;
+    const int n_sure = tokens_in(0, sure), n_between = tokens_in(sure + 1, none - 1);
+    if (none < SM_BINS && n_between <= SM_LIST - SM_LIST / 32) {
       // from `top` on a token is in a sure bin; the rest of those counts as between
       const float cut = cut_at(-(none - 0.49f) / SM_BIN);
       const float top = sure < 0 ? none_f : mx - (sure + 0.49f) / SM_BIN * T * 0.99999f + 1e-6f * fabsf(mx);
