@@ -743,27 +743,31 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
 // ----------------------------------------------------------------------------
 // Tensor cores, many rows: tcgen05 (bfloat16, head_dim 64 and 128)
 // ----------------------------------------------------------------------------
-// One CTA an SM. An item is two tiles of 128 MMA rows (row = query * G + head) that share every block of 128 keys (two
-// pages), so that the tensor cores work on one tile while the other tile's softmax runs:
+// One CTA an SM. An item is two tiles of 128 MMA rows (row = query * G + head) that share every block of 64 keys (a page):
 //   warps 0-3, 4-7  softmax of tile 0 and 1, one thread a row: S from tensor memory, mask, running maximum (refreshed lazily)
 //                   and sum in float32, P in bf16 back to tensor memory, where it is the A operand of P V; at the end O out;
 //   warp 8          producer: q of both tiles, then K and V of every block, through tensor maps;
-//   warp 9          issues S = Q K^T and O += P V (V taken as an MN-major operand).
+//   warps 9, 10     issue S = Q K^T and O += P V (V taken as an MN-major operand) of tile 0 and 1: at a block of 64 keys one
+//                   thread for both was slower than the tensor cores (2.0k to 2.5k cycles a block).
 // In an item's last block the softmax warps of the last queries zero V behind them (P = 0 does not cancel an infinity).
-// Tensor memory: S of both tiles (128 columns each) and O of both. At head_dim 128 that is all 512 columns, so P overwrites
-// its S; one thread's MMAs run in order, so the next S of a tile may be issued right behind the P V that reads P. At head_dim
-// 64 P has columns of its own and the next S is issued as soon as the softmax has read the one before.
-constexpr int PAIR_THREADS = 320;
+// Tensor memory: O of both tiles (head_dim columns each) and two S buffers of 64 columns a tile; P overwrites its S. One
+// thread's MMAs run in order, so S of block i + 2 is issued right behind the P V of block i that reads the buffer, and the
+// softmax of block i + 1 finds its S ready when it is done with block i. With blocks of 128 keys there is room for one S a tile
+// only: a tile's chain S, softmax, P V was then 4.8k cycles a block, 2.0k of them MMAs (4 x 2048 tokens over up to 10240
+// entries, 16 / 8 heads x 128: 485 us).
+constexpr int PAIR_THREADS = 352;
 
 template <int HD>
 struct PairShape {
-  static constexpr int ATOMS = HD / 64, COL = 128 * 128, T_BYTES = ATOMS * COL;  // a tile of 128 rows
-  static constexpr int NST = HD == 128 ? 4 : 8;  // K, V ring
-  static constexpr int OFF_KV = 2 * T_BYTES, OFF_BAR = OFF_KV + NST * T_BYTES, NBAR = 2 * NST + 2 + 8 + 2;
-  static constexpr int OFF_INT = OFF_BAR + NBAR * 8, OFF_BASE = OFF_INT + 48;
+  static constexpr int ATOMS = HD / 64, QCOL = 128 * 128, Q_BYTES = ATOMS * QCOL;  // a tile of 128 rows of q
+  static constexpr int COL = 64 * 128, T_BYTES = ATOMS * COL;                      // 64 rows of K or V
+  static constexpr int NST = HD == 128 ? 4 : 8;  // of the K ring and of the V ring
+  static constexpr int OFF_K = 2 * Q_BYTES, OFF_V = OFF_K + NST * T_BYTES, OFF_BAR = OFF_V + NST * T_BYTES;
+  static constexpr int NBAR = 4 * NST + 2 + 4 + 4 + 4 + 2;
+  static constexpr int FLAGS = 16;  // more than the blocks that the producer can be ahead of the softmax
+  static constexpr int OFF_INT = OFF_BAR + NBAR * 8, OFF_BASE = OFF_INT + (FLAGS + 4) * 4;
   static int bytes(int n) { return std::max(OFF_BASE + (n + 1) * 8 + 1024, tmem_min_smem(512)); }
-  static constexpr bool SEP_P = HD == 64;
-  static constexpr uint32_t SCOL = 0, OCOL = 256, PCOL = SEP_P ? 384 : 0, P_STEP = SEP_P ? 64 : 128;
+  static constexpr uint32_t OCOL = 256;
 };
 
 // D(tmem) (+)= A(tmem) * B(smem desc)
@@ -782,6 +786,16 @@ __device__ __forceinline__ void tmem_put_16(uint32_t taddr, const uint32_t* r) {
       : "memory");
 }
 
+// One thread of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r));
+  return r != 0;
+}
 __device__ __forceinline__ void tmem_st_wait_done() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 template <int HD>
@@ -793,34 +807,41 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
   __shared__ long long s_red[33];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(sm + Sh::OFF_BAR);
-  volatile int* s_flag = reinterpret_cast<volatile int*>(sm + Sh::OFF_INT);  // [8] of a block: its pages that are not there
-  volatile int* abort_flag = s_flag + 8;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + Sh::OFF_INT) + 9;
+  volatile int* s_flag = reinterpret_cast<volatile int*>(sm + Sh::OFF_INT);  // the block's page is not there
+  volatile int* abort_flag = s_flag + Sh::FLAGS;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + Sh::OFF_INT) + Sh::FLAGS + 1;
   long long* s_base = reinterpret_cast<long long*>(sm + Sh::OFF_BASE);
   auto bar = [&](int i) { return smem_u32(&bars[i]); };
-  auto kv_full = [&](unsigned i) { return bar(i % NST); };
-  auto kv_empty = [&](unsigned i) { return bar(NST + i % NST); };
-  auto q_full = [&](int x) { return bar(2 * NST + x); };
-  auto s_full = [&](int x) { return bar(2 * NST + 2 + x); };  // S of tile x written
-  auto s_read = [&](int x) { return bar(2 * NST + 4 + x); };  // ... read by its softmax (SEP_P)
-  auto p_full = [&](int x) { return bar(2 * NST + 6 + x); };  // P of tile x written
-  auto o_done = [&](int x) { return bar(2 * NST + 8 + x); };  // its P V product done
-  const uint32_t q_free = bar(2 * NST + 10), v_tail = bar(2 * NST + 11);
+  // block b of this CTA: its place in the rings, and the use's parity
+  auto k_full = [&](unsigned b) { return bar(b % NST); };
+  auto k_empty = [&](unsigned b) { return bar(NST + b % NST); };
+  auto v_full = [&](unsigned b) { return bar(2 * NST + b % NST); };
+  auto v_empty = [&](unsigned b) { return bar(3 * NST + b % NST); };
+  auto q_full = [&](int x) { return bar(4 * NST + x); };
+  // block n of tile x: S written, P written, P V done; a barrier for even and one for odd blocks, since up to two phases may pass
+  // before the other side looks (S of block n is issued behind the P V of block n - 2: by then that one's barrier is free)
+  auto s_full = [&](int x, unsigned n) { return bar(4 * NST + 2 + 2 * x + (n & 1)); };
+  auto p_full = [&](int x, unsigned n) { return bar(4 * NST + 6 + 2 * x + (n & 1)); };
+  auto o_done = [&](int x, unsigned n) { return bar(4 * NST + 10 + 2 * x + (n & 1)); };
+  const uint32_t q_free = bar(4 * NST + 14), v_tail = bar(4 * NST + 15);
   const ChunkDev& c = a.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < NST; ++i) {
-      mbar_init(bar(i), 1);
-      mbar_init(bar(NST + i), 1);
+      mbar_init(k_full(i), 1);
+      mbar_init(k_empty(i), 2);
+      mbar_init(v_full(i), 1);
+      mbar_init(v_empty(i), 2);
     }
     for (int x = 0; x < 2; ++x) {
       mbar_init(q_full(x), 1);
-      mbar_init(s_full(x), 1);
-      mbar_init(s_read(x), 4);
-      mbar_init(p_full(x), 4);
-      mbar_init(o_done(x), 1);
+      for (unsigned n = 0; n < 2; ++n) {
+        mbar_init(s_full(x, n), 1);
+        mbar_init(p_full(x, n), 4);
+        mbar_init(o_done(x, n), 1);
+      }
     }
-    mbar_init(q_free, 1);
+    mbar_init(q_free, 2);
     mbar_init(v_tail, 4);
     *abort_flag = 0;
     fence_barrier_init();
@@ -844,6 +865,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
   const int qt_log = a.sp.qt_log, QT = 1 << (qt_log - 1);  // queries of a tile
   // a bounded wait; once any role has given up, the others skip their waits and wind down
   auto wait = [&](uint32_t b, uint32_t parity) {
+    if (mbar_try_wait(b, parity & 1u)) return true;
     if (*abort_flag) return false;
     if (mbar_wait(b, parity & 1u, a.werr)) return true;
     *abort_flag = 1;
@@ -866,7 +888,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
     for (int x = 0; x < 2; ++x) {
       s.nq[x] = max(0, min(QT, left - x * QT));
       const int last = s.see0 + x * QT + s.nq[x] - 1;  // entry of the tile's last query
-      const int nb = s.nq[x] > 0 ? (last < 0 ? 1 : last / 128 + 1) : 0;
+      const int nb = s.nq[x] > 0 ? (last < 0 ? 1 : last / 64 + 1) : 0;
       s.e[x] = max(0, min(s.kb1, nb) - s.kb0);
     }
     return s;
@@ -874,7 +896,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
 
   if (warp == 8) {
     // ---------------- producer ----------------
-    unsigned ring = 0, blk = 0, segs = 0;
+    unsigned blk = 0, segs = 0;
     while (pos < end) {
       const Seg s = segment(pos);
       const int E = s.kb1 - s.kb0;
@@ -883,42 +905,34 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         ok = segs == 0 || wait(q_free, segs - 1);
         for (int x = 0; x < 2; ++x) {
           if (!ok || s.e[x] == 0) continue;
-          mbar_arrive_expect_tx(q_full(x), Sh::T_BYTES);
+          mbar_arrive_expect_tx(q_full(x), Sh::Q_BYTES);
 #pragma unroll
           for (int k = 0; k < Sh::ATOMS; ++k)
-            tma_load_3d(smem_u32(sm + x * Sh::T_BYTES + k * Sh::COL), &q_map, k * 64, s.it.h << g_log, s.token0 + x * QT, q_full(x));
+            tma_load_3d(smem_u32(sm + x * Sh::Q_BYTES + k * Sh::QCOL), &q_map, k * 64, s.it.h << g_log, s.token0 + x * QT, q_full(x));
         }
       }
       const int rowK = (c.layer * 2 * c.Hkv + s.it.h) * 64, rowV = rowK + c.Hkv * 64;
-      const int last_page = (s.it.len - 1) / 64;
-      for (int g0 = 0; g0 < E; g0 += 16) {
-        // the pages of 16 blocks, one a lane; a block past the last page loads that one twice, one that is not there page 0
-        int mine = 0, bad = 0;
-        if (g0 + lane / 2 < E) {
-          const int p = min(2 * (s.kb0 + g0) + lane, max(last_page, 0));
-          mine = s.it.len > 0 ? chunk_page(c.page_table, c.max_pages, c.n_pages, s.it.b, p, c.err) : -1;
-          bad = mine < 0;
-          mine = max(mine, 0);
-        }
-        const unsigned bads = __ballot_sync(0xffffffffu, bad);
-        for (int i = 0; i < min(16, E - g0); ++i, ++blk, ring += 2) {
-          const int pg[2] = {__shfl_sync(0xffffffffu, mine, 2 * i), __shfl_sync(0xffffffffu, mine, 2 * i + 1)};
+      for (int g0 = 0; g0 < E; g0 += 32) {
+        int mine = -1;  // the pages of 32 blocks, one a lane; page 0 stands in for one that is not there
+        if (g0 + lane < E && (s.kb0 + g0 + lane) * 64 < s.it.len)
+          mine = chunk_page(c.page_table, c.max_pages, c.n_pages, s.it.b, s.kb0 + g0 + lane, c.err);
+        for (int i = 0; i < min(32, E - g0); ++i, ++blk) {
+          const int page = __shfl_sync(0xffffffffu, mine, i);
           if (lane == 0 && ok) {
-            s_flag[blk & 7] = (bads >> (2 * i)) & 3;
+            ok = blk < NST || wait(k_empty(blk), blk / NST - 1);
+            if (ok) {
+              s_flag[blk % Sh::FLAGS] = page < 0;
+              mbar_arrive_expect_tx(k_full(blk), Sh::T_BYTES);
 #pragma unroll
-            for (int kv = 0; kv < 2; ++kv) {
-              const unsigned r = ring + kv;
-              if (r >= NST && !wait(kv_empty(r), r / NST - 1)) {
-                ok = false;
-                break;
-              }
-              mbar_arrive_expect_tx(kv_full(r), Sh::T_BYTES);
-              const uint32_t dst = smem_u32(sm + Sh::OFF_KV + (r % NST) * Sh::T_BYTES);
+              for (int k = 0; k < Sh::ATOMS; ++k)
+                tma_load_3d(smem_u32(sm + Sh::OFF_K + (blk % NST) * Sh::T_BYTES + k * Sh::COL), &pool_map, k * 64, rowK, max(page, 0), k_full(blk));
+              ok = blk < NST || wait(v_empty(blk), blk / NST - 1);
+            }
+            if (ok) {
+              mbar_arrive_expect_tx(v_full(blk), Sh::T_BYTES);
 #pragma unroll
-              for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int k = 0; k < Sh::ATOMS; ++k)
-                  tma_load_3d(dst + k * Sh::COL + h * (Sh::COL / 2), &pool_map, k * 64, kv ? rowV : rowK, pg[h], kv_full(r));
+              for (int k = 0; k < Sh::ATOMS; ++k)
+                tma_load_3d(smem_u32(sm + Sh::OFF_V + (blk % NST) * Sh::T_BYTES + k * Sh::COL), &pool_map, k * 64, rowV, max(page, 0), v_full(blk));
             }
           }
           __syncwarp();
@@ -927,89 +941,60 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       ++segs;
       pos = s.it.first + s.kb1;
     }
-  } else if (warp == 9) {
-    // ---------------- MMA issuer ----------------
-    if (lane == 0) {
-      constexpr uint32_t IDS = idesc_bf16_f32(128, 128), IDO = idesc_bf16_f32_bmn(128, HD);
-      constexpr uint64_t T_E = Sh::T_BYTES >> 4, COL_E = Sh::COL >> 4, V16_E = 2048 >> 4;
-      const uint64_t dq = smem_desc_sw128(smem_u32(sm)), dk = smem_desc_sw128(smem_u32(sm + Sh::OFF_KV));
-      const uint64_t dv = smem_desc_sw128_mn(smem_u32(sm + Sh::OFF_KV), Sh::COL);
-      unsigned ring = 0, ns[2] = {0, 0}, np[2] = {0, 0}, nqf[2] = {0, 0}, tails = 0;
-      auto issue_s = [&](int x, unsigned r) {
-        const uint64_t kd = dk + (uint64_t)(r % NST) * T_E, qd = dq + (uint64_t)x * T_E;
+  } else if (warp >= 9) {
+    // ---------------- MMA issuers, one a tile ----------------
+    if (elect_one()) {
+      constexpr uint32_t IDS = idesc_bf16_f32(128, 64), IDO = idesc_bf16_f32_bmn(128, HD);
+      constexpr uint64_t QCOL_E = Sh::QCOL >> 4, T_E = Sh::T_BYTES >> 4, COL_E = Sh::COL >> 4, V16_E = 2048 >> 4;
+      const int x = warp - 9;
+      const uint64_t qd = smem_desc_sw128(smem_u32(sm + x * Sh::Q_BYTES)), dk = smem_desc_sw128(smem_u32(sm + Sh::OFF_K));
+      const uint64_t dv = smem_desc_sw128_mn(smem_u32(sm + Sh::OFF_V), Sh::COL);
+      const uint32_t t_s = tmem + 128u * x, t_o = tmem + Sh::OCOL + (uint32_t)(HD * x);
+      unsigned blk = 0, tails = 0, qn = 0, n = 0;  // n: blocks of the tile whose P V has been issued
+      auto issue_s = [&](unsigned b, unsigned n) {
+        const uint64_t kd = dk + (uint64_t)(b % NST) * T_E;
 #pragma unroll
         for (int kc = 0; kc < Sh::ATOMS; ++kc)
 #pragma unroll
           for (int k = 0; k < 4; ++k)  // K = 16 an MMA: +32 bytes (encoded +2) inside the atom column
-            tc_mma_f16(tmem + Sh::SCOL + 128u * x, qd + kc * COL_E + 2 * k, kd + kc * COL_E + 2 * k, IDS, (kc | k) ? 1u : 0u);
-        tc_commit(s_full(x));
-        ++ns[x];
-      };
-      auto issue_pv = [&](int x, unsigned r, bool first) {
-        const uint64_t vd = dv + (uint64_t)(r % NST) * T_E;
-        const uint32_t d = tmem + Sh::OCOL + (uint32_t)(HD * x), pa = tmem + Sh::PCOL + Sh::P_STEP * (uint32_t)x;
-#pragma unroll
-        for (int k = 0; k < 8; ++k)  // K = 16 keys an MMA: 8 columns of P, +2048 bytes (16 rows) of V
-          mma_ts(d, pa + 8u * k, vd + V16_E * k, IDO, !first || k > 0 ? 1u : 0u);
-        tc_commit(o_done(x));
-        ++np[x];
+            tc_mma_f16(t_s + 64u * (n & 1), qd + kc * QCOL_E + 2 * k, kd + kc * COL_E + 2 * k, IDS, (kc | k) ? 1u : 0u);
+        tc_commit(s_full(x, n));
       };
       bool ok = true;
       while (pos < end && ok) {
         const Seg s = segment(pos);
-        const int E = s.kb1 - s.kb0;
-        auto full = [&](int i, int kv) { return wait(kv_full(ring + 2 * i + kv), (ring + 2 * i + kv) / NST); };
-        ok = full(0, 0);
-        for (int x = 0; x < 2 && ok; ++x)
-          if (s.e[x] > 0) {
-            ok = wait(q_full(x), nqf[x]++) && (!Sh::SEP_P || ns[x] == 0 || wait(s_read(x), ns[x] - 1));
-            if (!ok) break;
-            tc_fence_after();
-            issue_s(x, ring);
-          }
-        if (!ok) break;
-        tc_commit(kv_empty(ring));
-        if (E == 1) tc_commit(q_free);
-        for (int i = 0; i < E && ok; ++i) {
-          const bool next = i + 1 < E;
-          const unsigned kn = ring + 2 * (i + 1), v = ring + 2 * i + 1;
-          if (Sh::SEP_P && next) {
-            // both next S products first: each waits only for the softmax to have read the S before
-            ok = full(i + 1, 0);
-            for (int x = 0; x < 2 && ok; ++x)
-              if (i + 1 < s.e[x]) {
-                ok = wait(s_read(x), ns[x] - 1);
-                if (!ok) break;
-                tc_fence_after();
-                issue_s(x, kn);
-              }
-            if (!ok) break;
-            tc_commit(kv_empty(kn));
-            if (i + 2 == E) tc_commit(q_free);
-          }
-          ok = full(i, 1) && (s.kb0 + i + 1 < s.it.nb || wait(v_tail, tails++));
-          for (int x = 0; x < 2 && ok; ++x) {
-            if (i < s.e[x]) {
-              ok = wait(p_full(x), np[x]);
-              if (!ok) break;
-              tc_fence_after();
-              issue_pv(x, v, i == 0);
-            }
-            if (!Sh::SEP_P && i + 1 < s.e[x]) {
-              ok = full(i + 1, 0);
-              if (!ok) break;
-              tc_fence_after();
-              issue_s(x, kn);
-            }
-          }
+        const int E = s.kb1 - s.kb0, e = x ? s.e[1] : s.e[0];
+        ok = e == 0 || wait(q_full(x), qn++);
+        for (int i = 0; i < min(2, E) && ok; ++i) {  // S of the first two blocks
+          ok = wait(k_full(blk + i), (blk + i) / NST);
           if (!ok) break;
-          tc_commit(kv_empty(v));
-          if (!Sh::SEP_P && next) {
-            tc_commit(kv_empty(kn));
-            if (i + 2 == E) tc_commit(q_free);
-          }
+          tc_fence_after();
+          if (i < e) issue_s(blk + i, n + i);
+          tc_commit(k_empty(blk + i));
         }
-        ring += 2 * E;
+        if (ok && E <= 2) tc_commit(q_free);
+        for (int i = 0; i < E && ok; ++i) {
+          const unsigned b = blk + i;
+          const bool more = i + 2 < E;
+          // (what this tile does not use it waits for and releases all the same, in step with the other)
+          ok = wait(v_full(b), b / NST) && (s.kb0 + i + 1 < s.it.nb || wait(v_tail, tails++)) &&
+               (!more || wait(k_full(b + 2), (b + 2) / NST)) && (i >= e || wait(p_full(x, n), n >> 1));
+          if (!ok) break;
+          if (i < e) {
+            tc_fence_after();
+            const uint64_t vd = dv + (uint64_t)(b % NST) * T_E;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)  // K = 16 keys an MMA: 8 columns of P, +2048 bytes (16 rows) of V
+              mma_ts(t_o, t_s + 64u * (n & 1) + 8u * k, vd + V16_E * k, IDO, i > 0 || k > 0 ? 1u : 0u);
+            tc_commit(o_done(x, n));
+            if (i + 2 < e) issue_s(b + 2, n + 2);
+            ++n;
+          }
+          tc_commit(v_empty(b));
+          if (more) tc_commit(k_empty(b + 2));
+          if (i + 3 == E) tc_commit(q_free);
+        }
+        blk += E;
         pos = s.it.first + s.kb1;
       }
     }
@@ -1018,12 +1003,11 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
     // ---------------- softmax: thread = MMA row = TMEM lane ----------------
     const int x = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
     const uint32_t lane_off = (uint32_t)(quad * 32) << 16;
-    const uint32_t t_s = tmem + lane_off + Sh::SCOL + 128u * (uint32_t)x;
-    const uint32_t t_p = tmem + lane_off + Sh::PCOL + Sh::P_STEP * (uint32_t)x;
+    const uint32_t t_s = tmem + lane_off + 128u * (uint32_t)x;
     const uint32_t t_o = tmem + lane_off + Sh::OCOL + (uint32_t)(HD * x);
     const int qi = row >> g_log, g = row & ((1 << g_log) - 1);
     const float scale = a.scale, grow_by = 8.f / scale;
-    unsigned n = 0, blk = 0;  // blocks of this tile, and of the CTA (block i of the CTA: K, V in ring places 2 i, 2 i + 1)
+    unsigned n = 0, blk = 0;  // blocks of this tile, and of the CTA
     bool ok = true;
     // waits taken by the whole warp: the TMEM accesses after them are warp-collective
     auto wait_w = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, wait(b, parity)); };
@@ -1031,16 +1015,21 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       const Seg s = segment(pos);
       const bool row_ok = qi < s.nq[x];
       const int see = row_ok ? s.see0 + x * QT + qi : -1;  // a row past the tile's queries sees nothing
+      const int see0 = s.see0 + x * QT;                    // of the tile's first query
       float m_run = -INFINITY, l_run = 0.f;                // m in units of the raw scores
       for (int i = 0; i < s.e[x]; ++i, ++n) {
-        if (!wait_w(s_full(x), n)) { ok = false; break; }
+        if (!wait_w(s_full(x, n), n >> 1)) { ok = false; break; }
         tc_fence_after();
+        const uint32_t t_sn = t_s + 64u * (n & 1);
+        uint32_t su[64];
+        tmem_ld_32_issue(t_sn, su);
+        tmem_ld_32_issue(t_sn + 32, su + 32);
         if (s.kb0 + i + 1 == s.it.nb && x == (s.nq[1] > 0)) {
           // V's barrier is in this use's phase: the stage's use before was read by a P V before this S, and this one's use
           // ends with a P V that waits for v_tail
-          const unsigned r = 2 * (blk + i) + 1;
-          if (s.see0 + s.nq[0] + s.nq[1] <= (s.it.nb - 1) * 128 + row && wait(kv_full(r), r / NST)) {
-            uint8_t* v = sm + Sh::OFF_KV + (r % NST) * Sh::T_BYTES + row * 128;  // (a row keeps its place in the swizzle)
+          const unsigned b = blk + i;
+          if (row < 64 && s.see0 + s.nq[0] + s.nq[1] <= (s.it.nb - 1) * 64 + row && wait(v_full(b), b / NST)) {
+            uint8_t* v = sm + Sh::OFF_V + (b % NST) * Sh::T_BYTES + row * 128;  // (a row keeps its place in the swizzle)
 #pragma unroll
             for (int k = 0; k < 8 * Sh::ATOMS; ++k)
               *reinterpret_cast<uint4*>(v + (k / 8) * Sh::COL + (k % 8) * 16) = make_uint4(0, 0, 0, 0);
@@ -1049,38 +1038,26 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
           __syncwarp();
           if (lane == 0) mbar_arrive(v_tail);
         }
-        uint32_t su[128];
-#pragma unroll
-        for (int k = 0; k < 128; k += 32) tmem_ld_32_issue(t_s + (uint32_t)k, su + k);
+        const int key0 = (s.kb0 + i) * 64;
+        const bool gone = s_flag[(blk + i) % Sh::FLAGS] != 0;
         tmem_ld_wait();
-        if (Sh::SEP_P) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(s_read(x));
-        }
-        const int vis = see - (s.kb0 + i) * 128;  // columns 0..vis are visible
-        const int flag = s_flag[(blk + i) & 7];
-        float pm4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        if (__any_sync(0xffffffffu, vis < 127)) {
+        if (key0 + 63 > see0 || gone || !__all_sync(0xffffffffu, row_ok)) {
+          const int vis = gone ? -1 : see - key0;  // columns 0..vis are visible
 #pragma unroll
-          for (int k = 0; k < 128; ++k)
+          for (int k = 0; k < 64; ++k)
             if (k > vis) su[k] = 0xff800000u;  // -inf
         }
-        if (flag) {
+        float pm4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int k = 0; k < 128; ++k)
-            if (flag >> (k / 64) & 1) su[k] = 0xff800000u;
-        }
-#pragma unroll
-        for (int k = 0; k < 128; ++k) pm4[k & 3] = fmaxf(pm4[k & 3], __uint_as_float(su[k]));
+        for (int k = 0; k < 64; ++k) pm4[k & 3] = fmaxf(pm4[k & 3], __uint_as_float(su[k]));
         const float pm = fmaxf(fmaxf(pm4[0], pm4[1]), fmaxf(pm4[2], pm4[3]));
         // O is rescaled only when a row's maximum grows by more than 8 in base 2, after the P V before has landed
         const bool grow = pm > m_run + grow_by;
-        const float cr = grow ? exp2f((m_run - pm) * scale) : 1.f;  // 0 when m_run was -inf
-        if (i > 0 && (Sh::SEP_P || __any_sync(0xffffffffu, grow))) {
-          if (!wait_w(o_done(x), n - 1)) { ok = false; break; }  // (with its own columns, P is free too)
-          tc_fence_after();
-          if (__any_sync(0xffffffffu, grow)) {
+        if (__any_sync(0xffffffffu, grow)) {
+          const float cr = grow ? exp2f((m_run - pm) * scale) : 1.f;  // 0 when m_run was -inf
+          if (i > 0) {
+            if (!wait_w(o_done(x, n - 1), (n - 1) >> 1)) { ok = false; break; }
+            tc_fence_after();
 #pragma unroll
             for (int c0 = 0; c0 < HD; c0 += 16) {
               float o[16];
@@ -1090,15 +1067,15 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
               tmem_st_16(t_o + (uint32_t)c0, o);
             }
           }
-        }
-        if (grow) {
-          l_run *= cr;
-          m_run = pm;
+          if (grow) {
+            l_run *= cr;
+            m_run = pm;
+          }
         }
         const float mref = m_run == -INFINITY ? 0.f : m_run * scale;  // no visible key so far: any finite value
         float ps4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c0 = 0; c0 < 128; c0 += 32) {
+        for (int c0 = 0; c0 < 64; c0 += 32) {
           uint32_t pk[16];
 #pragma unroll
           for (int k = 0; k < 32; k += 2) {
@@ -1107,13 +1084,13 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
             ps4[(k >> 1) & 3] += p0 + p1;
             pk[k / 2] = pack_bf16(p0, p1);
           }
-          tmem_put_16(t_p + (uint32_t)(c0 / 2), pk);
+          tmem_put_16(t_sn + (uint32_t)(c0 / 2), pk);
         }
         l_run += (ps4[0] + ps4[1]) + (ps4[2] + ps4[3]);
         tmem_st_wait_done();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_full(x));
+        if (lane == 0) mbar_arrive(p_full(x, n));
       }
       // the last P V, then the row out: O / l, or its part
       const bool whole = s.kb0 == 0 && s.kb1 == s.it.nb;
@@ -1124,7 +1101,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       const bool wide = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && a.os % 8 == 0;
       bool bad = false;
       if (ok && s.e[x] > 0) {
-        if (!wait_w(o_done(x), n - 1)) break;
+        if (!wait_w(o_done(x, n - 1), (n - 1) >> 1)) break;
         tc_fence_after();
         const float inv = whole ? (l_run != 0.f ? 1.f / l_run : 0.f) : 1.f;
 #pragma unroll
@@ -1166,7 +1143,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         const int hh = __shfl_sync(0xffffffffu, head, src), see_r = __shfl_sync(0xffffffffu, see, src);
         const size_t pt = __shfl_sync(0xffffffffu, (unsigned long long)part, src);
         float mm, ll, oo[HD / 32];
-        chunk_redo<HD>(a, s.it.b, s.it.h, tk, hh, s.kb0 * 128, min(s.kb1 * 128, see_r + 1), mm, ll, oo);
+        chunk_redo<HD>(a, s.it.b, s.it.h, tk, hh, s.kb0 * 64, min(s.kb1 * 64, see_r + 1), mm, ll, oo);
         const float inv = ll != 0.f ? 1.f / ll : 0.f;
 #pragma unroll
         for (int k = 0; k < HD / 32; ++k) {
@@ -1440,6 +1417,7 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
   const long long end = pos + per < all ? pos + per : all;
   const int QT = 1 << wt.sp.qt_log;
   auto wait = [&](uint32_t b, uint32_t parity) {
+    if (mbar_try_wait(b, parity & 1u)) return true;
     if (*abort_flag) return false;
     if (mbar_wait(b, parity & 1u, a.werr)) return true;
     *abort_flag = 1;
@@ -1494,7 +1472,7 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
       return (bool)__all_sync(0xffffffffu, ok);
     }, no_end);
   } else if (warp == 9) {
-    if (lane == 0) {
+    if (elect_one()) {
       constexpr uint32_t IDS = idesc_bf16_f32(128, 128);
       constexpr uint64_t T_E = Sh::T_BYTES >> 4, COL_E = Sh::COL >> 4;
       const uint64_t dk = smem_desc_sw128(smem_u32(sm)), dq = smem_desc_sw128(smem_u32(sm + Sh::OFF_Q));
@@ -1776,7 +1754,7 @@ cudaError_t launch_chunk_attn(const ChunkDev& c, int dtype, const tlf_attn_chunk
   char* s = static_cast<char*>(scratch);
   ChunkAttn a{};
   a.c = c;
-  a.sp = ChunkSplit{pow2_log(std::max(1, p.rt / c.G)), p.pair ? 7 : 6};
+  a.sp = ChunkSplit{pow2_log(std::max(1, p.rt / c.G)), 6};
   a.q = args.q;
   a.qs = args.q_stride ? args.q_stride : (long long)c.Hq * c.hd;
   a.out = args.out;
