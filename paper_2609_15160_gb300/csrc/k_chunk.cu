@@ -145,7 +145,9 @@ __global__ void __launch_bounds__(256) k_chunk_join(ChunkAttn a) {
           w = exp2f(ml.x - ref);
           l += w * ml.y;
         }
-        for (int i = 0; i < min(32, parts - i0); ++i) add(i0 + i, __shfl_sync(0xffffffffu, w, i));
+        const int np = min(32, parts - i0);
+#pragma unroll 4
+        for (int i = 0; i < np; ++i) add(i0 + i, __shfl_sync(0xffffffffu, w, i));
       }
       l = warp_sum(l);
     }
@@ -1309,10 +1311,11 @@ __global__ void __launch_bounds__(256) k_chunk_weigh_scores(ChunkAttn a, const f
 // query rows, so sums need no exchange between threads and no atomics. A CTA goes over its units of the flat order (row, block
 // of 256 keys, head, tile of 128 query rows); K of a (block, head) stays in shared memory while the tiles of q stream through.
 //   warps 0-3, 4-7  keys 0-127 and 128-255 of the block: S from tensor memory, sums, the block's sums out at its end;
-//   warp 8          producer (tensor maps);  warp 9  issues S^T into one of two pairs of TMEM buffers;
-//   warp 10         the tile's lse into shared memory.
+//   warp 8          producer (tensor maps);
+//   warps 9, 10     issue S^T of keys 0-127 and 128-255 into one of two TMEM buffers each;
+//   warp 11         the tile's lse into shared memory.
 // A block inside one CTA's share is written out; parts of a shared one meet in k_weigh_join, in the CTAs' order.
-constexpr int WEIGH_THREADS = 352;
+constexpr int WEIGH_THREADS = 384;
 struct WeighTc {
   WeighSplit sp;
   const float* w_in;
@@ -1390,9 +1393,14 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
   const ChunkDev& c = a.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    for (int i = 0; i < 4 + 2 * NQ; ++i) mbar_init(bar(i), 1);
+    for (unsigned i = 0; i < NQ; ++i) {
+      mbar_init(q_full(i), 1);
+      mbar_init(q_empty(i), 2);
+    }
     for (unsigned i = 0; i < 2; ++i) {
-      mbar_init(s_full(i), 1);
+      mbar_init(k_full(i), 1);
+      mbar_init(k_empty(i), 2);
+      mbar_init(s_full(i), 2);
       mbar_init(s_read(i), 8);
       mbar_init(l_full(i), 1);
     }
@@ -1471,8 +1479,9 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
       }
       return (bool)__all_sync(0xffffffffu, ok);
     }, no_end);
-  } else if (warp == 9) {
+  } else if (warp == 9 || warp == 10) {
     if (elect_one()) {
+      const int x = warp - 9;
       constexpr uint32_t IDS = idesc_bf16_f32(128, 128);
       constexpr uint64_t T_E = Sh::T_BYTES >> 4, COL_E = Sh::COL >> 4;
       const uint64_t dk = smem_desc_sw128(smem_u32(sm)), dq = smem_desc_sw128(smem_u32(sm + Sh::OFF_Q));
@@ -1482,13 +1491,11 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
         if (!wait(q_full(n), n / NQ) || (n >= 2 && !wait(s_read(n), n / 2 - 1))) return false;
         tc_fence_after();
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int kc = 0; kc < Sh::ATOMS; ++kc)
 #pragma unroll
-          for (int kc = 0; kc < Sh::ATOMS; ++kc)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              tc_mma_f16(tmem + (n & 1) * 256 + 128u * x, dk + ((kl & 1) * 2 + x) * T_E + kc * COL_E + 2 * k,
-                         dq + (n % NQ) * T_E + kc * COL_E + 2 * k, IDS, (kc | k) ? 1u : 0u);
+          for (int k = 0; k < 4; ++k)
+            tc_mma_f16(tmem + (n & 1) * 256 + 128u * x, dk + ((kl & 1) * 2 + x) * T_E + kc * COL_E + 2 * k,
+                       dq + (n % NQ) * T_E + kc * COL_E + 2 * k, IDS, (kc | k) ? 1u : 0u);
         tc_commit(s_full(n));
         tc_commit(q_empty(n));
         if (k_last) {
@@ -1499,7 +1506,7 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
       }, no_end);
     }
     __syncwarp();
-  } else if (warp == 10) {
+  } else if (warp == 11) {
     each([&](const WeighBlock& w, int h, int t, unsigned n, bool, bool) {
       if (n >= 2 && !__all_sync(0xffffffffu, wait(s_read(n), n / 2 - 1))) return false;
       const int cols = min(QT, w.ql - t * QT) << g_log;
