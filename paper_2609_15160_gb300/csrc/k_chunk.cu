@@ -1530,7 +1530,7 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
       tc_fence_after();
       const int key = w.kb * 256 + x * 128 + row, cols = min(QT, w.ql - t * QT) << g_log;
       // query i of the row sees the key when s0 + i >= key: columns from lo on
-      const long long lo = ((long long)key - w.s0 - (long long)t * QT) << g_log;
+      const int lo = min(max(key - w.s0 - t * QT, 0), cols >> g_log) << g_log;
       const bool cut = cols < 128 || __any_sync(0xffffffffu, lo > 0);
       const float* l = s_lse + (n & 1) * 128;
       float p4[4] = {0.f, 0.f, 0.f, 0.f};
@@ -1551,8 +1551,10 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
           }
         } else {
 #pragma unroll
-          for (int j = 0; j < 64; ++j)
-            if (c0 + j >= lo && c0 + j < cols) p4[j & 3] += ex2_fast(fmaf(__uint_as_float(su[j]), scale, -l[c0 + j]));
+          for (int j = 0; j < 64; ++j) {
+            const float p = ex2_fast(fmaf(__uint_as_float(su[j]), scale, -l[c0 + j]));
+            p4[j & 3] += (unsigned)(c0 + j - lo) < (unsigned)(cols - lo) ? p : 0.f;
+          }
         }
       }
       sum += (p4[0] + p4[1]) + (p4[2] + p4[3]);
