@@ -112,45 +112,14 @@ __global__ void __launch_bounds__(256) k_chunk_join(ChunkAttn a) {
   const int c0 = blockIdx.x, parts = (int)((it.first + it.nb - 1) / per) - c0 + 1;
   const int qt = 1 << a.sp.qt_log, G = a.c.G, rows = min(qt, it.ql - it.t * qt) * G, lane = threadIdx.x & 31, hd = a.c.hd;
   const bool mine = lane * VW < hd;
-  for (int row = blockIdx.y * 8 + (threadIdx.x >> 5); row < rows; row += gridDim.y * 8) {
-    auto slot = [&](int i) { return (size_t)(i == 0 ? 2 * c0 + 1 : 2 * (c0 + i)) * a.rows + row; };
-    float m = -INFINITY, l = 0.f, o[VW];
-#pragma unroll
-    for (int k = 0; k < VW; ++k) o[k] = 0.f;
-    auto add = [&](int i, float w) {
-      if (w == 0.f || !mine) return;
-      const float* p = a.part_o + slot(i) * hd + lane * VW;
-      float v[VW];
-      if (VW == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(p);
-      else if (VW == 2) *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(p);
-      else v[0] = *p;
-#pragma unroll
-      for (int k = 0; k < VW; ++k) o[k] += w * v[k];
-    };
-    if (parts == 2) {  // the usual case, without the exchange
-      const float2 x = a.part_ml[slot(0)], y = a.part_ml[slot(1)];
-      m = fmaxf(x.x, y.x);
-      const float ref = m == -INFINITY ? 0.f : m, wx = exp2f(x.x - ref), wy = exp2f(y.x - ref);
-      l = wx * x.y + wy * y.y;
-      add(0, wx);
-      add(1, wy);
-    } else {
-      for (int i = lane; i < parts; i += 32) m = fmaxf(m, a.part_ml[slot(i)].x);
-      m = warp_max(m);
-      const float ref = m == -INFINITY ? 0.f : m;
-      for (int i0 = 0; i0 < parts; i0 += 32) {
-        float w = 0.f;
-        if (i0 + lane < parts) {
-          const float2 ml = a.part_ml[slot(i0 + lane)];
-          w = exp2f(ml.x - ref);
-          l += w * ml.y;
-        }
-        const int np = min(32, parts - i0);
-#pragma unroll 4
-        for (int i = 0; i < np; ++i) add(i0 + i, __shfl_sync(0xffffffffu, w, i));
-      }
-      l = warp_sum(l);
-    }
+  auto slot = [&](int i, int row) { return (size_t)(i == 0 ? 2 * c0 + 1 : 2 * (c0 + i)) * a.rows + row; };
+  auto get = [&](int i, int row, float (&v)[VW]) {
+    const float* p = a.part_o + slot(i, row) * hd + lane * VW;
+    if (VW == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(p);
+    else if (VW == 2) *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(p);
+    else v[0] = *p;
+  };
+  auto put = [&](int row, float m, float l, const float (&o)[VW]) {
     const int token = it.t0 + it.t * qt + row / G, head = it.h * G + row % G;
     T* out = static_cast<T*>(a.out) + token * a.os + (long long)head * hd + lane * VW;
     const float inv = l != 0.f ? 1.f / l : 0.f;
@@ -158,6 +127,67 @@ __global__ void __launch_bounds__(256) k_chunk_join(ChunkAttn a) {
 #pragma unroll
       for (int k = 0; k < VW; ++k) out[k] = from_f32<T>(o[k] * inv);
     if (lane == 0 && a.lse) a.lse[(long long)token * a.c.Hq + head] = l != 0.f ? (m + log2f(l)) * LN2 : -INFINITY;
+  };
+  const int first = blockIdx.y * 8 + (threadIdx.x >> 5), step = gridDim.y * 8;
+  if (parts == 2) {  // the usual case: U rows in flight, statistics and sums together
+    constexpr int U = 4;
+    for (int r0 = first; r0 < rows; r0 += U * step) {
+      float2 x[U], y[U];
+      float u[U][VW], v[U][VW];
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int row = r0 + k * step;
+        if (row >= rows) break;
+        x[k] = a.part_ml[slot(0, row)];
+        y[k] = a.part_ml[slot(1, row)];
+        if (mine) {
+          get(0, row, u[k]);
+          get(1, row, v[k]);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int row = r0 + k * step;
+        if (row >= rows) break;
+        const float m = fmaxf(x[k].x, y[k].x), ref = m == -INFINITY ? 0.f : m, wx = exp2f(x[k].x - ref), wy = exp2f(y[k].x - ref);
+        float o[VW];
+#pragma unroll
+        for (int d = 0; d < VW; ++d) o[d] = (wx != 0.f ? wx * u[k][d] : 0.f) + (wy != 0.f ? wy * v[k][d] : 0.f);
+        put(row, m, wx * x[k].y + wy * y[k].y, o);
+      }
+    }
+    return;
+  }
+  for (int row = first; row < rows; row += step) {
+    float m = -INFINITY, l = 0.f, o[VW];
+#pragma unroll
+    for (int k = 0; k < VW; ++k) o[k] = 0.f;
+    for (int i = lane; i < parts; i += 32) m = fmaxf(m, a.part_ml[slot(i, row)].x);
+    m = warp_max(m);
+    const float ref = m == -INFINITY ? 0.f : m;
+    for (int i0 = 0; i0 < parts; i0 += 32) {
+      float w = 0.f;
+      if (i0 + lane < parts) {
+        const float2 ml = a.part_ml[slot(i0 + lane, row)];
+        w = exp2f(ml.x - ref);
+        l += w * ml.y;
+      }
+      constexpr int U = 4;
+      for (int i = 0; i < min(32, parts - i0); i += U) {
+        float v[U][VW];
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+          if (mine && i0 + i + k < parts) get(i0 + i + k, row, v[k]);
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+          const float wi = __shfl_sync(0xffffffffu, w, i + k);
+          if (mine && i0 + i + k < parts && wi != 0.f)
+#pragma unroll
+            for (int d = 0; d < VW; ++d) o[d] += wi * v[k][d];
+        }
+      }
+    }
+    put(row, m, warp_sum(l), o);
   }
 }
 
@@ -1735,7 +1765,7 @@ static cudaError_t chunk_launch(const ChunkAttn& a, const tlf_attn_chunk_args& a
     e = a.c.hd == 16 ? simt_rows<16>(a, st) : a.c.hd == 32 ? simt_rows<32>(a, st) : a.c.hd == 64 ? simt_rows<64>(a, st) : simt_rows<128>(a, st);
   if (e) return e;
   const int base = (a.c.n + 1) * 8;
-  const dim3 jg(a.ctas - 1, a.rows == 256 ? 4 : (a.rows + 7) / 8);
+  const dim3 jg(a.ctas - 1, a.rows == 256 ? 8 : (a.rows + 7) / 8);
   e = a.c.hd == 128  ? launch_k(k_chunk_join<T, 4>, jg, dim3(256), base, st, a)
       : a.c.hd == 64 ? launch_k(k_chunk_join<T, 2>, jg, dim3(256), base, st, a)
                      : launch_k(k_chunk_join<T, 1>, jg, dim3(256), base, st, a);
