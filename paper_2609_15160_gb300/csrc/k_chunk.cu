@@ -68,7 +68,7 @@ __device__ __forceinline__ long long chunk_share(const ChunkAttn& a, long long a
 struct ChunkItem {
   int b, h, t, nb;     // row, kv head, tile, its blocks
   int t0, s0, ql, len; // the row's first new token, old entries, new tokens, entries
-  long long first;     // the item's first block in the flat order
+  long long first;     // the item's first block in the flat order (may lie behind `pos`, which then is in its pad)
 };
 __device__ __forceinline__ ChunkItem chunk_item(const ChunkDev& c, const ChunkSplit& sp, const long long* base, long long pos) {
   int lo = 0, hi = c.n;  // largest b with base[b] <= pos (rows without tokens have no blocks)
@@ -89,7 +89,7 @@ __device__ __forceinline__ ChunkItem chunk_item(const ChunkDev& c, const ChunkSp
   const long long at = rel - it.h * per;
   it.t = sp.tile_of(it.s0, it.ql, at);
   it.nb = sp.blocks(it.s0, it.ql, it.t);
-  it.first = base[lo] + it.h * per + sp.before(it.s0, it.ql, it.t);
+  it.first = base[lo] + it.h * per + sp.before(it.s0, it.ql, it.t) + sp.pad;
   return it;
 }
 
@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(256) k_chunk_join(ChunkAttn a) {
   const long long all = s_base[a.c.n], per = chunk_share(a, all), pos = (blockIdx.x + 1) * per;
   if (pos >= all) return;
   const ChunkItem it = chunk_item(a.c, a.sp, s_base, pos);
-  if (it.first == pos || it.first / per != blockIdx.x) return;
+  if (it.first >= pos || it.first / per != blockIdx.x) return;
   const int c0 = blockIdx.x, parts = (int)((it.first + it.nb - 1) / per) - c0 + 1;
   const int qt = 1 << a.sp.qt_log, G = a.c.G, rows = min(qt, it.ql - it.t * qt) * G, lane = threadIdx.x & 31, hd = a.c.hd;
   const bool mine = lane * VW < hd;
@@ -222,6 +222,8 @@ __global__ void __launch_bounds__(256) k_chunk_simt(ChunkAttn a) {
   const int tid = threadIdx.x, x = tid & 15, y = tid >> 4, G = c.G, qt = 1 << a.sp.qt_log;
   while (pos < end) {
     const ChunkItem it = chunk_item(c, a.sp, s_base, pos);
+    if (pos < it.first) pos = it.first;
+    if (pos >= end) break;
     const int kb0 = (int)(pos - it.first), kb1 = (int)(end - it.first < it.nb ? end - it.first : it.nb);
     const int nq = min(qt, it.ql - it.t * qt), rows = nq * G;
     const int token0 = it.t0 + it.t * qt, see0 = it.s0 + it.t * qt;  // the tile's first query sees entries 0..see0
@@ -375,6 +377,11 @@ __global__ void __launch_bounds__(256) k_chunk_simt(ChunkAttn a) {
 // V of keys that no row of the tile sees is zeroed in the fragments (0 times an infinity is not 0). Keys that only some rows
 // see can still spoil the others' O with a 0 x infinity: a row whose O is not finite is then done again by chunk_redo, over
 // the keys that it sees alone.
+struct MmaSeg {  // a CTA's part of an item: blocks kb0 .. kb1 - 1 of nb
+  long long first;  // the item's first block in the flat order
+  int b, h, token0, see0, nq, kb0, kb1, nb;
+  static constexpr int RING = 16;
+};
 template <int HD, int MT>
 struct MmaShape {
   static constexpr int RT = 16 * MT, KS = 8 / MT, KW = MT == 4 ? 32 : 16;  // rows, key groups, keys of a warp in a page
@@ -384,7 +391,8 @@ struct MmaShape {
   static constexpr int NST = HD == 128 ? 5 : HD == 64 ? 5 : 8;
   static constexpr int OS = HD + 8;                      // floats of a merge buffer's row
   static constexpr int OFF_O = NST * STAGE, OFF_ML = OFF_O + 4 * 16 * OS * 4, OFF_BAR = OFF_ML + KS * RT * 8,
-                       OFF_INT = OFF_BAR + 2 * NST * 8, OFF_BASE = OFF_INT + (NST + 2 + 64 + 1) / 2 * 8;
+                       OFF_INT = OFF_BAR + 2 * NST * 8, OFF_SEG = OFF_INT + (NST + 2 + 64 + 1) / 2 * 8,
+                       OFF_BASE = OFF_SEG + MmaSeg::RING * (int)sizeof(MmaSeg);
   static int bytes(int n) { return OFF_BASE + (n + 1) * 8 + 1024; }
   static constexpr int THREADS = 288;
 };
@@ -403,6 +411,20 @@ __device__ __forceinline__ void mma_16816(float* d, const uint32_t* a, uint32_t 
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void bar_named(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+// Barrier `id` of `threads` threads; whether any of them has p.
+__device__ __forceinline__ bool bar_any(int id, int threads, bool p) {
+  int r;
+  asm volatile(
+      "{\n\t.reg .pred q, s;\n\t"
+      "setp.ne.s32 q, %3, 0;\n\t"
+      "bar.red.or.pred s, %1, %2, q;\n\t"
+      "selp.s32 %0, 1, 0, s;\n\t}"
+      : "=r"(r)
+      : "r"(id), "r"(threads), "r"((int)p)
+      : "memory");
+  return r != 0;
+}
 
 __device__ __forceinline__ bool finite4(float4 v) {
   return fabsf(v.x) < INFINITY && fabsf(v.y) < INFINITY && fabsf(v.z) < INFINITY && fabsf(v.w) < INFINITY;
@@ -452,6 +474,7 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
   volatile int* abort_flag = s_skip + NST;
   volatile int* s_any = s_skip + NST + 1;
   volatile int* s_bad = s_skip + NST + 2;  // [RT]
+  MmaSeg* s_seg = reinterpret_cast<MmaSeg*>(sm + Sh::OFF_SEG);
   long long* s_base = reinterpret_cast<long long*>(sm + Sh::OFF_BASE);
   auto full = [&](int st) { return smem_u32(&bars[st]); };
   auto empty = [&](int st) { return smem_u32(&bars[NST + st]); };
@@ -484,9 +507,19 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
   unsigned seq = 0;  // pages that this CTA's ring has taken
 
   if (warp == 8) {
-    while (pos < end) {
+    for (unsigned segs = 0; pos < end; ++segs) {
       const ChunkItem it = chunk_item(c, a.sp, s_base, pos);
+      if (pos < it.first) pos = it.first;
+      if (pos >= end) {
+        if (segs == 0 && lane == 0) {
+          s_seg[0].nb = 0;
+          mbar_arrive(full(0));
+        }
+        break;
+      }
       const int kb0 = (int)(pos - it.first), kb1 = (int)(end - it.first < it.nb ? end - it.first : it.nb);
+      // the consumers find the item here when they see its first page
+      if (lane == 0) s_seg[segs % MmaSeg::RING] = MmaSeg{it.first, it.b, it.h, it.t0 + it.t * qt, it.s0 + it.t * qt, min(qt, it.ql - it.t * qt), kb0, kb1, it.nb};
       const int rowK = (c.layer * 2 * c.Hkv + it.h) * 64, rowV = rowK + c.Hkv * 64;
       for (int g0 = kb0; g0 < kb1; g0 += 32) {
         int mine = -1;
@@ -529,11 +562,14 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
   const int vk = slice * KW + ((lane >> 3) & 1) * 8 + (lane & 7), vc = lane >> 4;
   constexpr int CH = Sh::ROW / 16;  // 16-byte chunks of a row
   auto swz = [](int key) { return HD == 32 ? (key >> 1) & 3 : key & 7; };
-  while (pos < end) {
-    const ChunkItem it = chunk_item(c, a.sp, s_base, pos);
-    const int kb0 = (int)(pos - it.first), kb1 = (int)(end - it.first < it.nb ? end - it.first : it.nb);
-    const int nq = min(qt, it.ql - it.t * qt), rows = nq * G;
-    const int token0 = it.t0 + it.t * qt, see0 = it.s0 + it.t * qt, see_last = see0 + nq - 1;
+  bool go = pos < end;
+  for (unsigned segs = 0; go; ++segs) {
+    // the item is written before its first page's barrier is armed; the ring of pages keeps the producer less than RING ahead.
+    // The warps leave together or not at all: they meet at barriers below, which know no time limit
+    if (bar_any(1, 256, !wait(full(seq % NST), (seq / NST) & 1u))) break;
+    const MmaSeg it = s_seg[segs % MmaSeg::RING];
+    if (it.nb == 0) break;  // this share is all pad
+    const int kb0 = it.kb0, kb1 = it.kb1, nq = it.nq, rows = nq * G, token0 = it.token0, see0 = it.see0, see_last = see0 + nq - 1;
     const int r0 = mt * 16 + (lane >> 2), r1 = r0 + 8;
     // rows past the tile's see what its first query sees, with q = 0; nobody reads them
     const int sees[2] = {see0 + (r0 < rows ? r0 / G : 0), see0 + (r1 < rows ? r1 / G : 0)};
@@ -743,7 +779,7 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
         if (d == 0) a.part_ml[part + r] = ml;
       }
     }
-    bar_named(1, 256);
+    if (nq > 1) bar_named(1, 256);
     if (nq > 1 && *s_any) {
       for (int r = warp; r < rows; r += 8) {
         if (!s_bad[r]) continue;
@@ -767,7 +803,8 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
       if (tid == 0) *s_any = 0;
       bar_named(1, 256);
     }
-    pos = it.first + kb1;
+    // the next item lies behind its pad
+    go = kb1 == it.nb && it.first + it.nb + a.sp.pad < end;
   }
   pdl_trigger();
 }
@@ -908,10 +945,12 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
     ChunkItem it;
     int kb0, kb1, nq[2], e[2], token0, see0;
   };
-  auto segment = [&](long long at) {
-    Seg s;
-    s.it = chunk_item(c, a.sp, s_base, at);
-    s.kb0 = (int)(at - s.it.first);
+  auto segment = [&](Seg& s) {  // false: none left
+    if (pos >= end) return false;
+    s.it = chunk_item(c, a.sp, s_base, pos);
+    if (pos < s.it.first) pos = s.it.first;
+    if (pos >= end) return false;
+    s.kb0 = (int)(pos - s.it.first);
     s.kb1 = (int)(end - s.it.first < s.it.nb ? end - s.it.first : s.it.nb);
     const int q0 = s.it.t << qt_log, left = s.it.ql - q0;
     s.token0 = s.it.t0 + q0;
@@ -923,14 +962,15 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       const int nb = s.nq[x] > 0 ? (last < 0 ? 1 : last / 64 + 1) : 0;
       s.e[x] = max(0, min(s.kb1, nb) - s.kb0);
     }
-    return s;
+    pos = s.it.first + s.kb1;
+    return true;
   };
+  Seg s;
 
   if (warp == 8) {
     // ---------------- producer ----------------
     unsigned blk = 0, segs = 0;
-    while (pos < end) {
-      const Seg s = segment(pos);
+    while (segment(s)) {
       const int E = s.kb1 - s.kb0;
       bool ok = true;
       if (lane == 0) {
@@ -971,7 +1011,6 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         }
       }
       ++segs;
-      pos = s.it.first + s.kb1;
     }
   } else if (warp >= 9) {
     // ---------------- MMA issuers, one a tile ----------------
@@ -993,8 +1032,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         tc_commit(s_full(x, n));
       };
       bool ok = true;
-      while (pos < end && ok) {
-        const Seg s = segment(pos);
+      while (ok && segment(s)) {
         const int E = s.kb1 - s.kb0, e = x ? s.e[1] : s.e[0];
         ok = e == 0 || wait(q_full(x), qn++);
         for (int i = 0; i < min(2, E) && ok; ++i) {  // S of the first two blocks
@@ -1027,8 +1065,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
           if (i + 3 == E) tc_commit(q_free);
         }
         blk += E;
-        pos = s.it.first + s.kb1;
-      }
+        }
     }
     __syncwarp();
   } else {
@@ -1043,8 +1080,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
     bool ok = true;
     // waits taken by the whole warp: the TMEM accesses after them are warp-collective
     auto wait_w = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, wait(b, parity)); };
-    while (pos < end && ok) {
-      const Seg s = segment(pos);
+    while (ok && segment(s)) {
       const bool row_ok = qi < s.nq[x];
       const int see = row_ok ? s.see0 + x * QT + qi : -1;  // a row past the tile's queries sees nothing
       const int see0 = s.see0 + x * QT;                    // of the tile's first query
@@ -1189,7 +1225,6 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         __syncwarp();
       }
       blk += s.kb1 - s.kb0;
-      pos = s.it.first + s.kb1;
     }
   }
   if (*abort_flag) drain_copies();
@@ -1646,10 +1681,16 @@ __global__ void __launch_bounds__(256) k_weigh_join(ChunkAttn a, WeighTc wt, int
 // Launches
 // ----------------------------------------------------------------------------
 // Which kernel and split a call takes; a function of the arguments and the device alone.
+#ifndef PAD_PAIR
+#define PAD_PAIR 4
+#define PAD_MMA128 4
+#define PAD_MMA 10
+#endif
 struct ChunkPath {
   bool pair;    // k_chunk_pair
   int rt;       // rows of an item
   int ctas;
+  int pad;      // blocks that an item counts beside its own
   bool scores;  // k_chunk_mma leaves its scores for the weights
   size_t part_ml, lse, werr, scores_at, total;  // scratch offsets (part_o at 0)
 };
@@ -1669,6 +1710,7 @@ static ChunkPath chunk_path(const ChunkDev& c, int dtype, const tlf_attn_chunk_a
     p.pair = rows > 64 && c.hd >= 64 && pow2 && q16;
     p.rt = p.pair ? 256 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
     p.ctas = (c.hd == 128 || p.pair ? 1 : 2) * num_sms;
+    p.pad = p.pair ? PAD_PAIR : c.hd == 128 ? PAD_MMA128 : PAD_MMA;
   }
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o = (o + bytes + 255) / 256 * 256; return at; };
@@ -1793,7 +1835,7 @@ cudaError_t launch_chunk_attn(const ChunkDev& c, int dtype, const tlf_attn_chunk
   char* s = static_cast<char*>(scratch);
   ChunkAttn a{};
   a.c = c;
-  a.sp = ChunkSplit{pow2_log(std::max(1, p.rt / c.G)), 6};
+  a.sp = ChunkSplit{pow2_log(std::max(1, p.rt / c.G)), 6, p.pad};
   a.q = args.q;
   a.qs = args.q_stride ? args.q_stride : (long long)c.Hq * c.hd;
   a.out = args.out;

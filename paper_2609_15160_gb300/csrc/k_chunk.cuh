@@ -7,9 +7,11 @@ namespace tlf {
 // new tokens behind s0 = len - ql old entries sees the first nb(t) blocks; an item is a tile of one kv head. All items'
 // blocks lie in one flat order (row, head, tile, block), of which every CTA takes an equal share: it streams the same number
 // of blocks whatever the lengths, and items that it shares with other CTAs are joined afterwards. nb is at least 1, so that
-// queries that see nothing are answered too. The sums over tiles are closed forms: no list of items is ever written.
+// queries that see nothing are answered too. An item also costs its CTA something beside its blocks (look-ups, joining the
+// warps' parts, writing out): it counts as `pad` more blocks, which lie before its own in the flat order and which nobody
+// works on. The sums over tiles are closed forms: no list of items is ever written.
 struct ChunkSplit {
-  int qt_log, bk_log;
+  int qt_log, bk_log, pad;
 
   __host__ __device__ int tiles(int ql) const { return (ql + (1 << qt_log) - 1) >> qt_log; }
   __host__ __device__ int blocks(int s0, int ql, int t) const {
@@ -22,7 +24,7 @@ struct ChunkSplit {
     const long long q = n >> r, rem = n & ((1LL << r) - 1);
     return ((q * (q + 1) / 2) << r) + rem * (q + 1);
   }
-  // blocks of the row's first t tiles (of one head); only its last tile may be cut short, so tiles before it are whole
+  // blocks of the row's first t tiles (of one head), with what the items count beside; only its last tile may be cut short, so tiles before it are whole
   __host__ __device__ long long before(int s0, int ql, int t) const {
     const int nt = tiles(ql), whole = t < nt ? t : nt - 1;
     if (t <= 0 || nt <= 0) return 0;
@@ -41,7 +43,7 @@ struct ChunkSplit {
       if (k0 > whole) k0 = whole;
       sum = k0 + ceil_sum(a + whole > 0 ? a + whole : 0, rl) - ceil_sum(a + k0 > 0 ? a + k0 : 0, rl);
     }
-    return t < nt ? sum : sum + blocks(s0, ql, nt - 1);
+    return (t < nt ? sum : sum + blocks(s0, ql, nt - 1)) + (long long)t * pad;
   }
   // the tile that holds block `at` (counted from the row's first) of the row's head
   __host__ __device__ int tile_of(int s0, int ql, long long at) const {

@@ -170,7 +170,7 @@ SPLIT = r"""
 int main() {
   for (int bl = 6; bl <= 7; ++bl)
     for (int it = 0; it < 6000; ++it) {
-      const tlf::ChunkSplit s{rand() % 9, bl};
+      const tlf::ChunkSplit s{rand() % 9, bl, it % 3 ? rand() % 12 : 0};
       const int ql = rand() % 700, any = it % 5 ? rand() % 1500 - 700 : rand() % 100000, s0 = any < -ql ? -ql : any, nt = s.tiles(ql);
       long long sum = 0;
       if (nt != (ql + (1 << s.qt_log) - 1) / (1 << s.qt_log)) return 1;
@@ -179,8 +179,8 @@ int main() {
         if (t == nt) break;
         const int end = (t + 1) << s.qt_log, keys = s0 + (end < ql ? end : ql), want = keys <= 0 ? 1 : (keys + (1 << bl) - 1) / (1 << bl);
         if (s.blocks(s0, ql, t) != want) return 3;
-        if (s.tile_of(s0, ql, sum) != t || s.tile_of(s0, ql, sum + want - 1) != t) return 4;
-        sum += want;
+        if (s.tile_of(s0, ql, sum) != t || s.tile_of(s0, ql, sum + s.pad + want - 1) != t) return 4;
+        sum += s.pad + want;
       }
     }
   for (int it = 0; it < 6000; ++it) {
