@@ -10,7 +10,7 @@
 // k_chunk_mma    bfloat16, up to 64 query rows a tile: tensor cores through mma.sync.
 // k_chunk_simt   float32: tiles in shared memory, products on the CUDA cores.
 // With weights, exp(s - lse) of every entry added up over the queries that see it:
-// k_weigh_tc            behind k_chunk_pair: S^T again on tcgen05, a thread a key;
+// k_weigh_tc            more than 16 rows: S^T again on tcgen05, a thread a key;
 // k_chunk_weigh_scores  from the scores that k_chunk_mma leaves;
 // k_chunk_weigh         the rest, on the CUDA cores.
 #include <algorithm>
@@ -1681,18 +1681,20 @@ __global__ void __launch_bounds__(256) k_weigh_join(ChunkAttn a, WeighTc wt, int
 // Launches
 // ----------------------------------------------------------------------------
 // Which kernel and split a call takes; a function of the arguments and the device alone.
-#ifndef PAD_PAIR
-#define PAD_PAIR 4
-#define PAD_MMA128 4
-#define PAD_MMA 10
-#endif
+//
+// What an item counts beside its blocks (microseconds at 0 / 8 blocks of k_chunk_pair: 8192 causal tokens, 16 / 8 heads x 128,
+// 276 / 221, 4 x 1000 over 4000 entries 114 / 103; at 0 / 10 pages of k_chunk_mma with head_dim 64: 32 single tokens over up to
+// 8192 entries 119 / 105, 32 rows of up to 16 tokens 128 / 107; at 2 / 6 pages with head_dim 128: 100 single tokens over up to
+// 500 entries 45 / 40). Without, CTAs with many short items finished up to a third later than the others.
+constexpr int PAD_PAIR = 8, PAD_MMA128 = 6, PAD_MMA = 10, PAD_SIMT = 2;
 struct ChunkPath {
   bool pair;    // k_chunk_pair
   int rt;       // rows of an item
   int ctas;
   int pad;      // blocks that an item counts beside its own
-  bool scores;  // k_chunk_mma leaves its scores for the weights
-  size_t part_ml, lse, werr, scores_at, total;  // scratch offsets (part_o at 0)
+  bool weigh_tc;  // the weights from k_weigh_tc
+  bool scores;    // k_chunk_mma leaves its scores for the weights
+  size_t part_ml, lse, werr, weigh, scores_at, total;  // scratch offsets (part_o at 0)
 };
 static int pow2_log(int x) {  // largest l with 2^l <= x
   int l = 0;
@@ -1705,23 +1707,31 @@ static ChunkPath chunk_path(const ChunkDev& c, int dtype, const tlf_attn_chunk_a
   if (dtype == TLF_DTYPE_F32) {
     p.rt = rows <= 16 ? 16 : 64;
     p.ctas = 2 * num_sms;
+    p.pad = PAD_SIMT;
   } else {
-    const bool pow2 = (c.G & (c.G - 1)) == 0, q16 = reinterpret_cast<uintptr_t>(a.q) % 16 == 0 && a.q_stride % 8 == 0;
-    p.pair = rows > 64 && c.hd >= 64 && pow2 && q16;
+    // tcgen05: tiles of 128 rows of whole groups of heads, q through a tensor map
+    const bool tc = c.hd >= 64 && (c.G & (c.G - 1)) == 0 && reinterpret_cast<uintptr_t>(a.q) % 16 == 0 && a.q_stride % 8 == 0;
+    p.pair = rows > 64 && tc;
+    p.weigh_tc = a.weight_out && rows > 16 && tc;
     p.rt = p.pair ? 256 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
     p.ctas = (c.hd == 128 || p.pair ? 1 : 2) * num_sms;
     p.pad = p.pair ? PAD_PAIR : c.hd == 128 ? PAD_MMA128 : PAD_MMA;
   }
+  // no more CTAs than there can be blocks
+  const int qt_log = pow2_log(std::max(1, p.rt / c.G));
+  p.ctas = (int)std::min<long long>(p.ctas, std::max<long long>(1, ((long long)(c.T >> qt_log) + c.n) * c.Hkv * (c.max_pages + p.pad)));
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o = (o + bytes + 255) / 256 * 256; return at; };
   take((size_t)2 * p.ctas * p.rt * c.hd * 4);
   p.part_ml = take((size_t)2 * p.ctas * p.rt * 8);
   p.lse = take(a.weight_out && !a.lse ? (size_t)c.T * c.Hq * 4 : 0);
   p.werr = take(4);
-  // 4 bytes a (query, head, entry): less than reading K again while G x new tokens is below head_dim / 2, and the same kernel
-  // then serves all rows; a bound on the scratch, which the host can only size by the longest row
+  p.weigh = take(p.weigh_tc ? (size_t)2 * num_sms * 256 * 4 : 0);
+  // 4 bytes a (query, head, entry), written and read, instead of K again: up to 16 rows, and where k_weigh_tc cannot serve, up
+  // to a bound on the scratch, which the host can only size by the longest row (32 rows of up to 32 / 64 tokens over up to 8192
+  // entries, 16 heads x 64, with weights: ... us with k_weigh_tc)
   const long long score_bytes = (long long)c.T * c.Hq * c.max_pages * 256;
-  p.scores = dtype == TLF_DTYPE_BF16 && a.weight_out && !p.pair && score_bytes <= (256LL << 20);
+  p.scores = dtype == TLF_DTYPE_BF16 && a.weight_out && !p.weigh_tc && score_bytes <= (256LL << 20);
   p.scores_at = take(p.scores ? (size_t)score_bytes : 0);
   p.total = o;
   return p;
@@ -1767,14 +1777,14 @@ static cudaError_t pair_launch(const ChunkAttn& a, cudaStream_t st) {
   if (cudaError_t e = ensure_kernel_attrs(reinterpret_cast<const void*>(k_chunk_pair<HD>), Sh::bytes(SV_MAX_ROWS))) return e;
   return launch_k(k_chunk_pair<HD>, dim3(a.ctas), dim3(PAIR_THREADS), Sh::bytes(a.c.n), st, a, pow2_log(a.c.G), qm, pm);
 }
-// The weights behind k_chunk_pair; the parts lie where the attention's were (k_chunk_join has read them).
 template <int HD>
-static cudaError_t weigh_launch(const ChunkAttn& a, const tlf_attn_chunk_args& args, cudaStream_t st) {
+static cudaError_t weigh_launch(ChunkAttn a, const tlf_attn_chunk_args& args, float* part, int num_sms, cudaStream_t st) {
+  a.ctas = num_sms;
   CUtensorMap qm, pm;
   if (!q_map(&qm, a) || !pool_map(&pm, a.c)) return cudaErrorInvalidValue;
   using Sh = WeighShape<HD>;
   if (cudaError_t e = ensure_kernel_attrs(reinterpret_cast<const void*>(k_weigh_tc<HD>), Sh::bytes(SV_MAX_ROWS))) return e;
-  const WeighTc w{WeighSplit{a.sp.qt_log - 1, 8}, args.weight_in, args.weight_out, a.part_o};
+  const WeighTc w{WeighSplit{7 - pow2_log(a.c.G), 8}, args.weight_in, args.weight_out, part};
   if (cudaError_t e = launch_k(k_weigh_tc<HD>, dim3(a.ctas), dim3(WEIGH_THREADS), Sh::bytes(a.c.n), st, a, w, pow2_log(a.c.G), qm, pm))
     return e;
   const int per_row = std::max(1, std::min(8, 1024 / a.c.n));
@@ -1799,7 +1809,7 @@ static cudaError_t simt_rows(const ChunkAttn& a, cudaStream_t st) {
   return a.rows == 16 ? simt_launch<float, 16, HD>(a, st) : simt_launch<float, 64, HD>(a, st);
 }
 template <typename T>
-static cudaError_t chunk_launch(const ChunkAttn& a, const tlf_attn_chunk_args& args, int num_sms, cudaStream_t st) {
+static cudaError_t chunk_launch(const ChunkAttn& a, const tlf_attn_chunk_args& args, float* weigh, int num_sms, cudaStream_t st) {
   cudaError_t e;
   if (std::is_same<T, bf16>::value)
     e = a.c.hd == 32 ? mma_rows<32>(a, st) : a.c.hd == 64 ? mma_rows<64>(a, st) : mma_rows<128>(a, st);
@@ -1807,7 +1817,7 @@ static cudaError_t chunk_launch(const ChunkAttn& a, const tlf_attn_chunk_args& a
     e = a.c.hd == 16 ? simt_rows<16>(a, st) : a.c.hd == 32 ? simt_rows<32>(a, st) : a.c.hd == 64 ? simt_rows<64>(a, st) : simt_rows<128>(a, st);
   if (e) return e;
   const int base = (a.c.n + 1) * 8;
-  const dim3 jg(a.ctas - 1, a.rows == 256 ? 8 : (a.rows + 7) / 8);
+  const dim3 jg(std::max(1, a.ctas - 1), a.rows == 256 ? 8 : (a.rows + 7) / 8);
   e = a.c.hd == 128  ? launch_k(k_chunk_join<T, 4>, jg, dim3(256), base, st, a)
       : a.c.hd == 64 ? launch_k(k_chunk_join<T, 2>, jg, dim3(256), base, st, a)
                      : launch_k(k_chunk_join<T, 1>, jg, dim3(256), base, st, a);
@@ -1815,7 +1825,7 @@ static cudaError_t chunk_launch(const ChunkAttn& a, const tlf_attn_chunk_args& a
   if (!args.weight_out) return cudaSuccess;
   const dim3 grid(4 * num_sms);
   if constexpr (std::is_same<T, bf16>::value)
-    if (a.rows == 256) return a.c.hd == 64 ? weigh_launch<64>(a, args, st) : weigh_launch<128>(a, args, st);
+    if (weigh) return a.c.hd == 64 ? weigh_launch<64>(a, args, weigh, num_sms, st) : weigh_launch<128>(a, args, weigh, num_sms, st);
   if (a.scores) return launch_k(k_chunk_weigh_scores, grid, dim3(256), base, st, a, args.weight_in, args.weight_out);
   switch (a.c.hd) {
     case 16: return launch_k(k_chunk_weigh<T, 16>, grid, dim3(256), base, st, a, args.weight_in, args.weight_out);
@@ -1849,7 +1859,8 @@ cudaError_t launch_chunk_attn(const ChunkDev& c, int dtype, const tlf_attn_chunk
   a.werr = c.err ? c.err : reinterpret_cast<uint32_t*>(s + p.werr);
   a.part_o = reinterpret_cast<float*>(s);
   a.part_ml = reinterpret_cast<float2*>(s + p.part_ml);
-  return dtype == TLF_DTYPE_BF16 ? chunk_launch<bf16>(a, args, num_sms, st) : chunk_launch<float>(a, args, num_sms, st);
+  float* weigh = p.weigh_tc ? reinterpret_cast<float*>(s + p.weigh) : nullptr;
+  return dtype == TLF_DTYPE_BF16 ? chunk_launch<bf16>(a, args, weigh, num_sms, st) : chunk_launch<float>(a, args, weigh, num_sms, st);
 }
 
 }  // namespace tlf

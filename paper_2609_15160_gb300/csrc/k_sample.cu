@@ -112,8 +112,7 @@ struct SampleShared {
   uint32_t key[SM_LIST];
   int idx[SM_LIST];
   u64 mass[SM_SORT];      // of a digit of the select; of the list, sorted
-  unsigned bin[SM_BINS];  // tokens of this CTA's part, or threads' maxima
-  unsigned tot[SM_BINS];  // bin of the whole row
+  alignas(8) unsigned bin[SM_BINS];  // tokens of this CTA's part, or threads' maxima
   unsigned cnt[256];
   uint32_t skey[SM_SORT];
   int sidx[SM_SORT];
@@ -214,15 +213,20 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
     cl.sync();
     sum = 0.f;
     for (int r = 0; r < cs; ++r) sum += *cl.map_shared_rank(&S.sum, r);
-    for (int i = tid; i < SM_BINS; i += SM_THREADS) {
-      unsigned n = 0;
-      for (int r = 0; r < cs; ++r) n += cl.map_shared_rank(S.bin, r)[i];
-      S.tot[i] = n;
-    }
-  } else {
-    __syncthreads();
-    for (int i = tid; i < SM_BINS; i += SM_THREADS) S.tot[i] = S.bin[i];
   }
+  // tokens of this thread's two bins in the whole row
+  static_assert(SM_BINS == 2 * SM_THREADS && SM_SORT <= SM_THREADS, "two bins a thread");
+  const int bin0 = 2 * tid, bin1 = bin0 + 1;
+  uint2 tot = make_uint2(0u, 0u);
+  if (by_k || by_p) {
+    if (cs == 1) __syncthreads();
+    for (int r = 0; r < cs; ++r) {
+      const uint2 n = *reinterpret_cast<const uint2*>((cs > 1 ? cl.map_shared_rank(S.bin, r) : S.bin) + bin0);
+      tot.x += n.x;
+      tot.y += n.y;
+    }
+  }
+  const unsigned tot0 = tot.x, tot1 = bin1 < SM_BINS - 1 ? tot.y : 0u;
   __syncthreads();
 
   // the draw: largest z - log(-log u), ties to the lower index
@@ -272,9 +276,6 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
     });
     return mass;
   };
-  static_assert(SM_BINS == 2 * SM_THREADS && SM_SORT <= SM_THREADS, "two bins a thread");
-  const int bin0 = 2 * tid, bin1 = bin0 + 1;
-  const unsigned tot0 = S.tot[bin0], tot1 = bin1 < SM_BINS - 1 ? S.tot[bin1] : 0u;
   // tokens of bins first .. last
   auto tokens_in = [&](int first, int last) {
     return block_sum((bin0 >= first && bin0 <= last ? (int)tot0 : 0) + (bin1 >= first && bin1 <= last ? (int)tot1 : 0), S.redi);

@@ -551,3 +551,71 @@ def test_operators_in_a_cuda_graph(T):
     assert torch.equal(once[0], out) and torch.equal(once[1], tok) and torch.equal(once[2], w)
     assert abs(float(w.sum()) - 12) < 1e-3  # every query head of every row gives away 1
     assert int(d["err"][0].item()) == 0
+
+
+# ---- sizes at the edges of the types ----
+
+def test_a_thousand_rows(T):
+    """The most rows of a call; with one long row among them every kernel's tables are at their largest."""
+    rng = np.random.default_rng(0)
+    for new in (np.ones(1024, np.int64), np.where(np.arange(1024) == 700, 90, 1)):
+        c = R.Cache(rng.integers(0, 130, 1024), new, 2, 1, 64, "bf16", layers=1, layer=0, seed=9)
+        d = c.device()
+        ref = R.attention(c)
+        w_in = np.zeros((c.pages, 64), np.float32)
+        got = _attend(T, c, d, weights=True)
+        _hold_weights(c, got[2], w_in, ref, _hold(c, d, got, ref))
+
+
+@pytest.mark.parametrize("new", [1, 5, 100])
+def test_pages_beyond_32_bit_offsets(T, new):
+    """Pages whose elements lie past 2^32: append, attention with weights and eviction there."""
+    import torch
+    c = R.Cache([90, 200], [new, new], 4, 2, 128, "bf16", layers=2, layer=1, seed=7)
+    page = 2 * 2 * 2 * 64 * 128
+    far = (1 << 32) // page + 10
+    if torch.cuda.mem_get_info()[0] < (far + c.pages) * page * 2 + (4 << 30):
+        pytest.skip("needs 13 GB of the GPU's memory")
+    pool = torch.empty(far + c.pages, 2, 2, 2, 64, 128, dtype=torch.bfloat16, device="cuda")
+    pool[far:] = torch.tensor(c.pool).bfloat16().cuda()
+    side = lambda fill, dt: torch.full((far + c.pages, 64), fill, dtype=dt, device="cuda")  # noqa: E731
+    table = torch.tensor(np.where(c.table >= 0, c.table + far, -1)).cuda()
+    d = c.device()
+    # the new entries again, from the rows' own keys and values, unturned
+    kv = [c.kv(b) for b in range(2)]
+    k, v = (torch.tensor(np.concatenate([x[i][o:] for x, o in zip(kv, c.old)])).bfloat16().cuda() for i in (0, 1))
+    for b in range(2):
+        p, o = c.at(b, np.arange(c.old[b], c.lens[b]))
+        pool[torch.tensor(p + far).cuda().long(), 1, :, :, torch.tensor(o).cuda()] = 9
+    cs = torch.zeros(8, 64, 2, device="cuda")
+    cs[..., 0] = 1
+    qo, pos, w = torch.empty_like(d["q"]), side(-1, torch.int32), side(3.0, torch.float32)
+    b = T.chunk_args(pool, table, d["cu"], d["lens"], 4, c.T, layer=1, err=d["err"])
+    zero = torch.zeros(c.T, dtype=torch.int32, device="cuda")
+    T.tlf_rope_append(b, T.rope_args(d["q"], k, v, zero, cs, qo, entry_pos=pos, entry_weight=w))
+    got = _attend(T, c, dict(d, pool=pool, table=table), weights=False)
+    ref = R.attention(c)
+    _hold(c, d, got, ref)
+    out, lse = torch.empty_like(d["q"]), torch.empty(c.T, 4, device="cuda")
+    w_out = torch.zeros_like(w)
+    a = T.attn_chunk_args(d["q"], out, lse=lse, weight_in=w, weight_out=w_out)
+    n = T.tlf_attn_chunk_scratch_bytes(b, a)
+    T.tlf_attn_chunk(b, a, torch.empty(n, dtype=torch.uint8, device="cuda"), n)
+    for row in range(2):
+        p, o = c.at(row, np.arange(c.lens[row]))
+        seen = w_out[torch.tensor(p + far).cuda().long(), torch.tensor(o).cuda()].cpu().numpy()
+        prior = np.where(np.arange(c.lens[row]) < c.old[row], 3.0, 0.0)
+        assert np.abs(seen - prior - ref[4][row]).max() < 1e-3
+    nxt = torch.tensor([1000, 1000], dtype=torch.int32, device="cuda")
+    before = pool[far:].clone()
+    e = T.evict_args(pool, table, d["lens"], nxt, pos, pos, w_out, w_out, torch.empty_like(d["lens"]), budget=70, err=d["err"])
+    n = T.tlf_cache_evict_scratch_bytes(e)
+    T.tlf_cache_evict(e, torch.empty(n, dtype=torch.uint8, device="cuda"), n)
+    torch.cuda.synchronize()
+    assert int(d["err"][0].item()) == 0
+    after = pool[far:]
+    for row in range(2):
+        p, o = c.at(row, np.arange(c.lens[row]))
+        p, o = torch.tensor(p).cuda().long(), torch.tensor(o).cuda()
+        held = {x.tobytes() for x in before[p, :, :, :, o].float().cpu().numpy()}
+        assert all(x.tobytes() in held for x in after[p[:70], :, :, :, o[:70]].float().cpu().numpy())
