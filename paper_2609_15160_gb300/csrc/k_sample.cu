@@ -10,8 +10,8 @@
 //   top-k   tokens from the k-th largest of the threads' own maxima on (to the next 1/32 in z): at least k of them;
 //   top-p   a histogram over bins of z of width 1/32 (taken in the pass of the sum) bounds the weight up to every bin from
 //           both sides: bins that surely stay, bins that surely do not, and a few between them, where the threshold lies and
-//           which alone take part in finding it. The ones that stay go to the list too, or, where they are too many, take
-//           part in the draw at once.
+//           which alone take part in finding it. The ones that stay go to a list of their own, or, where they are too many,
+//           take part in the draw at once.
 // A short list is sorted by counting. A longer one takes a radix select over the keys: by count for top-k, by weight for top-p,
 // with weights in 2^-40 fixed point, so the order of the atomics does not matter. Where the candidates are too many for the
 // list (logits that are nearly all alike), the select goes over the whole row. A row is split over a cluster of up to eight
@@ -28,7 +28,8 @@ namespace cg = cooperative_groups;
 namespace tlf {
 
 constexpr int SM_THREADS = 512;
-constexpr int SM_LIST = 6144;
+constexpr int SM_LIST = 4096;   // candidates among which the threshold lies
+constexpr int SM_SURE = 12288;  // tokens that stay for sure
 constexpr int SM_SORT = 512;   // longest list that is sorted by counting
 constexpr int SM_CLUSTER = 8;  // most CTAs that share a row
 
@@ -111,6 +112,7 @@ __device__ __forceinline__ void add_mass(u64* at, u64 m) {
 struct SampleShared {
   uint32_t key[SM_LIST];
   int idx[SM_LIST];
+  int sure[SM_SURE];
   u64 mass[SM_SORT];      // of a digit of the select; of the list, sorted
   alignas(8) unsigned bin[SM_BINS];  // tokens of this CTA's part, or threads' maxima
   unsigned cnt[256];
@@ -284,9 +286,9 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
   int* sure_at = cs > 1 ? cl.map_shared_rank(&S.n_sure, 0) : &S.n_sure;
   uint32_t* key_to = cs > 1 ? cl.map_shared_rank(S.key, 0) : S.key;
   int* idx_to = cs > 1 ? cl.map_shared_rank(S.idx, 0) : S.idx;
-  // tokens from `cut` on into the list, those from `top` on (NaN: none) from its end down, or nowhere; the weight of the latter
+  int* sure_to = cs > 1 ? cl.map_shared_rank(S.sure, 0) : S.sure;
+  // tokens from `cut` on into the list; those from `top` on (NaN: none) into the one of the sure, or nowhere
   auto gather = [&](float cut, float top, bool keep) {
-    float mass = 0.f;
     sample_pass(row, v0, v1, wide, [&](const float (&e)[16], int i) {
       unsigned in = 0, high = 0;
 #pragma unroll
@@ -309,20 +311,23 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
         if (upto >> 16) back = atomicAdd(sure_at, upto >> 16);
       }
       front = __shfl_sync(0xffffffffu, front, 31) + ((upto - mine) & 0xffff);
-      back = SM_LIST - 1 - __shfl_sync(0xffffffffu, back, 31) - ((upto - mine) >> 16);
+      back = __shfl_sync(0xffffffffu, back, 31) + ((upto - mine) >> 16);
 #pragma unroll
       for (int x = 0; x < 16; ++x) {
         if (!(in >> x & 1)) continue;
-        const bool is_high = high >> x & 1;
-        if (is_high) mass += ex2_fast(z2_of(e[x]));
-        const int at = is_high ? back-- : front++;
-        if (at >= 0 && at < SM_LIST) {
-          key_to[at] = sample_key(sample_logit(e[x]));
-          idx_to[at] = i + (x >> 2) * SM_STEP + (x & 3);
+        const int idx = i + (x >> 2) * SM_STEP + (x & 3);
+        if (high >> x & 1) {
+          if (back < SM_SURE) sure_to[back] = idx;
+          ++back;
+        } else {
+          if (front < SM_LIST) {
+            key_to[front] = sample_key(sample_logit(e[x]));
+            idx_to[front] = idx;
+          }
+          ++front;
         }
       }
     });
-    return mass;
   };
 
   const float none_f = __int_as_float(0x7fffffff);
@@ -360,13 +365,12 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
       // from `top` on a token is in a sure bin; the rest of those counts as between
       const float cut = cut_at(-(none - 0.49f) / SM_BIN);
       const float top = sure < 0 ? none_f : mx - (sure + 0.49f) / SM_BIN * T * 0.99999f + 1e-6f * fabsf(mx);
-      if (n_sure + n_between <= SM_LIST - SM_LIST / 32) {
-        heavy = gather(cut, top, true);
+      if (n_sure <= SM_SURE) {
+        gather(cut, top, true);
       } else {
-        heavy = race_pass(top, std::true_type{});
+        heavy = block_sum(race_pass(top, std::true_type{}), S.redf);
         gather(cut, top, false);
       }
-      heavy = block_sum(heavy, S.redf);
       list = true;
     }
   } else {  // no limit but min-p
@@ -412,9 +416,9 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
     for (int r = 0; r < cs; ++r) heavy += S.heavy[r];
   }
   __syncthreads();
-  if (list && S.n + S.n_sure > SM_LIST) list = false;  // more tokens at the bound than the bins let expect
+  if (list && S.n > SM_LIST) list = false;  // more tokens at the bound than the bins let expect
   const int n = list ? S.n : V;
-  const u64 heavier = list ? (u64)(heavy * 1099511627776.f) : 0;
+  u64 heavier = list ? (u64)(heavy * 1099511627776.f) : 0;
   // list entries that take part: noise of four in flight
   auto race_list = [&](int first, int count, auto stays) {
     for (int i0 = 0; i0 < count; i0 += 4 * SM_THREADS) {
@@ -434,7 +438,29 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
       }
     }
   };
-  if (list && S.n_sure) race_list(SM_LIST - S.n_sure, S.n_sure, [](uint32_t, int) { return true; });
+  if (list && S.n_sure) {  // the tokens that stay for sure
+    u64 mass = 0;
+    for (int i0 = tid; i0 < S.n_sure; i0 += 4 * SM_THREADS) {
+      float l[4], u[4];
+      int idx[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int i = i0 + x * SM_THREADS;
+        idx[x] = i < S.n_sure ? S.sure[i] : -1;
+        l[x] = idx[x] >= 0 ? row[idx[x]] : -INFINITY;
+        u[x] = idx[x] >= 0 ? noise[idx[x]] : 0.f;
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        if (idx[x] < 0) continue;
+        mass += sample_mass(ex2_fast(z2_of(l[x])));
+        if (may_win(l[x], u[x])) race(sample_logit(l[x]), u[x], idx[x]);
+        lim = fmaxf(lim, best);
+      }
+    }
+    heavier += block_sum(mass, S.redl);
+  }
+
   if (list && n <= SM_SORT) {
     // sorted by (key, lower index): a token's place is the number of tokens before it
     if (tid < n) {
