@@ -31,7 +31,6 @@ struct ChunkAttn {
   float* lse;      // [T][Hq] or NULL
   float scale;     // of the scores, times log2 e
   int ctas, rows;  // CTAs that share the blocks; rows of a part
-  long long min_blocks;  // least share of a CTA
   float* scores;   // k_chunk_mma: [T][Hq][max_pages * 64] scores that it leaves for the weights, or NULL
   uint32_t* werr;  // error word of the waits: the caller's, or one in the scratch
   float* part_o;   // [2 ctas][rows][hd]
@@ -60,8 +59,7 @@ __device__ __forceinline__ void chunk_plan(const ChunkDev& c, const ChunkSplit& 
 }
 
 __device__ __forceinline__ long long chunk_share(const ChunkAttn& a, long long all) {
-  const long long per = (all + a.ctas - 1) / a.ctas;
-  return per > a.min_blocks ? per : a.min_blocks;
+  return all > 0 ? (all + a.ctas - 1) / a.ctas : 1;
 }
 
 // The item that holds block `pos` of the flat order.
@@ -203,7 +201,8 @@ struct SimtShape {
 };
 
 // 16 lanes share a row: lane x has keys x, x + 16, .. of a block in the first product and dims DW x .. in the second, so a
-// row's statistics and probabilities never leave its half warp.
+// row's statistics and probabilities never leave its half warp. Bound by launch and first loads on the models it serves
+// (4 rows of up to 5 tokens over up to 60 entries, 4 heads x 16: 8 us with the join, in a CUDA graph).
 template <typename T, int RT, int HD>
 __global__ void __launch_bounds__(256) k_chunk_simt(ChunkAttn a) {
   using Sh = SimtShape<RT, HD>;
@@ -377,6 +376,9 @@ __global__ void __launch_bounds__(256) k_chunk_simt(ChunkAttn a) {
 // V of keys that no row of the tile sees is zeroed in the fragments (0 times an infinity is not 0). Keys that only some rows
 // see can still spoil the others' O with a 0 x infinity: a row whose O is not finite is then done again by chunk_redo, over
 // the keys that it sees alone.
+//
+// Bound by HBM: 16 single tokens over 32k entries, 16 / 8 heads x 128: 311 us with the join, 6.8 TB/s (0.99 of the copy rate);
+// 32 over up to 8192 entries, 16 heads x 64: 105 us, 5.7 TB/s, the rest of it ramp, items' ends and the join.
 struct MmaSeg {  // a CTA's part of an item: blocks kb0 .. kb1 - 1 of nb
   long long first;  // the item's first block in the flat order
   int b, h, token0, see0, nq, kb0, kb1, nb;
@@ -823,7 +825,12 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
 // thread's MMAs run in order, so S of block i + 2 is issued right behind the P V of block i that reads the buffer, and the
 // softmax of block i + 1 finds its S ready when it is done with block i. With blocks of 128 keys there is room for one S a tile
 // only: a tile's chain S, softmax, P V was then 4.8k cycles a block, 2.0k of them MMAs (4 x 2048 tokens over up to 10240
-// entries, 16 / 8 heads x 128: 485 us).
+// entries, 16 / 8 heads x 128: 485 us, 330 so).
+//
+// What bounds it: at head_dim 128 the tensor cores (a block of a tile is 8 S products that read 6 KB of shared memory each, 48
+// cycles, and 4 P V products of 64 cycles: 1280 cycles for both tiles, 1670 measured); at head_dim 64 the exponentials (1024
+// cycles a block for both tiles, 1560 measured with what surrounds them). With the join: 363 us for the case above (1340
+// TFLOP/s, 0.70 of the measured bf16 rate), 351 us with 16 heads x 64 (690), 222 us for 8192 causal tokens (1240).
 constexpr int PAIR_THREADS = 352;
 
 template <int HD>
@@ -1324,7 +1331,8 @@ __global__ void __launch_bounds__(256) k_chunk_weigh(ChunkAttn a, const float* w
 }
 
 // The same from the scores that k_chunk_mma left: an item is 256 entries of a row; 64 threads x 4 entries, four groups of
-// threads that take every fourth (query, head). Reads 4 bytes a (query, head, entry) instead of K again.
+// threads that take every fourth (query, head). Reads 4 bytes a (query, head, entry) instead of K again: 32 single tokens over
+// up to 8192 entries, 16 heads x 64: 12 us.
 __global__ void __launch_bounds__(256) k_chunk_weigh_scores(ChunkAttn a, const float* w_in, float* w_out) {
   pdl_wait();
   extern __shared__ long long s_base[];
@@ -1380,6 +1388,8 @@ __global__ void __launch_bounds__(256) k_chunk_weigh_scores(ChunkAttn a, const f
 //   warps 9, 10     issue S^T of keys 0-127 and 128-255 into one of two TMEM buffers each;
 //   warp 11         the tile's lse into shared memory.
 // A block inside one CTA's share is written out; parts of a shared one meet in k_weigh_join, in the CTAs' order.
+// Bound by the exponentials, 2048 of 2640 cycles a unit: 4 x 1000 tokens over up to 5000 entries, 16 / 8 heads x 128: 58 us
+// behind 103 us of attention.
 constexpr int WEIGH_THREADS = 384;
 struct WeighTc {
   WeighSplit sp;
@@ -1693,7 +1703,7 @@ struct ChunkPath {
   int ctas;
   int pad;      // blocks that an item counts beside its own
   bool weigh_tc;  // the weights from k_weigh_tc
-  bool scores;    // k_chunk_mma leaves its scores for the weights
+  long long scores;  // bytes of the scores that k_chunk_mma leaves for the weights
   size_t part_ml, lse, werr, weigh, scores_at, total;  // scratch offsets (part_o at 0)
 };
 static int pow2_log(int x) {  // largest l with 2^l <= x
@@ -1712,7 +1722,14 @@ static ChunkPath chunk_path(const ChunkDev& c, int dtype, const tlf_attn_chunk_a
     // tcgen05: tiles of 128 rows of whole groups of heads, q through a tensor map
     const bool tc = c.hd >= 64 && (c.G & (c.G - 1)) == 0 && reinterpret_cast<uintptr_t>(a.q) % 16 == 0 && a.q_stride % 8 == 0;
     p.pair = rows > 64 && tc;
-    p.weigh_tc = a.weight_out && rows > 16 && tc;
+    // weights: the scores that k_chunk_mma has at hand, 4 bytes a (query, head, entry) written and read instead of K again, up to
+    // 16 rows (32 rows of up to 16 / 17 tokens over up to 8192 entries, 16 heads x 64: 177 us so, 217 with k_weigh_tc; at 32 and
+    // 64 rows the bytes are two and four times as many, k_weigh_tc takes 221 and 279) and up to a bound on the scratch, which
+    // the host can only size by the longest row; else S^T again, on the CUDA cores where the tiles do not fit (933 and 1593 us)
+    const long long score_bytes = (long long)c.T * c.Hq * c.max_pages * 256;
+    const bool fit = score_bytes <= (256LL << 20);
+    p.weigh_tc = a.weight_out && tc && (rows > 16 || !fit);
+    p.scores = a.weight_out && !p.weigh_tc && fit ? score_bytes : 0;
     p.rt = p.pair ? 256 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
     p.ctas = (c.hd == 128 || p.pair ? 1 : 2) * num_sms;
     p.pad = p.pair ? PAD_PAIR : c.hd == 128 ? PAD_MMA128 : PAD_MMA;
@@ -1727,12 +1744,7 @@ static ChunkPath chunk_path(const ChunkDev& c, int dtype, const tlf_attn_chunk_a
   p.lse = take(a.weight_out && !a.lse ? (size_t)c.T * c.Hq * 4 : 0);
   p.werr = take(4);
   p.weigh = take(p.weigh_tc ? (size_t)2 * num_sms * 256 * 4 : 0);
-  // 4 bytes a (query, head, entry), written and read, instead of K again: up to 16 rows, and where k_weigh_tc cannot serve, up
-  // to a bound on the scratch, which the host can only size by the longest row (32 rows of up to 32 / 64 tokens over up to 8192
-  // entries, 16 heads x 64, with weights: ... us with k_weigh_tc)
-  const long long score_bytes = (long long)c.T * c.Hq * c.max_pages * 256;
-  p.scores = dtype == TLF_DTYPE_BF16 && a.weight_out && !p.weigh_tc && score_bytes <= (256LL << 20);
-  p.scores_at = take(p.scores ? (size_t)score_bytes : 0);
+  p.scores_at = take((size_t)p.scores);
   p.total = o;
   return p;
 }
@@ -1828,7 +1840,10 @@ static cudaError_t chunk_launch(const ChunkAttn& a, const tlf_attn_chunk_args& a
     if (weigh) return a.c.hd == 64 ? weigh_launch<64>(a, args, weigh, num_sms, st) : weigh_launch<128>(a, args, weigh, num_sms, st);
   if (a.scores) return launch_k(k_chunk_weigh_scores, grid, dim3(256), base, st, a, args.weight_in, args.weight_out);
   switch (a.c.hd) {
-    case 16: return launch_k(k_chunk_weigh<T, 16>, grid, dim3(256), base, st, a, args.weight_in, args.weight_out);
+    case 16:
+      if constexpr (std::is_same<T, float>::value)
+        return launch_k(k_chunk_weigh<T, 16>, grid, dim3(256), base, st, a, args.weight_in, args.weight_out);
+      break;
     case 32: return launch_k(k_chunk_weigh<T, 32>, grid, dim3(256), base, st, a, args.weight_in, args.weight_out);
     case 64: return launch_k(k_chunk_weigh<T, 64>, grid, dim3(256), base, st, a, args.weight_in, args.weight_out);
     case 128: {
@@ -1854,7 +1869,6 @@ cudaError_t launch_chunk_attn(const ChunkDev& c, int dtype, const tlf_attn_chunk
   a.scale = (args.scale != 0.f ? args.scale : 1.f / sqrtf((float)c.hd)) * LOG2E;
   a.ctas = p.ctas;
   a.rows = p.rt;
-  a.min_blocks = 1;
   a.scores = p.scores ? reinterpret_cast<float*>(s + p.scores_at) : nullptr;
   a.werr = c.err ? c.err : reinterpret_cast<uint32_t*>(s + p.werr);
   a.part_o = reinterpret_cast<float*>(s);

@@ -3,6 +3,10 @@
 // Pair (x_a, x_b) of a head at position p becomes (x_a c - x_b s, x_b c + x_a s), (c, s) = table[p][pair]: what is
 // turned at position p and what is turned at p' then meet in q . k as a function of p - p'. The table is read, not computed:
 // a float32 angle p f_k loses log2(p f_k) bits of the turn, and a row of it is shared by every head of the token.
+//
+// Bound by HBM for many tokens (7157 tokens, 16 / 8 heads x 128, 64 dims turned, interleaved: 24.3 us, 4.9 TB/s; 40 us before
+// the table's rows went through shared memory and copied units stayed raw, 146 instructions a 16-byte unit), by the look-ups'
+// dependent loads for few (64 tokens, 16 heads x 64: 3.2 us in a CUDA graph).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>

@@ -17,6 +17,10 @@
 // list (logits that are nearly all alike), the select goes over the whole row. A row is split over a cluster of up to eight
 // CTAs while there are SMs left over. In the draw a token's -log(-log u) is first bounded by -log(1 - u), and only the few that
 // could beat the warp's best so far are computed.
+//
+// Bound by instructions and by the latency of the passes; the bytes' floor is the logits once (256 x 50304: 7.6 us). 256 rows of
+// 50304: 17 us greedy, 20 with top-k 50, 42 with top-p 0.95 (nucleus of 1600), 40 with no limit (the random numbers of all
+// tokens), 55 with all of these mixed, where the rows with the largest nuclei decide.
 #include <type_traits>
 
 #include <cooperative_groups.h>
@@ -644,9 +648,11 @@ __global__ void __launch_bounds__(SM_THREADS, 2) k_sample(SampleDev a, int cs) {
 cudaError_t launch_sample(const tlf_sample_args& a, int num_sms, cudaStream_t st) {
   SampleDev d{a.vocab, a.logits, a.logits_stride, a.noise, a.noise_stride, a.temperature, a.top_k, a.top_p, a.min_p,
               a.tokens, a.logprobs};
-  // rows are split over clusters while that leaves every CTA an SM's half: one row of 32000 takes ... us on one CTA, ... on eight
+  // rows are split over clusters while there is an SM for every CTA and a part is not too short for its share of the steps that
+  // every part has (on 1 / 2 / 4 / 8 CTAs a row, top-p 0.95: one row of 32000 tokens 18.8 / 17.6 / 15.5 / 15.6 us, one of 128000
+  // 48.6 / 35.4 / 27.0 / 23.1, 64 of 50304 30.8 / 27.2 / 27.9 / 45.3, 120 of 50304 31.3 / 34.6 / 48.4 / 72.2)
   int cs = 1;
-  while (cs < SM_CLUSTER && (long long)a.n * cs * 2 <= 2 * num_sms && a.vocab > 2048 * cs) cs *= 2;
+  while (cs < SM_CLUSTER && (long long)a.n * cs * 2 <= num_sms && a.vocab >= 16000 * cs) cs *= 2;
   if (cudaError_t e = ensure_kernel_attrs(reinterpret_cast<const void*>(k_sample), sizeof(SampleShared))) return e;
   return launch_cluster(k_sample, dim3(a.n * cs), dim3(SM_THREADS), cs, sizeof(SampleShared), st, d, cs);
 }
