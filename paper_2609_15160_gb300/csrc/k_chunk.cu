@@ -99,14 +99,16 @@ __device__ __forceinline__ ChunkItem chunk_item(const ChunkDev& c, const ChunkSp
 // a row at a time, VW dims a lane (hd = 32 VW, or 16 with VW = 1), and every eight-th row of a CTA's.
 template <typename T, int VW>
 __global__ void __launch_bounds__(256) k_chunk_join(ChunkAttn a) {
-  pdl_wait();
   extern __shared__ long long s_base[];
   __shared__ long long s_red[33];
   chunk_plan(a.c, a.sp, s_base, s_red);
   const long long all = s_base[a.c.n], per = chunk_share(a, all), pos = (blockIdx.x + 1) * per;
-  if (pos >= all) return;
-  const ChunkItem it = chunk_item(a.c, a.sp, s_base, pos);
-  if (it.first >= pos || it.first / per != blockIdx.x) return;
+  ChunkItem it{};
+  if (pos < all) it = chunk_item(a.c, a.sp, s_base, pos);
+  // The plan reads what no kernel of the call writes, so it runs beside the kernel before. Every CTA waits, those with nothing
+  // to join too: this grid's end tells the next one that the kernel before has ended.
+  pdl_wait();
+  if (pos >= all || it.first >= pos || it.first / per != blockIdx.x) return;
   const int c0 = blockIdx.x, parts = (int)((it.first + it.nb - 1) / per) - c0 + 1;
   const int qt = 1 << a.sp.qt_log, G = a.c.G, rows = min(qt, it.ql - it.t * qt) * G, lane = threadIdx.x & 31, hd = a.c.hd;
   const bool mine = lane * VW < hd;
@@ -215,6 +217,7 @@ __global__ void __launch_bounds__(256) k_chunk_simt(ChunkAttn a) {
   long long* s_base = reinterpret_cast<long long*>(sm + Sh::FLOATS);
   const ChunkDev& c = a.c;
   chunk_plan(c, a.sp, s_base, s_red);
+  pdl_trigger();
   const long long all = s_base[c.n], per = chunk_share(a, all);
   long long pos = blockIdx.x * per;
   const long long end = pos + per < all ? pos + per : all;
@@ -358,7 +361,6 @@ __global__ void __launch_bounds__(256) k_chunk_simt(ChunkAttn a) {
     }
     pos = it.first + kb1;
   }
-  pdl_trigger();
 }
 
 // ----------------------------------------------------------------------------
@@ -495,6 +497,7 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
   if (tid < Sh::RT) s_bad[tid] = 0;
   pdl_wait();
   chunk_plan(c, a.sp, s_base, s_red);
+  pdl_trigger();
   const long long all = s_base[c.n], per = chunk_share(a, all);
   long long pos = blockIdx.x * per;
   const long long end = pos + per < all ? pos + per : all;
@@ -552,7 +555,6 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
       pos = it.first + kb1;
     }
     if (*abort_flag) drain_copies();
-    pdl_trigger();
     return;
   }
 
@@ -808,7 +810,6 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
     // the next item lies behind its pad
     go = kb1 == it.nb && it.first + it.nb + a.sp.pad < end;
   }
-  pdl_trigger();
 }
 
 // ----------------------------------------------------------------------------
@@ -1659,12 +1660,12 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
 // Blocks that k_weigh_tc's CTAs share: the first CTA whose share starts inside one adds its parts (grid x < ctas - 1). The
 // other CTAs of the grid copy the weights of rows without new tokens.
 __global__ void __launch_bounds__(256) k_weigh_join(ChunkAttn a, WeighTc wt, int per_row) {
-  pdl_wait();
   extern __shared__ long long s_base[];
   __shared__ long long s_red[33];
   const ChunkDev& c = a.c;
   if ((int)blockIdx.x >= a.ctas - 1) {
     const int i = blockIdx.x - (a.ctas - 1), b = i / per_row;
+    pdl_wait();
     const ChunkRow r = chunk_row(c, b);
     if (r.ql > 0) return;
     for (int e = (i % per_row) * 256 + threadIdx.x; e < r.len; e += per_row * 256) {
@@ -1675,9 +1676,10 @@ __global__ void __launch_bounds__(256) k_weigh_join(ChunkAttn a, WeighTc wt, int
     return;
   }
   const long long all = weigh_plan(c, wt.sp, s_base, s_red), per = chunk_share(a, all), pos = (blockIdx.x + 1) * per;
-  if (pos >= all) return;
-  const WeighBlock w = weigh_block(c, wt.sp, s_base, pos);
-  if (w.begin == pos || w.begin / per != blockIdx.x) return;
+  WeighBlock w{};
+  if (pos < all) w = weigh_block(c, wt.sp, s_base, pos);
+  pdl_wait();  // (as in k_chunk_join)
+  if (pos >= all || w.begin == pos || w.begin / per != blockIdx.x) return;
   const int c0 = blockIdx.x, c1 = (int)((w.begin + (long long)w.vis * c.Hkv - 1) / per), key = w.kb * 256 + threadIdx.x;
   float sum = wt.part[(2 * c0 + 1) * 256 + threadIdx.x];
   for (int i = c0 + 1; i <= c1; ++i) sum += wt.part[2 * i * 256 + threadIdx.x];
@@ -1829,7 +1831,7 @@ static cudaError_t chunk_launch(const ChunkAttn& a, const tlf_attn_chunk_args& a
     e = a.c.hd == 16 ? simt_rows<16>(a, st) : a.c.hd == 32 ? simt_rows<32>(a, st) : a.c.hd == 64 ? simt_rows<64>(a, st) : simt_rows<128>(a, st);
   if (e) return e;
   const int base = (a.c.n + 1) * 8;
-  const dim3 jg(std::max(1, a.ctas - 1), a.rows == 256 ? 8 : (a.rows + 7) / 8);
+  const dim3 jg(std::max(1, a.ctas - 1), a.rows >= 64 ? 2 : 1);  // one wave of CTAs
   e = a.c.hd == 128  ? launch_k(k_chunk_join<T, 4>, jg, dim3(256), base, st, a)
       : a.c.hd == 64 ? launch_k(k_chunk_join<T, 2>, jg, dim3(256), base, st, a)
                      : launch_k(k_chunk_join<T, 1>, jg, dim3(256), base, st, a);
