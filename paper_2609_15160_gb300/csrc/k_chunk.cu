@@ -99,6 +99,7 @@ __device__ __forceinline__ ChunkItem chunk_item(const ChunkDev& c, const ChunkSp
 // a row at a time, VW dims a lane (hd = 32 VW, or 16 with VW = 1), and every eight-th row of a CTA's.
 template <typename T, int VW>
 __global__ void __launch_bounds__(256) k_chunk_join(ChunkAttn a) {
+  pdl_trigger();
   extern __shared__ long long s_base[];
   __shared__ long long s_red[33];
   chunk_plan(a.c, a.sp, s_base, s_red);
@@ -1382,16 +1383,19 @@ __global__ void __launch_bounds__(256) k_chunk_weigh_scores(ChunkAttn a, const f
 // Weights on tcgen05 (bfloat16, head_dim 64 and 128, many rows)
 // ----------------------------------------------------------------------------
 // S^T = K Q^T with the keys as MMA rows: a thread owns one key (TMEM lane) and adds exp(s - lse) over the columns, which are
-// query rows, so sums need no exchange between threads and no atomics. A CTA goes over its units of the flat order (row, block
+// query rows, so sums need no exchange between threads and no atomics. lse comes off inside the product: 16 more columns beside
+// head_dim, ones in K and -lse / scale in q, in three bfloat16 that hold 24 bits (read from shared memory by every thread it
+// took the port that the MMAs read their operands through). A CTA goes over its units of the flat order (row, block
 // of 256 keys, head, tile of 128 query rows); K of a (block, head) stays in shared memory while the tiles of q stream through.
-//   warps 0-3, 4-7  keys 0-127 and 128-255 of the block: S from tensor memory, sums, the block's sums out at its end;
-//   warp 8          producer (tensor maps);
-//   warps 9, 10     issue S^T of keys 0-127 and 128-255 into one of two TMEM buffers each;
-//   warp 11         the tile's lse into shared memory.
+//   warps 0-15      two sets of eight take turns at the units; warps 0-3 and 4-7 of a set have keys 0-127 and 128-255 of the
+//                   block: S from tensor memory, sums, and at the block's end the sum of both sets out;
+//   warp 16         producer (tensor maps);
+//   warps 17, 18    issue S^T of keys 0-127 and 128-255 into one of two TMEM buffers each;
+//   warp 19         the tile's lse into the columns beside q.
 // A block inside one CTA's share is written out; parts of a shared one meet in k_weigh_join, in the CTAs' order.
 // Bound by the exponentials, 2048 of 2640 cycles a unit: 4 x 1000 tokens over up to 5000 entries, 16 / 8 heads x 128: 58 us
 // behind 103 us of attention.
-constexpr int WEIGH_THREADS = 384;
+constexpr int WEIGH_THREADS = 640;
 struct WeighTc {
   WeighSplit sp;
   const float* w_in;
@@ -1401,12 +1405,17 @@ struct WeighTc {
 template <int HD>
 struct WeighShape {
   static constexpr int ATOMS = HD / 64, COL = 128 * 128, T_BYTES = ATOMS * COL;
-  static constexpr int NQ = HD == 128 ? 2 : 6;
+  static constexpr int NQ = HD == 128 ? 2 : 6, NL = 4;  // tiles of q and of lse on the way
+  static constexpr int X_BYTES = 128 * 32;              // 128 rows of the 16 columns beside head_dim
   static constexpr int OFF_Q = 4 * T_BYTES;  // K: two buffers of two tiles
-  static constexpr int OFF_LSE = OFF_Q + NQ * T_BYTES, OFF_BAR = OFF_LSE + 2 * 128 * 4, NBAR = 4 + 2 * NQ + 6;
-  static constexpr int OFF_INT = OFF_BAR + NBAR * 8, OFF_BASE = OFF_INT + 16;
+  static constexpr int OFF_X = OFF_Q + NQ * T_BYTES, OFF_SUM = OFF_X + (1 + NL) * X_BYTES, OFF_BAR = OFF_SUM + 2 * 256 * 4;
+  static constexpr int NBAR = 4 + 2 * NQ + 4 + 2 * NL, OFF_INT = OFF_BAR + NBAR * 8, OFF_BASE = OFF_INT + 16;
   static int bytes(int n) { return std::max(OFF_BASE + (n + 1) * 8 + 1024, tmem_min_smem(512)); }
 };
+// Descriptor of a K-major tile of 16 columns: rows of 32 bytes, swizzled in atoms of 8 rows (the halves of rows 4-7 change places).
+__device__ __forceinline__ uint64_t smem_desc_sw32(uint32_t saddr) {
+  return (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)1u << 16 | (uint64_t)(256u >> 4) << 32 | (uint64_t)1u << 46 | (uint64_t)6u << 61;
+}
 
 __device__ __forceinline__ long long weigh_plan(const ChunkDev& c, const WeighSplit& sp, long long* base, long long* red) {
   long long carry = 0;
@@ -1449,12 +1458,11 @@ template <int HD>
 __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, WeighTc wt, int g_log, const __grid_constant__ CUtensorMap q_map,
                                                                const __grid_constant__ CUtensorMap pool_map) {
   using Sh = WeighShape<HD>;
-  constexpr int NQ = Sh::NQ;
+  constexpr int NQ = Sh::NQ, NL = Sh::NL;
   extern __shared__ uint8_t smem_raw[];
   __shared__ long long s_red[33];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(sm + Sh::OFF_BAR);
-  float* s_lse = reinterpret_cast<float*>(sm + Sh::OFF_LSE);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(sm + Sh::OFF_INT);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + Sh::OFF_INT) + 1;
   long long* s_base = reinterpret_cast<long long*>(sm + Sh::OFF_BASE);
@@ -1465,7 +1473,8 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
   auto q_empty = [&](unsigned i) { return bar(4 + NQ + i % NQ); };
   auto s_full = [&](unsigned i) { return bar(4 + 2 * NQ + (i & 1)); };
   auto s_read = [&](unsigned i) { return bar(4 + 2 * NQ + 2 + (i & 1)); };
-  auto l_full = [&](unsigned i) { return bar(4 + 2 * NQ + 4 + (i & 1)); };
+  auto l_full = [&](unsigned i) { return bar(4 + 2 * NQ + 4 + i % NL); };
+  auto l_empty = [&](unsigned i) { return bar(4 + 2 * NQ + 4 + NL + i % NL); };
   const ChunkDev& c = a.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
@@ -1478,27 +1487,38 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
       mbar_init(k_empty(i), 2);
       mbar_init(s_full(i), 2);
       mbar_init(s_read(i), 8);
+    }
+    for (unsigned i = 0; i < NL; ++i) {
       mbar_init(l_full(i), 1);
+      mbar_init(l_empty(i), 2);
     }
     *abort_flag = 0;
     fence_barrier_init();
     prefetch_tensormap(&q_map);
     prefetch_tensormap(&pool_map);
   }
-  if (warp == 9) {
+  if (warp == 17) {
     tmem_alloc(smem_u32(tmem_slot), 512);
     tmem_relinquish();
   }
-  pdl_wait();
-  const long long all = weigh_plan(c, wt.sp, s_base, s_red);
+  for (int i = tid; i < (1 + NL) * 256; i += WEIGH_THREADS) {  // the keys' ones, and zeros
+    const int r = i >> 1 & 127, half = i & 1;
+    *reinterpret_cast<uint4*>(sm + Sh::OFF_X + (i >> 8) * Sh::X_BYTES + r * 32 + (half ^ (r >> 2 & 1)) * 16) =
+        i < 256 && half == 0 ? make_uint4(0x3f803f80u, 0x3f80u, 0u, 0u) : make_uint4(0u, 0u, 0u, 0u);
+  }
+  fence_proxy_async_smem();
+  // The plan, K and q are read without waiting for the kernels before, which write none of it; only the lse are theirs, so only
+  // warp 19 waits, and what this grid writes comes after an lse.
+  const long long all = weigh_plan(c, wt.sp, s_base, s_red), per = chunk_share(a, all);
+  long long pos = blockIdx.x * per;
+  const long long end = pos + per < all ? pos + per : all;
+  WeighBlock w{};
+  if (pos < end) w = weigh_block(c, wt.sp, s_base, pos);
   tc_fence_before();
   __syncthreads();  // barriers initialised, tensor memory allocated
   tc_fence_after();
   pdl_trigger();
   const uint32_t tmem = *tmem_slot;
-  const long long per = chunk_share(a, all);
-  long long pos = blockIdx.x * per;
-  const long long end = pos + per < all ? pos + per : all;
   const int QT = 1 << wt.sp.qt_log;
   auto wait = [&](uint32_t b, uint32_t parity) {
     if (mbar_try_wait(b, parity & 1u)) return true;
@@ -1509,9 +1529,8 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
   };
   // f(block, head, tile, unit's number in this CTA, first unit of its K here, last one) for this CTA's units; false ends it
   auto each = [&](auto&& f, auto&& block_end) {
-    unsigned n = 0;
-    while (pos < end) {
-      const WeighBlock w = weigh_block(c, wt.sp, s_base, pos);
+    for (unsigned n = 0; pos < end;) {
+      if (n > 0) w = weigh_block(c, wt.sp, s_base, pos);
       const long long stop = w.begin + (long long)w.vis * c.Hkv < end ? w.begin + (long long)w.vis * c.Hkv : end, start = pos;
       int h = (int)((pos - w.begin) / w.vis), t = (int)((pos - w.begin) % w.vis);
       for (bool k_new = true; pos < stop; ++pos, ++n) {
@@ -1525,7 +1544,7 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
   };
   auto no_end = [](const WeighBlock&, long long, long long) { return true; };
 
-  if (warp == 8) {
+  if (warp == 16) {
     unsigned kl = 0;
     each([&](const WeighBlock& w, int h, int t, unsigned n, bool k_new, bool) {
       bool ok = true;
@@ -1555,12 +1574,13 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
       }
       return (bool)__all_sync(0xffffffffu, ok);
     }, no_end);
-  } else if (warp == 9 || warp == 10) {
+  } else if (warp == 17 || warp == 18) {
     if (elect_one()) {
-      const int x = warp - 9;
+      const int x = warp - 17;
       constexpr uint32_t IDS = idesc_bf16_f32(128, 128);
       constexpr uint64_t T_E = Sh::T_BYTES >> 4, COL_E = Sh::COL >> 4;
       const uint64_t dk = smem_desc_sw128(smem_u32(sm)), dq = smem_desc_sw128(smem_u32(sm + Sh::OFF_Q));
+      const uint64_t d_one = smem_desc_sw32(smem_u32(sm + Sh::OFF_X)), d_lse = smem_desc_sw32(smem_u32(sm + Sh::OFF_X + Sh::X_BYTES));
       unsigned kl = 0;
       each([&](const WeighBlock&, int, int, unsigned n, bool k_new, bool k_last) {
         if (k_new && !wait(k_full(kl), kl / 2)) return false;
@@ -1572,63 +1592,82 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
           for (int k = 0; k < 4; ++k)
             tc_mma_f16(tmem + (n & 1) * 256 + 128u * x, dk + ((kl & 1) * 2 + x) * T_E + kc * COL_E + 2 * k,
                        dq + (n % NQ) * T_E + kc * COL_E + 2 * k, IDS, (kc | k) ? 1u : 0u);
-        tc_commit(s_full(n));
         tc_commit(q_empty(n));
         if (k_last) {
           tc_commit(k_empty(kl));
           ++kl;
         }
+        if (!wait(l_full(n), n / NL)) return false;
+        tc_fence_after();
+        tc_mma_f16(tmem + (n & 1) * 256 + 128u * x, d_one, d_lse + (n % NL) * (uint64_t)(Sh::X_BYTES >> 4), IDS, 1u);
+        tc_commit(l_empty(n));
+        tc_commit(s_full(n));
         return true;
       }, no_end);
     }
     __syncwarp();
-  } else if (warp == 11) {
-    each([&](const WeighBlock& w, int h, int t, unsigned n, bool, bool) {
-      if (n >= 2 && !__all_sync(0xffffffffu, wait(s_read(n), n / 2 - 1))) return false;
-      const int cols = min(QT, w.ql - t * QT) << g_log;
+  } else if (warp == 19) {
+    pdl_wait();
+    const float by = -LOG2E / a.scale;
+    float ahead[4];  // the next unit's, on their way
+    auto put = [&](unsigned n, const float (&v)[4]) {
+      if (n >= NL && !__all_sync(0xffffffffu, wait(l_empty(n), n / NL - 1))) return false;
 #pragma unroll
-      for (int j = lane; j < 128; j += 32) {
-        float l = 0.f;
-        if (j < cols) l = a.lse[(long long)(w.t0 + t * QT + (j >> g_log)) * c.Hq + (h << g_log) + (j & ((1 << g_log) - 1))] * LOG2E;
-        s_lse[(n & 1) * 128 + j] = l;
+      for (int i = 0; i < 4; ++i) {
+        const float x = v[i] * by, hi = __bfloat162float(__float2bfloat16(x)), r1 = x - hi, mid = __bfloat162float(__float2bfloat16(r1));
+        const bool fin = fabsf(hi) < INFINITY;  // else hi alone
+        const int j = lane + 32 * i;
+        *reinterpret_cast<uint4*>(sm + Sh::OFF_X + (1 + n % NL) * Sh::X_BYTES + j * 32 + (j >> 2 & 1) * 16) =
+            make_uint4(pack_bf16(hi, fin ? mid : 0.f), pack_bf16(fin ? r1 - mid : 0.f, 0.f), 0u, 0u);
       }
+      fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(l_full(n));
       return true;
+    };
+    unsigned got = 0;
+    each([&](const WeighBlock& w, int h, int t, unsigned n, bool, bool) {
+      const int cols = min(QT, w.ql - t * QT) << g_log;
+      float l[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int j = lane + 32 * i;
+        l[i] = j < cols ? a.lse[(long long)(w.t0 + t * QT + (j >> g_log)) * c.Hq + (h << g_log) + (j & ((1 << g_log) - 1))] : 0.f;
+      }
+      if (n > 0 && !put(n - 1, ahead)) return false;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) ahead[i] = l[i];
+      got = n + 1;
+      return true;
     }, no_end);
+    if (got > 0 && pos >= end) put(got - 1, ahead);
   } else {
-    const int x = warp >> 2, row = (warp & 3) * 32 + lane;
+    const int set = warp >> 3, x = warp >> 2 & 1, row = (warp & 3) * 32 + lane;
     const uint32_t t_s = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 128u * (uint32_t)x;
     const float scale = a.scale;
     float sum = 0.f;
+    unsigned ends = 0;
+    // a failed wait does not end the loop: all sixteen warps meet at the blocks' ends
     each([&](const WeighBlock& w, int, int t, unsigned n, bool, bool) {
-      if (!__all_sync(0xffffffffu, wait(s_full(n), n / 2) && wait(l_full(n), n / 2))) return false;
+      if ((n & 1) != set || !__all_sync(0xffffffffu, wait(s_full(n), n / 2))) return true;
       tc_fence_after();
       const int key = w.kb * 256 + x * 128 + row, cols = min(QT, w.ql - t * QT) << g_log;
       // query i of the row sees the key when s0 + i >= key: columns from lo on
       const int lo = min(max(key - w.s0 - t * QT, 0), cols >> g_log) << g_log;
-      const bool cut = cols < 128 || __any_sync(0xffffffffu, lo > 0);
-      const float* l = s_lse + (n & 1) * 128;
       float p4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-      for (int c0 = 0; c0 < cols; c0 += 64) {
-        uint32_t su[64];
+      for (int c0 = 0; c0 < cols; c0 += 32) {
+        if (__all_sync(0xffffffffu, lo >= c0 + 32)) continue;
+        uint32_t su[32];
         tmem_ld_32_issue(t_s + (n & 1) * 256 + (uint32_t)c0, su);
-        tmem_ld_32_issue(t_s + (n & 1) * 256 + (uint32_t)c0 + 32, su + 32);
         tmem_ld_wait();
-        if (!cut) {
+        if (cols >= c0 + 32 && __all_sync(0xffffffffu, lo <= c0)) {
 #pragma unroll
-          for (int j = 0; j < 64; j += 4) {
-            const float4 v = *reinterpret_cast<const float4*>(l + c0 + j);
-            p4[0] += ex2_fast(fmaf(__uint_as_float(su[j]), scale, -v.x));
-            p4[1] += ex2_fast(fmaf(__uint_as_float(su[j + 1]), scale, -v.y));
-            p4[2] += ex2_fast(fmaf(__uint_as_float(su[j + 2]), scale, -v.z));
-            p4[3] += ex2_fast(fmaf(__uint_as_float(su[j + 3]), scale, -v.w));
-          }
+          for (int j = 0; j < 32; ++j) p4[j & 3] += ex2_fast(__uint_as_float(su[j]) * scale);
         } else {
 #pragma unroll
-          for (int j = 0; j < 64; ++j) {
-            const float p = ex2_fast(fmaf(__uint_as_float(su[j]), scale, -l[c0 + j]));
+          for (int j = 0; j < 32; ++j) {
+            const float p = ex2_fast(__uint_as_float(su[j]) * scale);
             p4[j & 3] += (unsigned)(c0 + j - lo) < (unsigned)(cols - lo) ? p : 0.f;
           }
         }
@@ -1639,13 +1678,20 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
       if (lane == 0) mbar_arrive(s_read(n));
       return true;
     }, [&](const WeighBlock& w, long long start, long long stop) {
-      const int key = w.kb * 256 + x * 128 + row;
-      if (start != w.begin || stop != w.begin + (long long)w.vis * c.Hkv) {
-        wt.part[(2 * blockIdx.x + (start == w.begin)) * 256 + x * 128 + row] = sum;
-      } else if (key < w.len) {
-        const int page = chunk_page(c.page_table, c.max_pages, c.n_pages, w.b, key / 64, nullptr);
-        const long long at = (long long)page * 64 + key % 64;
-        if (page >= 0) wt.w_out[at] = (wt.w_in ? wt.w_in[at] : 0.f) + sum;
+      // the other set's sums, through one of two buffers in turn: one is written again only after the barrier in between
+      float* other = reinterpret_cast<float*>(sm + Sh::OFF_SUM) + (ends++ & 1) * 256 + x * 128 + row;
+      if (set == 1) *other = sum;
+      bar_named(1, 512);
+      if (set == 0) {
+        sum += *other;
+        const int key = w.kb * 256 + x * 128 + row;
+        if (start != w.begin || stop != w.begin + (long long)w.vis * c.Hkv) {
+          wt.part[(2 * blockIdx.x + (start == w.begin)) * 256 + x * 128 + row] = sum;
+        } else if (key < w.len) {
+          const int page = chunk_page(c.page_table, c.max_pages, c.n_pages, w.b, key / 64, nullptr);
+          const long long at = (long long)page * 64 + key % 64;
+          if (page >= 0) wt.w_out[at] = (wt.w_in ? wt.w_in[at] : 0.f) + sum;
+        }
       }
       sum = 0.f;
       return true;
@@ -1654,7 +1700,7 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
   if (*abort_flag) drain_copies();
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) tmem_dealloc(tmem, 512);
+  if (warp == 17) tmem_dealloc(tmem, 512);
 }
 
 // Blocks that k_weigh_tc's CTAs share: the first CTA whose share starts inside one adds its parts (grid x < ctas - 1). The
@@ -1730,7 +1776,9 @@ static ChunkPath chunk_path(const ChunkDev& c, int dtype, const tlf_attn_chunk_a
     // the host can only size by the longest row; else S^T again, on the CUDA cores where the tiles do not fit (933 and 1593 us)
     const long long score_bytes = (long long)c.T * c.Hq * c.max_pages * 256;
     const bool fit = score_bytes <= (256LL << 20);
-    p.weigh_tc = a.weight_out && tc && (rows > 16 || !fit);
+    const float scale = a.scale > 0.f ? a.scale : 1.f;
+    const bool lse_fits = scale >= 0x1p-64f && scale <= 0x1p64f;  // k_weigh_tc divides by it
+    p.weigh_tc = a.weight_out && tc && (rows > 16 || !fit) && lse_fits;
     p.scores = a.weight_out && !p.weigh_tc && fit ? score_bytes : 0;
     p.rt = p.pair ? 256 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
     p.ctas = (c.hd == 128 || p.pair ? 1 : 2) * num_sms;
@@ -1831,7 +1879,7 @@ static cudaError_t chunk_launch(const ChunkAttn& a, const tlf_attn_chunk_args& a
     e = a.c.hd == 16 ? simt_rows<16>(a, st) : a.c.hd == 32 ? simt_rows<32>(a, st) : a.c.hd == 64 ? simt_rows<64>(a, st) : simt_rows<128>(a, st);
   if (e) return e;
   const int base = (a.c.n + 1) * 8;
-  const dim3 jg(std::max(1, a.ctas - 1), a.rows >= 64 ? 2 : 1);  // one wave of CTAs
+  const dim3 jg(std::max(1, a.ctas - 1), std::max(1, a.rows / 64));
   e = a.c.hd == 128  ? launch_k(k_chunk_join<T, 4>, jg, dim3(256), base, st, a)
       : a.c.hd == 64 ? launch_k(k_chunk_join<T, 2>, jg, dim3(256), base, st, a)
                      : launch_k(k_chunk_join<T, 1>, jg, dim3(256), base, st, a);
