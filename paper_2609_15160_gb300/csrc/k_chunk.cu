@@ -104,8 +104,13 @@ __global__ void __launch_bounds__(256) k_chunk_join(ChunkAttn a) {
   __shared__ long long s_red[33];
   chunk_plan(a.c, a.sp, s_base, s_red);
   const long long all = s_base[a.c.n], per = chunk_share(a, all), pos = (blockIdx.x + 1) * per;
-  ChunkItem it{};
-  if (pos < all) it = chunk_item(a.c, a.sp, s_base, pos);
+  __shared__ ChunkItem s_it;  // (found by one thread: what all find takes the kernel before its issue slots)
+  if (threadIdx.x == 0) {
+    s_it.first = pos;
+    if (pos < all) s_it = chunk_item(a.c, a.sp, s_base, pos);
+  }
+  __syncthreads();
+  const ChunkItem it = s_it;
   // The plan reads what no kernel of the call writes, so it runs beside the kernel before. Every CTA waits, those with nothing
   // to join too: this grid's end tells the next one that the kernel before has ended.
   pdl_wait();
@@ -1512,13 +1517,14 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
   const long long all = weigh_plan(c, wt.sp, s_base, s_red), per = chunk_share(a, all);
   long long pos = blockIdx.x * per;
   const long long end = pos + per < all ? pos + per : all;
-  WeighBlock w{};
-  if (pos < end) w = weigh_block(c, wt.sp, s_base, pos);
+  __shared__ WeighBlock s_first;
+  if (tid == 0 && pos < end) s_first = weigh_block(c, wt.sp, s_base, pos);
   tc_fence_before();
   __syncthreads();  // barriers initialised, tensor memory allocated
   tc_fence_after();
   pdl_trigger();
   const uint32_t tmem = *tmem_slot;
+  WeighBlock w = s_first;
   const int QT = 1 << wt.sp.qt_log;
   auto wait = [&](uint32_t b, uint32_t parity) {
     if (mbar_try_wait(b, parity & 1u)) return true;
@@ -1722,8 +1728,13 @@ __global__ void __launch_bounds__(256) k_weigh_join(ChunkAttn a, WeighTc wt, int
     return;
   }
   const long long all = weigh_plan(c, wt.sp, s_base, s_red), per = chunk_share(a, all), pos = (blockIdx.x + 1) * per;
-  WeighBlock w{};
-  if (pos < all) w = weigh_block(c, wt.sp, s_base, pos);
+  __shared__ WeighBlock s_w;
+  if (threadIdx.x == 0) {
+    s_w.begin = pos;
+    if (pos < all) s_w = weigh_block(c, wt.sp, s_base, pos);
+  }
+  __syncthreads();
+  const WeighBlock w = s_w;
   pdl_wait();  // (as in k_chunk_join)
   if (pos >= all || w.begin == pos || w.begin / per != blockIdx.x) return;
   const int c0 = blockIdx.x, c1 = (int)((w.begin + (long long)w.vis * c.Hkv - 1) / per), key = w.kb * 256 + threadIdx.x;
@@ -1879,7 +1890,7 @@ static cudaError_t chunk_launch(const ChunkAttn& a, const tlf_attn_chunk_args& a
     e = a.c.hd == 16 ? simt_rows<16>(a, st) : a.c.hd == 32 ? simt_rows<32>(a, st) : a.c.hd == 64 ? simt_rows<64>(a, st) : simt_rows<128>(a, st);
   if (e) return e;
   const int base = (a.c.n + 1) * 8;
-  const dim3 jg(std::max(1, a.ctas - 1), std::max(1, a.rows / 64));
+  const dim3 jg(std::max(1, a.ctas - 1), std::max(1, a.rows / 32));
   e = a.c.hd == 128  ? launch_k(k_chunk_join<T, 4>, jg, dim3(256), base, st, a)
       : a.c.hd == 64 ? launch_k(k_chunk_join<T, 2>, jg, dim3(256), base, st, a)
                      : launch_k(k_chunk_join<T, 1>, jg, dim3(256), base, st, a);
