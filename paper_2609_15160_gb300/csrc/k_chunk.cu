@@ -1663,14 +1663,18 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
       float p4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
       for (int c0 = 0; c0 < cols; c0 += 32) {
-        if (__all_sync(0xffffffffu, lo >= c0 + 32)) continue;
         uint32_t su[32];
         tmem_ld_32_issue(t_s + (n & 1) * 256 + (uint32_t)c0, su);
         tmem_ld_wait();
+        if (c0 + 32 >= cols) {  // S is in registers: the buffer is free
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(s_read(n));
+        }
         if (cols >= c0 + 32 && __all_sync(0xffffffffu, lo <= c0)) {
 #pragma unroll
           for (int j = 0; j < 32; ++j) p4[j & 3] += ex2_fast(__uint_as_float(su[j]) * scale);
-        } else {
+        } else if (!__all_sync(0xffffffffu, lo >= c0 + 32)) {
 #pragma unroll
           for (int j = 0; j < 32; ++j) {
             const float p = ex2_fast(__uint_as_float(su[j]) * scale);
@@ -1679,9 +1683,6 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
         }
       }
       sum += (p4[0] + p4[1]) + (p4[2] + p4[3]);
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(s_read(n));
       return true;
     }, [&](const WeighBlock& w, long long start, long long stop) {
       // the other set's sums, through one of two buffers in turn: one is written again only after the barrier in between
