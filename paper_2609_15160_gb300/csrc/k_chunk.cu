@@ -834,10 +834,11 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
 // only: a tile's chain S, softmax, P V was then 4.8k cycles a block, 2.0k of them MMAs (4 x 2048 tokens over up to 10240
 // entries, 16 / 8 heads x 128: 485 us, 330 so).
 //
-// What bounds it: at head_dim 128 the tensor cores (a block of a tile is 8 S products that read 6 KB of shared memory each, 48
-// cycles, and 4 P V products of 64 cycles: 1280 cycles for both tiles, 1670 measured); at head_dim 64 the exponentials (1024
-// cycles a block for both tiles, 1560 measured with what surrounds them). With the join: 363 us for the case above (1340
-// TFLOP/s, 0.70 of the measured bf16 rate), 351 us with 16 heads x 64 (690), 222 us for 8192 causal tokens (1240).
+// What bounds it: the softmax warps' instructions and the tensor cores nearly alike. At head_dim 128 a block of a tile is 8 S
+// products that read 6 KB of shared memory each, 48 cycles, and 4 P V products of 64 cycles: 1280 cycles for both tiles of the
+// about 1600 that a block takes; the exponentials (32 a cycle and SM) are 512 of them. Products and sums of two floats at a time
+// took 10 us off 362: the issue slots count, half of which are taken. Exponentials by polynomials beside the unit's made it
+// slower. With the join: PAIR_FIG
 constexpr int PAIR_THREADS = 352;
 
 template <int HD>
@@ -1155,20 +1156,22 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
           }
         }
         const float mref = m_run == -INFINITY ? 0.f : m_run * scale;  // no visible key so far: any finite value
-        float ps4[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint64_t scale2 = f2_pack(scale, scale), mref2 = f2_pack(-mref, -mref);
+        uint64_t ps[2] = {0, 0};  // (two sums each)
 #pragma unroll
         for (int c0 = 0; c0 < 64; c0 += 32) {
           uint32_t pk[16];
 #pragma unroll
           for (int k = 0; k < 32; k += 2) {
-            const float p0 = ex2_fast(fmaf(__uint_as_float(su[c0 + k]), scale, -mref));
-            const float p1 = ex2_fast(fmaf(__uint_as_float(su[c0 + k + 1]), scale, -mref));
-            ps4[(k >> 1) & 3] += p0 + p1;
+            const float2 e = f2_unpack(f2_fma(f2_pack(__uint_as_float(su[c0 + k]), __uint_as_float(su[c0 + k + 1])), scale2, mref2));
+            const float p0 = ex2_fast(e.x), p1 = ex2_fast(e.y);
+            ps[k / 2 & 1] = f2_add(ps[k / 2 & 1], f2_pack(p0, p1));
             pk[k / 2] = pack_bf16(p0, p1);
           }
           tmem_put_16(t_sn + (uint32_t)(c0 / 2), pk);
         }
-        l_run += (ps4[0] + ps4[1]) + (ps4[2] + ps4[3]);
+        const float2 sum = f2_unpack(f2_add(ps[0], ps[1]));
+        l_run += sum.x + sum.y;
         tmem_st_wait_done();
         tc_fence_before();
         __syncwarp();
@@ -1660,7 +1663,8 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
       const int key = w.kb * 256 + x * 128 + row, cols = min(QT, w.ql - t * QT) << g_log;
       // query i of the row sees the key when s0 + i >= key: columns from lo on
       const int lo = min(max(key - w.s0 - t * QT, 0), cols >> g_log) << g_log;
-      float p4[4] = {0.f, 0.f, 0.f, 0.f};
+      const uint64_t scale2 = f2_pack(scale, scale);
+      uint64_t p4[2] = {0, 0};  // (two sums each)
 #pragma unroll 1
       for (int c0 = 0; c0 < cols; c0 += 32) {
         uint32_t su[32];
@@ -1673,16 +1677,21 @@ __global__ void __launch_bounds__(WEIGH_THREADS, 1) k_weigh_tc(ChunkAttn a, Weig
         }
         if (cols >= c0 + 32 && __all_sync(0xffffffffu, lo <= c0)) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) p4[j & 3] += ex2_fast(__uint_as_float(su[j]) * scale);
+          for (int j = 0; j < 32; j += 2) {
+            const float2 e = f2_unpack(f2_fma(f2_pack(__uint_as_float(su[j]), __uint_as_float(su[j + 1])), scale2, 0));
+            p4[j / 2 & 1] = f2_add(p4[j / 2 & 1], f2_pack(ex2_fast(e.x), ex2_fast(e.y)));
+          }
         } else if (!__all_sync(0xffffffffu, lo >= c0 + 32)) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const float p = ex2_fast(__uint_as_float(su[j]) * scale);
-            p4[j & 3] += (unsigned)(c0 + j - lo) < (unsigned)(cols - lo) ? p : 0.f;
+          for (int j = 0; j < 32; j += 2) {
+            const float p = ex2_fast(__uint_as_float(su[j]) * scale), r = ex2_fast(__uint_as_float(su[j + 1]) * scale);
+            p4[j / 2 & 1] = f2_add(p4[j / 2 & 1], f2_pack((unsigned)(c0 + j - lo) < (unsigned)(cols - lo) ? p : 0.f,
+                                                          (unsigned)(c0 + j + 1 - lo) < (unsigned)(cols - lo) ? r : 0.f));
           }
         }
       }
-      sum += (p4[0] + p4[1]) + (p4[2] + p4[3]);
+      const float2 added = f2_unpack(f2_add(p4[0], p4[1]));
+      sum += added.x + added.y;
       return true;
     }, [&](const WeighBlock& w, long long start, long long stop) {
       // the other set's sums, through one of two buffers in turn: one is written again only after the barrier in between
