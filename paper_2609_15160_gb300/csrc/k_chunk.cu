@@ -35,6 +35,7 @@ struct ChunkAttn {
   uint32_t* werr;  // error word of the waits: the caller's, or one in the scratch
   float* part_o;   // [2 ctas][rows][hd]
   float2* part_ml; // [2 ctas][rows]
+  int4* join;      // [ctas] what each CTA leaves to k_chunk_join
 };
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -94,29 +95,28 @@ __device__ __forceinline__ ChunkItem chunk_item(const ChunkDev& c, const ChunkSp
 // ----------------------------------------------------------------------------
 // Joining the parts of shared items
 // ----------------------------------------------------------------------------
-// blockIdx.x + 1 = a CTA whose share starts inside an item; the first such CTA of an item joins it. CTA c's first item has
-// its part at 2c if it began in an earlier share, the part of an item that goes on past its share is at 2c + 1. A warp takes
-// a row at a time, VW dims a lane (hd = 32 VW, or 16 with VW = 1), and every eight-th row of a CTA's.
+// The first CTA whose share starts inside an item notes it: {the tile's first token, kv head, rows, parts}, parts = 0 where there
+// is none. CTA c's first item has its part at 2c if it began in an earlier share, the part of an item that goes on past its
+// share is at 2c + 1. One thread of every CTA calls this, before any wait; it: what the CTA's share starts with, or NULL.
+__device__ __forceinline__ void join_note(const ChunkAttn& a, const ChunkItem* it, long long per) {
+  int4 j = make_int4(0, 0, 0, 0);
+  const long long pos = blockIdx.x * per;
+  if (it && it->first < pos && it->first >= pos - per) {
+    const int qt = 1 << a.sp.qt_log, last = (int)((it->first + it->nb - 1) / per);  // the last CTA with a part
+    j = make_int4(it->t0 + it->t * qt, it->h, min(qt, it->ql - it->t * qt) * a.c.G, last - (int)blockIdx.x + 2);
+  }
+  a.join[blockIdx.x] = j;
+}
+// A warp takes a row at a time, VW dims a lane (hd = 32 VW, or 16 with VW = 1), and every eight-th row of a CTA's. It reads the
+// notes rather than plan again: the plan took 3 us, beside k_chunk_pair too, whose registers leave no room for a CTA of this.
 template <typename T, int VW>
 __global__ void __launch_bounds__(256) k_chunk_join(ChunkAttn a) {
   pdl_trigger();
-  extern __shared__ long long s_base[];
-  __shared__ long long s_red[33];
-  chunk_plan(a.c, a.sp, s_base, s_red);
-  const long long all = s_base[a.c.n], per = chunk_share(a, all), pos = (blockIdx.x + 1) * per;
-  __shared__ ChunkItem s_it;  // (found by one thread: what all find takes the kernel before its issue slots)
-  if (threadIdx.x == 0) {
-    s_it.first = pos;
-    if (pos < all) s_it = chunk_item(a.c, a.sp, s_base, pos);
-  }
-  __syncthreads();
-  const ChunkItem it = s_it;
-  // The plan reads what no kernel of the call writes, so it runs beside the kernel before. Every CTA waits, those with nothing
-  // to join too: this grid's end tells the next one that the kernel before has ended.
   pdl_wait();
-  if (pos >= all || it.first >= pos || it.first / per != blockIdx.x) return;
-  const int c0 = blockIdx.x, parts = (int)((it.first + it.nb - 1) / per) - c0 + 1;
-  const int qt = 1 << a.sp.qt_log, G = a.c.G, rows = min(qt, it.ql - it.t * qt) * G, lane = threadIdx.x & 31, hd = a.c.hd;
+  const int4 note = a.join[blockIdx.x + 1];
+  const int parts = note.w;
+  if (parts == 0) return;
+  const int c0 = blockIdx.x, G = a.c.G, rows = note.z, lane = threadIdx.x & 31, hd = a.c.hd;
   const bool mine = lane * VW < hd;
   auto slot = [&](int i, int row) { return (size_t)(i == 0 ? 2 * c0 + 1 : 2 * (c0 + i)) * a.rows + row; };
   auto get = [&](int i, int row, float (&v)[VW]) {
@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(256) k_chunk_join(ChunkAttn a) {
     else v[0] = *p;
   };
   auto put = [&](int row, float m, float l, const float (&o)[VW]) {
-    const int token = it.t0 + it.t * qt + row / G, head = it.h * G + row % G;
+    const int token = note.x + row / G, head = note.y * G + row % G;
     T* out = static_cast<T*>(a.out) + token * a.os + (long long)head * hd + lane * VW;
     const float inv = l != 0.f ? 1.f / l : 0.f;
     if (mine)
@@ -228,8 +228,10 @@ __global__ void __launch_bounds__(256) k_chunk_simt(ChunkAttn a) {
   long long pos = blockIdx.x * per;
   const long long end = pos + per < all ? pos + per : all;
   const int tid = threadIdx.x, x = tid & 15, y = tid >> 4, G = c.G, qt = 1 << a.sp.qt_log;
-  while (pos < end) {
+  if (pos >= end && tid == 0) join_note(a, nullptr, per);
+  for (bool first = true; pos < end; first = false) {
     const ChunkItem it = chunk_item(c, a.sp, s_base, pos);
+    if (first && tid == 0) join_note(a, &it, per);
     if (pos < it.first) pos = it.first;
     if (pos >= end) break;
     const int kb0 = (int)(pos - it.first), kb1 = (int)(end - it.first < it.nb ? end - it.first : it.nb);
@@ -518,8 +520,10 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
   unsigned seq = 0;  // pages that this CTA's ring has taken
 
   if (warp == 8) {
+    if (pos >= end && lane == 0) join_note(a, nullptr, per);
     for (unsigned segs = 0; pos < end; ++segs) {
       const ChunkItem it = chunk_item(c, a.sp, s_base, pos);
+      if (segs == 0 && lane == 0) join_note(a, &it, per);
       if (pos < it.first) pos = it.first;
       if (pos >= end) {
         if (segs == 0 && lane == 0) {
@@ -838,7 +842,8 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
 // products that read 6 KB of shared memory each, 48 cycles, and 4 P V products of 64 cycles: 1280 cycles for both tiles of the
 // about 1600 that a block takes; the exponentials (32 a cycle and SM) are 512 of them. Products and sums of two floats at a time
 // took 10 us off 362: the issue slots count, half of which are taken. Exponentials by polynomials beside the unit's made it
-// slower. With the join: PAIR_FIG
+// slower. With the join: 355 us for the case above (1370
+// TFLOP/s, 0.71 of the measured bf16 rate), 333 us with 16 heads x 64 (730), 212 us for 8192 causal tokens (1300).
 constexpr int PAIR_THREADS = 352;
 
 template <int HD>
@@ -1095,7 +1100,10 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
     bool ok = true;
     // waits taken by the whole warp: the TMEM accesses after them are warp-collective
     auto wait_w = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, wait(b, parity)); };
+    bool noted = false;
     while (ok && segment(s)) {
+      if (!noted && tid == 0) join_note(a, &s.it, per);
+      noted = true;
       const bool row_ok = qi < s.nq[x];
       const int see = row_ok ? s.see0 + x * QT + qi : -1;  // a row past the tile's queries sees nothing
       const int see0 = s.see0 + x * QT;                    // of the tile's first query
@@ -1243,6 +1251,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       }
       blk += s.kb1 - s.kb0;
     }
+    if (!noted && tid == 0) join_note(a, nullptr, per);
   }
   if (*abort_flag) drain_copies();
   tc_fence_before();
@@ -1773,7 +1782,7 @@ struct ChunkPath {
   int pad;      // blocks that an item counts beside its own
   bool weigh_tc;  // the weights from k_weigh_tc
   long long scores;  // bytes of the scores that k_chunk_mma leaves for the weights
-  size_t part_ml, lse, werr, weigh, scores_at, total;  // scratch offsets (part_o at 0)
+  size_t part_ml, join, lse, werr, weigh, scores_at, total;  // scratch offsets (part_o at 0)
 };
 static int pow2_log(int x) {  // largest l with 2^l <= x
   int l = 0;
@@ -1812,6 +1821,7 @@ static ChunkPath chunk_path(const ChunkDev& c, int dtype, const tlf_attn_chunk_a
   auto take = [&](size_t bytes) { const size_t at = o; o = (o + bytes + 255) / 256 * 256; return at; };
   take((size_t)2 * p.ctas * p.rt * c.hd * 4);
   p.part_ml = take((size_t)2 * p.ctas * p.rt * 8);
+  p.join = take((size_t)p.ctas * 16);
   p.lse = take(a.weight_out && !a.lse ? (size_t)c.T * c.Hq * 4 : 0);
   p.werr = take(4);
   p.weigh = take(p.weigh_tc ? (size_t)2 * num_sms * 256 * 4 : 0);
@@ -1900,10 +1910,11 @@ static cudaError_t chunk_launch(const ChunkAttn& a, const tlf_attn_chunk_args& a
     e = a.c.hd == 16 ? simt_rows<16>(a, st) : a.c.hd == 32 ? simt_rows<32>(a, st) : a.c.hd == 64 ? simt_rows<64>(a, st) : simt_rows<128>(a, st);
   if (e) return e;
   const int base = (a.c.n + 1) * 8;
-  const dim3 jg(std::max(1, a.ctas - 1), std::max(1, a.rows / 32));
-  e = a.c.hd == 128  ? launch_k(k_chunk_join<T, 4>, jg, dim3(256), base, st, a)
-      : a.c.hd == 64 ? launch_k(k_chunk_join<T, 2>, jg, dim3(256), base, st, a)
-                     : launch_k(k_chunk_join<T, 1>, jg, dim3(256), base, st, a);
+  const dim3 jg(a.ctas - 1, std::max(1, a.rows / 32));
+  if (a.ctas > 1)
+    e = a.c.hd == 128  ? launch_k(k_chunk_join<T, 4>, jg, dim3(256), 0, st, a)
+        : a.c.hd == 64 ? launch_k(k_chunk_join<T, 2>, jg, dim3(256), 0, st, a)
+                       : launch_k(k_chunk_join<T, 1>, jg, dim3(256), 0, st, a);
   if (e) return e;
   if (!args.weight_out) return cudaSuccess;
   const dim3 grid(4 * num_sms);
@@ -1944,6 +1955,7 @@ cudaError_t launch_chunk_attn(const ChunkDev& c, int dtype, const tlf_attn_chunk
   a.werr = c.err ? c.err : reinterpret_cast<uint32_t*>(s + p.werr);
   a.part_o = reinterpret_cast<float*>(s);
   a.part_ml = reinterpret_cast<float2*>(s + p.part_ml);
+  a.join = reinterpret_cast<int4*>(s + p.join);
   float* weigh = p.weigh_tc ? reinterpret_cast<float*>(s + p.weigh) : nullptr;
   return dtype == TLF_DTYPE_BF16 ? chunk_launch<bf16>(a, args, weigh, num_sms, st) : chunk_launch<float>(a, args, weigh, num_sms, st);
 }
