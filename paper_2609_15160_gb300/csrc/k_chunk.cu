@@ -33,7 +33,7 @@ struct ChunkAttn {
   int ctas, rows;  // CTAs that share the blocks; rows of a part
   float* scores;   // k_chunk_mma: [T][Hq][max_pages * 64] scores that it leaves for the weights, or NULL
   uint32_t* werr;  // error word of the waits: the caller's, or one in the scratch
-  float* part_o;   // [2 ctas][rows][hd]
+  float* part_o;   // [2 ctas][rows][hd]; of k_chunk_pair [2 ctas][hd / 4][rows][4]
   float2* part_ml; // [2 ctas][rows]
   int4* join;      // [ctas] what each CTA leaves to k_chunk_join
 };
@@ -108,7 +108,7 @@ __device__ __forceinline__ void join_note(const ChunkAttn& a, const ChunkItem* i
   a.join[blockIdx.x] = j;
 }
 // A warp takes a row at a time, VW dims a lane (hd = 32 VW, or 16 with VW = 1), and every eight-th row of a CTA's. It reads the
-// notes rather than plan again: the plan took 3 us, beside k_chunk_pair too, whose registers leave no room for a CTA of this.
+// notes rather than plan again, which took 3 us.
 template <typename T, int VW>
 __global__ void __launch_bounds__(256) k_chunk_join(ChunkAttn a) {
   pdl_trigger();
@@ -195,6 +195,72 @@ __global__ void __launch_bounds__(256) k_chunk_join(ChunkAttn a) {
     }
     put(row, m, warp_sum(l), o);
   }
+}
+
+// The parts of k_chunk_pair, whose threads have a row each: they leave four dims of all rows side by side, so that a warp writes
+// whole lines (row by row, 16 bytes a lane in 32 lines, a part of 256 rows took 4 us). A warp here has 8 rows and half the
+// dims; a lane one row and every fourth 16 bytes of it.
+constexpr int PAIR_ROWS = 256;
+__device__ __forceinline__ size_t pair_part(int slot, int row, int d, int hd) {  // of 16 bytes from dim d on
+  return (size_t)slot * PAIR_ROWS * hd + ((size_t)(d >> 2) * PAIR_ROWS + row) * 4 + (d & 3);
+}
+template <int HD>
+__global__ void __launch_bounds__(256) k_pair_join(ChunkAttn a) {  // grid y = 8
+  pdl_trigger();
+  pdl_wait();
+  const int4 note = a.join[blockIdx.x + 1];
+  const int parts = note.w, c0 = blockIdx.x, G = a.c.G, lane = threadIdx.x & 31, quarter = lane >> 3;
+  const int unit = blockIdx.y * 8 + (threadIdx.x >> 5), row = (unit & 31) * 8 + (lane & 7), d0 = (unit >> 5) * (HD / 2) + quarter * 4;
+  if (parts == 0 || (unit & 31) * 8 >= note.z) return;
+  constexpr int V = HD / 32;  // 16-byte pieces of a lane
+  auto slot = [&](int i) { return i == 0 ? 2 * c0 + 1 : 2 * (c0 + i); };
+  auto stat = [&](int i) { return a.part_ml[(size_t)slot(i) * PAIR_ROWS + row]; };
+  auto get = [&](int i, float4 (&v)[V]) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] = *reinterpret_cast<const float4*>(a.part_o + pair_part(slot(i), row, d0 + 16 * k, HD));
+  };
+  float4 o[V], v[V];
+  const float2 x = stat(0), y = stat(1);
+  get(0, o);
+  get(1, v);
+  float m = fmaxf(x.x, y.x);
+  for (int i = 2 + quarter; i < parts; i += 4) m = fmaxf(m, stat(i).x);
+  m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+  m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+  const float ref = m == -INFINITY ? 0.f : m, wx = exp2f(x.x - ref), wy = exp2f(y.x - ref);
+  auto scaled = [](float w, float4 u) { return w != 0.f ? make_float4(w * u.x, w * u.y, w * u.z, w * u.w) : make_float4(0.f, 0.f, 0.f, 0.f); };
+  auto add = [](float4& s, float4 u) { s.x += u.x, s.y += u.y, s.z += u.z, s.w += u.w; };
+  float l = wx * x.y + wy * y.y;
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    o[k] = scaled(wx, o[k]);
+    add(o[k], scaled(wy, v[k]));
+  }
+#pragma unroll 4
+  for (int i = 2; i < parts; ++i) {
+    const float2 ml = stat(i);
+    get(i, v);
+    const float w = exp2f(ml.x - ref);
+    l += w * ml.y;
+#pragma unroll
+    for (int k = 0; k < V; ++k) add(o[k], scaled(w, v[k]));
+  }
+  if (row >= note.z) return;
+  const int token = note.x + row / G, head = note.y * G + row % G;
+  const float inv = l != 0.f ? 1.f / l : 0.f;
+  bf16* out = static_cast<bf16*>(a.out) + token * a.os + (long long)head * HD + d0;
+  const bool wide = reinterpret_cast<uintptr_t>(a.out) % 8 == 0 && a.os % 4 == 0;
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    if (wide) {
+      *reinterpret_cast<uint2*>(out + 16 * k) = make_uint2(pack_bf16(o[k].x * inv, o[k].y * inv), pack_bf16(o[k].z * inv, o[k].w * inv));
+    } else {
+      const float e[4] = {o[k].x, o[k].y, o[k].z, o[k].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) out[16 * k + j] = from_f32<bf16>(e[j] * inv);
+    }
+  }
+  if (d0 == 0 && a.lse) a.lse[(long long)token * a.c.Hq + head] = l != 0.f ? (m + log2f(l)) * LN2 : -INFINITY;
 }
 
 // ----------------------------------------------------------------------------
@@ -1189,7 +1255,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       const bool whole = s.kb0 == 0 && s.kb1 == s.it.nb;
       const long long token = s.token0 + x * QT + qi;
       const int head = (s.it.h << g_log) + g;
-      const size_t part = ((size_t)(2 * blockIdx.x + (s.kb0 == 0)) * a.rows + x * 128 + row);
+      const int slot = 2 * blockIdx.x + (s.kb0 == 0), prow = x * 128 + row;  // of the part
       bf16* orow = static_cast<bf16*>(a.out) + token * a.os + (long long)head * HD;
       const bool wide = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && a.os % 8 == 0;
       bool bad = false;
@@ -1207,7 +1273,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
           if (!whole) {
 #pragma unroll
             for (int k = 0; k < 32; k += 4)
-              *reinterpret_cast<float4*>(a.part_o + part * HD + c0 + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+              *reinterpret_cast<float4*>(a.part_o + pair_part(slot, prow, c0 + k, HD)) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
           } else if (wide) {
 #pragma unroll
             for (int k = 0; k < 32; k += 8)
@@ -1221,10 +1287,10 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         }
         tc_fence_before();
       } else if (row_ok && !whole) {  // the tile has no block here: an empty part
-        for (int k = 0; k < HD; ++k) a.part_o[part * HD + k] = 0.f;
+        for (int k = 0; k < HD; ++k) a.part_o[pair_part(slot, prow, k, HD)] = 0.f;
       }
       if (row_ok) {
-        if (!whole) a.part_ml[part] = make_float2(m_run == -INFINITY ? -INFINITY : m_run * scale, l_run);
+        if (!whole) a.part_ml[(size_t)slot * PAIR_ROWS + prow] = make_float2(m_run == -INFINITY ? -INFINITY : m_run * scale, l_run);
         else if (a.lse) a.lse[token * c.Hq + head] = l_run != 0.f ? (m_run * scale + log2f(l_run)) * LN2 : -INFINITY;
       }
       // rows that a 0 x infinity of a key which only others see has spoilt: again, over what they see
@@ -1234,17 +1300,17 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         again &= again - 1;
         const long long tk = __shfl_sync(0xffffffffu, token, src);
         const int hh = __shfl_sync(0xffffffffu, head, src), see_r = __shfl_sync(0xffffffffu, see, src);
-        const size_t pt = __shfl_sync(0xffffffffu, (unsigned long long)part, src);
+        const int pr = __shfl_sync(0xffffffffu, prow, src);
         float mm, ll, oo[HD / 32];
         chunk_redo<HD>(a, s.it.b, s.it.h, tk, hh, s.kb0 * 64, min(s.kb1 * 64, see_r + 1), mm, ll, oo);
         const float inv = ll != 0.f ? 1.f / ll : 0.f;
 #pragma unroll
         for (int k = 0; k < HD / 32; ++k) {
           if (whole) static_cast<bf16*>(a.out)[tk * a.os + (long long)hh * HD + lane + 32 * k] = from_f32<bf16>(oo[k] * inv);
-          else a.part_o[pt * HD + lane + 32 * k] = oo[k];
+          else a.part_o[pair_part(slot, pr, lane + 32 * k, HD)] = oo[k];
         }
         if (lane == 0) {
-          if (!whole) a.part_ml[pt] = make_float2(mm, ll);
+          if (!whole) a.part_ml[(size_t)slot * PAIR_ROWS + pr] = make_float2(mm, ll);
           else if (a.lse) a.lse[tk * c.Hq + hh] = ll != 0.f ? (mm + log2f(ll)) * LN2 : -INFINITY;
         }
         __syncwarp();
@@ -1810,7 +1876,7 @@ static ChunkPath chunk_path(const ChunkDev& c, int dtype, const tlf_attn_chunk_a
     const bool lse_fits = scale >= 0x1p-64f && scale <= 0x1p64f;  // k_weigh_tc divides by it
     p.weigh_tc = a.weight_out && tc && (rows > 16 || !fit) && lse_fits;
     p.scores = a.weight_out && !p.weigh_tc && fit ? score_bytes : 0;
-    p.rt = p.pair ? 256 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+    p.rt = p.pair ? PAIR_ROWS : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
     p.ctas = (c.hd == 128 || p.pair ? 1 : 2) * num_sms;
     p.pad = p.pair ? PAD_PAIR : c.hd == 128 ? PAD_MMA128 : PAD_MMA;
   }
@@ -1912,9 +1978,10 @@ static cudaError_t chunk_launch(const ChunkAttn& a, const tlf_attn_chunk_args& a
   const int base = (a.c.n + 1) * 8;
   const dim3 jg(a.ctas - 1, std::max(1, a.rows / 32));
   if (a.ctas > 1)
-    e = a.c.hd == 128  ? launch_k(k_chunk_join<T, 4>, jg, dim3(256), 0, st, a)
+    e = a.rows == PAIR_ROWS ? (a.c.hd == 128 ? launch_k(k_pair_join<128>, jg, dim3(256), 0, st, a) : launch_k(k_pair_join<64>, jg, dim3(256), 0, st, a))
+        : a.c.hd == 128 ? launch_k(k_chunk_join<T, 4>, jg, dim3(256), 0, st, a)
         : a.c.hd == 64 ? launch_k(k_chunk_join<T, 2>, jg, dim3(256), 0, st, a)
-                       : launch_k(k_chunk_join<T, 1>, jg, dim3(256), 0, st, a);
+                        : launch_k(k_chunk_join<T, 1>, jg, dim3(256), 0, st, a);
   if (e) return e;
   if (!args.weight_out) return cudaSuccess;
   const dim3 grid(4 * num_sms);
