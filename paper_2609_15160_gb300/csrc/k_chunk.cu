@@ -6,8 +6,8 @@
 // O = sum 2^(s - m) v, all in float32. An item inside one CTA's share is written out; the parts of a shared one go to the
 // scratch, and k_chunk_join adds them: M = max m_c, O = sum 2^(m_c - M) O_c / sum 2^(m_c - M) l_c.
 //
-// k_chunk_pair   bfloat16, more rows: tcgen05 on pairs of 128-row tiles.
-// k_chunk_mma    bfloat16, up to 64 query rows a tile: tensor cores through mma.sync.
+// k_chunk_pair   bfloat16, more than 16 or 32 query rows an item: tcgen05 on pairs of 128-row tiles.
+// k_chunk_mma    bfloat16, fewer rows, and what the tiles of the other do not fit: tensor cores through mma.sync.
 // k_chunk_simt   float32: tiles in shared memory, products on the CUDA cores.
 // With weights, exp(s - lse) of every entry added up over the queries that see it:
 // k_weigh_tc            more than 16 rows: S^T again on tcgen05, a thread a key;
@@ -912,15 +912,21 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
 // TFLOP/s, 0.71 of the measured bf16 rate), 333 us with 16 heads x 64 (730), 212 us for 8192 causal tokens (1300).
 constexpr int PAIR_THREADS = 352;
 
+struct PairSeg {  // a CTA's part of an item: blocks kb0 .. kb1 - 1 of nb, of which tile x has the first e[x]; nb = 0: no more
+  int b, h, token0, see0, nq[2], e[2], kb0, kb1, nb, none;
+  static constexpr int RING = 4;
+};
+
 template <int HD>
 struct PairShape {
   static constexpr int ATOMS = HD / 64, QCOL = 128 * 128, Q_BYTES = ATOMS * QCOL;  // a tile of 128 rows of q
   static constexpr int COL = 64 * 128, T_BYTES = ATOMS * COL;                      // 64 rows of K or V
   static constexpr int NST = HD == 128 ? 4 : 8;  // of the K ring and of the V ring
   static constexpr int OFF_K = 2 * Q_BYTES, OFF_V = OFF_K + NST * T_BYTES, OFF_BAR = OFF_V + NST * T_BYTES;
-  static constexpr int NBAR = 4 * NST + 2 + 4 + 4 + 4 + 2;
+  static constexpr int NBAR = 4 * NST + 2 + 4 + 4 + 4 + 2 + 2 * PairSeg::RING;
   static constexpr int FLAGS = 16;  // more than the blocks that the producer can be ahead of the softmax
-  static constexpr int OFF_INT = OFF_BAR + NBAR * 8, OFF_BASE = OFF_INT + (FLAGS + 4) * 4;
+  static constexpr int OFF_INT = OFF_BAR + NBAR * 8, OFF_SEG = OFF_INT + (FLAGS + 4) * 4;
+  static constexpr int OFF_BASE = OFF_SEG + PairSeg::RING * (int)sizeof(PairSeg);
   static int bytes(int n) { return std::max(OFF_BASE + (n + 1) * 8 + 1024, tmem_min_smem(512)); }
   static constexpr uint32_t OCOL = 256;
 };
@@ -965,6 +971,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
   volatile int* s_flag = reinterpret_cast<volatile int*>(sm + Sh::OFF_INT);  // the block's page is not there
   volatile int* abort_flag = s_flag + Sh::FLAGS;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + Sh::OFF_INT) + Sh::FLAGS + 1;
+  PairSeg* s_seg = reinterpret_cast<PairSeg*>(sm + Sh::OFF_SEG);
   long long* s_base = reinterpret_cast<long long*>(sm + Sh::OFF_BASE);
   auto bar = [&](int i) { return smem_u32(&bars[i]); };
   // block b of this CTA: its place in the rings, and the use's parity
@@ -979,6 +986,8 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
   auto p_full = [&](int x, unsigned n) { return bar(4 * NST + 6 + 2 * x + (n & 1)); };
   auto o_done = [&](int x, unsigned n) { return bar(4 * NST + 10 + 2 * x + (n & 1)); };
   const uint32_t q_free = bar(4 * NST + 14), v_tail = bar(4 * NST + 15);
+  auto seg_full = [&](unsigned i) { return bar(4 * NST + 16 + i % PairSeg::RING); };
+  auto seg_empty = [&](unsigned i) { return bar(4 * NST + 16 + PairSeg::RING + i % PairSeg::RING); };
   const ChunkDev& c = a.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
@@ -998,6 +1007,10 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
     }
     mbar_init(q_free, 2);
     mbar_init(v_tail, 4);
+    for (unsigned i = 0; i < PairSeg::RING; ++i) {
+      mbar_init(seg_full(i), 1);
+      mbar_init(seg_empty(i), 10);  // the other warps
+    }
     *abort_flag = 0;
     fence_barrier_init();
     prefetch_tensormap(&q_map);
@@ -1026,54 +1039,59 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
     *abort_flag = 1;
     return false;
   };
-  // this CTA's part of the item at `pos`: blocks kb0 .. kb1 - 1, of which tile x has the first e[x]
-  struct Seg {
-    ChunkItem it;
-    int kb0, kb1, nq[2], e[2], token0, see0;
-  };
-  auto segment = [&](Seg& s) {  // false: none left
-    if (pos >= end) return false;
-    s.it = chunk_item(c, a.sp, s_base, pos);
-    if (pos < s.it.first) pos = s.it.first;
-    if (pos >= end) return false;
-    s.kb0 = (int)(pos - s.it.first);
-    s.kb1 = (int)(end - s.it.first < s.it.nb ? end - s.it.first : s.it.nb);
-    const int q0 = s.it.t << qt_log, left = s.it.ql - q0;
-    s.token0 = s.it.t0 + q0;
-    s.see0 = s.it.s0 + q0;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      s.nq[x] = max(0, min(QT, left - x * QT));
-      const int last = s.see0 + x * QT + s.nq[x] - 1;  // entry of the tile's last query
-      const int nb = s.nq[x] > 0 ? (last < 0 ? 1 : last / 64 + 1) : 0;
-      s.e[x] = max(0, min(s.kb1, nb) - s.kb0);
-    }
-    pos = s.it.first + s.kb1;
-    return true;
-  };
-  Seg s;
+  PairSeg s;
+  unsigned segs = 0;  // read or published
 
   if (warp == 8) {
     // ---------------- producer ----------------
-    unsigned blk = 0, segs = 0;
-    while (segment(s)) {
-      const int E = s.kb1 - s.kb0;
-      bool ok = true;
+    // finds the items (1.5 us each, ahead of the others) and publishes them
+    unsigned blk = 0;
+    for (bool ok = true;;) {
+      s.nb = 0;
+      ChunkItem it{};
+      if (pos < end) {
+        it = chunk_item(c, a.sp, s_base, pos);
+        if (segs == 0 && lane == 0) join_note(a, &it, per);
+        if (pos < it.first) pos = it.first;
+      } else if (segs == 0 && lane == 0) {
+        join_note(a, nullptr, per);
+      }
+      if (pos < end) {
+        const int q0 = it.t << qt_log, left = it.ql - q0;
+        s = PairSeg{it.b, it.h, it.t0 + q0, it.s0 + q0, {}, {}, (int)(pos - it.first), (int)(end - it.first < it.nb ? end - it.first : it.nb), it.nb, 0};
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          s.nq[x] = max(0, min(QT, left - x * QT));
+          const int last = s.see0 + x * QT + s.nq[x] - 1;  // entry of the tile's last query
+          const int nb = s.nq[x] > 0 ? (last < 0 ? 1 : last / 64 + 1) : 0;
+          s.e[x] = max(0, min(s.kb1, nb) - s.kb0);
+        }
+        pos = it.first + s.kb1;
+      }
       if (lane == 0) {
-        ok = segs == 0 || wait(q_free, segs - 1);
+        ok = ok && (segs < PairSeg::RING || wait(seg_empty(segs), segs / PairSeg::RING - 1));
+        if (ok) {
+          s_seg[segs % PairSeg::RING] = s;
+          mbar_arrive(seg_full(segs));
+        }
+      }
+      if (s.nb == 0) break;
+      const int E = s.kb1 - s.kb0;
+      if (lane == 0) {
+        ok = ok && (segs == 0 || wait(q_free, segs - 1));
         for (int x = 0; x < 2; ++x) {
           if (!ok || s.e[x] == 0) continue;
           mbar_arrive_expect_tx(q_full(x), Sh::Q_BYTES);
 #pragma unroll
           for (int k = 0; k < Sh::ATOMS; ++k)
-            tma_load_3d(smem_u32(sm + x * Sh::Q_BYTES + k * Sh::QCOL), &q_map, k * 64, s.it.h << g_log, s.token0 + x * QT, q_full(x));
+            tma_load_3d(smem_u32(sm + x * Sh::Q_BYTES + k * Sh::QCOL), &q_map, k * 64, s.h << g_log, s.token0 + x * QT, q_full(x));
         }
       }
-      const int rowK = (c.layer * 2 * c.Hkv + s.it.h) * 64, rowV = rowK + c.Hkv * 64;
+      const int rowK = (c.layer * 2 * c.Hkv + s.h) * 64, rowV = rowK + c.Hkv * 64;
       for (int g0 = 0; g0 < E; g0 += 32) {
         int mine = -1;  // the pages of 32 blocks, one a lane; page 0 stands in for one that is not there
-        if (g0 + lane < E && (s.kb0 + g0 + lane) * 64 < s.it.len)
-          mine = chunk_page(c.page_table, c.max_pages, c.n_pages, s.it.b, s.kb0 + g0 + lane, c.err);
+        if (g0 + lane < E && (s.kb0 + g0 + lane) * 64 < it.len)
+          mine = chunk_page(c.page_table, c.max_pages, c.n_pages, s.b, s.kb0 + g0 + lane, c.err);
         for (int i = 0; i < min(32, E - g0); ++i, ++blk) {
           const int page = __shfl_sync(0xffffffffu, mine, i);
           if (lane == 0 && ok) {
@@ -1118,7 +1136,14 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         tc_commit(s_full(x, n));
       };
       bool ok = true;
-      while (ok && segment(s)) {
+      auto next = [&] {
+        if (!wait(seg_full(segs), segs / PairSeg::RING)) return false;
+        s = s_seg[segs % PairSeg::RING];
+        mbar_arrive(seg_empty(segs));
+        ++segs;
+        return s.nb > 0;
+      };
+      while (ok && next()) {
         const int E = s.kb1 - s.kb0, e = x ? s.e[1] : s.e[0];
         ok = e == 0 || wait(q_full(x), qn++);
         for (int i = 0; i < min(2, E) && ok; ++i) {  // S of the first two blocks
@@ -1133,7 +1158,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
           const unsigned b = blk + i;
           const bool more = i + 2 < E;
           // (what this tile does not use it waits for and releases all the same, in step with the other)
-          ok = wait(v_full(b), b / NST) && (s.kb0 + i + 1 < s.it.nb || wait(v_tail, tails++)) &&
+          ok = wait(v_full(b), b / NST) && (s.kb0 + i + 1 < s.nb || wait(v_tail, tails++)) &&
                (!more || wait(k_full(b + 2), (b + 2) / NST)) && (i >= e || wait(p_full(x, n), n >> 1));
           if (!ok) break;
           if (i < e) {
@@ -1166,10 +1191,15 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
     bool ok = true;
     // waits taken by the whole warp: the TMEM accesses after them are warp-collective
     auto wait_w = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, wait(b, parity)); };
-    bool noted = false;
-    while (ok && segment(s)) {
-      if (!noted && tid == 0) join_note(a, &s.it, per);
-      noted = true;
+    auto next = [&] {
+      if (!wait_w(seg_full(segs), segs / PairSeg::RING)) return false;
+      s = s_seg[segs % PairSeg::RING];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(seg_empty(segs));
+      ++segs;
+      return s.nb > 0;
+    };
+    while (ok && next()) {
       const bool row_ok = qi < s.nq[x];
       const int see = row_ok ? s.see0 + x * QT + qi : -1;  // a row past the tile's queries sees nothing
       const int see0 = s.see0 + x * QT;                    // of the tile's first query
@@ -1181,11 +1211,11 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         uint32_t su[64];
         tmem_ld_32_issue(t_sn, su);
         tmem_ld_32_issue(t_sn + 32, su + 32);
-        if (s.kb0 + i + 1 == s.it.nb && x == (s.nq[1] > 0)) {
+        if (s.kb0 + i + 1 == s.nb && x == (s.nq[1] > 0)) {
           // V's barrier is in this use's phase: the stage's use before was read by a P V before this S, and this one's use
           // ends with a P V that waits for v_tail
           const unsigned b = blk + i;
-          if (row < 64 && s.see0 + s.nq[0] + s.nq[1] <= (s.it.nb - 1) * 64 + row && wait(v_full(b), b / NST)) {
+          if (row < 64 && s.see0 + s.nq[0] + s.nq[1] <= (s.nb - 1) * 64 + row && wait(v_full(b), b / NST)) {
             uint8_t* v = sm + Sh::OFF_V + (b % NST) * Sh::T_BYTES + row * 128;  // (a row keeps its place in the swizzle)
 #pragma unroll
             for (int k = 0; k < 8 * Sh::ATOMS; ++k)
@@ -1252,9 +1282,9 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         if (lane == 0) mbar_arrive(p_full(x, n));
       }
       // the last P V, then the row out: O / l, or its part
-      const bool whole = s.kb0 == 0 && s.kb1 == s.it.nb;
+      const bool whole = s.kb0 == 0 && s.kb1 == s.nb;
       const long long token = s.token0 + x * QT + qi;
-      const int head = (s.it.h << g_log) + g;
+      const int head = (s.h << g_log) + g;
       const int slot = 2 * blockIdx.x + (s.kb0 == 0), prow = x * 128 + row;  // of the part
       bf16* orow = static_cast<bf16*>(a.out) + token * a.os + (long long)head * HD;
       const bool wide = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && a.os % 8 == 0;
@@ -1302,7 +1332,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         const int hh = __shfl_sync(0xffffffffu, head, src), see_r = __shfl_sync(0xffffffffu, see, src);
         const int pr = __shfl_sync(0xffffffffu, prow, src);
         float mm, ll, oo[HD / 32];
-        chunk_redo<HD>(a, s.it.b, s.it.h, tk, hh, s.kb0 * 64, min(s.kb1 * 64, see_r + 1), mm, ll, oo);
+        chunk_redo<HD>(a, s.b, s.h, tk, hh, s.kb0 * 64, min(s.kb1 * 64, see_r + 1), mm, ll, oo);
         const float inv = ll != 0.f ? 1.f / ll : 0.f;
 #pragma unroll
         for (int k = 0; k < HD / 32; ++k) {
@@ -1317,7 +1347,6 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       }
       blk += s.kb1 - s.kb0;
     }
-    if (!noted && tid == 0) join_note(a, nullptr, per);
   }
   if (*abort_flag) drain_copies();
   tc_fence_before();
@@ -1836,11 +1865,11 @@ __global__ void __launch_bounds__(256) k_weigh_join(ChunkAttn a, WeighTc wt, int
 // ----------------------------------------------------------------------------
 // Which kernel and split a call takes; a function of the arguments and the device alone.
 //
-// What an item counts beside its blocks (microseconds at 0 / 8 blocks of k_chunk_pair: 8192 causal tokens, 16 / 8 heads x 128,
-// 276 / 221, 4 x 1000 over 4000 entries 114 / 103; at 0 / 10 pages of k_chunk_mma with head_dim 64: 32 single tokens over up to
+// What an item counts beside its blocks (microseconds at 0 / 4 blocks of k_chunk_pair: 8192 causal tokens, 16 / 8 heads x 128,
+// 225 / 194, 4 x 1000 over 4000 entries 87 / 81; at 0 / 10 pages of k_chunk_mma with head_dim 64: 32 single tokens over up to
 // 8192 entries 119 / 105, 32 rows of up to 16 tokens 128 / 107; at 2 / 6 pages with head_dim 128: 100 single tokens over up to
 // 500 entries 45 / 40). Without, CTAs with many short items finished up to a third later than the others.
-constexpr int PAD_PAIR = 8, PAD_MMA128 = 6, PAD_MMA = 10, PAD_SIMT = 2;
+constexpr int PAD_PAIR = 4, PAD_MMA128 = 6, PAD_MMA = 10, PAD_SIMT = 2;
 struct ChunkPath {
   bool pair;    // k_chunk_pair
   int rt;       // rows of an item
@@ -1865,16 +1894,21 @@ static ChunkPath chunk_path(const ChunkDev& c, int dtype, const tlf_attn_chunk_a
   } else {
     // tcgen05: tiles of 128 rows of whole groups of heads, q through a tensor map
     const bool tc = c.hd >= 64 && (c.G & (c.G - 1)) == 0 && reinterpret_cast<uintptr_t>(a.q) % 16 == 0 && a.q_stride % 8 == 0;
-    p.pair = rows > 64 && tc;
+    // k_weigh_tc divides lse by the scale; out of this range the weights come from the scores, or from the CUDA cores
+    const float scale = a.scale > 0.f ? a.scale : 1.f;
+    const bool weigh_fits = !a.weight_out || (scale >= 0x1p-64f && scale <= 0x1p64f);
+    // k_chunk_pair also where its tiles are mostly padding: k_chunk_mma's products cost it more from 17 rows on at head_dim 128
+    // (32 rows of 16 / 32 tokens over up to 8192 entries, 16 / 8 heads: 109 / 112 us against 115 / 179; 8 tokens, 16 rows: 108
+    // against 101), from 33 on at 64 (32 rows of 48 / 64 tokens, 16 heads: 179 / 177 against 183 / 187, 4 rows of 64 over up to
+    // 1000: 16 against 24; 32 rows of 17 / 32 tokens: 178 / 177 against 132 / 134)
+    p.pair = tc && weigh_fits && rows > (c.hd == 128 ? 16 : 32);
     // weights: the scores that k_chunk_mma has at hand, 4 bytes a (query, head, entry) written and read instead of K again, up to
     // 16 rows (32 rows of up to 16 / 17 tokens over up to 8192 entries, 16 heads x 64: 177 us so, 217 with k_weigh_tc; at 32 and
     // 64 rows the bytes are two and four times as many, k_weigh_tc takes 221 and 279) and up to a bound on the scratch, which
     // the host can only size by the longest row; else S^T again, on the CUDA cores where the tiles do not fit (933 and 1593 us)
     const long long score_bytes = (long long)c.T * c.Hq * c.max_pages * 256;
     const bool fit = score_bytes <= (256LL << 20);
-    const float scale = a.scale > 0.f ? a.scale : 1.f;
-    const bool lse_fits = scale >= 0x1p-64f && scale <= 0x1p64f;  // k_weigh_tc divides by it
-    p.weigh_tc = a.weight_out && tc && (rows > 16 || !fit) && lse_fits;
+    p.weigh_tc = a.weight_out && tc && weigh_fits && (rows > 16 || !fit);
     p.scores = a.weight_out && !p.weigh_tc && fit ? score_bytes : 0;
     p.rt = p.pair ? PAIR_ROWS : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
     p.ctas = (c.hd == 128 || p.pair ? 1 : 2) * num_sms;

@@ -118,6 +118,48 @@ def test_attention_of_a_chunk(T, name):
     assert all(torch.equal(x[:c.T] if i < 2 else x, y[:c.T] if i < 2 else y) for i, (x, y) in enumerate(zip(got, again)))
 
 
+MIDDLE = {
+    # old, new, hq, hkv, hd: where one kernel takes over from the other, and rows shared by many CTAs
+    "128-16": ([500, 0, 63, 64], [8, 1, 8, 3], 4, 2, 128),
+    "128-17": ([500, 0, 63, 64], [17, 1, 8, 0], 2, 2, 128),
+    "128-g3": ([500, 10], [11, 20], 3, 1, 128),
+    "64-32": ([130, 4000], [8, 5], 8, 2, 64),
+    "64-33": ([130, 4000, 0], [33, 5, 30], 2, 2, 64),
+    "64-64": ([0, 63, 700], [16, 16, 15], 4, 1, 64),
+    "64-g64": ([1, 190], [1, 1], 64, 1, 64),
+    "short": ([0] * 40, [40, 1, 20, 33] * 10, 2, 2, 64),
+    "shared": ([7000], [65], 2, 1, 64),
+}
+
+
+@pytest.mark.parametrize("name", MIDDLE)
+def test_attention_between_few_and_many_rows(T, name):
+    import torch
+    old, new, hq, hkv, hd = MIDDLE[name]
+    c = R.Cache(old, new, hq, hkv, hd, "bf16", seed=len(name) + 100)
+    d = c.device()
+    ref = R.attention(c)
+    _hold(c, d, _attend(T, c, d), ref)
+    w_in = torch.rand(c.pages, 64, device="cuda")
+    got = _attend(T, c, d, weights=True, weight_in=w_in)
+    seen = _hold_weights(c, got[2], w_in.cpu().numpy(), ref, _hold(c, d, got, ref))
+    assert (got[2].cpu().numpy()[~seen] == -7).all()
+
+
+@pytest.mark.parametrize("new", [[1, 1], [20, 9], [130, 64]], ids=["one", "few", "many"])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_accounts_at_a_tiny_scale(T, new, hd):
+    """All scores alike: every visible entry gets the same weight, and lse over the scale is far outside of float32."""
+    import torch
+    c = R.Cache([70, 300], new, 4, 2, hd, "bf16", seed=hd)
+    d = c.device()
+    ref = R.attention(c, scale=1e-38)
+    w_in = torch.rand(c.pages, 64, device="cuda")
+    got = _attend(T, c, d, weights=True, weight_in=w_in, scale=1e-38)
+    p_rel = _hold(c, d, got, ref, scale=1e-38)
+    _hold_weights(c, got[2], w_in.cpu().numpy(), ref, p_rel)
+
+
 @pytest.mark.parametrize("new,max_chunk", [([1, 1, 1], 1), ([3, 1, 0], 3), ([90, 150, 1], 150)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rows_that_see_nothing_and_rows_without_entries(T, new, max_chunk, dtype):
