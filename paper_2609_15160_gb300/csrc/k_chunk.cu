@@ -902,14 +902,14 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
 // thread's MMAs run in order, so S of block i + 2 is issued right behind the P V of block i that reads the buffer, and the
 // softmax of block i + 1 finds its S ready when it is done with block i. With blocks of 128 keys there is room for one S a tile
 // only: a tile's chain S, softmax, P V was then 4.8k cycles a block, 2.0k of them MMAs (4 x 2048 tokens over up to 10240
-// entries, 16 / 8 heads x 128: 485 us, 330 so).
+// entries, 16 / 8 heads x 128: 485 us, 343 so at first).
 //
 // What bounds it: the softmax warps' instructions and the tensor cores nearly alike. At head_dim 128 a block of a tile is 8 S
 // products that read 6 KB of shared memory each, 48 cycles, and 4 P V products of 64 cycles: 1280 cycles for both tiles of the
 // about 1600 that a block takes; the exponentials (32 a cycle and SM) are 512 of them. Products and sums of two floats at a time
 // took 10 us off 362: the issue slots count, half of which are taken. Exponentials by polynomials beside the unit's made it
-// slower. With the join: 355 us for the case above (1370
-// TFLOP/s, 0.71 of the measured bf16 rate), 333 us with 16 heads x 64 (730), 212 us for 8192 causal tokens (1300).
+// slower. With the join: 344 us for the case above (1410 TFLOP/s, 0.73 of the measured bf16 rate; 386 in a long loop, where the
+// clock falls), 325 us with 16 heads x 64 (750), 195 us for 8192 causal tokens (1400).
 constexpr int PAIR_THREADS = 352;
 
 struct PairSeg {  // a CTA's part of an item: blocks kb0 .. kb1 - 1 of nb, of which tile x has the first e[x]; nb = 0: no more
@@ -1505,8 +1505,8 @@ __global__ void __launch_bounds__(256) k_chunk_weigh_scores(ChunkAttn a, const f
 //   warps 17, 18    issue S^T of keys 0-127 and 128-255 into one of two TMEM buffers each;
 //   warp 19         the tile's lse into the columns beside q.
 // A block inside one CTA's share is written out; parts of a shared one meet in k_weigh_join, in the CTAs' order.
-// Bound by the exponentials, 2048 of 2640 cycles a unit: 4 x 1000 tokens over up to 5000 entries, 16 / 8 heads x 128: 58 us
-// behind 103 us of attention.
+// Bound by the MMAs, 1150 cycles a unit of about 1600 with the softmax warps' latencies and the start: 4 x 1000 tokens over up
+// to 5000 entries, 16 / 8 heads x 128: 45 us behind 83 us of attention (65 with lse from shared memory and eight softmax warps).
 constexpr int WEIGH_THREADS = 640;
 struct WeighTc {
   WeighSplit sp;
@@ -1903,12 +1903,14 @@ static ChunkPath chunk_path(const ChunkDev& c, int dtype, const tlf_attn_chunk_a
     // 1000: 16 against 24; 32 rows of 17 / 32 tokens: 178 / 177 against 132 / 134)
     p.pair = tc && weigh_fits && rows > (c.hd == 128 ? 16 : 32);
     // weights: the scores that k_chunk_mma has at hand, 4 bytes a (query, head, entry) written and read instead of K again, up to
-    // 16 rows (32 rows of up to 16 / 17 tokens over up to 8192 entries, 16 heads x 64: 177 us so, 217 with k_weigh_tc; at 32 and
-    // 64 rows the bytes are two and four times as many, k_weigh_tc takes 221 and 279) and up to a bound on the scratch, which
-    // the host can only size by the longest row; else S^T again, on the CUDA cores where the tiles do not fit (933 and 1593 us)
+    // 16 rows (32 rows of 8 tokens over up to 8192 entries, 16 / 8 heads x 128: 142 us so, 155 with k_weigh_tc; of 16 tokens with
+    // 16 heads x 64 170 both ways, and twice the bytes at 32) and up to a bound on the scratch, which the host can only size by
+    // the longest row. With few entries the sums over the queries of a block of 256 entries are a chain that nothing hides: there
+    // k_weigh_tc from 9 rows on (4 rows of 16 tokens over up to 1000 entries, 16 heads x 64: 40 us from the scores, 23 so; one of
+    // 8 over 8000, 16 / 8 heads x 128: 33 / 27). S^T on the CUDA cores where the tiles do not fit.
     const long long score_bytes = (long long)c.T * c.Hq * c.max_pages * 256;
-    const bool fit = score_bytes <= (256LL << 20);
-    p.weigh_tc = a.weight_out && tc && weigh_fits && (rows > 16 || !fit);
+    const bool fit = score_bytes <= (256LL << 20), few = (long long)c.n * ((c.max_pages + 3) / 4) < num_sms;
+    p.weigh_tc = a.weight_out && tc && weigh_fits && (rows > 16 || !fit || (few && rows > 8));
     p.scores = a.weight_out && !p.weigh_tc && fit ? score_bytes : 0;
     p.rt = p.pair ? PAIR_ROWS : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
     p.ctas = (c.hd == 128 || p.pair ? 1 : 2) * num_sms;
