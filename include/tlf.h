@@ -369,7 +369,8 @@ int tlf_attn_decode_static(const tlf_attn_args* a, void* stream);
 typedef struct tlf_chunk {
   int32_t n;            /* rows (sequences), 1..1024 */
   int32_t n_tokens;     /* new tokens of all rows; 0 is allowed */
-  int32_t max_chunk;    /* an upper bound of the new tokens of a row (more sets err bit 2 and is cut); 0 = n_tokens */
+  int32_t max_chunk;    /* an upper bound of the new tokens of a row (more sets err bit 2 and is cut); 0 = n_tokens. It
+                           picks the kernels and sizes the workspace: steps of single tokens should say 1 */
   int32_t n_heads;      /* Hq */
   int32_t n_kv_heads;   /* Hkv, divides Hq */
   int32_t head_dim;     /* 16, 32, 64 or 128 (bf16: 32, 64 or 128) */
