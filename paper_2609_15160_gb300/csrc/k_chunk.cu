@@ -1387,7 +1387,6 @@ __device__ __forceinline__ int item_row(const long long* base, int n, long long 
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) k_chunk_weigh(ChunkAttn a, const float* w_in, float* w_out) {
   constexpr int KS = HD + 4, QR = HD == 128 ? 16 : 32;
-  pdl_wait();
   extern __shared__ long long s_base[];
   __shared__ long long s_red[33];
   __shared__ __align__(16) float sK[64 * KS];
@@ -1398,6 +1397,7 @@ __global__ void __launch_bounds__(256) k_chunk_weigh(ChunkAttn a, const float* w
   const ChunkDev& c = a.c;
   const int tid = threadIdx.x, key = tid & 63, part = tid >> 6, G = c.G;
   const long long items = weigh_items(c, 64, s_base, s_red);
+  pdl_wait();
   for (long long item = blockIdx.x; item < items; item += gridDim.x) {
     const int lo = item_row(s_base, c.n, item);
     const int pg = (int)(item - s_base[lo]), page = chunk_page(c.page_table, c.max_pages, c.n_pages, lo, pg, c.err);
@@ -1446,15 +1446,16 @@ __global__ void __launch_bounds__(256) k_chunk_weigh(ChunkAttn a, const float* w
 
 // The same from the scores that k_chunk_mma left: an item is 256 entries of a row; 64 threads x 4 entries, four groups of
 // threads that take every fourth (query, head). Reads 4 bytes a (query, head, entry) instead of K again: 32 single tokens over
-// up to 8192 entries, 16 heads x 64: 12 us.
+// up to 8192 entries, 16 heads x 64: 8 us.
 __global__ void __launch_bounds__(256) k_chunk_weigh_scores(ChunkAttn a, const float* w_in, float* w_out) {
-  pdl_wait();
   extern __shared__ long long s_base[];
   __shared__ long long s_red[33];
   __shared__ float4 s_sum[4][64];
   const ChunkDev& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, part = tid >> 6;
-  const long long items = weigh_items(c, 256, s_base, s_red), width = (long long)c.max_pages * 64;
+  const long long items = weigh_items(c, 256, s_base, s_red);  // (of lengths alone: beside the kernels before)
+  pdl_wait();
+  const long long width = (long long)c.max_pages * 64;
   for (long long item = blockIdx.x; item < items; item += gridDim.x) {
     const int b = item_row(s_base, c.n, item);
     const ChunkRow r = chunk_row(c, b);
@@ -2023,7 +2024,7 @@ static cudaError_t chunk_launch(const ChunkAttn& a, const tlf_attn_chunk_args& a
   const dim3 grid(4 * num_sms);
   if constexpr (std::is_same<T, bf16>::value)
     if (weigh) return a.c.hd == 64 ? weigh_launch<64>(a, args, weigh, num_sms, st) : weigh_launch<128>(a, args, weigh, num_sms, st);
-  if (a.scores) return launch_k(k_chunk_weigh_scores, grid, dim3(256), base, st, a, args.weight_in, args.weight_out);
+  if (a.scores) return launch_k(k_chunk_weigh_scores, dim3(8 * num_sms), dim3(256), base, st, a, args.weight_in, args.weight_out);
   switch (a.c.hd) {
     case 16:
       if constexpr (std::is_same<T, float>::value)
