@@ -203,6 +203,32 @@ def test_what_a_query_may_not_see_does_not_reach_it(T, new, dtype, bad):
     assert not np.isfinite(out.float().cpu().numpy()[last]).all()
 
 
+@pytest.mark.parametrize("new,hq,hd", [([9, 12], 4, 128), ([20, 1], 2, 128), ([40, 33], 2, 64), ([130, 64], 4, 128)])
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+def test_what_a_query_may_not_see_does_not_reach_the_accounts(T, new, hq, hd, bad):
+    """The same where tiles are mostly padding, and for the weights: entries behind the caches and pages of nobody."""
+    import torch
+    c = R.Cache([70, 300], new, hq, 2, hd, "bf16", seed=13)
+    ref = R.attention(c)
+    keep = np.ones((c.pages, 64), bool)
+    for b in range(c.n):
+        keep[c.at(b, np.arange(c.lens[b]))] = False
+    c.pool = np.where(keep[:, None, None, None, :, None], np.float32(bad), c.pool)
+    d = c.device()
+    w_in = torch.rand(c.pages, 64, device="cuda")
+    got = _attend(T, c, d, weights=True, weight_in=w_in)
+    seen = _hold_weights(c, got[2], w_in.cpu().numpy(), ref, _hold(c, d, got, ref))
+    assert (got[2].cpu().numpy()[~seen] == -7).all()
+    # the last new token's key: earlier queries' output and lse are as before
+    for b in range(c.n):
+        p, o = c.at(b, np.array([c.lens[b] - 1]))
+        c.pool[p, c.layer, :, :, o] = bad
+    again = _attend(T, c, c.device())
+    others = torch.as_tensor(np.setdiff1d(np.arange(c.T), c.cu[1:] - 1), device="cuda")
+    assert torch.isfinite(again[0][others].float()).all()
+    assert (again[0][others].float() - got[0][others].float()).abs().max().item() <= 2 * RB * got[0].float().abs().max().item()
+
+
 def test_a_value_that_is_infinite_reaches_those_that_see_it(T):
     for new in ([1], [5], [130]):
         c = R.Cache([100], new, 2, 1, 64, "bf16", seed=5)
