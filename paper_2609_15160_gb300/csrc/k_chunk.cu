@@ -440,8 +440,8 @@ __global__ void __launch_bounds__(256) k_chunk_simt(ChunkAttn a) {
 // ----------------------------------------------------------------------------
 // Tensor cores, few rows: mma.sync (bfloat16)
 // ----------------------------------------------------------------------------
-// A kv head's keys meet at most 64 query rows here, so a page's 2 x 64 x hd x rows products take less time than its bytes
-// (a tcgen05 tile would be 128 rows of mostly padding and its scores a trip through tensor memory). A producer warp copies
+// A kv head's keys meet few query rows here (up to 64 where k_chunk_pair's tiles do not fit the heads or q), so a page's 2 x 64 x
+// hd x rows products take about as long as its bytes or less, and a tcgen05 tile would be 128 rows of mostly padding. A producer warp copies
 // K and V of each page through a tensor map (128-byte swizzle; 64 at head_dim 32) into a ring; eight warps share it:
 //   MT = 1 (up to 16 rows)  two teams of four warps take the pages in turn, each warp 16 of a page's keys,
 //   MT = 2, 4 (32, 64 rows) warp w has rows 16 (w mod MT).. and 64 MT / 8 keys of every page.
