@@ -923,7 +923,7 @@ struct PairShape {
   static constexpr int COL = 64 * 128, T_BYTES = ATOMS * COL;                      // 64 rows of K or V
   static constexpr int NST = HD == 128 ? 4 : 8;  // of the K ring and of the V ring
   static constexpr int OFF_K = 2 * Q_BYTES, OFF_V = OFF_K + NST * T_BYTES, OFF_BAR = OFF_V + NST * T_BYTES;
-  static constexpr int NBAR = 4 * NST + 2 + 4 + 4 + 4 + 2 + 2 * PairSeg::RING;
+  static constexpr int NBAR = 5 * NST + 2 + 4 + 4 + 4 + 1 + 2 * PairSeg::RING;
   static constexpr int FLAGS = 16;  // more than the blocks that the producer can be ahead of the softmax
   static constexpr int OFF_INT = OFF_BAR + NBAR * 8, OFF_SEG = OFF_INT + (FLAGS + 4) * 4;
   static constexpr int OFF_BASE = OFF_SEG + PairSeg::RING * (int)sizeof(PairSeg);
@@ -985,9 +985,12 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
   auto s_full = [&](int x, unsigned n) { return bar(4 * NST + 2 + 2 * x + (n & 1)); };
   auto p_full = [&](int x, unsigned n) { return bar(4 * NST + 6 + 2 * x + (n & 1)); };
   auto o_done = [&](int x, unsigned n) { return bar(4 * NST + 10 + 2 * x + (n & 1)); };
-  const uint32_t q_free = bar(4 * NST + 14), v_tail = bar(4 * NST + 15);
-  auto seg_full = [&](unsigned i) { return bar(4 * NST + 16 + i % PairSeg::RING); };
-  auto seg_empty = [&](unsigned i) { return bar(4 * NST + 16 + PairSeg::RING + i % PairSeg::RING); };
+  const uint32_t q_free = bar(4 * NST + 14);
+  // V of block b fit for the products. One barrier a stage, and its writers wait for V first: the stage's next phase then lies
+  // behind both issuers' release of this use, so neither can find two phases gone by, which a parity does not tell from none
+  auto v_tail = [&](unsigned b) { return bar(4 * NST + 15 + b % NST); };
+  auto seg_full = [&](unsigned i) { return bar(5 * NST + 15 + i % PairSeg::RING); };
+  auto seg_empty = [&](unsigned i) { return bar(5 * NST + 15 + PairSeg::RING + i % PairSeg::RING); };
   const ChunkDev& c = a.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
@@ -996,6 +999,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       mbar_init(k_empty(i), 2);
       mbar_init(v_full(i), 1);
       mbar_init(v_empty(i), 2);
+      mbar_init(v_tail(i), 4);
     }
     for (int x = 0; x < 2; ++x) {
       mbar_init(q_full(x), 1);
@@ -1006,7 +1010,6 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       }
     }
     mbar_init(q_free, 2);
-    mbar_init(v_tail, 4);
     for (unsigned i = 0; i < PairSeg::RING; ++i) {
       mbar_init(seg_full(i), 1);
       mbar_init(seg_empty(i), 10);  // the other warps
@@ -1125,7 +1128,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       const uint64_t qd = smem_desc_sw128(smem_u32(sm + x * Sh::Q_BYTES)), dk = smem_desc_sw128(smem_u32(sm + Sh::OFF_K));
       const uint64_t dv = smem_desc_sw128_mn(smem_u32(sm + Sh::OFF_V), Sh::COL);
       const uint32_t t_s = tmem + 128u * x, t_o = tmem + Sh::OCOL + (uint32_t)(HD * x);
-      unsigned blk = 0, tails = 0, qn = 0, n = 0;  // n: blocks of the tile whose P V has been issued
+      unsigned blk = 0, tails = 0, qn = 0, n = 0;  // tails: a bit a stage, v_tail's parity; n: blocks of the tile whose P V has been issued
       auto issue_s = [&](unsigned b, unsigned n) {
         const uint64_t kd = dk + (uint64_t)(b % NST) * T_E;
 #pragma unroll
@@ -1156,11 +1159,12 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         if (ok && E <= 2) tc_commit(q_free);
         for (int i = 0; i < E && ok; ++i) {
           const unsigned b = blk + i;
-          const bool more = i + 2 < E;
+          const bool more = i + 2 < E, tail = s.kb0 + i + 1 == s.nb;
           // (what this tile does not use it waits for and releases all the same, in step with the other)
-          ok = wait(v_full(b), b / NST) && (s.kb0 + i + 1 < s.nb || wait(v_tail, tails++)) &&
+          ok = wait(v_full(b), b / NST) && (!tail || wait(v_tail(b), tails >> b % NST)) &&
                (!more || wait(k_full(b + 2), (b + 2) / NST)) && (i >= e || wait(p_full(x, n), n >> 1));
           if (!ok) break;
+          if (tail) tails ^= 1u << b % NST;
           if (i < e) {
             tc_fence_after();
             const uint64_t vd = dv + (uint64_t)(b % NST) * T_E;
@@ -1215,7 +1219,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
           // V's barrier is in this use's phase: the stage's use before was read by a P V before this S, and this one's use
           // ends with a P V that waits for v_tail
           const unsigned b = blk + i;
-          if (row < 64 && s.see0 + s.nq[0] + s.nq[1] <= (s.nb - 1) * 64 + row && wait(v_full(b), b / NST)) {
+          if (wait_w(v_full(b), b / NST) && row < 64 && s.see0 + s.nq[0] + s.nq[1] <= (s.nb - 1) * 64 + row) {
             uint8_t* v = sm + Sh::OFF_V + (b % NST) * Sh::T_BYTES + row * 128;  // (a row keeps its place in the swizzle)
 #pragma unroll
             for (int k = 0; k < 8 * Sh::ATOMS; ++k)
@@ -1223,7 +1227,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
             fence_proxy_async_smem();
           }
           __syncwarp();
-          if (lane == 0) mbar_arrive(v_tail);
+          if (lane == 0) mbar_arrive(v_tail(b));
         }
         const int key0 = (s.kb0 + i) * 64;
         const bool gone = s_flag[(blk + i) % Sh::FLAGS] != 0;
