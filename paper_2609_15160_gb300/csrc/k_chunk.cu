@@ -1092,7 +1092,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       }
       const int rowK = (c.layer * 2 * c.Hkv + s.h) * 64, rowV = rowK + c.Hkv * 64;
       for (int g0 = 0; g0 < E; g0 += 32) {
-        int mine = -1;  // the pages of 32 blocks, one a lane; page 0 stands in for one that is not there
+        int mine = -1;  // the pages of 32 blocks, one a lane; for one that is not there K is left as it is, V is zeros
         if (g0 + lane < E && (s.kb0 + g0 + lane) * 64 < it.len)
           mine = chunk_page(c.page_table, c.max_pages, c.n_pages, s.b, s.kb0 + g0 + lane, c.err);
         for (int i = 0; i < min(32, E - g0); ++i, ++blk) {
@@ -1101,20 +1101,31 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
             ok = blk < NST || wait(k_empty(blk), blk / NST - 1);
             if (ok) {
               s_flag[blk % Sh::FLAGS] = page < 0;
-              mbar_arrive_expect_tx(k_full(blk), Sh::T_BYTES);
+              if (page < 0) {
+                mbar_arrive(k_full(blk));
+              } else {
+                mbar_arrive_expect_tx(k_full(blk), Sh::T_BYTES);
 #pragma unroll
-              for (int k = 0; k < Sh::ATOMS; ++k)
-                tma_load_3d(smem_u32(sm + Sh::OFF_K + (blk % NST) * Sh::T_BYTES + k * Sh::COL), &pool_map, k * 64, rowK, max(page, 0), k_full(blk));
+                for (int k = 0; k < Sh::ATOMS; ++k)
+                  tma_load_3d(smem_u32(sm + Sh::OFF_K + (blk % NST) * Sh::T_BYTES + k * Sh::COL), &pool_map, k * 64, rowK, page, k_full(blk));
+              }
               ok = blk < NST || wait(v_empty(blk), blk / NST - 1);
             }
-            if (ok) {
+            if (ok && page >= 0) {
               mbar_arrive_expect_tx(v_full(blk), Sh::T_BYTES);
 #pragma unroll
               for (int k = 0; k < Sh::ATOMS; ++k)
-                tma_load_3d(smem_u32(sm + Sh::OFF_V + (blk % NST) * Sh::T_BYTES + k * Sh::COL), &pool_map, k * 64, rowV, max(page, 0), v_full(blk));
+                tma_load_3d(smem_u32(sm + Sh::OFF_V + (blk % NST) * Sh::T_BYTES + k * Sh::COL), &pool_map, k * 64, rowV, page, v_full(blk));
             }
           }
           __syncwarp();
+          if (page < 0 && __shfl_sync(0xffffffffu, (int)ok, 0)) {  // P = 0 does not cancel an infinity
+            uint4* v = reinterpret_cast<uint4*>(sm + Sh::OFF_V + (blk % NST) * Sh::T_BYTES);
+            for (int k = lane; k < Sh::T_BYTES / 16; k += 32) v[k] = make_uint4(0, 0, 0, 0);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(v_full(blk));
+          }
         }
       }
       ++segs;

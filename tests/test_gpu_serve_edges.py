@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 import _serve_ref as R
-from test_gpu_serve_ops import RB, T, U, _attend, _draw, _hold, _hold_weights  # noqa: F401
+from test_gpu_serve_ops import RB, T, U, _attend, _draw, _hold  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +37,62 @@ def test_rows_without_a_number_leave_the_others_alone(T):
     for b in bad:
         assert not np.isfinite(out[c.cu[b]:c.cu[b] + 64].float().cpu().numpy()).any()
         _hold_tokens(c, out, ref, np.arange(c.cu[b] + 64, c.cu[b + 1]))
+
+
+def _without(c, gone):
+    """R.attention with the entries of pages `gone` (row, page of the row) left out: out, lse, spread, terms, weights."""
+    out, spread = np.zeros((c.T, c.hq, c.hd)), np.zeros((c.T, c.hq, c.hd))
+    lse, terms = np.full((c.T, c.hq), -np.inf), np.zeros((c.T, c.hq))
+    weights, G = [np.zeros(n) for n in c.lens], c.hq // c.hkv
+    for b in range(c.n):
+        k, v = (x.astype(np.float64) for x in c.kv(b))
+        there = np.array([(b, e // 64) not in gone for e in range(c.lens[b])])
+        for i in range(c.new[b]):
+            t = c.cu[b] + i
+            e = np.nonzero(there[:c.old[b] + i + 1])[0]
+            if len(e) == 0:
+                continue
+            for h in range(c.hq):
+                q = c.q[t, h].astype(np.float64)
+                s = k[e, h // G] @ q / np.sqrt(c.hd)
+                terms[t, h] = (np.abs(k[e, h // G]) @ np.abs(q)).max() / np.sqrt(c.hd)
+                lse[t, h] = s.max() + np.log(np.exp(s - s.max()).sum())
+                p = np.exp(s - lse[t, h])
+                out[t, h], spread[t, h] = p @ v[e, h // G], p @ np.abs(v[e, h // G])
+                weights[b][e] += p
+    return out, lse, spread, terms, weights
+
+
+@pytest.mark.parametrize("new", [[1, 1, 1], [1, 6, 3], [1, 90, 150], [1, 20, 257]], ids=["one", "few", "many", "mixed"])
+@pytest.mark.parametrize("dtype,hd", [("f32", 64), ("bf16", 64), ("bf16", 128)])
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+def test_a_page_that_is_not_there_is_left_out(T, new, dtype, hd, bad):
+    """Page ids outside the pool, in rows of one token beside longer ones, while page 0 holds no number at all. The long rows
+    put several blocks into a CTA's share, missing ones among them."""
+    import torch
+    c = R.Cache([300, 200, 0] + [5000] * 8, new + [1] * 8, 4, 2, hd, dtype, seed=31)
+    spare = np.setdiff1d(np.arange(c.pages), c.table)[0]
+    if 0 in c.table:  # page 0 is nobody's
+        c.pool[spare] = c.pool[0]
+        c.table[c.table == 0] = spare
+    c.pool[0] = bad
+    gone = {(0, 1): c.pages + 7, (0, 3): -1, (1, 0): 1 << 30, (1, 2): -9, (2, 0): c.pages}
+    gone.update({(b, p): -1 for b in range(3, 11) for p in range(b, 79, 5)})
+    ref = _without(c, gone)
+    d = c.device()
+    for (b, p), page in gone.items():
+        d["table"][b, p] = page
+    w_in = torch.rand(c.pages, 64, device="cuda")
+    out, lse, w = _attend(T, c, d, weights=True, weight_in=w_in)
+    plain = _attend(T, c, d, max_chunk=max(new))  # (a tighter bound may take another kernel)
+    assert int(d["err"][0].item()) == 2
+    d["err"].zero_()
+    _hold(c, d, (out, lse), ref)
+    _hold(c, d, plain, ref)
+    w, before = w.cpu().numpy().astype(np.float64), w_in.cpu().numpy()
+    for b in range(c.n):
+        e = np.array([e for e in range(c.lens[b]) if (b, e // 64) not in gone], int)
+        want = before[c.at(b, e)] + ref[4][b][e]
+        assert (np.abs(w[c.at(b, e)] - want) <= 2.0 ** -11 * ref[4][b][e] + 4 * U * want).all()
+        lost = np.setdiff1d(np.arange(c.lens[b]), e)
+        assert (w[c.at(b, lost)] == -7).all()
