@@ -1201,7 +1201,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
     const uint32_t t_s = tmem + lane_off + 128u * (uint32_t)x;
     const uint32_t t_o = tmem + lane_off + Sh::OCOL + (uint32_t)(HD * x);
     const int qi = row >> g_log, g = row & ((1 << g_log) - 1);
-    const float scale = a.scale, grow_by = 8.f / scale;
+    const float scale = a.scale;
     unsigned n = 0, blk = 0;  // blocks of this tile, and of the CTA
     bool ok = true;
     // waits taken by the whole warp: the TMEM accesses after them are warp-collective
@@ -1253,8 +1253,9 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
 #pragma unroll
         for (int k = 0; k < 64; ++k) pm4[k & 3] = fmaxf(pm4[k & 3], __uint_as_float(su[k]));
         const float pm = fmaxf(fmaxf(pm4[0], pm4[1]), fmaxf(pm4[2], pm4[3]));
-        // O is rescaled only when a row's maximum grows by more than 8 in base 2, after the P V before has landed
-        const bool grow = pm > m_run + grow_by;
+        // O is rescaled only when a row's maximum grows by more than 8 in base 2, after the P V before has landed (the first
+        // visible key: by infinity, at any scale; -inf - -inf, none so far, is not a number)
+        const bool grow = (pm - m_run) * scale > 8.f;
         if (__any_sync(0xffffffffu, grow)) {
           const float cr = grow ? exp2f((m_run - pm) * scale) : 1.f;  // 0 when m_run was -inf
           if (i > 0) {

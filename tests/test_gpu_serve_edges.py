@@ -96,3 +96,15 @@ def test_a_page_that_is_not_there_is_left_out(T, new, dtype, hd, bad):
         assert (np.abs(w[c.at(b, e)] - want) <= 2.0 ** -11 * ref[4][b][e] + 4 * U * want).all()
         lost = np.setdiff1d(np.arange(c.lens[b]), e)
         assert (w[c.at(b, lost)] == -7).all()
+
+
+# ---- the ends of the types ----
+
+@pytest.mark.parametrize("scale", [1.6e-38, 1e-38, 1e-41, 1e-45])
+@pytest.mark.parametrize("old,new,hq,hkv,hd", [([70, 300], [20, 33], 4, 2, 64), ([70, 300], [130, 64], 4, 2, 128), ([7000], [65], 2, 1, 64),
+                                               ([7000], [65], 2, 1, 128), ([100, 30], [5, 1], 4, 2, 64)])
+def test_a_tiny_scale_without_accounts(T, scale, old, new, hq, hkv, hd):
+    """All scores alike, in items of one CTA and in shared ones: means over what is seen, lse the logarithm of its number."""
+    c = R.Cache(old, new, hq, hkv, hd, "bf16", seed=hd)
+    d = c.device()
+    _hold(c, d, _attend(T, c, d, scale=scale), R.attention(c, scale=scale), scale=scale)
