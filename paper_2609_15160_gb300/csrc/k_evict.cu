@@ -38,7 +38,7 @@ struct EvictDev {
 };
 
 __device__ __forceinline__ uint32_t ordered_key(float w) {
-  const uint32_t u = __float_as_uint(w);
+  const uint32_t u = __float_as_uint(w + 0.f);  // -0 weighs what 0 does
   if (w != w) return 0u;
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }

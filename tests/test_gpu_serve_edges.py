@@ -108,3 +108,26 @@ def test_a_tiny_scale_without_accounts(T, scale, old, new, hq, hkv, hd):
     c = R.Cache(old, new, hq, hkv, hd, "bf16", seed=hd)
     d = c.device()
     _hold(c, d, _attend(T, c, d, scale=scale), R.attention(c, scale=scale), scale=scale)
+
+
+def test_eviction_takes_the_two_zeros_for_equal(T):
+    """Weights 0 and -0: the lower index stays, whichever zero it has."""
+    import torch
+    rng = np.random.default_rng(5)
+    lens = [100, 300, 3000]
+    c = R.Cache(lens, [0] * 3, 1, 1, 64, "bf16", layers=1, layer=0, seed=2)
+    w = np.where(rng.random((c.pages, 64)) < 0.5, np.float32(-0.0), np.float32(0.0))
+    w[rng.random(w.shape) < 0.1] = 1
+    w[rng.random(w.shape) < 0.1] = -1
+    pos = np.zeros((c.pages, 64), np.int32)
+    for b, n in enumerate(lens):
+        pos[c.at(b, np.arange(n))] = np.arange(n)
+    d = c.device(w=w, pos=pos, nxt=np.asarray(lens, np.int32))
+    wo, po, lo = torch.zeros_like(d["w"]), torch.zeros_like(d["pos"]), torch.zeros_like(d["lens"])
+    a = T.evict_args(d["pool"], d["table"], d["lens"], d["nxt"], d["pos"], po, d["w"], wo, lo, budget=60, n_first=2, n_recent=8)
+    n = T.tlf_cache_evict_scratch_bytes(a)
+    T.tlf_cache_evict(a, torch.empty(n, dtype=torch.uint8, device="cuda"), n)
+    for b, n in enumerate(lens):
+        e = np.arange(n)
+        src = R.evict(w[c.at(b, e)], pos[c.at(b, e)], n, 60, 2, 8)
+        assert np.array_equal(po.cpu().numpy()[c.at(b, np.arange(60))], src)
