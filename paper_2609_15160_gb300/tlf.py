@@ -381,15 +381,16 @@ def rope_args(q, k, v, positions, table, q_out, layout: str = "half", entry_pos=
 
 
 def _pair(c: TlfChunk, a):
-    """The arguments' tensors are large enough for the batch (looked at once for a pair of them)."""
-    if getattr(a, "batch", None) is c:
+    """The arguments' tensors are large enough for the batch (looked at once for the same numbers: a program may change them)."""
+    batch = (c.n_tokens, c.n_heads, c.n_kv_heads, c.head_dim, c.dtype, c.n_pages)
+    if getattr(a, "batch", None) == batch:
         return
     rows, hq, kh, hd, dt, pages = a.fits
     if rows < c.n_tokens or hq != c.n_heads or (kh and kh != c.n_kv_heads) or hd != c.head_dim or dt != c.dtype or any(
             p != c.n_pages for p in pages):
         raise ValueError(f"the arguments are for {rows} tokens of {hq} heads of {hd} and caches of {pages} pages, the batch has "
                          f"{c.n_tokens} tokens of {c.n_heads} heads of {c.head_dim} and {c.n_pages} pages")
-    a.batch = c
+    a.batch = batch
 
 
 def tlf_rope_append(c: TlfChunk, a: TlfRopeArgs, stream=None):

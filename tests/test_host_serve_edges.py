@@ -1,0 +1,36 @@
+"""CPU tests of what the operators on paged caches and logits refuse at the ends of their arguments' ranges."""
+import ctypes as C
+
+import pytest
+
+from paper_2609_15160_gb300 import build, tlf
+
+P = 1 << 20  # a made-up device address, aligned; nothing is launched by a refused call
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return tlf.load_library()
+
+
+def test_a_batch_that_changes_is_looked_at_again():
+    """Fields of a batch that a program keeps may change between calls: tensors that no longer fit are refused."""
+    torch = pytest.importorskip("torch")
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    pool = torch.zeros(9, 2, 2, 2, 64, 64, dtype=torch.bfloat16)
+    q = torch.zeros(7, 4, 64, dtype=torch.bfloat16)
+    for field, value in (("n_tokens", 8), ("n_heads", 2), ("head_dim", 32), ("dtype", 0), ("n_pages", 10)):
+        c = tlf.chunk_args(pool, i32(3, 4), i32(4), i32(3), 4, 7)
+        a = tlf.attn_chunk_args(q, q, weight_out=torch.zeros(9, 64))
+        tlf._pair(c, a)
+        tlf._pair(c, a)
+        setattr(c, field, value)
+        with pytest.raises(ValueError):
+            tlf.tlf_attn_chunk(c, a, None, 0)
+    c = tlf.chunk_args(pool, i32(3, 4), i32(4), i32(3), 4, 7)
+    r = tlf.rope_args(q, q[:, :2], q[:, 2:], i32(7), torch.zeros(9, 32, 2), torch.zeros_like(q))
+    tlf._pair(c, r)
+    c.n_kv_heads = 1
+    with pytest.raises(ValueError):
+        tlf.tlf_rope_append(c, r)
