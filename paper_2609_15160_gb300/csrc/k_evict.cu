@@ -238,12 +238,15 @@ __global__ void __launch_bounds__(EV_MOVE_THREADS) k_evict_move(EvictDev a, uint
   pdl_trigger();
 }
 
+// The budget as far as a row can reach it: a caller may give any number for no limit.
+static int evict_budget(const tlf_evict_args& a) { return std::min(a.budget, a.max_pages * SV_PAGE); }
+
 size_t evict_scratch(const tlf_evict_args& a) {
-  return ((size_t)a.n * 4 + 15) / 16 * 16 + (size_t)a.n * a.budget * sizeof(int2);
+  return ((size_t)a.n * 4 + 15) / 16 * 16 + (size_t)a.n * evict_budget(a) * sizeof(int2);
 }
 
 cudaError_t launch_evict(const tlf_evict_args& a, void* scratch, int num_sms, cudaStream_t st) {
-  EvictDev d{a.n, a.max_pages, a.budget, a.n_first, a.n_recent, a.n_pages, a.page_table, a.lens, a.next_pos, a.pos_in,
+  EvictDev d{a.n, a.max_pages, evict_budget(a), a.n_first, a.n_recent, a.n_pages, a.page_table, a.lens, a.next_pos, a.pos_in,
              a.pos_out, a.weight_in, a.weight_out, a.lens_out, a.err, static_cast<int*>(scratch),
              reinterpret_cast<int2*>(static_cast<char*>(scratch) + ((size_t)a.n * 4 + 15) / 16 * 16)};
   // CTAs of a row: as many as leave one to an SM

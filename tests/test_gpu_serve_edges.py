@@ -131,3 +131,19 @@ def test_eviction_takes_the_two_zeros_for_equal(T):
         e = np.arange(n)
         src = R.evict(w[c.at(b, e)], pos[c.at(b, e)], n, 60, 2, 8)
         assert np.array_equal(po.cpu().numpy()[c.at(b, np.arange(60))], src)
+
+
+def test_eviction_with_a_budget_that_nothing_reaches(T):
+    """The workspace goes by the entries that a row can have, and nothing changes."""
+    import torch
+    c = R.Cache([200, 64, 0], [0] * 3, 1, 1, 64, "bf16", layers=1, layer=0, seed=2)
+    rng = np.random.default_rng(1)
+    w, pos = rng.random((c.pages, 64)).astype(np.float32), rng.integers(0, 99, (c.pages, 64)).astype(np.int32)
+    d = c.device(w=w, pos=pos, nxt=np.asarray([200, 64, 0], np.int32))
+    a = T.evict_args(d["pool"], d["table"], d["lens"], d["nxt"], d["pos"], d["pos"], d["w"], d["w"], d["lens"], budget=2 ** 31 - 1,
+                     n_recent=5)
+    n = T.tlf_cache_evict_scratch_bytes(a)
+    assert 0 < n < 1 << 16
+    T.tlf_cache_evict(a, torch.empty(n, dtype=torch.uint8, device="cuda"), n)
+    assert d["lens"].tolist() == [200, 64, 0] and np.array_equal(d["w"].cpu().numpy(), w) and np.array_equal(d["pos"].cpu().numpy(), pos)
+    assert np.array_equal(d["pool"].float().cpu().numpy(), c.pool)

@@ -34,3 +34,10 @@ def test_a_batch_that_changes_is_looked_at_again():
     c.n_kv_heads = 1
     with pytest.raises(ValueError):
         tlf.tlf_rope_append(c, r)
+
+
+def test_evictions_scratch_goes_by_what_a_row_can_hold(lib):
+    a = dict(n=2, n_kv_heads=2, head_dim=64, n_layers=1, page_size=64, dtype=1, max_pages=4, n_first=4, n_recent=10, n_pages=9, pool=P,
+             page_table=P, lens=P, next_pos=P, pos_in=P, pos_out=P, weight_in=P, weight_out=P, lens_out=P)
+    size = lambda b: lib.tlf_cache_evict_scratch_bytes(C.byref(tlf.TlfEvictArgs(budget=b, **a)))  # noqa: E731
+    assert size(100) < size(256) == size(257) == size(2 ** 31 - 1) < 1 << 13
