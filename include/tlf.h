@@ -378,7 +378,7 @@ typedef struct tlf_chunk {
   int32_t layer;        /* the layer that the call reads or writes */
   int32_t page_size;    /* 64 */
   int32_t dtype;        /* tlf_dtype of the pool, q, k, v and out */
-  int32_t max_pages;    /* entries per page-table row */
+  int32_t max_pages;    /* entries per page-table row, 1..2^25 - 65 */
   int32_t reserved0;    /* must be 0 */
   int64_t n_pages;      /* pages in the pool */
   void* pool;           /* KV pages, 16-byte aligned */
@@ -472,7 +472,7 @@ typedef struct tlf_evict_args {
   int32_t n_kv_heads, head_dim, n_layers;
   int32_t page_size;    /* 64 */
   int32_t dtype;        /* tlf_dtype */
-  int32_t max_pages;
+  int32_t max_pages;    /* 1..2^25 - 65 */
   int32_t budget;       /* >= 1, n_first + n_recent <= budget */
   int32_t n_first;      /* >= 0 */
   int32_t n_recent;     /* >= 0 */

@@ -20,7 +20,8 @@ static const char* cache_validate(int n, int hkv, int hd, int layers, int page_s
     return "head_dim must be 32, 64 or 128 (or 16 with float32)";
   if (page_size != SV_PAGE) return "page_size must be 64";
   if ((int64_t)layers * 2 * hkv * SV_PAGE > 0x7fffffff) return "n_layers * n_kv_heads is too large";
-  if (max_pages < 1 || max_pages > 0x7fffffff / SV_PAGE) return "max_pages * 64 must be in the int32 range";
+  // (the kernels step through entries in strides of up to 2048 and round their number up: room for that below 2^31)
+  if (max_pages < 1 || max_pages > 0x7fffffff / SV_PAGE - 64) return "max_pages must be in 1..2^25 - 65";
   if (n_pages < 1 || n_pages > 0x7fffffff) return "n_pages must be in 1..2^31 - 1";
   if (!pool || !page_table || !lens) return "a device pointer is NULL";
   if (!aligned(pool, 16)) return "pool must be aligned to 16 bytes";

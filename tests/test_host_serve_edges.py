@@ -41,3 +41,17 @@ def test_evictions_scratch_goes_by_what_a_row_can_hold(lib):
              page_table=P, lens=P, next_pos=P, pos_in=P, pos_out=P, weight_in=P, weight_out=P, lens_out=P)
     size = lambda b: lib.tlf_cache_evict_scratch_bytes(C.byref(tlf.TlfEvictArgs(budget=b, **a)))  # noqa: E731
     assert size(100) < size(256) == size(257) == size(2 ** 31 - 1) < 1 << 13
+
+
+@pytest.mark.parametrize("max_pages", [(1 << 25) - 1, (1 << 25) - 64])
+def test_page_tables_that_leave_no_room_below_32_bits_are_refused(lib, max_pages):
+    """Entries are counted in 32 bits, in strides and rounded up: the last 4096 numbers are room for that."""
+    size = lambda m: lib.tlf_cache_evict_scratch_bytes(C.byref(tlf.TlfEvictArgs(  # noqa: E731
+        n=2, n_kv_heads=2, head_dim=64, n_layers=1, page_size=64, dtype=1, max_pages=m, budget=9, n_pages=9, pool=P, page_table=P, lens=P,
+        next_pos=P, pos_in=P, pos_out=P, weight_in=P, weight_out=P, lens_out=P)))
+    assert size(max_pages) == 0 and size((1 << 25) - 65) > 0
+    c = tlf.TlfChunk(n=2, n_tokens=5, n_heads=4, n_kv_heads=2, head_dim=64, n_layers=2, page_size=64, dtype=1, max_pages=max_pages,
+                     n_pages=20, pool=P, page_table=P, cu_tokens=P, lens=P)
+    a = tlf.TlfAttnChunkArgs(q=P, out=P)
+    assert lib.tlf_attn_chunk(C.byref(c), C.byref(a), P, 1 << 40, None) == tlf.CODES["INVALID_ARG"]
+    assert "max_pages" in lib.tlf_last_error(None).decode()
