@@ -452,7 +452,7 @@ typedef struct tlf_attn_chunk_args {
   float* lse;           /* optional [n_tokens][Hq] */
   const float* weight_in; /* optional [n_pages][64] */
   float* weight_out;    /* optional [n_pages][64] */
-  float scale;          /* > 0, or 0 = 1 / sqrt(head_dim) */
+  float scale;          /* 0..2e38; 0 = 1 / sqrt(head_dim) */
   int32_t reserved0;    /* must be 0 */
 } tlf_attn_chunk_args;
 /* Scratch bytes of the call on the current device; 0 for arguments that the call refuses. */

@@ -88,7 +88,7 @@ static const char* attn_validate(const tlf_chunk* c, const tlf_attn_chunk_args* 
   if ((a->q_stride && a->q_stride < row) || (a->out_stride && a->out_stride < row))
     return "a stride is smaller than a token's heads";
   if (a->weight_in && !a->weight_out) return "weight_in without weight_out";
-  if (!(a->scale >= 0.f) || !std::isfinite(a->scale)) return "scale must be finite and not negative";
+  if (!(a->scale >= 0.f) || a->scale > 2e38f) return "scale must be in 0..2e38";  // (finite times log2 e too)
   if (a->reserved0) return "reserved0 must be 0";
   return nullptr;
 }

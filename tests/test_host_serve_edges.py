@@ -55,3 +55,12 @@ def test_page_tables_that_leave_no_room_below_32_bits_are_refused(lib, max_pages
     a = tlf.TlfAttnChunkArgs(q=P, out=P)
     assert lib.tlf_attn_chunk(C.byref(c), C.byref(a), P, 1 << 40, None) == tlf.CODES["INVALID_ARG"]
     assert "max_pages" in lib.tlf_last_error(None).decode()
+
+
+@pytest.mark.parametrize("scale", [2.5e38, 3.4028234663852886e38, float("inf"), float("-inf"), -1e-45, float("nan")])
+def test_a_scale_that_is_not_finite_in_base_2_is_refused(lib, scale):
+    c = tlf.TlfChunk(n=2, n_tokens=5, n_heads=4, n_kv_heads=2, head_dim=64, n_layers=2, page_size=64, dtype=1, max_pages=9, n_pages=20,
+                     pool=P, page_table=P, cu_tokens=P, lens=P)
+    a = tlf.TlfAttnChunkArgs(q=P, out=P, scale=scale)
+    assert lib.tlf_attn_chunk(C.byref(c), C.byref(a), None, 0, None) == tlf.CODES["INVALID_ARG"]
+    assert "scale" in lib.tlf_last_error(None).decode()
