@@ -1925,17 +1925,17 @@ static ChunkPath chunk_path(const ChunkDev& c, int dtype, const tlf_attn_chunk_a
     // the longest row. With few entries the sums over the queries of a block of 256 entries are a chain that nothing hides: there
     // k_weigh_tc from 9 rows on (4 rows of 16 tokens over up to 1000 entries, 16 heads x 64: 40 us from the scores, 23 so; one of
     // 8 over 8000, 16 / 8 heads x 128: 33 / 27). S^T on the CUDA cores where the tiles do not fit.
-    const long long score_bytes = (long long)c.T * c.Hq * c.max_pages * 256;
-    const bool fit = score_bytes <= (256LL << 20), few = (long long)c.n * ((c.max_pages + 3) / 4) < num_sms;
+    // (the largest arguments pass 2^63 here and below)
+    const bool fit = (double)c.T * c.Hq * c.max_pages * 256 <= (256 << 20), few = (long long)c.n * ((c.max_pages + 3) / 4) < num_sms;
     p.weigh_tc = a.weight_out && tc && weigh_fits && (rows > 16 || !fit || (few && rows > 8));
-    p.scores = a.weight_out && !p.weigh_tc && fit ? score_bytes : 0;
+    p.scores = a.weight_out && !p.weigh_tc && fit ? (long long)c.T * c.Hq * c.max_pages * 256 : 0;
     p.rt = p.pair ? PAIR_ROWS : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
     p.ctas = (c.hd == 128 || p.pair ? 1 : 2) * num_sms;
     p.pad = p.pair ? PAD_PAIR : c.hd == 128 ? PAD_MMA128 : PAD_MMA;
   }
   // no more CTAs than there can be blocks
   const int qt_log = pow2_log(std::max(1, p.rt / c.G));
-  p.ctas = (int)std::min<long long>(p.ctas, std::max<long long>(1, ((long long)(c.T >> qt_log) + c.n) * c.Hkv * (c.max_pages + p.pad)));
+  p.ctas = (int)std::min<double>(p.ctas, std::max(1.0, ((double)(c.T >> qt_log) + c.n) * c.Hkv * ((double)c.max_pages + p.pad)));
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o = (o + bytes + 255) / 256 * 256; return at; };
   take((size_t)2 * p.ctas * p.rt * c.hd * 4);

@@ -147,3 +147,18 @@ def test_eviction_with_a_budget_that_nothing_reaches(T):
     T.tlf_cache_evict(a, torch.empty(n, dtype=torch.uint8, device="cuda"), n)
     assert d["lens"].tolist() == [200, 64, 0] and np.array_equal(d["w"].cpu().numpy(), w) and np.array_equal(d["pos"].cpu().numpy(), pos)
     assert np.array_equal(d["pool"].float().cpu().numpy(), c.pool)
+
+
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("hq,hkv", [(16, 16), (1024, 1024), (64, 2)])
+def test_the_largest_arguments_have_a_workspace(T, weights, hq, hkv):
+    """Tokens x heads x pages pass 64 bits: the size is that of the kernels' parts and of lse. (Nothing is launched.)"""
+    import ctypes as C
+    P = 1 << 20
+    c = T.TlfChunk(n=2, n_tokens=1 << 26, max_chunk=0, n_heads=hq, n_kv_heads=hkv, head_dim=32, n_layers=1, page_size=64, dtype=1,
+                   max_pages=(1 << 25) - 65, n_pages=9, pool=P, page_table=P, cu_tokens=P, lens=P)
+    n = T.load_library().tlf_attn_chunk_scratch_bytes(C.byref(c), C.byref(T.TlfAttnChunkArgs(q=P, out=P, weight_out=P if weights else None)))
+    lse = (1 << 26) * hq * 4 if weights else 0
+    sms = __import__("torch").cuda.get_device_properties(0).multi_processor_count
+    part = 2 * 2 * sms * 64 * (32 * 4 + 8)  # two parts a CTA, of 64 rows
+    assert lse + part <= n <= lse + 2 * part
