@@ -449,9 +449,8 @@ __global__ void __launch_bounds__(256) k_chunk_simt(ChunkAttn a) {
 // fragment is the A fragment of the second product). The running maximum is refreshed lazily: O is rescaled only when a row's
 // maximum grows by more than 8 in base 2. At an item's end the warps' parts meet in shared memory.
 //
-// V of keys that no row of the tile sees is zeroed in the fragments (0 times an infinity is not 0). Keys that only some rows
-// see can still spoil the others' O with a 0 x infinity: a row whose O is not finite is then done again by chunk_redo, over
-// the keys that it sees alone.
+// 0 times an infinity is not 0: V of keys that no row of the tile sees is zeroed in the fragments, and so are elements that are
+// not finite of keys that only some rows see. Those rows get them from chunk_left_out at the item's end.
 //
 // Bound by HBM: 16 single tokens over 32k entries, 16 / 8 heads x 128: 311 us with the join, 6.8 TB/s (0.99 of the copy rate);
 // 32 over up to 8192 entries, 16 heads x 64: 105 us, 5.7 TB/s, the rest of it ramp, items' ends and the join.
@@ -469,7 +468,7 @@ struct MmaShape {
   static constexpr int NST = HD == 128 ? 5 : HD == 64 ? 5 : 8;
   static constexpr int OS = HD + 8;                      // floats of a merge buffer's row
   static constexpr int OFF_O = NST * STAGE, OFF_ML = OFF_O + 4 * 16 * OS * 4, OFF_BAR = OFF_ML + KS * RT * 8,
-                       OFF_INT = OFF_BAR + 2 * NST * 8, OFF_SEG = OFF_INT + (NST + 2 + 64 + 1) / 2 * 8,
+                       OFF_INT = OFF_BAR + 2 * NST * 8, OFF_SEG = OFF_INT + (NST + 2 + 1) / 2 * 8,
                        OFF_BASE = OFF_SEG + MmaSeg::RING * (int)sizeof(MmaSeg);
   static int bytes(int n) { return OFF_BASE + (n + 1) * 8 + 1024; }
   static constexpr int THREADS = 288;
@@ -504,36 +503,31 @@ __device__ __forceinline__ bool bar_any(int id, int threads, bool p) {
   return r != 0;
 }
 
-__device__ __forceinline__ bool finite4(float4 v) {
-  return fabsf(v.x) < INFINITY && fabsf(v.y) < INFINITY && fabsf(v.z) < INFINITY && fabsf(v.w) < INFINITY;
-}
+// 0xffff for each half that is an infinity or NaN of bfloat16.
+__device__ __forceinline__ uint32_t bf16x2_not_finite(uint32_t v) { return __vcmpeq2(v & 0x7f807f80u, 0x7f807f80u); }
 
-// Query row (token, head) over entries e0 .. e1 - 1 of row b alone, by one warp: m (times log2 e), l and O.
+// Entries e .. e1 - 1 of row b, new tokens that some queries of a tile see and others do not: adds to x the elements of V that are
+// not finite, which the tile's products left out. A query that sees the entries has p > 0 for each of them, so that its sums plus
+// x are what the formula gives: infinities and NaN. By one warp; a lane has dims lane * HD / 32 .. Later queries see what earlier
+// ones do: a warp goes over its rows in order and goes on with x.
 template <int HD>
-__device__ __noinline__ void chunk_redo(const ChunkAttn& a, int b, int h, long long token, int head, int e0, int e1, float& m,
-                                        float& l, float (&o)[(HD + 31) / 32]) {
-  constexpr int D = HD / 32;
-  const int lane = threadIdx.x & 31;
-  const bf16* q = static_cast<const bf16*>(a.q) + token * a.qs + (long long)head * HD;
-  float qv[D];
+__device__ __noinline__ void chunk_left_out(const ChunkAttn& a, int b, int h, int& e, int e1, float (&x)[HD / 32]) {
+  constexpr int D = HD / 32, U = 8;  // in flight
+  const bf16* pv = static_cast<const bf16*>(a.c.pool) + ((long long)(a.c.layer * 2 + 1) * a.c.Hkv + h) * 64 * HD + (threadIdx.x & 31) * D;
+  for (; e < e1; e = min(e + U, e1)) {
+    float f[U][D];
 #pragma unroll
-  for (int d = 0; d < D; ++d) qv[d] = to_f32(q[lane + 32 * d]), o[d] = 0.f;
-  m = -INFINITY;
-  l = 0.f;
-  for (int e = e0; e < e1; ++e) {
-    const int page = a.c.page_table[(size_t)b * a.c.max_pages + e / 64];
-    if (page < 0 || page >= a.c.n_pages) continue;
-    const bf16* k = static_cast<const bf16*>(a.c.pool) + page * a.c.page_elems + ((long long)a.c.layer * 2 * a.c.Hkv + h) * 64 * HD + (e % 64) * HD;
-    const bf16* v = k + (long long)a.c.Hkv * 64 * HD;
-    float s = 0.f;
+    for (int u = 0; u < U; ++u) {
+      const int page = e + u < e1 ? a.c.page_table[(size_t)b * a.c.max_pages + (e + u) / 64] : -1;
+      const bool there = page >= 0 && page < a.c.n_pages;
 #pragma unroll
-    for (int d = 0; d < D; ++d) s += qv[d] * to_f32(k[lane + 32 * d]);
-    s = warp_sum(s) * a.scale;
-    const float mn = fmaxf(m, s), ref = mn == -INFINITY ? 0.f : mn, cr = exp2f(m - ref), p = exp2f(s - ref);
-    m = mn;
-    l = l * cr + p;
+      for (int d = 0; d < D; ++d) f[u][d] = there ? to_f32(pv[page * a.c.page_elems + ((e + u) % 64) * HD + d]) : 0.f;
+    }
 #pragma unroll
-    for (int d = 0; d < D; ++d) o[d] = o[d] * cr + p * to_f32(v[lane + 32 * d]);
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int d = 0; d < D; ++d)
+        if (!(fabsf(f[u][d]) < INFINITY)) x[d] += f[u][d];
   }
 }
 
@@ -550,8 +544,7 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
   uint64_t* bars = reinterpret_cast<uint64_t*>(sm + Sh::OFF_BAR);
   volatile int* s_skip = reinterpret_cast<volatile int*>(sm + Sh::OFF_INT);  // [NST] the stage holds nothing to see
   volatile int* abort_flag = s_skip + NST;
-  volatile int* s_any = s_skip + NST + 1;
-  volatile int* s_bad = s_skip + NST + 2;  // [RT]
+  volatile int* s_any = s_skip + NST + 1;  // something was left out of the item's products
   MmaSeg* s_seg = reinterpret_cast<MmaSeg*>(sm + Sh::OFF_SEG);
   long long* s_base = reinterpret_cast<long long*>(sm + Sh::OFF_BASE);
   auto full = [&](int st) { return smem_u32(&bars[st]); };
@@ -568,7 +561,6 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
     fence_barrier_init();
     prefetch_tensormap(&pool_map);
   }
-  if (tid < Sh::RT) s_bad[tid] = 0;
   pdl_wait();
   chunk_plan(c, a.sp, s_base, s_red);
   pdl_trigger();
@@ -752,27 +744,39 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
             l[x] += p0 + p1;
             p[i / 2][(i & 1) * 2 + x] = pack_bf16(p0, p1);
           }
-        const bool cut = key0 + KW - 1 > see_last;
+        auto products = [&](auto masked) {
 #pragma unroll
-        for (int g = 0; g < KW / 16; ++g) {
-          uint32_t keep[2] = {0xffffffffu, 0xffffffffu};
-          if (cut) {
+          for (int g = 0; g < KW / 16; ++g) {
+            uint32_t keep[2], look[2];  // keys that some row sees; and some do not
+            if constexpr (masked) {
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              const int key = key0 + g * 16 + x * 8 + (lane & 3) * 2;
-              keep[x] = (key <= see_last ? 0xffffu : 0u) | (key + 1 <= see_last ? 0xffff0000u : 0u);
+              for (int x = 0; x < 2; ++x) {
+                const int key = key0 + g * 16 + x * 8 + (lane & 3) * 2;
+                keep[x] = (key <= see_last ? 0xffffu : 0u) | (key + 1 <= see_last ? 0xffff0000u : 0u);
+                look[x] = keep[x] & ((key > see0 ? 0xffffu : 0u) | (key + 1 > see0 ? 0xffff0000u : 0u));
+              }
+            }
+#pragma unroll
+            for (int d = 0; d < HD / 16; ++d) {
+              uint32_t b[4];
+              const int key = vk + g * 16, ch = 2 * d + vc;
+              ldsm4_t(sv + (ch / CH) * Sh::ATOM + key * Sh::ROW + (((ch % CH) ^ swz(key)) << 4), b);
+              if constexpr (masked) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                  b[x] &= keep[x & 1];
+                  const uint32_t out = bf16x2_not_finite(b[x]) & look[x & 1];
+                  b[x] &= ~out;
+                  if (out) *s_any = 1;
+                }
+              }
+              mma_16816(o[2 * d], p[g], b[0], b[1]);
+              mma_16816(o[2 * d + 1], p[g], b[2], b[3]);
             }
           }
-#pragma unroll
-          for (int d = 0; d < HD / 16; ++d) {
-            uint32_t b[4];
-            const int key = vk + g * 16, ch = 2 * d + vc;
-            ldsm4_t(sv + (ch / CH) * Sh::ATOM + key * Sh::ROW + (((ch % CH) ^ swz(key)) << 4), b);
-            if (cut) b[0] &= keep[0], b[1] &= keep[1], b[2] &= keep[0], b[3] &= keep[1];
-            mma_16816(o[2 * d], p[g], b[0], b[1]);
-            mma_16816(o[2 * d + 1], p[g], b[2], b[3]);
-          }
-        }
+        };
+        if (tail) products(std::true_type{});
+        else products(std::false_type{});
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(empty(st));
@@ -835,10 +839,6 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
         const float4 u = *reinterpret_cast<const float4*>(s_o + ((g * MT + r / 16) * 16 + r % 16) * OS + d);
         v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
       }
-      if (nq > 1 && !finite4(v)) {
-        s_bad[r] = 1;
-        *s_any = 1;
-      }
       const float2 ml = row_ml(r);
       if (whole) {
         const long long token = token0 + r / G;
@@ -859,27 +859,22 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
         if (d == 0) a.part_ml[part + r] = ml;
       }
     }
-    if (nq > 1) bar_named(1, 256);
-    if (nq > 1 && *s_any) {
+    if (nq > 1 && *s_any) {  // (written before the barriers above)
+      bar_named(1, 256);     // the rows are written
+      float x[HD / 32] = {};
+      int e = max(kb0 * 64, see0 + 1);
       for (int r = warp; r < rows; r += 8) {
-        if (!s_bad[r]) continue;
-        const long long token = token0 + r / G;
-        const int head = it.h * G + r % G;
-        float mm, ll, oo[HD / 32];
-        chunk_redo<HD>(a, it.b, it.h, token, head, kb0 * 64, min(kb1 * 64, see0 + r / G + 1), mm, ll, oo);
-        const float inv = !whole ? 1.f : ll != 0.f ? 1.f / ll : 0.f;
+        chunk_left_out<HD>(a, it.b, it.h, e, min(kb1 * 64, see0 + r / G + 1), x);
+        bf16* out = static_cast<bf16*>(a.out) + (token0 + r / G) * a.os + (long long)(it.h * G + r % G) * HD + lane * (HD / 32);
+        float* po = a.part_o + (part + r) * HD + lane * (HD / 32);
 #pragma unroll
         for (int d = 0; d < HD / 32; ++d) {
-          if (whole) static_cast<bf16*>(a.out)[token * a.os + (long long)head * HD + lane + 32 * d] = from_f32<bf16>(oo[d] * inv);
-          else a.part_o[(part + r) * HD + lane + 32 * d] = oo[d];
-        }
-        if (lane == 0) {
-          if (!whole) a.part_ml[part + r] = make_float2(mm, ll);
-          else if (a.lse) a.lse[token * c.Hq + head] = ll != 0.f ? (mm + log2f(ll)) * LN2 : -INFINITY;
+          if (x[d] == 0.f) continue;
+          if (whole) out[d] = from_f32<bf16>(to_f32(out[d]) + x[d]);
+          else po[d] += x[d];
         }
       }
       bar_named(1, 256);
-      if (tid < Sh::RT) s_bad[tid] = 0;
       if (tid == 0) *s_any = 0;
       bar_named(1, 256);
     }
@@ -896,8 +891,11 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
 //                   and sum in float32, P in bf16 back to tensor memory, where it is the A operand of P V; at the end O out;
 //   warp 8          producer: q of both tiles, then K and V of every block, through tensor maps;
 //   warps 9, 10     issue S = Q K^T and O += P V (V taken as an MN-major operand) of tile 0 and 1: at a block of 64 keys one
-//                   thread for both was slower than the tensor cores (2.0k to 2.5k cycles a block).
-// In an item's last block the softmax warps of the last queries zero V behind them (P = 0 does not cancel an infinity).
+//                   thread for both was slower than the tensor cores (2.0k to 2.5k cycles a block);
+//   warp 11         makes V fit for the products, as below.
+// P = 0 does not cancel an infinity: in blocks with keys that some of the item's queries do not see, warp 11 zeroes V of keys
+// behind the last query and elements that are not finite of the new tokens' V before the products read them. The rows that see
+// such a token get its infinities and NaN from chunk_left_out at the item's end.
 // Tensor memory: O of both tiles (head_dim columns each) and two S buffers of 64 columns a tile; P overwrites its S. One
 // thread's MMAs run in order, so S of block i + 2 is issued right behind the P V of block i that reads the buffer, and the
 // softmax of block i + 1 finds its S ready when it is done with block i. With blocks of 128 keys there is room for one S a tile
@@ -910,7 +908,7 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
 // took 10 us off 362: the issue slots count, half of which are taken. Exponentials by polynomials beside the unit's made it
 // slower. With the join: 344 us for the case above (1410 TFLOP/s, 0.73 of the measured bf16 rate; 386 in a long loop, where the
 // clock falls), 325 us with 16 heads x 64 (750), 195 us for 8192 causal tokens (1400).
-constexpr int PAIR_THREADS = 352;
+constexpr int PAIR_THREADS = 384;
 
 struct PairSeg {  // a CTA's part of an item: blocks kb0 .. kb1 - 1 of nb, of which tile x has the first e[x]; nb = 0: no more
   int b, h, token0, see0, nq[2], e[2], kb0, kb1, nb, none;
@@ -925,7 +923,7 @@ struct PairShape {
   static constexpr int OFF_K = 2 * Q_BYTES, OFF_V = OFF_K + NST * T_BYTES, OFF_BAR = OFF_V + NST * T_BYTES;
   static constexpr int NBAR = 5 * NST + 2 + 4 + 4 + 4 + 1 + 2 * PairSeg::RING;
   static constexpr int FLAGS = 16;  // more than the blocks that the producer can be ahead of the softmax
-  static constexpr int OFF_INT = OFF_BAR + NBAR * 8, OFF_SEG = OFF_INT + (FLAGS + 4) * 4;
+  static constexpr int OFF_INT = OFF_BAR + NBAR * 8, OFF_SEG = OFF_INT + (FLAGS + 4 + PairSeg::RING) * 4;
   static constexpr int OFF_BASE = OFF_SEG + PairSeg::RING * (int)sizeof(PairSeg);
   static int bytes(int n) { return std::max(OFF_BASE + (n + 1) * 8 + 1024, tmem_min_smem(512)); }
   static constexpr uint32_t OCOL = 256;
@@ -971,6 +969,8 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
   volatile int* s_flag = reinterpret_cast<volatile int*>(sm + Sh::OFF_INT);  // the block's page is not there
   volatile int* abort_flag = s_flag + Sh::FLAGS;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + Sh::OFF_INT) + Sh::FLAGS + 1;
+  // [RING] the last item (its number in this CTA) that had something left out of its products
+  volatile unsigned* s_left = reinterpret_cast<volatile unsigned*>(sm + Sh::OFF_INT) + Sh::FLAGS + 4;
   PairSeg* s_seg = reinterpret_cast<PairSeg*>(sm + Sh::OFF_SEG);
   long long* s_base = reinterpret_cast<long long*>(sm + Sh::OFF_BASE);
   auto bar = [&](int i) { return smem_u32(&bars[i]); };
@@ -986,8 +986,8 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
   auto p_full = [&](int x, unsigned n) { return bar(4 * NST + 6 + 2 * x + (n & 1)); };
   auto o_done = [&](int x, unsigned n) { return bar(4 * NST + 10 + 2 * x + (n & 1)); };
   const uint32_t q_free = bar(4 * NST + 14);
-  // V of block b fit for the products. One barrier a stage, and its writers wait for V first: the stage's next phase then lies
-  // behind both issuers' release of this use, so neither can find two phases gone by, which a parity does not tell from none
+  // V of block b fit for the products, where that needs a look. One barrier a stage: its next phase lies behind both issuers'
+  // release of this use, so neither can find two phases gone by, which a parity does not tell from none
   auto v_tail = [&](unsigned b) { return bar(4 * NST + 15 + b % NST); };
   auto seg_full = [&](unsigned i) { return bar(5 * NST + 15 + i % PairSeg::RING); };
   auto seg_empty = [&](unsigned i) { return bar(5 * NST + 15 + PairSeg::RING + i % PairSeg::RING); };
@@ -998,8 +998,8 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       mbar_init(k_full(i), 1);
       mbar_init(k_empty(i), 2);
       mbar_init(v_full(i), 1);
-      mbar_init(v_empty(i), 2);
-      mbar_init(v_tail(i), 4);
+      mbar_init(v_empty(i), 3);
+      mbar_init(v_tail(i), 1);
     }
     for (int x = 0; x < 2; ++x) {
       mbar_init(q_full(x), 1);
@@ -1012,7 +1012,8 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
     mbar_init(q_free, 2);
     for (unsigned i = 0; i < PairSeg::RING; ++i) {
       mbar_init(seg_full(i), 1);
-      mbar_init(seg_empty(i), 10);  // the other warps
+      mbar_init(seg_empty(i), 11);  // the other warps
+      s_left[i] = ~0u;
     }
     *abort_flag = 0;
     fence_barrier_init();
@@ -1130,6 +1131,61 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       }
       ++segs;
     }
+  } else if (warp == 11) {
+    // ---------------- V of keys that not every query sees ----------------
+    // (every block is waited for and released, so that no phase goes by unseen)
+    auto wait_w = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, wait(b, parity)); };
+    unsigned b = 0;
+    for (bool ok = true; ok && wait_w(seg_full(segs), segs / PairSeg::RING); ++segs) {
+      s = s_seg[segs % PairSeg::RING];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(seg_empty(segs));
+      if (s.nb == 0) break;
+      const int behind = s.see0 + s.nq[0] + s.nq[1];  // no query sees entries from here on
+      for (int kb = s.kb0; kb < s.kb1; ++kb, ++b) {
+        if (!wait_w(v_full(b), b / NST)) { ok = false; break; }
+        if (kb * 64 + 63 > s.see0) {
+          bool wrote = false;
+          uint4* v = reinterpret_cast<uint4*>(sm + Sh::OFF_V + (b % NST) * Sh::T_BYTES) + lane;
+          for (int r0 = max(0, s.see0 + 1 - kb * 64) & ~15; r0 < 64; r0 += 16) {  // 16 keys; four of them take the warp's lanes
+            uint4 u[4][Sh::ATOMS];
+            uint32_t any = 0;  // the sign bits: exponents that are all ones
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int k = 0; k < Sh::ATOMS; ++k) u[i][k] = v[(r0 + 4 * i) * 8 + k * (Sh::COL / 16)];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int k = 0; k < Sh::ATOMS; ++k)
+                any |= ((u[i][k].x & 0x7f807f80u) + 0x00800080u) | ((u[i][k].y & 0x7f807f80u) + 0x00800080u) |
+                       ((u[i][k].z & 0x7f807f80u) + 0x00800080u) | ((u[i][k].w & 0x7f807f80u) + 0x00800080u);
+            if (!(any & 0x80008000u) && kb * 64 + r0 + 15 < behind) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int key = kb * 64 + r0 + 4 * i + (lane >> 3);
+#pragma unroll
+              for (int k = 0; k < Sh::ATOMS; ++k) {  // (a row keeps its place in the swizzle)
+                const uint4 w = u[i][k], out = make_uint4(bf16x2_not_finite(w.x), bf16x2_not_finite(w.y), bf16x2_not_finite(w.z), bf16x2_not_finite(w.w));
+                uint4& at = v[(r0 + 4 * i) * 8 + k * (Sh::COL / 16)];
+                if (key >= behind) {
+                  at = make_uint4(0, 0, 0, 0);
+                  wrote = true;
+                } else if (key > s.see0 && (out.x | out.y | out.z | out.w)) {
+                  at = make_uint4(w.x & ~out.x, w.y & ~out.y, w.z & ~out.z, w.w & ~out.w);
+                  s_left[segs % PairSeg::RING] = segs;
+                  wrote = true;
+                }
+              }
+            }
+          }
+          if (wrote) fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(v_tail(b));
+        }
+        if (lane == 0) mbar_arrive(v_empty(b));
+      }
+    }
   } else if (warp >= 9) {
     // ---------------- MMA issuers, one a tile ----------------
     if (elect_one()) {
@@ -1170,7 +1226,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         if (ok && E <= 2) tc_commit(q_free);
         for (int i = 0; i < E && ok; ++i) {
           const unsigned b = blk + i;
-          const bool more = i + 2 < E, tail = s.kb0 + i + 1 == s.nb;
+          const bool more = i + 2 < E, tail = (s.kb0 + i) * 64 + 63 > s.see0;
           // (what this tile does not use it waits for and releases all the same, in step with the other)
           ok = wait(v_full(b), b / NST) && (!tail || wait(v_tail(b), tails >> b % NST)) &&
                (!more || wait(k_full(b + 2), (b + 2) / NST)) && (i >= e || wait(p_full(x, n), n >> 1));
@@ -1209,8 +1265,6 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
     auto next = [&] {
       if (!wait_w(seg_full(segs), segs / PairSeg::RING)) return false;
       s = s_seg[segs % PairSeg::RING];
-      __syncwarp();
-      if (lane == 0) mbar_arrive(seg_empty(segs));
       ++segs;
       return s.nb > 0;
     };
@@ -1222,25 +1276,11 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       for (int i = 0; i < s.e[x]; ++i, ++n) {
         if (!wait_w(s_full(x, n), n >> 1)) { ok = false; break; }
         tc_fence_after();
+        const int key0 = (s.kb0 + i) * 64;
         const uint32_t t_sn = t_s + 64u * (n & 1);
         uint32_t su[64];
         tmem_ld_32_issue(t_sn, su);
         tmem_ld_32_issue(t_sn + 32, su + 32);
-        if (s.kb0 + i + 1 == s.nb && x == (s.nq[1] > 0)) {
-          // V's barrier is in this use's phase: the stage's use before was read by a P V before this S, and this one's use
-          // ends with a P V that waits for v_tail
-          const unsigned b = blk + i;
-          if (wait_w(v_full(b), b / NST) && row < 64 && s.see0 + s.nq[0] + s.nq[1] <= (s.nb - 1) * 64 + row) {
-            uint8_t* v = sm + Sh::OFF_V + (b % NST) * Sh::T_BYTES + row * 128;  // (a row keeps its place in the swizzle)
-#pragma unroll
-            for (int k = 0; k < 8 * Sh::ATOMS; ++k)
-              *reinterpret_cast<uint4*>(v + (k / 8) * Sh::COL + (k % 8) * 16) = make_uint4(0, 0, 0, 0);
-            fence_proxy_async_smem();
-          }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(v_tail(b));
-        }
-        const int key0 = (s.kb0 + i) * 64;
         const bool gone = s_flag[(blk + i) % Sh::FLAGS] != 0;
         tmem_ld_wait();
         if (key0 + 63 > see0 || gone || !__all_sync(0xffffffffu, row_ok)) {
@@ -1304,7 +1344,6 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       const int slot = 2 * blockIdx.x + (s.kb0 == 0), prow = x * 128 + row;  // of the part
       bf16* orow = static_cast<bf16*>(a.out) + token * a.os + (long long)head * HD;
       const bool wide = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && a.os % 8 == 0;
-      bool bad = false;
       if (ok && s.e[x] > 0) {
         if (!wait_w(o_done(x, n - 1), (n - 1) >> 1)) break;
         tc_fence_after();
@@ -1313,8 +1352,6 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         for (int c0 = 0; c0 < HD; c0 += 32) {
           float o[32];
           tmem_ld_32(t_o + (uint32_t)c0, o);
-#pragma unroll
-          for (int k = 0; k < 32; ++k) bad |= !(fabsf(o[k]) < INFINITY);
           if (!row_ok) continue;
           if (!whole) {
 #pragma unroll
@@ -1339,29 +1376,28 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         if (!whole) a.part_ml[(size_t)slot * PAIR_ROWS + prow] = make_float2(m_run == -INFINITY ? -INFINITY : m_run * scale, l_run);
         else if (a.lse) a.lse[token * c.Hq + head] = l_run != 0.f ? (m_run * scale + log2f(l_run)) * LN2 : -INFINITY;
       }
-      // rows that a 0 x infinity of a key which only others see has spoilt: again, over what they see
-      unsigned again = __ballot_sync(0xffffffffu, bad && row_ok && s.nq[0] + s.nq[1] > 1);
-      while (again) {
-        const int src = __ffs(again) - 1;
-        again &= again - 1;
-        const long long tk = __shfl_sync(0xffffffffu, token, src);
-        const int hh = __shfl_sync(0xffffffffu, head, src), see_r = __shfl_sync(0xffffffffu, see, src);
-        const int pr = __shfl_sync(0xffffffffu, prow, src);
-        float mm, ll, oo[HD / 32];
-        chunk_redo<HD>(a, s.b, s.h, tk, hh, s.kb0 * 64, min(s.kb1 * 64, see_r + 1), mm, ll, oo);
-        const float inv = ll != 0.f ? 1.f / ll : 0.f;
+      if (ok && s_left[(segs - 1) % PairSeg::RING] == segs - 1) {  // (written before the last P V that it concerns)
+        __syncwarp();  // the rows are written
+        float left[HD / 32] = {};
+        int e = max(s.kb0 * 64, s.see0 + 1);
+        for (int i = 0; i < 32; ++i) {
+          const int see_r = __shfl_sync(0xffffffffu, see, i), head_r = __shfl_sync(0xffffffffu, head, i), prow_r = __shfl_sync(0xffffffffu, prow, i);
+          const long long token_r = __shfl_sync(0xffffffffu, token, i);
+          if (see_r < 0) continue;
+          chunk_left_out<HD>(a, s.b, s.h, e, min(s.kb1 * 64, see_r + 1), left);
+          bf16* out = static_cast<bf16*>(a.out) + token_r * a.os + (long long)head_r * HD + lane * (HD / 32);
 #pragma unroll
-        for (int k = 0; k < HD / 32; ++k) {
-          if (whole) static_cast<bf16*>(a.out)[tk * a.os + (long long)hh * HD + lane + 32 * k] = from_f32<bf16>(oo[k] * inv);
-          else a.part_o[pair_part(slot, pr, lane + 32 * k, HD)] = oo[k];
-        }
-        if (lane == 0) {
-          if (!whole) a.part_ml[(size_t)slot * PAIR_ROWS + pr] = make_float2(mm, ll);
-          else if (a.lse) a.lse[tk * c.Hq + hh] = ll != 0.f ? (mm + log2f(ll)) * LN2 : -INFINITY;
+          for (int k = 0; k < HD / 32; ++k) {
+            if (left[k] == 0.f) continue;
+            if (whole) out[k] = from_f32<bf16>(to_f32(out[k]) + left[k]);
+            else a.part_o[pair_part(slot, prow_r, lane * (HD / 32) + k, HD)] += left[k];
+          }
         }
         __syncwarp();
       }
       blk += s.kb1 - s.kb0;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(seg_empty(segs - 1));  // only now: s_left's word was this item's until here
     }
   }
   if (*abort_flag) drain_copies();

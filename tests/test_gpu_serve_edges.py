@@ -98,6 +98,76 @@ def test_a_page_that_is_not_there_is_left_out(T, new, dtype, hd, bad):
         assert (w[c.at(b, lost)] == -7).all()
 
 
+SPOILT = [  # old, new, hq, hkv, hd
+    ([70, 300], [9, 12], 4, 2, 128), ([70, 0], [20, 31], 2, 2, 64), ([10, 500], [60, 64], 2, 2, 32), ([0, 64], [20, 33], 6, 2, 64),
+    ([70, 3000], [33, 130], 4, 2, 128), ([0, 1000], [300, 80], 2, 2, 64), ([4000], [257], 4, 2, 64), ([5, 63], [64, 40], 16, 1, 128)]
+
+
+@pytest.mark.parametrize("old,new,hq,hkv,hd", SPOILT, ids=lambda v: str(v))
+def test_a_new_tokens_infinite_value_reaches_those_that_see_it_and_nobody_else(T, old, new, hq, hkv, hd):
+    """Values of tokens amid the chunks hold infinities and NaN in a few dims: earlier queries do not see them at all, later ones
+    in those dims only; infinities of both signs meet as NaN."""
+    c = R.Cache(old, new, hq, hkv, hd, "bf16", seed=hd + hq)
+    ref = R.attention(c)  # of the finite values
+    want = ref[0].copy()
+    for b in range(c.n):
+        for i, dim, x in ((c.new[b] // 3, 5, np.inf), (c.new[b] // 3, 9, -np.inf), (c.new[b] // 2, 30, np.nan), (c.new[b] - 2, 9, np.inf)):
+            p, o = c.at(b, np.array([c.old[b] + i]))
+            c.pool[p, c.layer, 1, :, o, dim] = x
+            with np.errstate(invalid="ignore"):
+                want[c.cu[b] + i:c.cu[b + 1], :, dim] += x
+    d = c.device()
+    out, lse, _ = _attend(T, c, d)
+    got, fin = out.float().cpu().numpy().astype(np.float64), np.isfinite(want)
+    assert np.array_equal(got[~fin], want[~fin], equal_nan=True)
+    r = RB
+    p_rel = 2 * (c.hd + 4) * U * ref[3] + 2.0 ** -20
+    bound = (p_rel[..., None] + r) * ref[2] + (r + 4 * U) * np.abs(ref[0]) * (1 + r) + 1e-30
+    # (the values that were replaced are part of ref in the dims that are not looked at)
+    assert (np.abs(got[fin] - want[fin]) <= bound[fin]).all()
+    clean = _attend(T, c, d)[1]
+    assert np.abs(clean.cpu().numpy() - ref[1]).max() < 1e-4 and int(d["err"][0].item()) == 0
+
+
+def _time(T, c, d, **kw):
+    """Milliseconds of a call, the best of five."""
+    import torch
+    out = torch.empty(c.T, c.hq, c.hd, dtype=d["q"].dtype, device="cuda")
+    b = T.chunk_args(d["pool"], d["table"], d["cu"], d["lens"], c.hq, c.T, layer=c.layer, err=d["err"], **kw)
+    a = T.attn_chunk_args(d["q"], out)
+    n = T.tlf_attn_chunk_scratch_bytes(b, a)
+    scratch = torch.empty(n, dtype=torch.uint8, device="cuda")
+    best = np.inf
+    for _ in range(6):
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        T.tlf_attn_chunk(b, a, scratch, n, torch.cuda.current_stream())
+        e1.record()
+        torch.cuda.synchronize()
+        best = min(best, e0.elapsed_time(e1))
+    return best
+
+
+@pytest.mark.parametrize("new,hq,hd", [([8, 5], 4, 128), ([20, 17], 4, 64), ([200, 300], 4, 64), ([200, 300], 4, 128)])
+def test_values_that_are_not_finite_cost_little_time(T, new, hq, hd):
+    """An infinite value early in a long cache, a query that is NaN, and a chunk whose values all are: no more than a few times
+    the usual time (and 0.2 ms for what is done once an item)."""
+    c = R.Cache([8000, 6000], new, hq, 2, hd, "bf16", seed=3)
+    usual = _time(T, c, c.device())
+    pool, q = c.pool.copy(), c.q.copy()
+    c.pool[c.table[:, 0], c.layer, 1, :, 5] = np.inf
+    early = _time(T, c, c.device())
+    c.pool[:] = pool
+    c.q[c.cu[1] // 2] = np.nan
+    query = _time(T, c, c.device())
+    c.q[:] = q
+    for b in range(2):
+        p, o = c.at(b, np.arange(c.old[b], c.lens[b]))
+        c.pool[p, c.layer, 1, :, o] = np.nan
+    chunk = _time(T, c, c.device())
+    assert max(early, query, chunk) <= 4 * usual + 0.2, (usual, early, query, chunk)
+
+
 # ---- the ends of the types ----
 
 @pytest.mark.parametrize("scale", [1.6e-38, 1e-38, 1e-41, 1e-45])
