@@ -232,3 +232,73 @@ def test_the_largest_arguments_have_a_workspace(T, weights, hq, hkv):
     sms = __import__("torch").cuda.get_device_properties(0).multi_processor_count
     part = 2 * 2 * sms * 64 * (32 * 4 + 8)  # two parts a CTA, of 64 rows
     assert lse + part <= n <= lse + 2 * part
+
+
+# ---- paths that only large calls take ----
+
+def _evict_rows(T, lens, budget, first, recent, in_place, seed):
+    import torch
+    c = R.Cache(lens, [0] * len(lens), 1, 1, 16, "f32", layers=1, layer=0, seed=seed)
+    rng = np.random.default_rng(seed)
+    w = np.round(rng.exponential(1, (c.pages, 64)), 3).astype(np.float32)  # ties
+    w[rng.random(w.shape) < 0.05] = np.nan
+    pos = np.zeros((c.pages, 64), np.int32)
+    for b, n in enumerate(lens):
+        pos[c.at(b, np.arange(n))] = np.arange(n)
+    d = c.device(w=w, pos=pos, nxt=np.asarray(lens, np.int32))
+    wo = d["w"] if in_place else torch.full((c.pages, 64), -7.0, device="cuda")
+    po = d["pos"] if in_place else torch.full((c.pages, 64), -7, dtype=torch.int32, device="cuda")
+    lo = torch.zeros_like(d["lens"])
+    a = T.evict_args(d["pool"], d["table"], d["lens"], d["nxt"], d["pos"], po, d["w"], wo, lo, budget=budget, n_first=first,
+                     n_recent=recent, err=d["err"])
+    n = T.tlf_cache_evict_scratch_bytes(a)
+    T.tlf_cache_evict(a, torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda"), n)
+    assert int(d["err"][0].item()) == 0 and lo.tolist() == [min(n, budget) for n in lens]
+    pool, wx, px = d["pool"].cpu().numpy(), wo.cpu().numpy(), po.cpu().numpy()
+    for b, n in enumerate(lens):
+        e = np.arange(n)
+        src = R.evict(w[c.at(b, e)], pos[c.at(b, e)], n, budget, first, recent)
+        to, fr = c.at(b, np.arange(len(src))), c.at(b, src)
+        assert np.array_equal(px[to], pos[fr]) and np.array_equal(wx[to], w[fr], equal_nan=True)
+        assert np.array_equal(pool[to[0], 0, :, :, to[1]], c.pool[fr[0], 0, :, :, fr[1]])
+        if not in_place:
+            rest = c.at(b, np.arange(len(src), n))
+            assert (wx[rest] == -7).all() and (px[rest] == -7).all()
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_eviction_of_rows_that_clusters_share(T, in_place):
+    """Several rows, each split over CTAs, of unlike lengths."""
+    _evict_rows(T, [20000, 5, 9999, 8192, 0, 16001], 8192, 4, 100, in_place, 11)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("lens", [[340000], [45000] + [70] * 80], ids=["cluster", "one-cta"])
+def test_eviction_of_rows_that_shared_memory_does_not_hold(T, lens, in_place):
+    """More keys a CTA than it keeps: they are read again in every level."""
+    _evict_rows(T, lens, lens[0] // 3, 4, 64, in_place, 12)
+
+
+@pytest.mark.parametrize("rows,V", [(1, 64000), (1, 128256), (1, 262144), (3, 262144), (9, 128256), (9, 262144), (40, 64000), (40, 128256)])
+def test_sampling_from_large_vocabularies(T, rows, V):
+    """Rows split over two to eight CTAs, all limits among them."""
+    import torch
+    rng = np.random.default_rng(V + rows)
+    l = (rng.standard_normal((rows, V)) * 3).astype(np.float32)
+    l[rng.random((rows, V)) < 0.01] = -np.inf
+    u = rng.random((rows, V), dtype=np.float32)
+    for kw in (dict(), dict(temperature=0.0), dict(temperature=0.7, top_k=50), dict(top_p=0.95), dict(min_p=0.05),
+               dict(temperature=1.3, top_k=5000, top_p=0.9, min_p=0.001), dict(temperature=6.0, top_p=0.8)):
+        tok, lp = _draw(T, torch.tensor(l).cuda(), torch.tensor(u).cuda(), **kw)
+        names = dict(temperature="T")
+        for b in range(rows):
+            par = {names.get(k, k): v for k, v in kw.items()}
+            _, wlp, _ = R.sample(l[b], u[b], **par)
+            # limits that float32 does not tell apart: the winner among a few tokens less, or a few more
+            top_p, min_p = par.pop("top_p", 1.0), par.pop("min_p", 0.0)
+            less = R.sample(l[b], u[b], top_p=top_p - 1e-5 if top_p < 1 else 1.0, min_p=min_p * (1 + 1e-5), **par)
+            more = R.sample(l[b], u[b], top_p=top_p + 1e-5 if top_p < 1 else 1.0, min_p=min_p * (1 - 1e-5), **par)
+            assert tok[b] in (less[0], more[0]), (kw, b, tok[b], less, more)
+            if less[0] == more[0]:
+                z = abs(l[b][tok[b]] - l[b].max()) / (kw.get("temperature") or 1.0)
+                assert abs(lp[b] - wlp) <= 4 * U * z + 2.0 ** -19 + 2 * U * abs(wlp), (kw, b, lp[b], wlp)
