@@ -449,6 +449,8 @@ __global__ void __launch_bounds__(256) k_chunk_simt(ChunkAttn a) {
 // fragment is the A fragment of the second product). The running maximum is refreshed lazily: O is rescaled only when a row's
 // maximum grows by more than 8 in base 2. At an item's end the warps' parts meet in shared memory.
 //
+// P is rounded to bf16, the type of the second product's operands (as in k_chunk_pair; l adds up P before the rounding).
+//
 // 0 times an infinity is not 0: V of keys that no row of the tile sees is zeroed in the fragments, and so are elements that are
 // not finite of keys that only some rows see. Those rows get them from chunk_left_out at the item's end.
 //
@@ -902,12 +904,17 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
 // only: a tile's chain S, softmax, P V was then 4.8k cycles a block, 2.0k of them MMAs (4 x 2048 tokens over up to 10240
 // entries, 16 / 8 heads x 128: 485 us, 343 so at first).
 //
-// What bounds it: the softmax warps' instructions and the tensor cores nearly alike. At head_dim 128 a block of a tile is 8 S
-// products that read 6 KB of shared memory each, 48 cycles, and 4 P V products of 64 cycles: 1280 cycles for both tiles of the
-// about 1600 that a block takes; the exponentials (32 a cycle and SM) are 512 of them. Products and sums of two floats at a time
-// took 10 us off 362: the issue slots count, half of which are taken. Exponentials by polynomials beside the unit's made it
-// slower. With the join: 344 us for the case above (1410 TFLOP/s, 0.73 of the measured bf16 rate; 386 in a long loop, where the
-// clock falls), 325 us with 16 heads x 64 (750), 195 us for 8192 causal tokens (1400).
+// P is rounded to bf16 because the second product takes 16-bit operands of one type: with P in two bf16 terms it would be two
+// products. l adds up P before the rounding. Against 64 bits the output is then off by 2.3e-3 where it is off by 1.7e-3 with P in
+// float32, most of which is the rounding of the output itself.
+//
+// What bounds it: the softmax warps' chain from S to P. A block of 64 keys and two tiles takes 1410 cycles at head_dim 128 and 1340
+// at 64, of which the tensor pipe works 990 and 510; the exponentials (32 a cycle and SM) are 512, and nearly half of the issue
+// slots are taken. Products and sums of two floats at a time took 10 us off 362: the issue slots count. Exponentials by polynomials
+// beside the unit's made it slower. Warp 11 instead of the softmax warps for V (134.5 us there, 132 so and with no look at V at all:
+// 4 x 1000 tokens with weights) has 16 keys in flight (four: 139). With the join: 327 us for the case above in single calls (1455
+// TFLOP/s, 0.76 of the measured bf16 rate; 371 to 386 in a long loop, where the clock falls), 284 us with 16 heads x 64 (838), 195 us
+// for 8192 causal tokens (1405).
 constexpr int PAIR_THREADS = 384;
 
 struct PairSeg {  // a CTA's part of an item: blocks kb0 .. kb1 - 1 of nb, of which tile x has the first e[x]; nb = 0: no more
