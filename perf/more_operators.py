@@ -219,7 +219,8 @@ def _quantised(x):
     g = torch.nan_to_num(x, nan=0.0, posinf=LARGEST, neginf=-LARGEST).clamp(-LARGEST, LARGEST)
     g = g.unflatten(-1, (_groups(x.shape[-1]), -1))
     lo = g.amin(-1, keepdim=True).bfloat16()
-    d = ((g.amax(-1, keepdim=True) - lo.float()).clamp_min(0) / 15).bfloat16()
+    reach = (g.amax(-1, keepdim=True) - lo.float()).clamp_min(0)
+    d = (reach / torch.full_like(reach, 15)).bfloat16()  # (by a tensor: by a number it would be a product with its inverse)
     n = ((g - lo.float()) / torch.where(d > 0, d, 1).float()).round().clamp(0, 15)
     n = torch.where(d > 0, n, 0).to(torch.uint8).flatten(-2)
     return n[..., 0::2] | n[..., 1::2] << 4, torch.cat([d, lo], -1)
