@@ -358,8 +358,8 @@ int tlf_attn_decode_static(const tlf_attn_args* a, void* stream);
  * in flight as long as those that overlap share no scratch and no output. A refused call (INVALID_ARG, CUDA, with the
  * message in tlf_last_error(NULL) on the calling thread) has launched nothing unless the code is CUDA. What only the
  * device can see (a page id, an offset or a position out of range, a bounded wait that ran out) sets a bit of *err and
- * is skipped, never followed: bit 1 = a bounded wait expired, bit 2 = a bad index. *err is OR-ed into; err = NULL drops
- * the report, not the check. */
+ * is skipped, never followed: bit 1 = a bounded wait expired, bit 2 = a bad index, bit 8 = a value that a 4-bit cache cannot
+ * hold, bit 16 = no free page. *err is OR-ed into; err = NULL drops the report, not the check. */
 
 /* A batch of chunks: row b has the new tokens cu_tokens[b] .. cu_tokens[b+1]-1 of the batch (none is allowed) and a
  * cache of lens[b] entries that ends with them: its i-th new token is entry lens[b] - (new tokens of b) + i. Entry e sits
@@ -516,6 +516,125 @@ typedef struct tlf_sample_args {
   float* logprobs;      /* [n] or NULL */
 } tlf_sample_args;
 int tlf_sample(const tlf_sample_args* a, void* stream);
+
+/* ---- caches in 4 bits, windows, and who owns a page ----------------------- */
+
+/* A cache in 4 bits. The values of an entry (one layer, K or V, one head) are held in groups of gs = min(head_dim, 64): a
+ * group is a code n_i in 0..15 for each value and a pair (d, lo) of bfloat16, and stands for lo + d n_i. A page is laid out
+ * [n_layers][2 (K, V)][n_kv_heads] blocks of tlf_kv4_block_bytes(head_dim) bytes: 64 x head_dim / 2 bytes of codes (byte j of
+ * an entry: dim 2j in the low half, dim 2j + 1 in the high one), then 64 x (head_dim / gs) pairs (d first). That is 4.5 bits a
+ * value at head_dim 64 and 128, 5 at 32 and 6 at 16. What a call writes has finite d >= 0 and lo; of entries that no query sees
+ * nothing is asked. */
+enum tlf_kv_format { TLF_KV_PLAIN = 0, TLF_KV_4BIT = 1 };
+/* Bytes of a block, 0 for a head_dim that is not 16, 32, 64 or 128. */
+int64_t tlf_kv4_block_bytes(int32_t head_dim);
+
+/* tlf_rope_append into a cache in 4 bits: c describes the batch as there, with c->pool the 4-bit pages and c->dtype the type
+ * of q, k, v (head_dim 16 with float32 alone). The turned keys and the values are rounded to the dtype, as a plain cache would
+ * hold them (NaN counts as 0, magnitudes past 2^126 as 2^126; either sets err bit 8), and quantised group by group:
+ *   lo = bfloat16(min x), d = bfloat16(max(0, max x - lo) / 15), n_i = d > 0 ? clamp(round((x_i - lo) / d), 0, 15) : 0
+ * with float32 arithmetic, rounding to nearest, ties to even. The same inputs give the same bytes. */
+int tlf_kv4_append(const tlf_chunk* c, const tlf_rope_args* a, void* stream);
+
+/* What the entries of the batch's new tokens stand for, out of a cache in 4 bits: lo + d n rounded to the dtype. (A batch whose
+ * rows have all their entries as new tokens reads whole sequences.) A token without an entry gets zeros. */
+typedef struct tlf_kv4_read_args {
+  void* k;              /* token t's heads [Hkv][head_dim] at k + t * k_stride elements; likewise v; NULL: not wanted */
+  void* v;
+  int64_t k_stride, v_stride; /* in elements; 0 = Hkv * head_dim */
+} tlf_kv4_read_args;
+int tlf_kv4_read(const tlf_chunk* c, const tlf_kv4_read_args* a, void* stream);
+
+/* Attention of a chunk of new tokens over a paged cache, of which a query may see a window and the first entries alone. As
+ * tlf_attn_chunk, but a query at entry E sees the entries e <= E of its row with e > E - window or e < n_first (window 0: all).
+ * Entries are counted, not positions: a cache that tokens left entries out of has a window of so many entries. Pages whose
+ * entries no query of the call sees are not looked up: their places in the page table may hold anything.
+ * The cache is in the dtype, or in 4 bits (kv_format), which is read as the values that it stands for, unrounded in the scores;
+ * float32 softmax statistics and sums as in tlf_attn_chunk. */
+typedef struct tlf_attn_window_args {
+  const void* q;        /* as in tlf_attn_chunk_args */
+  int64_t q_stride;
+  void* out;
+  int64_t out_stride;
+  float* lse;           /* optional [n_tokens][Hq] */
+  float scale;          /* 0..2e38; 0 = 1 / sqrt(head_dim) */
+  int32_t window;       /* >= 0; 0: no window */
+  int32_t n_first;      /* >= 0: first entries that stay visible (nothing beside a window of 0) */
+  int32_t kv_format;    /* tlf_kv_format of c->pool */
+} tlf_attn_window_args;
+/* Scratch bytes of the call on the current device; 0 for arguments that the call refuses. */
+size_t tlf_attn_window_scratch_bytes(const tlf_chunk* c, const tlf_attn_window_args* a);
+int tlf_attn_window(const tlf_chunk* c, const tlf_attn_window_args* a, void* scratch, size_t scratch_bytes, void* stream);
+
+/* Pages and their owners. refs[p] counts the page-table entries that name page p, of the call's rows and of all others that
+ * share the pool; a page with refs 0 is free. A row holds the pages that its table names; -1 (any id out of range, with err
+ * bit 2) names none. Reservations, forks, frees and cuts of rows are one call on the device, which a graph can hold:
+ *
+ * n_out new rows take the place of n_in old ones. New row b goes on from old row parents[b] (any number of rows from the same
+ * one; -1: starts empty). With len the parent's entries, full = len / 64 and need = ceil((len + reserve) / 64), slot s of its
+ * table row gets
+ *   s < full         the parent's page, shared; -1 if the window leaves it: 64 (s + 1) <= len - window + 1 and 64 s >= n_first
+ *                    (window > 0: the next tokens of a row of len entries can no longer see it);
+ *   full <= s < need the parent's page if the row is the parent's first (lowest b) and nobody else holds it (refs 1);
+ *                    otherwise a new page, into which the len % 64 entries behind the full pages are copied (s = full);
+ *   need <= s        -1.
+ * New pages are the free ones, lowest first, in the order of (b, s). Where none is left (or the parent's page with the entries
+ * to copy is not there) the slot gets -1, err bit 16 (or 2) is set, and lens_out[b] is cut to the entries before the slot if the
+ * row had any there. refs_out = refs less the old rows' entries, plus the new rows': what no new row goes on from is freed.
+ * To free rows, leave them out of parents; to grow rows, parents[b] = b; to admit a row, -1.
+ * Copies go into free pages alone: the old rows' entries stay as they are until somebody writes to the pages. table_out may not
+ * overlap page_table; lens_out and refs_out may be the inputs' own buffers. */
+typedef struct tlf_fork_args {
+  int32_t n_in;         /* old rows, 1..65535 */
+  int32_t n_out;        /* new rows, 1..65535 */
+  int32_t n_kv_heads, head_dim, n_layers;
+  int32_t page_size;    /* 64 */
+  int32_t dtype;        /* tlf_dtype (of a plain pool) */
+  int32_t kv_format;    /* tlf_kv_format */
+  int32_t max_pages;    /* entries of a row of either table, 1..2^25 - 65 */
+  int32_t reserve;      /* >= 0: tokens that every new row is to have room for */
+  int32_t window;       /* >= 0; 0: no window */
+  int32_t n_first;      /* >= 0 */
+  int64_t n_pages;
+  void* pool;
+  const int32_t* page_table; /* [n_in][max_pages] */
+  const int32_t* lens;       /* [n_in], 0..max_pages * 64 */
+  const int32_t* parents;    /* [n_out] */
+  const int32_t* refs;       /* [n_pages] */
+  int32_t* table_out;        /* [n_out][max_pages] */
+  int32_t* lens_out;         /* [n_out] */
+  int32_t* refs_out;         /* [n_pages] */
+  int32_t* entry_pos;        /* optional [n_pages][64]: copied along */
+  float* entry_weight;       /* optional [n_pages][64]: copied along */
+  uint32_t* err;        /* optional */
+} tlf_fork_args;
+size_t tlf_cache_fork_scratch_bytes(const tlf_fork_args* a);
+int tlf_cache_fork(const tlf_fork_args* a, void* scratch, size_t scratch_bytes, void* stream);
+
+/* The pages in use to the front of the pool. With L pages of refs > 0, the k-th page in use at or past L moves (all layers, K
+ * and V, positions and weights) to the k-th free page below L; table_out names the pages' new places, refs_out counts them, and
+ * n_live gets L: pages from L on hold nothing any more and may be given back. The tables must be all that name pages of the
+ * pool. table_out and refs_out may be the inputs' own buffers. */
+typedef struct tlf_compact_args {
+  int32_t n;            /* rows, 1..65535 */
+  int32_t n_kv_heads, head_dim, n_layers;
+  int32_t page_size;    /* 64 */
+  int32_t dtype;        /* tlf_dtype (of a plain pool) */
+  int32_t kv_format;    /* tlf_kv_format */
+  int32_t max_pages;    /* 1..2^25 - 65 */
+  int64_t n_pages;
+  void* pool;
+  const int32_t* page_table; /* [n][max_pages] */
+  const int32_t* refs;       /* [n_pages] */
+  int32_t* table_out;        /* [n][max_pages] */
+  int32_t* refs_out;         /* [n_pages] */
+  int32_t* n_live;           /* [1] */
+  int32_t* entry_pos;        /* optional [n_pages][64]: moved along */
+  float* entry_weight;       /* optional [n_pages][64]: moved along */
+  uint32_t* err;        /* optional */
+} tlf_compact_args;
+size_t tlf_cache_compact_scratch_bytes(const tlf_compact_args* a);
+int tlf_cache_compact(const tlf_compact_args* a, void* scratch, size_t scratch_bytes, void* stream);
 
 /* ---- inspection ---------------------------------------------------------- */
 

@@ -1,4 +1,4 @@
-// Attention of chunks of new tokens over paged caches (tlf_attn_chunk).
+// Attention of chunks of new tokens over paged caches (tlf_attn_chunk), under a window (tlf_attn_window), in 4 bits.
 //
 // A work item is a tile of queries of one row with the G query heads of one kv head (MMA or thread row r = query * G + head);
 // its keys are the row's cache up to the tile's last query. The items' key blocks are dealt out evenly (k_chunk.cuh). A CTA
@@ -17,6 +17,7 @@
 #include <type_traits>
 
 #include "k_chunk.cuh"
+#include "k_kv4.cuh"
 #include "k_serve.cuh"
 
 namespace tlf {
@@ -36,12 +37,27 @@ struct ChunkAttn {
   float* part_o;   // [2 ctas][rows][hd]; of k_chunk_pair [2 ctas][hd / 4][rows][4]
   float2* part_ml; // [2 ctas][rows]
   int4* join;      // [ctas] what each CTA leaves to k_chunk_join
+  int window, first;  // tlf_attn_window's; 2^31 - 1 and 0 where there is no window
 };
+
+// What a kernel's keys are: every entry up to the query's, of a cache in the dtype; those of a window; those of a window, of a
+// cache in 4 bits.
+enum ChunkKeys { KEYS_ALL = 0, KEYS_WINDOW = 1, KEYS_4BIT = 2 };
+template <int MODE>
+__device__ __forceinline__ auto split_of(const ChunkAttn& a) {
+  if constexpr (MODE == KEYS_ALL) return a.sp;
+  else return WindowSplit{a.sp, a.window, a.first};
+}
+// Number in its row of an item's block i; the last entry of a row that the window hides from a query at entry `see`.
+template <int MODE>
+__device__ __forceinline__ int block_at(int i, int sinks, int skip) { return MODE == KEYS_ALL || i < sinks ? i : i + skip; }
+__device__ __forceinline__ int hidden_to(int see, int window) { return see < window ? -1 : see - window; }
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // base[b] = blocks of the rows before b; base[n] = all. By the whole block.
-__device__ __forceinline__ void chunk_plan(const ChunkDev& c, const ChunkSplit& sp, long long* base, long long* red) {
+template <class Split>
+__device__ __forceinline__ void chunk_plan(const ChunkDev& c, const Split& sp, long long* base, long long* red) {
   long long carry = 0;
   for (int b0 = 0; b0 < c.n; b0 += blockDim.x) {
     const int b = b0 + threadIdx.x;
@@ -68,8 +84,10 @@ struct ChunkItem {
   int b, h, t, nb;     // row, kv head, tile, its blocks
   int t0, s0, ql, len; // the row's first new token, old entries, new tokens, entries
   long long first;     // the item's first block in the flat order (may lie behind `pos`, which then is in its pad)
+  int skip;            // blocks behind those of the first entries that the window leaves out
 };
-__device__ __forceinline__ ChunkItem chunk_item(const ChunkDev& c, const ChunkSplit& sp, const long long* base, long long pos) {
+template <class Split>
+__device__ __forceinline__ ChunkItem chunk_item(const ChunkDev& c, const Split& sp, const long long* base, long long pos) {
   int lo = 0, hi = c.n;  // largest b with base[b] <= pos (rows without tokens have no blocks)
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -89,6 +107,8 @@ __device__ __forceinline__ ChunkItem chunk_item(const ChunkDev& c, const ChunkSp
   it.t = sp.tile_of(it.s0, it.ql, at);
   it.nb = sp.blocks(it.s0, it.ql, it.t);
   it.first = base[lo] + it.h * per + sp.before(it.s0, it.ql, it.t) + sp.pad;
+  it.skip = 0;
+  if constexpr (std::is_same<Split, WindowSplit>::value) it.skip = sp.skip(it.s0, it.t);
   return it;
 }
 
@@ -277,7 +297,7 @@ struct SimtShape {
 // 16 lanes share a row: lane x has keys x, x + 16, .. of a block in the first product and dims DW x .. in the second, so a
 // row's statistics and probabilities never leave its half warp. Bound by launch and first loads on the models it serves
 // (4 rows of up to 5 tokens over up to 60 entries, 4 heads x 16: 8 us with the join, in a CUDA graph).
-template <typename T, int RT, int HD>
+template <typename T, int RT, int HD, int MODE>
 __global__ void __launch_bounds__(256) k_chunk_simt(ChunkAttn a) {
   using Sh = SimtShape<RT, HD>;
   constexpr int RW = Sh::RW, DW = Sh::DW, KS = Sh::KS, PS = Sh::PS;
@@ -288,7 +308,8 @@ __global__ void __launch_bounds__(256) k_chunk_simt(ChunkAttn a) {
   float *sQ = sm, *sK = sm + Sh::OFF_K, *sV = sm + Sh::OFF_V, *sP = sm + Sh::OFF_P;
   long long* s_base = reinterpret_cast<long long*>(sm + Sh::FLOATS);
   const ChunkDev& c = a.c;
-  chunk_plan(c, a.sp, s_base, s_red);
+  const auto sp = split_of<MODE>(a);
+  chunk_plan(c, sp, s_base, s_red);
   pdl_trigger();
   const long long all = s_base[c.n], per = chunk_share(a, all);
   long long pos = blockIdx.x * per;
@@ -296,7 +317,7 @@ __global__ void __launch_bounds__(256) k_chunk_simt(ChunkAttn a) {
   const int tid = threadIdx.x, x = tid & 15, y = tid >> 4, G = c.G, qt = 1 << a.sp.qt_log;
   if (pos >= end && tid == 0) join_note(a, nullptr, per);
   for (bool first = true; pos < end; first = false) {
-    const ChunkItem it = chunk_item(c, a.sp, s_base, pos);
+    const ChunkItem it = chunk_item(c, sp, s_base, pos);
     if (first && tid == 0) join_note(a, &it, per);
     if (pos < it.first) pos = it.first;
     if (pos >= end) break;
@@ -311,6 +332,8 @@ __global__ void __launch_bounds__(256) k_chunk_simt(ChunkAttn a) {
         v = to_f32(static_cast<const T*>(a.q)[(token0 + r / G) * a.qs + (long long)(it.h * G + r % G) * HD + d]) * a.scale;
       sQ[i] = v;
     }
+    int sinks = 0;
+    if constexpr (MODE != KEYS_ALL) sinks = sp.sinks();
     int see[RW];
     float m[RW], l[RW], o[RW][DW];
 #pragma unroll
@@ -322,17 +345,26 @@ __global__ void __launch_bounds__(256) k_chunk_simt(ChunkAttn a) {
 #pragma unroll
       for (int d = 0; d < DW; ++d) o[i][d] = 0.f;
     }
-    for (int kb = kb0; kb < kb1; ++kb) {
+    for (int i = kb0; i < kb1; ++i) {
+      const int kb = block_at<MODE>(i, sinks, it.skip);
       const int page = kb * 64 < it.len ? chunk_page(c.page_table, c.max_pages, c.n_pages, it.b, kb, c.err) : -1;
       if (page < 0) continue;  // nothing to see there
-      const T* pk = static_cast<const T*>(c.pool) + page * c.page_elems + ((long long)c.layer * 2 * c.Hkv + it.h) * 64 * HD;
-      const T* pv = pk + (long long)c.Hkv * 64 * HD;
       __syncthreads();
-      constexpr int VEC = Vec16<T>::N;
+      constexpr int VEC = MODE == KEYS_4BIT ? 8 : Vec16<T>::N;
       for (int i = tid * VEC; i < 64 * HD; i += 256 * VEC) {
         float kk[VEC], vv[VEC];
-        Vec16<T>::load(pk + i, kk);
-        Vec16<T>::load(pv + i, vv);
+        if constexpr (MODE == KEYS_4BIT) {
+          using F = Kv4<HD>;
+          const uint8_t* pk = static_cast<const uint8_t*>(c.pool) + page * c.page_elems + ((long long)c.layer * 2 * c.Hkv + it.h) * F::BLOCK;
+          const uint8_t* pv = pk + (long long)c.Hkv * F::BLOCK;
+          const int pair = F::CODES + ((i / HD) * F::NG + i % HD / F::GS) * 4;
+          kv4_values(*reinterpret_cast<const uint32_t*>(pk + i / 2), kv4_pair(*reinterpret_cast<const uint32_t*>(pk + pair)), kk);
+          kv4_values(*reinterpret_cast<const uint32_t*>(pv + i / 2), kv4_pair(*reinterpret_cast<const uint32_t*>(pv + pair)), vv);
+        } else {
+          const T* pk = static_cast<const T*>(c.pool) + page * c.page_elems + ((long long)c.layer * 2 * c.Hkv + it.h) * 64 * HD;
+          Vec16<T>::load(pk + i, kk);
+          Vec16<T>::load(pk + (long long)c.Hkv * 64 * HD + i, vv);
+        }
         float* dk = sK + (i / HD) * KS + i % HD;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
@@ -363,11 +395,14 @@ __global__ void __launch_bounds__(256) k_chunk_simt(ChunkAttn a) {
 #pragma unroll
       for (int i = 0; i < RW; ++i) {
         const int vis = see[i] - kb * 64;  // keys 0..vis of the block
-        mixed |= vis < 63;
+        // but for those from past..low: hidden by the window and not among the first
+        const int past = MODE == KEYS_ALL ? 64 : a.first - kb * 64, low = MODE == KEYS_ALL ? -1 : hidden_to(see[i], a.window) - kb * 64;
+        auto hidden = [&](int key) { return key > vis || (MODE != KEYS_ALL && key >= past && key <= low); };
+        mixed |= vis < 63 || (MODE != KEYS_ALL && low >= 0 && past < 64);
         float mx = -INFINITY;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          if (x + 16 * j > vis) s[i][j] = -INFINITY;
+          if (hidden(x + 16 * j)) s[i][j] = -INFINITY;
           mx = fmaxf(mx, s[i][j]);
         }
 #pragma unroll
@@ -376,7 +411,7 @@ __global__ void __launch_bounds__(256) k_chunk_simt(ChunkAttn a) {
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float p = x + 16 * j > vis ? 0.f : exp2f(s[i][j] - ref);
+          const float p = hidden(x + 16 * j) ? 0.f : exp2f(s[i][j] - ref);
           sP[(y + 16 * i) * PS + x + 16 * j] = p;
           sum += p;
         }
@@ -405,7 +440,9 @@ __global__ void __launch_bounds__(256) k_chunk_simt(ChunkAttn a) {
 #pragma unroll
         for (int i = 0; i < RW; ++i) {
           const int vis = min(63, see[i] - kb * 64);
+          const int past = a.first - kb * 64, low = hidden_to(see[i], a.window) - kb * 64;
           for (int key = 0; key <= vis; ++key) {
+            if (MODE != KEYS_ALL && key >= past && key <= low) continue;
             const float p = sP[(y + 16 * i) * PS + key];
 #pragma unroll
             for (int d = 0; d < DW; ++d) o[i][d] += p * sV[key * HD + x * DW + d];
@@ -1995,12 +2032,12 @@ size_t chunk_attn_scratch(const ChunkDev& c, int dtype, const tlf_attn_chunk_arg
   return chunk_path(c, dtype, a, num_sms).total;
 }
 
-template <typename T, int RT, int HD>
+template <typename T, int RT, int HD, int MODE>
 static cudaError_t simt_launch(const ChunkAttn& a, cudaStream_t st) {
   const int smem = SimtShape<RT, HD>::bytes(a.c.n);
-  if (cudaError_t e = ensure_kernel_attrs(reinterpret_cast<const void*>(k_chunk_simt<T, RT, HD>), SimtShape<RT, HD>::bytes(SV_MAX_ROWS)))
+  if (cudaError_t e = ensure_kernel_attrs(reinterpret_cast<const void*>(k_chunk_simt<T, RT, HD, MODE>), SimtShape<RT, HD>::bytes(SV_MAX_ROWS)))
     return e;
-  return launch_k(k_chunk_simt<T, RT, HD>, dim3(a.ctas), dim3(256), smem, st, a);
+  return launch_k(k_chunk_simt<T, RT, HD, MODE>, dim3(a.ctas), dim3(256), smem, st, a);
 }
 // 3-D map over the pool: {head_dim, rows of a page, pages}, boxes of 64 rows of one 128-byte (head_dim 32: 64-byte) column.
 static bool pool_map(CUtensorMap* m, const ChunkDev& c) {
@@ -2059,9 +2096,25 @@ static cudaError_t mma_rows(const ChunkAttn& a, cudaStream_t st) {
     if (a.rows == 256) return pair_launch<HD>(a, st);
   return a.rows == 16 ? mma_launch<HD, 1>(a, st) : a.rows == 32 ? mma_launch<HD, 2>(a, st) : mma_launch<HD, 4>(a, st);
 }
-template <int HD>
+template <typename T, int MODE>
 static cudaError_t simt_rows(const ChunkAttn& a, cudaStream_t st) {
-  return a.rows == 16 ? simt_launch<float, 16, HD>(a, st) : simt_launch<float, 64, HD>(a, st);
+  if constexpr (std::is_same<T, float>::value)
+    if (a.c.hd == 16) return a.rows == 16 ? simt_launch<T, 16, 16, MODE>(a, st) : simt_launch<T, 64, 16, MODE>(a, st);
+  switch (a.c.hd) {
+    case 32: return a.rows == 16 ? simt_launch<T, 16, 32, MODE>(a, st) : simt_launch<T, 64, 32, MODE>(a, st);
+    case 64: return a.rows == 16 ? simt_launch<T, 16, 64, MODE>(a, st) : simt_launch<T, 64, 64, MODE>(a, st);
+    case 128: return a.rows == 16 ? simt_launch<T, 16, 128, MODE>(a, st) : simt_launch<T, 64, 128, MODE>(a, st);
+  }
+  return cudaErrorInvalidValue;
+}
+template <typename T>
+static cudaError_t join_launch(const ChunkAttn& a, cudaStream_t st) {
+  const dim3 jg(a.ctas - 1, std::max(1, a.rows / 32));
+  if (a.ctas <= 1) return cudaSuccess;
+  return a.rows == PAIR_ROWS ? (a.c.hd == 128 ? launch_k(k_pair_join<128>, jg, dim3(256), 0, st, a) : launch_k(k_pair_join<64>, jg, dim3(256), 0, st, a))
+         : a.c.hd == 128 ? launch_k(k_chunk_join<T, 4>, jg, dim3(256), 0, st, a)
+         : a.c.hd == 64 ? launch_k(k_chunk_join<T, 2>, jg, dim3(256), 0, st, a)
+                         : launch_k(k_chunk_join<T, 1>, jg, dim3(256), 0, st, a);
 }
 template <typename T>
 static cudaError_t chunk_launch(const ChunkAttn& a, const tlf_attn_chunk_args& args, float* weigh, int num_sms, cudaStream_t st) {
@@ -2069,16 +2122,10 @@ static cudaError_t chunk_launch(const ChunkAttn& a, const tlf_attn_chunk_args& a
   if (std::is_same<T, bf16>::value)
     e = a.c.hd == 32 ? mma_rows<32>(a, st) : a.c.hd == 64 ? mma_rows<64>(a, st) : mma_rows<128>(a, st);
   else
-    e = a.c.hd == 16 ? simt_rows<16>(a, st) : a.c.hd == 32 ? simt_rows<32>(a, st) : a.c.hd == 64 ? simt_rows<64>(a, st) : simt_rows<128>(a, st);
+    e = simt_rows<T, KEYS_ALL>(a, st);
   if (e) return e;
   const int base = (a.c.n + 1) * 8;
-  const dim3 jg(a.ctas - 1, std::max(1, a.rows / 32));
-  if (a.ctas > 1)
-    e = a.rows == PAIR_ROWS ? (a.c.hd == 128 ? launch_k(k_pair_join<128>, jg, dim3(256), 0, st, a) : launch_k(k_pair_join<64>, jg, dim3(256), 0, st, a))
-        : a.c.hd == 128 ? launch_k(k_chunk_join<T, 4>, jg, dim3(256), 0, st, a)
-        : a.c.hd == 64 ? launch_k(k_chunk_join<T, 2>, jg, dim3(256), 0, st, a)
-                        : launch_k(k_chunk_join<T, 1>, jg, dim3(256), 0, st, a);
-  if (e) return e;
+  if ((e = join_launch<T>(a, st))) return e;
   if (!args.weight_out) return cudaSuccess;
   const dim3 grid(4 * num_sms);
   if constexpr (std::is_same<T, bf16>::value)
@@ -2119,8 +2166,68 @@ cudaError_t launch_chunk_attn(const ChunkDev& c, int dtype, const tlf_attn_chunk
   a.part_o = reinterpret_cast<float*>(s);
   a.part_ml = reinterpret_cast<float2*>(s + p.part_ml);
   a.join = reinterpret_cast<int4*>(s + p.join);
+  a.window = 0x7fffffff;
   float* weigh = p.weigh_tc ? reinterpret_cast<float*>(s + p.weigh) : nullptr;
   return dtype == TLF_DTYPE_BF16 ? chunk_launch<bf16>(a, args, weigh, num_sms, st) : chunk_launch<float>(a, args, weigh, num_sms, st);
+}
+
+// tlf_attn_window. A window of 0 over a cache in the dtype is tlf_attn_chunk's case, and its kernels'.
+struct WindowPath {
+  int rt, ctas, pad;  // as in ChunkPath
+  size_t part_ml, join, werr, total;
+};
+static WindowPath window_path(const ChunkDev& c, int dtype, const tlf_attn_window_args& a, int num_sms) {
+  WindowPath p{};
+  const long long rows = (long long)c.max_chunk * c.G;
+  p.rt = rows <= 16 ? 16 : 64;
+  p.ctas = 2 * num_sms;
+  p.pad = PAD_SIMT;
+  const int qt_log = pow2_log(std::max(1, p.rt / c.G));
+  p.ctas = (int)std::min<double>(p.ctas, std::max(1.0, ((double)(c.T >> qt_log) + c.n) * c.Hkv * ((double)c.max_pages + p.pad)));
+  size_t o = 0;
+  auto take = [&](size_t bytes) { const size_t at = o; o = (o + bytes + 255) / 256 * 256; return at; };
+  take((size_t)2 * p.ctas * p.rt * c.hd * 4);
+  p.part_ml = take((size_t)2 * p.ctas * p.rt * 8);
+  p.join = take((size_t)p.ctas * 16);
+  p.werr = take(4);
+  p.total = o;
+  return p;
+}
+static tlf_attn_chunk_args plain_args(const tlf_attn_window_args& a) {
+  return tlf_attn_chunk_args{a.q, a.q_stride, a.out, a.out_stride, a.lse, nullptr, nullptr, a.scale, 0};
+}
+size_t window_attn_scratch(const ChunkDev& c, int dtype, const tlf_attn_window_args& a, int num_sms) {
+  if (a.window == 0 && a.kv_format == TLF_KV_PLAIN) return chunk_attn_scratch(c, dtype, plain_args(a), num_sms);
+  return window_path(c, dtype, a, num_sms).total;
+}
+template <typename T>
+static cudaError_t window_launch(const ChunkAttn& a, int kv_format, cudaStream_t st) {
+  if (cudaError_t e = kv_format == TLF_KV_4BIT ? simt_rows<T, KEYS_4BIT>(a, st) : simt_rows<T, KEYS_WINDOW>(a, st)) return e;
+  return join_launch<T>(a, st);
+}
+cudaError_t launch_window_attn(const ChunkDev& c, int dtype, const tlf_attn_window_args& args, void* scratch, int num_sms,
+                               cudaStream_t st) {
+  if (args.window == 0 && args.kv_format == TLF_KV_PLAIN) return launch_chunk_attn(c, dtype, plain_args(args), scratch, num_sms, st);
+  const WindowPath p = window_path(c, dtype, args, num_sms);
+  char* s = static_cast<char*>(scratch);
+  ChunkAttn a{};
+  a.c = c;
+  a.sp = ChunkSplit{pow2_log(std::max(1, p.rt / c.G)), 6, p.pad};
+  a.q = args.q;
+  a.qs = args.q_stride ? args.q_stride : (long long)c.Hq * c.hd;
+  a.out = args.out;
+  a.os = args.out_stride ? args.out_stride : (long long)c.Hq * c.hd;
+  a.lse = args.lse;
+  a.scale = (args.scale != 0.f ? args.scale : 1.f / sqrtf((float)c.hd)) * LOG2E;
+  a.ctas = p.ctas;
+  a.rows = p.rt;
+  a.werr = c.err ? c.err : reinterpret_cast<uint32_t*>(s + p.werr);
+  a.part_o = reinterpret_cast<float*>(s);
+  a.part_ml = reinterpret_cast<float2*>(s + p.part_ml);
+  a.join = reinterpret_cast<int4*>(s + p.join);
+  a.window = args.window > 0 ? args.window : 0x7fffffff;
+  a.first = args.window > 0 ? args.n_first : 0;
+  return dtype == TLF_DTYPE_BF16 ? window_launch<bf16>(a, args.kv_format, st) : window_launch<float>(a, args.kv_format, st);
 }
 
 }  // namespace tlf

@@ -57,6 +57,52 @@ struct ChunkSplit {
   }
 };
 
+// The same under a window: a query at entry E sees the entries e <= E with e > E - window or e < first. Tile t, whose first query
+// is at entry E0, then reads the blocks of the first entries, block numbers below sinks(), and those from that of entry
+// E0 - window + 1 on: the skip(t) blocks in between are left out, and block i of an item is block i + skip(t) of the row where
+// i >= sinks(). Queries that come later in the tile leave up to (2^qt_log - 1) entries more out, by masks.
+struct WindowSplit : ChunkSplit {
+  int window, first;  // window 2^31 - 1: none
+
+  __host__ __device__ int sinks() const { return (int)(((long long)first + (1 << bk_log) - 1) >> bk_log); }
+  __host__ __device__ int skip(int s0, int t) const {
+    const long long low = s0 + ((long long)t << qt_log) - window + 1;
+    const long long n = (low > 0 ? low >> bk_log : 0) - sinks();
+    return n > 0 ? (int)n : 0;
+  }
+  __host__ __device__ int blocks(int s0, int ql, int t) const { return ChunkSplit::blocks(s0, ql, t) - skip(s0, t); }
+  // sum over u = 0 .. n - 1 of floor(u / 2^r)
+  __host__ __device__ static long long floor_sum(long long n, int r) {
+    const long long q = n >> r, rem = n & ((1LL << r) - 1);
+    return ((q * (q - 1) / 2) << r) + rem * q;
+  }
+  // sum of skip() over the row's first t tiles: floor((a + i 2^qt_log) / 2^bk_log) - sinks where that is positive, from i0 on
+  __host__ __device__ long long skipped(int s0, int t) const {
+    const long long a = (long long)s0 - window + 1, edge = ((long long)sinks() + 1) << bk_log;
+    long long i0 = edge > a ? (edge - a + (1 << qt_log) - 1) >> qt_log : 0;
+    if (i0 >= t) return 0;
+    const long long n = t - i0;
+    if (qt_log >= bk_log) {
+      const long long f = (a >> bk_log) - sinks();
+      return n * f + ((i0 + t - 1) * n / 2 << (qt_log - bk_log));
+    }
+    const long long u = a >> qt_log;
+    return floor_sum(u + t, bk_log - qt_log) - floor_sum(u + i0, bk_log - qt_log) - n * sinks();
+  }
+  __host__ __device__ long long before(int s0, int ql, int t) const {
+    return t <= 0 ? 0 : ChunkSplit::before(s0, ql, t) - skipped(s0, t);
+  }
+  __host__ __device__ int tile_of(int s0, int ql, long long at) const {
+    int lo = 0, hi = tiles(ql);
+    while (hi - lo > 1) {
+      const int mid = lo + (hi - lo) / 2;
+      if (before(s0, ql, mid) <= at) lo = mid;
+      else hi = mid;
+    }
+    return lo;
+  }
+};
+
 // The split of the tensor-core weights (k_weigh_tc): a row's cache in blocks of 2^bk_log entries, its queries in tiles of
 // 2^qt_log <= 2^bk_log. A unit is one tile that sees something of a block, for one kv head; the flat order is (row, block,
 // head, tile), shared out like the above. Tile t sees block kb when its last query sees the block's first entry:

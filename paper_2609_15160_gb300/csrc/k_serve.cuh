@@ -19,6 +19,9 @@ struct ChunkDev {
   uint32_t* err;  // may be NULL
 };
 
+// Bits of a caller's error word beside those of the library's own (DEVERR_WAIT, DEVERR_INDEX).
+enum : uint32_t { SVERR_VALUE = 8u, SVERR_PAGES = 16u };
+
 __device__ __forceinline__ void sv_report(uint32_t* err, uint32_t bit) {
   if (err) atomicOr(err, bit);
 }
@@ -160,8 +163,18 @@ size_t chunk_attn_scratch(const ChunkDev& c, int dtype, const tlf_attn_chunk_arg
 cudaError_t launch_chunk_attn(const ChunkDev& c, int dtype, const tlf_attn_chunk_args& a, void* scratch, int num_sms,
                               cudaStream_t st);
 
+// The same under a window, or over a cache in 4 bits (c's page_elems then counts bytes).
+size_t window_attn_scratch(const ChunkDev& c, int dtype, const tlf_attn_window_args& a, int num_sms);
+cudaError_t launch_window_attn(const ChunkDev& c, int dtype, const tlf_attn_window_args& a, void* scratch, int num_sms,
+                               cudaStream_t st);
+
 size_t evict_scratch(const tlf_evict_args& a);
 cudaError_t launch_evict(const tlf_evict_args& a, void* scratch, int num_sms, cudaStream_t st);
+
+size_t fork_scratch(const tlf_fork_args& a);
+cudaError_t launch_fork(const tlf_fork_args& a, void* scratch, int num_sms, cudaStream_t st);
+size_t compact_scratch(const tlf_compact_args& a);
+cudaError_t launch_compact(const tlf_compact_args& a, void* scratch, int num_sms, cudaStream_t st);
 
 cudaError_t launch_sample(const tlf_sample_args& a, int num_sms, cudaStream_t st);
 

@@ -1,8 +1,10 @@
 // Entry points of the operators on a caller's paged caches and logits (declared in include/tlf.h): checks of arguments, and
 // the launches. Nothing here allocates or synchronises.
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 
+#include "k_kv4.cuh"
 #include "k_serve.cuh"
 #include "tlf.h"
 
@@ -66,6 +68,13 @@ static ChunkDev chunk_dev(const tlf_chunk* c) {
   return d;
 }
 
+// c as the kernels of a cache in 4 bits take it: page_elems counts bytes.
+static ChunkDev chunk_dev4(const tlf_chunk* c) {
+  ChunkDev d = chunk_dev(c);
+  d.page_elems = (long long)c->n_layers * 2 * c->n_kv_heads * kv4_block_bytes(c->head_dim);
+  return d;
+}
+
 static const char* rope_validate(const tlf_chunk* c, const tlf_rope_args* a) {
   if (!a) return "the arguments are NULL";
   if (!a->q || !a->k || !a->v || !a->positions || !a->table || !a->q_out) return "a device pointer is NULL";
@@ -90,6 +99,57 @@ static const char* attn_validate(const tlf_chunk* c, const tlf_attn_chunk_args* 
   if (a->weight_in && !a->weight_out) return "weight_in without weight_out";
   if (!(a->scale >= 0.f) || a->scale > 2e38f) return "scale must be in 0..2e38";  // (finite times log2 e too)
   if (a->reserved0) return "reserved0 must be 0";
+  return nullptr;
+}
+
+static const char* window_validate(const tlf_chunk* c, const tlf_attn_window_args* a) {
+  if (!a) return "the arguments are NULL";
+  const tlf_attn_chunk_args plain{a->q, a->q_stride, a->out, a->out_stride, a->lse, nullptr, nullptr, a->scale, 0};
+  if (const char* why = attn_validate(c, &plain)) return why;
+  if (a->window < 0 || a->n_first < 0) return "window and n_first must not be negative";
+  if (a->kv_format != TLF_KV_PLAIN && a->kv_format != TLF_KV_4BIT) return "unknown kv_format";
+  return nullptr;
+}
+
+static const char* read_validate(const tlf_chunk* c, const tlf_kv4_read_args* a) {
+  if (const char* why = chunk_validate(c)) return why;
+  if (!a) return "the arguments are NULL";
+  const int64_t row = (int64_t)c->n_kv_heads * c->head_dim;
+  if ((a->k_stride && a->k_stride < row) || (a->v_stride && a->v_stride < row)) return "a stride is smaller than a token's heads";
+  return nullptr;
+}
+
+// What the calls on pages have in common.
+static const char* pages_validate(int hkv, int hd, int layers, int page_size, int dtype, int kv_format, int max_pages, int64_t n_pages,
+                                  const void* pool, const void* table, const void* table_out, const void* refs, const void* refs_out) {
+  if (const char* why = cache_validate(1, hkv, hd, layers, page_size, dtype, max_pages, n_pages, pool, table, refs)) return why;
+  if (kv_format != TLF_KV_PLAIN && kv_format != TLF_KV_4BIT) return "unknown kv_format";
+  if (!table_out || !refs_out) return "a device pointer is NULL";
+  return nullptr;
+}
+static bool row_count(int n) { return n >= 1 && n <= 65535; }
+static const char* fork_validate(const tlf_fork_args* a) {
+  if (!a) return "the arguments are NULL";
+  if (const char* why = pages_validate(a->n_kv_heads, a->head_dim, a->n_layers, a->page_size, a->dtype, a->kv_format, a->max_pages,
+                                       a->n_pages, a->pool, a->page_table, a->table_out, a->refs, a->refs_out))
+    return why;
+  if (!row_count(a->n_in) || !row_count(a->n_out)) return "n_in and n_out must be in 1..65535";
+  if (!a->lens || !a->parents || !a->lens_out) return "a device pointer is NULL";
+  if (a->reserve < 0 || a->window < 0 || a->n_first < 0) return "reserve, window and n_first must not be negative";
+  const int64_t each = std::min<int64_t>(a->max_pages, (int64_t)a->reserve / SV_PAGE + 2);
+  if (each * a->n_out > 0x7fffffff) return "reserve is too large for so many rows";
+  const char *in = reinterpret_cast<const char*>(a->page_table), *out = reinterpret_cast<const char*>(a->table_out);
+  if (in < out + (int64_t)a->n_out * a->max_pages * 4 && out < in + (int64_t)a->n_in * a->max_pages * 4)
+    return "table_out must not overlap page_table";
+  return nullptr;
+}
+static const char* compact_validate(const tlf_compact_args* a) {
+  if (!a) return "the arguments are NULL";
+  if (const char* why = pages_validate(a->n_kv_heads, a->head_dim, a->n_layers, a->page_size, a->dtype, a->kv_format, a->max_pages,
+                                       a->n_pages, a->pool, a->page_table, a->table_out, a->refs, a->refs_out))
+    return why;
+  if (!row_count(a->n)) return "n must be in 1..65535";
+  if (!a->n_live) return "a device pointer is NULL";
   return nullptr;
 }
 
@@ -183,6 +243,75 @@ extern "C" int tlf_attn_chunk(const tlf_chunk* c, const tlf_attn_chunk_args* a, 
     if (!scratch || !aligned(scratch, 16) || scratch_bytes < chunk_attn_scratch(d, c->dtype, *a, sms))
       return refuse("tlf_attn_chunk", "scratch too small or not aligned to 16 bytes");
     return done(launch_chunk_attn(d, c->dtype, *a, scratch, sms, static_cast<cudaStream_t>(stream)));
+  });
+}
+
+extern "C" int64_t tlf_kv4_block_bytes(int32_t head_dim) {
+  return head_dim == 16 || head_dim == 32 || head_dim == 64 || head_dim == 128 ? kv4_block_bytes(head_dim) : 0;
+}
+
+extern "C" int tlf_kv4_append(const tlf_chunk* c, const tlf_rope_args* a, void* stream) {
+  return guarded([&] {
+    if (const char* why = chunk_validate(c)) return refuse("tlf_kv4_append", why);
+    if (const char* why = rope_validate(c, a)) return refuse("tlf_kv4_append", why);
+    if (c->n_tokens == 0) return (int)TLF_OK;
+    const int sms = current_num_sms();
+    if (sms <= 0) return set_thread_error(TLF_ERR_CUDA, "no current CUDA device");
+    return done(launch_kv4_append(chunk_dev4(c), c->dtype, *a, sms, static_cast<cudaStream_t>(stream)));
+  });
+}
+
+extern "C" int tlf_kv4_read(const tlf_chunk* c, const tlf_kv4_read_args* a, void* stream) {
+  return guarded([&] {
+    if (const char* why = read_validate(c, a)) return refuse("tlf_kv4_read", why);
+    if (c->n_tokens == 0 || (!a->k && !a->v)) return (int)TLF_OK;
+    const int sms = current_num_sms();
+    if (sms <= 0) return set_thread_error(TLF_ERR_CUDA, "no current CUDA device");
+    return done(launch_kv4_read(chunk_dev4(c), c->dtype, *a, sms, static_cast<cudaStream_t>(stream)));
+  });
+}
+
+extern "C" size_t tlf_attn_window_scratch_bytes(const tlf_chunk* c, const tlf_attn_window_args* a) {
+  if (window_validate(c, a)) return 0;
+  const int sms = current_num_sms();
+  return sms <= 0 ? 0 : window_attn_scratch(a->kv_format == TLF_KV_4BIT ? chunk_dev4(c) : chunk_dev(c), c->dtype, *a, sms);
+}
+
+extern "C" int tlf_attn_window(const tlf_chunk* c, const tlf_attn_window_args* a, void* scratch, size_t scratch_bytes, void* stream) {
+  return guarded([&] {
+    if (const char* why = window_validate(c, a)) return refuse("tlf_attn_window", why);
+    const int sms = current_num_sms();
+    if (sms <= 0) return set_thread_error(TLF_ERR_CUDA, "no current CUDA device");
+    const ChunkDev d = a->kv_format == TLF_KV_4BIT ? chunk_dev4(c) : chunk_dev(c);
+    if (!scratch || !aligned(scratch, 16) || scratch_bytes < window_attn_scratch(d, c->dtype, *a, sms))
+      return refuse("tlf_attn_window", "scratch too small or not aligned to 16 bytes");
+    return done(launch_window_attn(d, c->dtype, *a, scratch, sms, static_cast<cudaStream_t>(stream)));
+  });
+}
+
+extern "C" size_t tlf_cache_fork_scratch_bytes(const tlf_fork_args* a) { return fork_validate(a) ? 0 : fork_scratch(*a); }
+
+extern "C" int tlf_cache_fork(const tlf_fork_args* a, void* scratch, size_t scratch_bytes, void* stream) {
+  return guarded([&] {
+    if (const char* why = fork_validate(a)) return refuse("tlf_cache_fork", why);
+    if (!scratch || !aligned(scratch, 16) || scratch_bytes < fork_scratch(*a))
+      return refuse("tlf_cache_fork", "scratch too small or not aligned to 16 bytes");
+    const int sms = current_num_sms();
+    if (sms <= 0) return set_thread_error(TLF_ERR_CUDA, "no current CUDA device");
+    return done(launch_fork(*a, scratch, sms, static_cast<cudaStream_t>(stream)));
+  });
+}
+
+extern "C" size_t tlf_cache_compact_scratch_bytes(const tlf_compact_args* a) { return compact_validate(a) ? 0 : compact_scratch(*a); }
+
+extern "C" int tlf_cache_compact(const tlf_compact_args* a, void* scratch, size_t scratch_bytes, void* stream) {
+  return guarded([&] {
+    if (const char* why = compact_validate(a)) return refuse("tlf_cache_compact", why);
+    if (!scratch || !aligned(scratch, 16) || scratch_bytes < compact_scratch(*a))
+      return refuse("tlf_cache_compact", "scratch too small or not aligned to 16 bytes");
+    const int sms = current_num_sms();
+    if (sms <= 0) return set_thread_error(TLF_ERR_CUDA, "no current CUDA device");
+    return done(launch_compact(*a, scratch, sms, static_cast<cudaStream_t>(stream)));
   });
 }
 

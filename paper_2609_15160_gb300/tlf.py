@@ -28,6 +28,7 @@ GEMM = {"auto": 0, "simt": 1}
 ABLATION = {"none": 0, "no_gather": 1, "dense_cache": 2}
 ROPE_SCALING = {"none": 0, "linear": 1, "ntk": 2, "ramp": 3}
 ROPE_LAYOUT = {"half": 0, "interleaved": 1}
+KV_FORMAT = {"plain": 0, "4bit": 1}
 
 
 class TlfConfig(C.Structure):
@@ -92,6 +93,29 @@ class TlfSampleArgs(C.Structure):
         (n, C.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p", "tokens", "logprobs")]
 
 
+class TlfKv4ReadArgs(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_stride", C.c_int64), ("v_stride", C.c_int64)]
+
+
+class TlfAttnWindowArgs(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_stride", C.c_int64), ("out", C.c_void_p), ("out_stride", C.c_int64), ("lse", C.c_void_p),
+                ("scale", C.c_float)] + [(n, C.c_int32) for n in ("window", "n_first", "kv_format")]
+
+
+class TlfForkArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_in", "n_out", "n_kv_heads", "head_dim", "n_layers", "page_size", "dtype", "kv_format",
+                                         "max_pages", "reserve", "window", "n_first")] + [("n_pages", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("pool", "page_table", "lens", "parents", "refs", "table_out", "lens_out", "refs_out",
+                                  "entry_pos", "entry_weight", "err")]
+
+
+class TlfCompactArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n", "n_kv_heads", "head_dim", "n_layers", "page_size", "dtype", "kv_format",
+                                         "max_pages")] + [("n_pages", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("pool", "page_table", "refs", "table_out", "refs_out", "n_live", "entry_pos", "entry_weight",
+                                  "err")]
+
+
 class TlfError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"{ERRORS.get(code, code)}: {msg}")
@@ -132,6 +156,15 @@ _SIGS = {
     "tlf_cache_evict_scratch_bytes": (C.c_size_t, [C.POINTER(TlfEvictArgs)]),
     "tlf_cache_evict": (C.c_int, [C.POINTER(TlfEvictArgs), _P, C.c_size_t, _P]),
     "tlf_sample": (C.c_int, [C.POINTER(TlfSampleArgs), _P]),
+    "tlf_kv4_block_bytes": (C.c_int64, [C.c_int32]),
+    "tlf_kv4_append": (C.c_int, [C.POINTER(TlfChunk), C.POINTER(TlfRopeArgs), _P]),
+    "tlf_kv4_read": (C.c_int, [C.POINTER(TlfChunk), C.POINTER(TlfKv4ReadArgs), _P]),
+    "tlf_attn_window_scratch_bytes": (C.c_size_t, [C.POINTER(TlfChunk), C.POINTER(TlfAttnWindowArgs)]),
+    "tlf_attn_window": (C.c_int, [C.POINTER(TlfChunk), C.POINTER(TlfAttnWindowArgs), _P, C.c_size_t, _P]),
+    "tlf_cache_fork_scratch_bytes": (C.c_size_t, [C.POINTER(TlfForkArgs)]),
+    "tlf_cache_fork": (C.c_int, [C.POINTER(TlfForkArgs), _P, C.c_size_t, _P]),
+    "tlf_cache_compact_scratch_bytes": (C.c_size_t, [C.POINTER(TlfCompactArgs)]),
+    "tlf_cache_compact": (C.c_int, [C.POINTER(TlfCompactArgs), _P, C.c_size_t, _P]),
 }
 
 
@@ -380,13 +413,18 @@ def rope_args(q, k, v, positions, table, q_out, layout: str = "half", entry_pos=
     return a
 
 
+def _format(c: TlfChunk, four_bits: bool):
+    if getattr(c, "four_bits", False) != four_bits:
+        raise ValueError("the batch's cache is in 4 bits (chunk4_args) and the call is for one in the dtype, or the other way round")
+
+
 def _pair(c: TlfChunk, a):
     """The arguments' tensors are large enough for the batch (looked at once for the same numbers: a program may change them)."""
     batch = (c.n_tokens, c.n_heads, c.n_kv_heads, c.head_dim, c.dtype, c.n_pages)
     if getattr(a, "batch", None) == batch:
         return
     rows, hq, kh, hd, dt, pages = a.fits
-    if rows < c.n_tokens or hq != c.n_heads or (kh and kh != c.n_kv_heads) or hd != c.head_dim or dt != c.dtype or any(
+    if rows < c.n_tokens or (hq and hq != c.n_heads) or (kh and kh != c.n_kv_heads) or hd != c.head_dim or dt != c.dtype or any(
             p != c.n_pages for p in pages):
         raise ValueError(f"the arguments are for {rows} tokens of {hq} heads of {hd} and caches of {pages} pages, the batch has "
                          f"{c.n_tokens} tokens of {c.n_heads} heads of {c.head_dim} and {c.n_pages} pages")
@@ -394,6 +432,7 @@ def _pair(c: TlfChunk, a):
 
 
 def tlf_rope_append(c: TlfChunk, a: TlfRopeArgs, stream=None):
+    _format(c, False)
     _pair(c, a)
     _check(load_library().tlf_rope_append(C.byref(c), C.byref(a), _stream(stream)), None)
 
@@ -419,6 +458,7 @@ def tlf_attn_chunk_scratch_bytes(c: TlfChunk, a: TlfAttnChunkArgs) -> int:
 
 
 def tlf_attn_chunk(c: TlfChunk, a: TlfAttnChunkArgs, scratch, scratch_bytes: int, stream=None):
+    _format(c, False)
     _pair(c, a)
     _check(load_library().tlf_attn_chunk(C.byref(c), C.byref(a), _addr(scratch), scratch_bytes, _stream(stream)), None)
 
@@ -472,6 +512,155 @@ def sample_args(logits, noise, tokens, logprobs=None, temperature=None, top_k=No
 
 def tlf_sample(a: TlfSampleArgs, stream=None):
     _check(load_library().tlf_sample(C.byref(a), _stream(stream)), None)
+
+
+# ---- caches in 4 bits, windows, and who owns a page ----
+
+def kv4_block_bytes(head_dim: int) -> int:
+    """Bytes of a block (one layer, K or V, one head) of a page in 4 bits."""
+    if head_dim not in (16, 32, 64, 128):
+        raise ValueError(f"head_dim {head_dim}: 16, 32, 64 or 128 is wanted")
+    return 64 * (head_dim // 2 + 4 * max(1, head_dim // 64))
+
+
+def _pool4(pool, head_dim: int):
+    size = kv4_block_bytes(head_dim)
+    if len(pool.shape) != 5 or pool.shape[2] != 2 or pool.shape[4] != size:
+        raise ValueError(f"pool: [pages, layers, 2, kv heads, {size}] bytes are wanted for a cache in 4 bits with head_dim "
+                         f"{head_dim}, got {tuple(pool.shape)}")
+    _dense("pool", pool, "uint8", *pool.shape)
+
+
+def chunk4_args(pool, page_table, cu_tokens, lens, n_heads: int, n_tokens: int, head_dim: int, dtype: str = "bf16", layer: int = 0,
+                max_chunk: int = 0, err=None) -> TlfChunk:
+    """chunk_args for a cache in 4 bits: pool [pages, layers, 2, kv heads, kv4_block_bytes(head_dim)] uint8; dtype: of the queries,
+    keys, values and outputs."""
+    _pool4(pool, head_dim)
+    n = page_table.shape[0]
+    _dense("page_table", page_table, "int32", n, None)
+    _dense("cu_tokens", cu_tokens, "int32", n + 1)
+    _dense("lens", lens, "int32", n)
+    c = TlfChunk(n=n, n_tokens=n_tokens, max_chunk=max_chunk, n_heads=n_heads, n_kv_heads=pool.shape[3], head_dim=head_dim,
+                 n_layers=pool.shape[1], layer=layer, page_size=64, dtype=DTYPE[dtype], max_pages=page_table.shape[1],
+                 n_pages=pool.shape[0], pool=_addr(pool), page_table=_addr(page_table), cu_tokens=_addr(cu_tokens),
+                 lens=_addr(lens), err=_addr(err))
+    c.kept = (pool, page_table, cu_tokens, lens, err)
+    c.four_bits = True
+    return c
+
+
+def tlf_kv4_append(c: TlfChunk, a: TlfRopeArgs, stream=None):
+    """tlf_rope_append (its rope_args) into a cache in 4 bits."""
+    _format(c, True)
+    _pair(c, a)
+    _check(load_library().tlf_kv4_append(C.byref(c), C.byref(a), _stream(stream)), None)
+
+
+def kv4_read_args(k=None, v=None) -> TlfKv4ReadArgs:
+    """k, v: [tokens, kv heads, head_dim], rows any stride apart; None: not wanted."""
+    t = k if k is not None else v
+    if t is None:
+        raise ValueError("k or v is wanted")
+    _, kh, hd = t.shape
+    dt = _torch_dtype(t)
+    a = TlfKv4ReadArgs(k=_addr(k), v=_addr(v), k_stride=0 if k is None else _heads("k", k, dt, 0, kh, hd),
+                       v_stride=0 if v is None else _heads("v", v, dt, 0, kh, hd))
+    a.kept = (k, v)
+    a.fits = (min(x.shape[0] for x in (k, v) if x is not None), 0, kh, hd, dt, [])
+    return a
+
+
+def tlf_kv4_read(c: TlfChunk, a: TlfKv4ReadArgs, stream=None):
+    _format(c, True)
+    _pair(c, a)
+    _check(load_library().tlf_kv4_read(C.byref(c), C.byref(a), _stream(stream)), None)
+
+
+def attn_window_args(q, out, lse=None, window: int = 0, n_first: int = 0, kv4: bool = False, scale: float = 0.0) -> TlfAttnWindowArgs:
+    """As attn_chunk_args, without weights; window 0: no window; kv4: the batch's cache is in 4 bits (chunk4_args)."""
+    _, hq, hd = q.shape
+    _dense("lse", lse, "float32", None, hq)
+    dt = _torch_dtype(q)
+    a = TlfAttnWindowArgs(q=_addr(q), q_stride=_heads("q", q, dt, 0, hq, hd), out=_addr(out),
+                          out_stride=_heads("out", out, dt, q.shape[0], hq, hd), lse=_addr(lse), scale=scale, window=window,
+                          n_first=n_first, kv_format=int(kv4))
+    a.kept = (q, out, lse)
+    a.fits = (min(x.shape[0] for x in (q, out, lse) if x is not None), hq, 0, hd, dt, [])
+    return a
+
+
+def tlf_attn_window_scratch_bytes(c: TlfChunk, a: TlfAttnWindowArgs) -> int:
+    return load_library().tlf_attn_window_scratch_bytes(C.byref(c), C.byref(a))
+
+
+def tlf_attn_window(c: TlfChunk, a: TlfAttnWindowArgs, scratch, scratch_bytes: int, stream=None):
+    _format(c, a.kv_format == KV_FORMAT["4bit"])
+    _pair(c, a)
+    _check(load_library().tlf_attn_window(C.byref(c), C.byref(a), _addr(scratch), scratch_bytes, _stream(stream)), None)
+
+
+def _page_pool(pool, head_dim: Optional[int]) -> dict:
+    """The shape fields of a pool: [pages, layers, 2, kv heads, 64, head_dim], or in 4 bits (head_dim given) [.., block bytes] uint8."""
+    if head_dim is not None:
+        _pool4(pool, head_dim)
+        return dict(n_kv_heads=pool.shape[3], head_dim=head_dim, n_layers=pool.shape[1], page_size=64,
+                    dtype=DTYPE["f32" if head_dim == 16 else "bf16"], kv_format=KV_FORMAT["4bit"], n_pages=pool.shape[0], pool=_addr(pool))
+    if len(pool.shape) != 6 or pool.shape[2] != 2:
+        raise ValueError(f"pool: [pages, layers, 2, kv heads, 64, head_dim] is wanted, got {tuple(pool.shape)}")
+    _dense("pool", pool, None, *pool.shape)
+    return dict(n_kv_heads=pool.shape[3], head_dim=pool.shape[5], n_layers=pool.shape[1], page_size=pool.shape[4],
+                dtype=_torch_dtype(pool), kv_format=KV_FORMAT["plain"], n_pages=pool.shape[0], pool=_addr(pool))
+
+
+def fork_args(pool, page_table, lens, parents, refs, table_out, lens_out, refs_out, reserve: int = 0, window: int = 0,
+              n_first: int = 0, entry_pos=None, entry_weight=None, head_dim: Optional[int] = None, err=None) -> TlfForkArgs:
+    """page_table [old rows, most pages], lens [old rows]; parents, lens_out [new rows], table_out [new rows, most pages]; refs,
+    refs_out [pages]; entry_pos, entry_weight [pages, 64]. head_dim: of a pool in 4 bits (None: the pool has its dtype)."""
+    n_in, width = page_table.shape
+    n_out, pages = parents.shape[0], pool.shape[0]
+    for what, t, shape in (("page_table", page_table, (n_in, width)), ("lens", lens, (n_in,)), ("parents", parents, (n_out,)),
+                           ("table_out", table_out, (n_out, width)), ("lens_out", lens_out, (n_out,)), ("refs", refs, (pages,)),
+                           ("refs_out", refs_out, (pages,)), ("entry_pos", entry_pos, (pages, 64))):
+        _dense(what, t, "int32", *shape)
+    _dense("entry_weight", entry_weight, "float32", pages, 64)
+    a = TlfForkArgs(n_in=n_in, n_out=n_out, max_pages=width, reserve=reserve, window=window, n_first=n_first,
+                    page_table=_addr(page_table), lens=_addr(lens), parents=_addr(parents), refs=_addr(refs),
+                    table_out=_addr(table_out), lens_out=_addr(lens_out), refs_out=_addr(refs_out), entry_pos=_addr(entry_pos),
+                    entry_weight=_addr(entry_weight), err=_addr(err), **_page_pool(pool, head_dim))
+    a.kept = (pool, page_table, lens, parents, refs, table_out, lens_out, refs_out, entry_pos, entry_weight, err)
+    return a
+
+
+def tlf_cache_fork_scratch_bytes(a: TlfForkArgs) -> int:
+    return load_library().tlf_cache_fork_scratch_bytes(C.byref(a))
+
+
+def tlf_cache_fork(a: TlfForkArgs, scratch, scratch_bytes: int, stream=None):
+    _check(load_library().tlf_cache_fork(C.byref(a), _addr(scratch), scratch_bytes, _stream(stream)), None)
+
+
+def compact_args(pool, page_table, refs, table_out, refs_out, n_live, entry_pos=None, entry_weight=None,
+                 head_dim: Optional[int] = None, err=None) -> TlfCompactArgs:
+    """Shapes as in fork_args; table_out as page_table, n_live [1] int32."""
+    n, width = page_table.shape
+    pages = pool.shape[0]
+    for what, t, shape in (("page_table", page_table, (n, width)), ("table_out", table_out, (n, width)), ("refs", refs, (pages,)),
+                           ("refs_out", refs_out, (pages,)), ("n_live", n_live, (1,)), ("entry_pos", entry_pos, (pages, 64))):
+        _dense(what, t, "int32", *shape)
+    _dense("entry_weight", entry_weight, "float32", pages, 64)
+    a = TlfCompactArgs(n=n, max_pages=width, page_table=_addr(page_table), refs=_addr(refs), table_out=_addr(table_out),
+                       refs_out=_addr(refs_out), n_live=_addr(n_live), entry_pos=_addr(entry_pos), entry_weight=_addr(entry_weight),
+                       err=_addr(err), **_page_pool(pool, head_dim))
+    a.kept = (pool, page_table, refs, table_out, refs_out, n_live, entry_pos, entry_weight, err)
+    return a
+
+
+def tlf_cache_compact_scratch_bytes(a: TlfCompactArgs) -> int:
+    return load_library().tlf_cache_compact_scratch_bytes(C.byref(a))
+
+
+def tlf_cache_compact(a: TlfCompactArgs, scratch, scratch_bytes: int, stream=None):
+    _check(load_library().tlf_cache_compact(C.byref(a), _addr(scratch), scratch_bytes, _stream(stream)), None)
 
 
 # ----------------------------------------------------------------------------
