@@ -570,7 +570,25 @@ __device__ __noinline__ void chunk_left_out(const ChunkAttn& a, int b, int h, in
   }
 }
 
-template <int HD, int MT>
+// The same under a window, for one row of a tile: a query at entry `see` of a tile with queries see0 .. see_last, in the item's blocks
+// kb0 .. kb1 - 1. Left out were the entries from `first` on that the last query no longer sees, and the new tokens'. What one row
+// sees does not hold what another one does: x starts from zero.
+template <int HD>
+__device__ __noinline__ void window_left_out(const ChunkAttn& a, int b, int h, int see, int see0, int see_last, int kb0, int kb1, int sinks,
+                                             int skip, float (&x)[HD / 32]) {
+  const int low = hidden_to(see, a.window) + 1;
+  auto scan = [&](int lo, int hi) {  // entries lo .. hi of the blocks
+    int e = max(lo, kb0 * 64);
+    chunk_left_out<HD>(a, b, h, e, min(hi, min(kb1, sinks) * 64 - 1) + 1, x);
+    e = max(lo, (max(kb0, sinks) + skip) * 64);
+    if (kb1 > sinks) chunk_left_out<HD>(a, b, h, e, min(hi, (kb1 + skip) * 64 - 1) + 1, x);
+  };
+  scan(max(a.first, low), min(see0, hidden_to(see_last, a.window)));
+  scan(see0 + 1, min(see, a.first - 1));
+  scan(max(see0 + 1, max(a.first, low)), see);
+}
+
+template <int HD, int MT, int MODE>
 __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(ChunkAttn a,
                                                                              const __grid_constant__ CUtensorMap pool_map) {
   using Sh = MmaShape<HD, MT>;
@@ -601,7 +619,10 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
     prefetch_tensormap(&pool_map);
   }
   pdl_wait();
-  chunk_plan(c, a.sp, s_base, s_red);
+  const auto sp = split_of<MODE>(a);
+  int sinks = 0;
+  if constexpr (MODE != KEYS_ALL) sinks = sp.sinks();
+  chunk_plan(c, sp, s_base, s_red);
   pdl_trigger();
   const long long all = s_base[c.n], per = chunk_share(a, all);
   long long pos = blockIdx.x * per;
@@ -619,7 +640,7 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
   if (warp == 8) {
     if (pos >= end && lane == 0) join_note(a, nullptr, per);
     for (unsigned segs = 0; pos < end; ++segs) {
-      const ChunkItem it = chunk_item(c, a.sp, s_base, pos);
+      const ChunkItem it = chunk_item(c, sp, s_base, pos);
       if (segs == 0 && lane == 0) join_note(a, &it, per);
       if (pos < it.first) pos = it.first;
       if (pos >= end) {
@@ -635,8 +656,8 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
       const int rowK = (c.layer * 2 * c.Hkv + it.h) * 64, rowV = rowK + c.Hkv * 64;
       for (int g0 = kb0; g0 < kb1; g0 += 32) {
         int mine = -1;
-        if (g0 + lane < kb1 && (g0 + lane) * 64 < it.len)
-          mine = chunk_page(c.page_table, c.max_pages, c.n_pages, it.b, g0 + lane, c.err);
+        const int at = block_at<MODE>(g0 + lane, sinks, it.skip);
+        if (g0 + lane < kb1 && at * 64 < it.len) mine = chunk_page(c.page_table, c.max_pages, c.n_pages, it.b, at, c.err);
         for (int i = 0; i < min(32, kb1 - g0); ++i, ++seq) {
           const int page = __shfl_sync(0xffffffffu, mine, i), st = seq % NST;
           if (lane == 0) {
@@ -684,6 +705,15 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
     const int r0 = mt * 16 + (lane >> 2), r1 = r0 + 8;
     // rows past the tile's see what its first query sees, with q = 0; nobody reads them
     const int sees[2] = {see0 + (r0 < rows ? r0 / G : 0), see0 + (r1 < rows ? r1 / G : 0)};
+    // under a window: the entries from `first` up to hid are hidden, from all queries up to gone_to
+    int skip = 0, hid[2] = {-1, -1}, gone_to = -1, edge_to = -1;
+    if constexpr (MODE != KEYS_ALL) {
+      skip = sp.skip_at(see0);
+      hid[0] = hidden_to(sees[0], a.window);
+      hid[1] = hidden_to(sees[1], a.window);
+      gone_to = hidden_to(see0, a.window);
+      edge_to = hidden_to(see_last, a.window);
+    }
     uint32_t qf[HD / 16][4];
     {
       const bf16* base = static_cast<const bf16*>(a.q) + (long long)(it.h * G) * HD + (lane & 3) * 2;
@@ -717,7 +747,7 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
       const int st = seq % NST;
       const bool ok = __all_sync(0xffffffffu, wait(full(st), (seq / NST) & 1u));
       const bool mine = MT > 1 || (int)(seq & 1u) == grp >> 2;
-      const int key0 = kb * 64 + slice * KW;
+      const int key0 = block_at<MODE>(kb, sinks, skip) * 64 + slice * KW;
       if (ok && mine && key0 <= see_last && !s_skip[st]) {
         const uint32_t sk = smem_u32(sm + st * Sh::STAGE), sv = sk + Sh::SEG;
         float s[NT][4];
@@ -735,14 +765,15 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
             mma_16816(s[2 * g], qf[k], b[0], b[1]);
             mma_16816(s[2 * g + 1], qf[k], b[2], b[3]);
           }
-        const bool tail = key0 + KW - 1 > see0;
+        const bool tail = key0 + KW - 1 > see0 || (MODE != KEYS_ALL && key0 <= edge_to && key0 + KW - 1 >= a.first);
         float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
         for (int i = 0; i < NT; ++i)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             s[i][j] *= a.scale;
-            if (tail && key0 + i * 8 + (lane & 3) * 2 + (j & 1) > sees[j >> 1]) s[i][j] = -INFINITY;
+            const int key = key0 + i * 8 + (lane & 3) * 2 + (j & 1);
+            if (tail && (key > sees[j >> 1] || (MODE != KEYS_ALL && key >= a.first && key <= hid[j >> 1]))) s[i][j] = -INFINITY;
             mx[j >> 1] = fmaxf(mx[j >> 1], s[i][j]);
           }
         if (a.scores) {
@@ -791,8 +822,10 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
 #pragma unroll
               for (int x = 0; x < 2; ++x) {
                 const int key = key0 + g * 16 + x * 8 + (lane & 3) * 2;
-                keep[x] = (key <= see_last ? 0xffffu : 0u) | (key + 1 <= see_last ? 0xffff0000u : 0u);
-                look[x] = keep[x] & ((key > see0 ? 0xffffu : 0u) | (key + 1 > see0 ? 0xffff0000u : 0u));
+                auto seen = [&](int k) { return k <= see_last && (MODE == KEYS_ALL || k < a.first || k > gone_to); };
+                auto mixed = [&](int k) { return k > see0 || (MODE != KEYS_ALL && k >= a.first && k <= edge_to); };
+                keep[x] = (seen(key) ? 0xffffu : 0u) | (seen(key + 1) ? 0xffff0000u : 0u);
+                look[x] = keep[x] & ((mixed(key) ? 0xffffu : 0u) | (mixed(key + 1) ? 0xffff0000u : 0u));
               }
             }
 #pragma unroll
@@ -903,7 +936,13 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
       float x[HD / 32] = {};
       int e = max(kb0 * 64, see0 + 1);
       for (int r = warp; r < rows; r += 8) {
-        chunk_left_out<HD>(a, it.b, it.h, e, min(kb1 * 64, see0 + r / G + 1), x);
+        if constexpr (MODE == KEYS_ALL) {
+          chunk_left_out<HD>(a, it.b, it.h, e, min(kb1 * 64, see0 + r / G + 1), x);
+        } else {
+#pragma unroll
+          for (int d = 0; d < HD / 32; ++d) x[d] = 0.f;
+          window_left_out<HD>(a, it.b, it.h, see0 + r / G, see0, see_last, kb0, kb1, sinks, skip, x);
+        }
         bf16* out = static_cast<bf16*>(a.out) + (token0 + r / G) * a.os + (long long)(it.h * G + r % G) * HD + lane * (HD / 32);
         float* po = a.part_o + (part + r) * HD + lane * (HD / 32);
 #pragma unroll
@@ -1001,7 +1040,7 @@ __device__ __forceinline__ bool elect_one() {
 }
 __device__ __forceinline__ void tmem_st_wait_done() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-template <int HD>
+template <int HD, int MODE>
 __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int g_log, const __grid_constant__ CUtensorMap q_map,
                                                                 const __grid_constant__ CUtensorMap pool_map) {
   using Sh = PairShape<HD>;
@@ -1069,7 +1108,10 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
     tmem_relinquish();
   }
   pdl_wait();
-  chunk_plan(c, a.sp, s_base, s_red);
+  const auto sp = split_of<MODE>(a);
+  int sinks = 0;
+  if constexpr (MODE != KEYS_ALL) sinks = sp.sinks();
+  chunk_plan(c, sp, s_base, s_red);
   tc_fence_before();
   __syncthreads();  // barriers initialised, tensor memory allocated
   tc_fence_after();
@@ -1089,6 +1131,14 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
   };
   PairSeg s;
   unsigned segs = 0;  // read or published
+  auto skip_of = [&](int see0) {  // of the item whose first query is at entry see0
+    if constexpr (MODE == KEYS_ALL) return 0;
+    else return sp.skip_at(see0);
+  };
+  // does block kb of a row hold keys that some of the queries at entries see0 .. see_last see and others do not, or nobody?
+  auto partly_seen = [&](int kb, int see0, int see_last) {
+    return kb * 64 + 63 > see0 || (MODE != KEYS_ALL && kb * 64 <= hidden_to(see_last, a.window) && kb * 64 + 63 >= a.first);
+  };
 
   if (warp == 8) {
     // ---------------- producer ----------------
@@ -1098,7 +1148,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       s.nb = 0;
       ChunkItem it{};
       if (pos < end) {
-        it = chunk_item(c, a.sp, s_base, pos);
+        it = chunk_item(c, sp, s_base, pos);
         if (segs == 0 && lane == 0) join_note(a, &it, per);
         if (pos < it.first) pos = it.first;
       } else if (segs == 0 && lane == 0) {
@@ -1111,7 +1161,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         for (int x = 0; x < 2; ++x) {
           s.nq[x] = max(0, min(QT, left - x * QT));
           const int last = s.see0 + x * QT + s.nq[x] - 1;  // entry of the tile's last query
-          const int nb = s.nq[x] > 0 ? (last < 0 ? 1 : last / 64 + 1) : 0;
+          const int nb = s.nq[x] > 0 ? (last < 0 ? 1 : last / 64 + 1 - it.skip) : 0;
           s.e[x] = max(0, min(s.kb1, nb) - s.kb0);
         }
         pos = it.first + s.kb1;
@@ -1138,8 +1188,8 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       const int rowK = (c.layer * 2 * c.Hkv + s.h) * 64, rowV = rowK + c.Hkv * 64;
       for (int g0 = 0; g0 < E; g0 += 32) {
         int mine = -1;  // the pages of 32 blocks, one a lane; for one that is not there K is left as it is, V is zeros
-        if (g0 + lane < E && (s.kb0 + g0 + lane) * 64 < it.len)
-          mine = chunk_page(c.page_table, c.max_pages, c.n_pages, s.b, s.kb0 + g0 + lane, c.err);
+        const int at = block_at<MODE>(s.kb0 + g0 + lane, sinks, it.skip);
+        if (g0 + lane < E && at * 64 < it.len) mine = chunk_page(c.page_table, c.max_pages, c.n_pages, s.b, at, c.err);
         for (int i = 0; i < min(32, E - g0); ++i, ++blk) {
           const int page = __shfl_sync(0xffffffffu, mine, i);
           if (lane == 0 && ok) {
@@ -1186,12 +1236,17 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       if (lane == 0) mbar_arrive(seg_empty(segs));
       if (s.nb == 0) break;
       const int behind = s.see0 + s.nq[0] + s.nq[1];  // no query sees entries from here on
-      for (int kb = s.kb0; kb < s.kb1; ++kb, ++b) {
+      const int skip = skip_of(s.see0);
+      // nor, under a window, those from `first` up to gone_to; those up to edge_to not all queries
+      const int gone_to = MODE == KEYS_ALL ? -1 : hidden_to(s.see0, a.window), edge_to = MODE == KEYS_ALL ? -1 : hidden_to(behind - 1, a.window);
+      for (int i = s.kb0; i < s.kb1; ++i, ++b) {
+        const int kb = block_at<MODE>(i, sinks, skip);
         if (!wait_w(v_full(b), b / NST)) { ok = false; break; }
-        if (kb * 64 + 63 > s.see0) {
+        if (partly_seen(kb, s.see0, behind - 1)) {
           bool wrote = false;
           uint4* v = reinterpret_cast<uint4*>(sm + Sh::OFF_V + (b % NST) * Sh::T_BYTES) + lane;
-          for (int r0 = max(0, s.see0 + 1 - kb * 64) & ~15; r0 < 64; r0 += 16) {  // 16 keys; four of them take the warp's lanes
+          const bool edge = MODE != KEYS_ALL && kb * 64 <= edge_to;
+          for (int r0 = edge ? 0 : max(0, s.see0 + 1 - kb * 64) & ~15; r0 < 64; r0 += 16) {  // 16 keys; four of them take the warp's lanes
             uint4 u[4][Sh::ATOMS];
             uint32_t any = 0;  // the sign bits: exponents that are all ones
 #pragma unroll
@@ -1212,10 +1267,11 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
               for (int k = 0; k < Sh::ATOMS; ++k) {  // (a row keeps its place in the swizzle)
                 const uint4 w = u[i][k], out = make_uint4(bf16x2_not_finite(w.x), bf16x2_not_finite(w.y), bf16x2_not_finite(w.z), bf16x2_not_finite(w.w));
                 uint4& at = v[(r0 + 4 * i) * 8 + k * (Sh::COL / 16)];
-                if (key >= behind) {
+                const bool hides = MODE != KEYS_ALL && key >= a.first;
+                if (key >= behind || (hides && key <= gone_to)) {
                   at = make_uint4(0, 0, 0, 0);
                   wrote = true;
-                } else if (key > s.see0 && (out.x | out.y | out.z | out.w)) {
+                } else if ((key > s.see0 || (hides && key <= edge_to)) && (out.x | out.y | out.z | out.w)) {
                   at = make_uint4(w.x & ~out.x, w.y & ~out.y, w.z & ~out.z, w.w & ~out.w);
                   s_left[segs % PairSeg::RING] = segs;
                   wrote = true;
@@ -1258,7 +1314,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         return s.nb > 0;
       };
       while (ok && next()) {
-        const int E = s.kb1 - s.kb0, e = x ? s.e[1] : s.e[0];
+        const int E = s.kb1 - s.kb0, e = x ? s.e[1] : s.e[0], skip = skip_of(s.see0), see_last = s.see0 + s.nq[0] + s.nq[1] - 1;
         ok = e == 0 || wait(q_full(x), qn++);
         for (int i = 0; i < min(2, E) && ok; ++i) {  // S of the first two blocks
           ok = wait(k_full(blk + i), (blk + i) / NST);
@@ -1270,7 +1326,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         if (ok && E <= 2) tc_commit(q_free);
         for (int i = 0; i < E && ok; ++i) {
           const unsigned b = blk + i;
-          const bool more = i + 2 < E, tail = (s.kb0 + i) * 64 + 63 > s.see0;
+          const bool more = i + 2 < E, tail = partly_seen(block_at<MODE>(s.kb0 + i, sinks, skip), s.see0, see_last);
           // (what this tile does not use it waits for and releases all the same, in step with the other)
           ok = wait(v_full(b), b / NST) && (!tail || wait(v_tail(b), tails >> b % NST)) &&
                (!more || wait(k_full(b + 2), (b + 2) / NST)) && (i >= e || wait(p_full(x, n), n >> 1));
@@ -1316,22 +1372,24 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       const bool row_ok = qi < s.nq[x];
       const int see = row_ok ? s.see0 + x * QT + qi : -1;  // a row past the tile's queries sees nothing
       const int see0 = s.see0 + x * QT;                    // of the tile's first query
+      const int skip = skip_of(s.see0), see_last = see0 + s.nq[x] - 1, hid = MODE == KEYS_ALL ? -1 : hidden_to(see, a.window);
       float m_run = -INFINITY, l_run = 0.f;                // m in units of the raw scores
       for (int i = 0; i < s.e[x]; ++i, ++n) {
         if (!wait_w(s_full(x, n), n >> 1)) { ok = false; break; }
         tc_fence_after();
-        const int key0 = (s.kb0 + i) * 64;
+        const int key0 = block_at<MODE>(s.kb0 + i, sinks, skip) * 64;
         const uint32_t t_sn = t_s + 64u * (n & 1);
         uint32_t su[64];
         tmem_ld_32_issue(t_sn, su);
         tmem_ld_32_issue(t_sn + 32, su + 32);
         const bool gone = s_flag[(blk + i) % Sh::FLAGS] != 0;
         tmem_ld_wait();
-        if (key0 + 63 > see0 || gone || !__all_sync(0xffffffffu, row_ok)) {
-          const int vis = gone ? -1 : see - key0;  // columns 0..vis are visible
+        if (partly_seen(key0 / 64, see0, see_last) || gone || !__all_sync(0xffffffffu, row_ok)) {
+          const int vis = gone ? -1 : see - key0;  // columns 0..vis are visible, but for past..low under a window
+          const int past = a.first - key0, low = hid - key0;
 #pragma unroll
           for (int k = 0; k < 64; ++k)
-            if (k > vis) su[k] = 0xff800000u;  // -inf
+            if (k > vis || (MODE != KEYS_ALL && k >= past && k <= low)) su[k] = 0xff800000u;  // -inf
         }
         float pm4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -1428,7 +1486,13 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
           const int see_r = __shfl_sync(0xffffffffu, see, i), head_r = __shfl_sync(0xffffffffu, head, i), prow_r = __shfl_sync(0xffffffffu, prow, i);
           const long long token_r = __shfl_sync(0xffffffffu, token, i);
           if (see_r < 0) continue;
-          chunk_left_out<HD>(a, s.b, s.h, e, min(s.kb1 * 64, see_r + 1), left);
+          if constexpr (MODE == KEYS_ALL) {
+            chunk_left_out<HD>(a, s.b, s.h, e, min(s.kb1 * 64, see_r + 1), left);
+          } else {
+#pragma unroll
+            for (int k = 0; k < HD / 32; ++k) left[k] = 0.f;
+            window_left_out<HD>(a, s.b, s.h, see_r, s.see0, s.see0 + s.nq[0] + s.nq[1] - 1, s.kb0, s.kb1, sinks, skip, left);
+          }
           bf16* out = static_cast<bf16*>(a.out) + token_r * a.os + (long long)head_r * HD + lane * (HD / 32);
 #pragma unroll
           for (int k = 0; k < HD / 32; ++k) {
@@ -2061,13 +2125,13 @@ static bool q_map(CUtensorMap* m, const ChunkAttn& a) {
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.q), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-template <int HD>
+template <int HD, int MODE>
 static cudaError_t pair_launch(const ChunkAttn& a, cudaStream_t st) {
   CUtensorMap qm, pm;
   if (!q_map(&qm, a) || !pool_map(&pm, a.c)) return cudaErrorInvalidValue;
   using Sh = PairShape<HD>;
-  if (cudaError_t e = ensure_kernel_attrs(reinterpret_cast<const void*>(k_chunk_pair<HD>), Sh::bytes(SV_MAX_ROWS))) return e;
-  return launch_k(k_chunk_pair<HD>, dim3(a.ctas), dim3(PAIR_THREADS), Sh::bytes(a.c.n), st, a, pow2_log(a.c.G), qm, pm);
+  if (cudaError_t e = ensure_kernel_attrs(reinterpret_cast<const void*>(k_chunk_pair<HD, MODE>), Sh::bytes(SV_MAX_ROWS))) return e;
+  return launch_k(k_chunk_pair<HD, MODE>, dim3(a.ctas), dim3(PAIR_THREADS), Sh::bytes(a.c.n), st, a, pow2_log(a.c.G), qm, pm);
 }
 template <int HD>
 static cudaError_t weigh_launch(ChunkAttn a, const tlf_attn_chunk_args& args, float* part, int num_sms, cudaStream_t st) {
@@ -2082,19 +2146,23 @@ static cudaError_t weigh_launch(ChunkAttn a, const tlf_attn_chunk_args& args, fl
   const int per_row = std::max(1, std::min(8, 1024 / a.c.n));
   return launch_k(k_weigh_join, dim3(a.ctas - 1 + per_row * a.c.n), dim3(256), (a.c.n + 1) * 8, st, a, w, per_row);
 }
-template <int HD, int MT>
+template <int HD, int MT, int MODE>
 static cudaError_t mma_launch(const ChunkAttn& a, cudaStream_t st) {
   CUtensorMap map;
   if (!pool_map(&map, a.c)) return cudaErrorInvalidValue;
   using Sh = MmaShape<HD, MT>;
-  if (cudaError_t e = ensure_kernel_attrs(reinterpret_cast<const void*>(k_chunk_mma<HD, MT>), Sh::bytes(SV_MAX_ROWS))) return e;
-  return launch_k(k_chunk_mma<HD, MT>, dim3(a.ctas), dim3(Sh::THREADS), Sh::bytes(a.c.n), st, a, map);
+  if (cudaError_t e = ensure_kernel_attrs(reinterpret_cast<const void*>(k_chunk_mma<HD, MT, MODE>), Sh::bytes(SV_MAX_ROWS))) return e;
+  return launch_k(k_chunk_mma<HD, MT, MODE>, dim3(a.ctas), dim3(Sh::THREADS), Sh::bytes(a.c.n), st, a, map);
 }
-template <int HD>
+template <int HD, int MODE>
 static cudaError_t mma_rows(const ChunkAttn& a, cudaStream_t st) {
   if constexpr (HD >= 64)
-    if (a.rows == 256) return pair_launch<HD>(a, st);
-  return a.rows == 16 ? mma_launch<HD, 1>(a, st) : a.rows == 32 ? mma_launch<HD, 2>(a, st) : mma_launch<HD, 4>(a, st);
+    if (a.rows == 256) return pair_launch<HD, MODE>(a, st);
+  return a.rows == 16 ? mma_launch<HD, 1, MODE>(a, st) : a.rows == 32 ? mma_launch<HD, 2, MODE>(a, st) : mma_launch<HD, 4, MODE>(a, st);
+}
+template <int MODE>
+static cudaError_t bf16_launch(const ChunkAttn& a, cudaStream_t st) {
+  return a.c.hd == 32 ? mma_rows<32, MODE>(a, st) : a.c.hd == 64 ? mma_rows<64, MODE>(a, st) : mma_rows<128, MODE>(a, st);
 }
 template <typename T, int MODE>
 static cudaError_t simt_rows(const ChunkAttn& a, cudaStream_t st) {
@@ -2120,7 +2188,7 @@ template <typename T>
 static cudaError_t chunk_launch(const ChunkAttn& a, const tlf_attn_chunk_args& args, float* weigh, int num_sms, cudaStream_t st) {
   cudaError_t e;
   if (std::is_same<T, bf16>::value)
-    e = a.c.hd == 32 ? mma_rows<32>(a, st) : a.c.hd == 64 ? mma_rows<64>(a, st) : mma_rows<128>(a, st);
+    e = bf16_launch<KEYS_ALL>(a, st);
   else
     e = simt_rows<T, KEYS_ALL>(a, st);
   if (e) return e;
@@ -2171,6 +2239,10 @@ cudaError_t launch_chunk_attn(const ChunkDev& c, int dtype, const tlf_attn_chunk
   return dtype == TLF_DTYPE_BF16 ? chunk_launch<bf16>(a, args, weigh, num_sms, st) : chunk_launch<float>(a, args, weigh, num_sms, st);
 }
 
+static tlf_attn_chunk_args plain_args(const tlf_attn_window_args& a) {
+  return tlf_attn_chunk_args{a.q, a.q_stride, a.out, a.out_stride, a.lse, nullptr, nullptr, a.scale, 0};
+}
+
 // tlf_attn_window. A window of 0 over a cache in the dtype is tlf_attn_chunk's case, and its kernels'.
 struct WindowPath {
   int rt, ctas, pad;  // as in ChunkPath
@@ -2179,9 +2251,16 @@ struct WindowPath {
 static WindowPath window_path(const ChunkDev& c, int dtype, const tlf_attn_window_args& a, int num_sms) {
   WindowPath p{};
   const long long rows = (long long)c.max_chunk * c.G;
-  p.rt = rows <= 16 ? 16 : 64;
-  p.ctas = 2 * num_sms;
-  p.pad = PAD_SIMT;
+  if (dtype == TLF_DTYPE_BF16 && a.kv_format == TLF_KV_PLAIN) {  // as without a window
+    const ChunkPath whole = chunk_path(c, dtype, plain_args(a), num_sms);
+    p.rt = whole.rt;
+    p.ctas = whole.ctas;
+    p.pad = whole.pad;
+  } else {
+    p.rt = rows <= 16 ? 16 : 64;
+    p.ctas = 2 * num_sms;
+    p.pad = PAD_SIMT;
+  }
   const int qt_log = pow2_log(std::max(1, p.rt / c.G));
   p.ctas = (int)std::min<double>(p.ctas, std::max(1.0, ((double)(c.T >> qt_log) + c.n) * c.Hkv * ((double)c.max_pages + p.pad)));
   size_t o = 0;
@@ -2193,16 +2272,17 @@ static WindowPath window_path(const ChunkDev& c, int dtype, const tlf_attn_windo
   p.total = o;
   return p;
 }
-static tlf_attn_chunk_args plain_args(const tlf_attn_window_args& a) {
-  return tlf_attn_chunk_args{a.q, a.q_stride, a.out, a.out_stride, a.lse, nullptr, nullptr, a.scale, 0};
-}
 size_t window_attn_scratch(const ChunkDev& c, int dtype, const tlf_attn_window_args& a, int num_sms) {
   if (a.window == 0 && a.kv_format == TLF_KV_PLAIN) return chunk_attn_scratch(c, dtype, plain_args(a), num_sms);
   return window_path(c, dtype, a, num_sms).total;
 }
 template <typename T>
 static cudaError_t window_launch(const ChunkAttn& a, int kv_format, cudaStream_t st) {
-  if (cudaError_t e = kv_format == TLF_KV_4BIT ? simt_rows<T, KEYS_4BIT>(a, st) : simt_rows<T, KEYS_WINDOW>(a, st)) return e;
+  cudaError_t e;
+  if (kv_format == TLF_KV_4BIT) e = simt_rows<T, KEYS_4BIT>(a, st);
+  else if constexpr (std::is_same<T, bf16>::value) e = bf16_launch<KEYS_WINDOW>(a, st);
+  else e = simt_rows<T, KEYS_WINDOW>(a, st);
+  if (e) return e;
   return join_launch<T>(a, st);
 }
 cudaError_t launch_window_attn(const ChunkDev& c, int dtype, const tlf_attn_window_args& args, void* scratch, int num_sms,

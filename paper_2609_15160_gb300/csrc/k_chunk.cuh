@@ -65,11 +65,11 @@ struct WindowSplit : ChunkSplit {
   int window, first;  // window 2^31 - 1: none
 
   __host__ __device__ int sinks() const { return (int)(((long long)first + (1 << bk_log) - 1) >> bk_log); }
-  __host__ __device__ int skip(int s0, int t) const {
-    const long long low = s0 + ((long long)t << qt_log) - window + 1;
-    const long long n = (low > 0 ? low >> bk_log : 0) - sinks();
+  __host__ __device__ int skip_at(long long entry) const {  // of a tile by its first query's entry
+    const long long low = entry - window + 1, n = (low > 0 ? low >> bk_log : 0) - sinks();
     return n > 0 ? (int)n : 0;
   }
+  __host__ __device__ int skip(int s0, int t) const { return skip_at(s0 + ((long long)t << qt_log)); }
   __host__ __device__ int blocks(int s0, int ql, int t) const { return ChunkSplit::blocks(s0, ql, t) - skip(s0, t); }
   // sum over u = 0 .. n - 1 of floor(u / 2^r)
   __host__ __device__ static long long floor_sum(long long n, int r) {
