@@ -14,119 +14,16 @@
 // k_chunk_weigh_scores  from the scores that k_chunk_mma leaves;
 // k_chunk_weigh         the rest, on the CUDA cores.
 #include <algorithm>
-#include <type_traits>
 
-#include "k_chunk.cuh"
+#include "k_chunk4.cuh"
+#include "k_chunk_dev.cuh"
 #include "k_kv4.cuh"
-#include "k_serve.cuh"
 
 namespace tlf {
-
-struct ChunkAttn {
-  ChunkDev c;
-  ChunkSplit sp;
-  const void* q;
-  long long qs;
-  void* out;
-  long long os;
-  float* lse;      // [T][Hq] or NULL
-  float scale;     // of the scores, times log2 e
-  int ctas, rows;  // CTAs that share the blocks; rows of a part
-  float* scores;   // k_chunk_mma: [T][Hq][max_pages * 64] scores that it leaves for the weights, or NULL
-  uint32_t* werr;  // error word of the waits: the caller's, or one in the scratch
-  float* part_o;   // [2 ctas][rows][hd]; of k_chunk_pair [2 ctas][hd / 4][rows][4]
-  float2* part_ml; // [2 ctas][rows]
-  int4* join;      // [ctas] what each CTA leaves to k_chunk_join
-  int window, first;  // tlf_attn_window's; 2^31 - 1 and 0 where there is no window
-};
-
-// What a kernel's keys are: every entry up to the query's, of a cache in the dtype; those of a window; those of a window, of a
-// cache in 4 bits.
-enum ChunkKeys { KEYS_ALL = 0, KEYS_WINDOW = 1, KEYS_4BIT = 2 };
-template <int MODE>
-__device__ __forceinline__ auto split_of(const ChunkAttn& a) {
-  if constexpr (MODE == KEYS_ALL) return a.sp;
-  else return WindowSplit{a.sp, a.window, a.first};
-}
-// Number in its row of an item's block i; the last entry of a row that the window hides from a query at entry `see`.
-template <int MODE>
-__device__ __forceinline__ int block_at(int i, int sinks, int skip) { return MODE == KEYS_ALL || i < sinks ? i : i + skip; }
-__device__ __forceinline__ int hidden_to(int see, int window) { return see < window ? -1 : see - window; }
-
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-
-// base[b] = blocks of the rows before b; base[n] = all. By the whole block.
-template <class Split>
-__device__ __forceinline__ void chunk_plan(const ChunkDev& c, const Split& sp, long long* base, long long* red) {
-  long long carry = 0;
-  for (int b0 = 0; b0 < c.n; b0 += blockDim.x) {
-    const int b = b0 + threadIdx.x;
-    long long u = 0;
-    if (b < c.n) {
-      const ChunkRow r = chunk_row(c, b);
-      u = sp.before(r.len - r.ql, r.ql, sp.tiles(r.ql)) * c.Hkv;
-    }
-    long long total;
-    const long long at = carry + block_scan(u, red, &total);
-    if (b < c.n) base[b] = at;
-    carry += total;
-  }
-  if (threadIdx.x == 0) base[c.n] = carry;
-  __syncthreads();
-}
-
-__device__ __forceinline__ long long chunk_share(const ChunkAttn& a, long long all) {
-  return all > 0 ? (all + a.ctas - 1) / a.ctas : 1;
-}
-
-// The item that holds block `pos` of the flat order.
-struct ChunkItem {
-  int b, h, t, nb;     // row, kv head, tile, its blocks
-  int t0, s0, ql, len; // the row's first new token, old entries, new tokens, entries
-  long long first;     // the item's first block in the flat order (may lie behind `pos`, which then is in its pad)
-  int skip;            // blocks behind those of the first entries that the window leaves out
-};
-template <class Split>
-__device__ __forceinline__ ChunkItem chunk_item(const ChunkDev& c, const Split& sp, const long long* base, long long pos) {
-  int lo = 0, hi = c.n;  // largest b with base[b] <= pos (rows without tokens have no blocks)
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (base[mid] <= pos) lo = mid;
-    else hi = mid;
-  }
-  const ChunkRow r = chunk_row(c, lo);
-  ChunkItem it;
-  it.b = lo;
-  it.t0 = r.t0;
-  it.ql = r.ql;
-  it.len = r.len;
-  it.s0 = r.len - r.ql;
-  const long long rel = pos - base[lo], per = (base[lo + 1] - base[lo]) / c.Hkv;
-  it.h = (int)(rel / per);
-  const long long at = rel - it.h * per;
-  it.t = sp.tile_of(it.s0, it.ql, at);
-  it.nb = sp.blocks(it.s0, it.ql, it.t);
-  it.first = base[lo] + it.h * per + sp.before(it.s0, it.ql, it.t) + sp.pad;
-  it.skip = 0;
-  if constexpr (std::is_same<Split, WindowSplit>::value) it.skip = sp.skip(it.s0, it.t);
-  return it;
-}
 
 // ----------------------------------------------------------------------------
 // Joining the parts of shared items
 // ----------------------------------------------------------------------------
-// The first CTA whose share starts inside an item notes it: {the tile's first token, kv head, rows, parts}, parts = 0 where there
-// is none. CTA c's first item has its part at 2c if it began in an earlier share, the part of an item that goes on past its
-// share is at 2c + 1. One thread of every CTA calls this, before any wait; it: what the CTA's share starts with, or NULL.
-__device__ __forceinline__ void join_note(const ChunkAttn& a, const ChunkItem* it, long long per) {
-  int4 j = make_int4(0, 0, 0, 0);
-  const long long pos = blockIdx.x * per;
-  if (it && it->first < pos && it->first >= pos - per) {
-    const int qt = 1 << a.sp.qt_log, last = (int)((it->first + it->nb - 1) / per);  // the last CTA with a part
-    j = make_int4(it->t0 + it->t * qt, it->h, min(qt, it->ql - it->t * qt) * a.c.G, last - (int)blockIdx.x + 2);
-  }
-  a.join[blockIdx.x] = j;
-}
 // A warp takes a row at a time, VW dims a lane (hd = 32 VW, or 16 with VW = 1), and every eight-th row of a CTA's. It reads the
 // notes rather than plan again, which took 3 us.
 template <typename T, int VW>
@@ -217,13 +114,7 @@ __global__ void __launch_bounds__(256) k_chunk_join(ChunkAttn a) {
   }
 }
 
-// The parts of k_chunk_pair, whose threads have a row each: they leave four dims of all rows side by side, so that a warp writes
-// whole lines (row by row, 16 bytes a lane in 32 lines, a part of 256 rows took 4 us). A warp here has 8 rows and half the
-// dims; a lane one row and every fourth 16 bytes of it.
-constexpr int PAIR_ROWS = 256;
-__device__ __forceinline__ size_t pair_part(int slot, int row, int d, int hd) {  // of 16 bytes from dim d on
-  return (size_t)slot * PAIR_ROWS * hd + ((size_t)(d >> 2) * PAIR_ROWS + row) * 4 + (d & 3);
-}
+// The parts of k_chunk_pair: a warp has 8 rows and half the dims, a lane one row and every fourth 16 bytes of it.
 template <int HD>
 __global__ void __launch_bounds__(256) k_pair_join(ChunkAttn a) {  // grid y = 8
   pdl_trigger();
@@ -526,22 +417,6 @@ __device__ __forceinline__ void mma_16816(float* d, const uint32_t* a, uint32_t 
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void bar_named(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-
-// Barrier `id` of `threads` threads; whether any of them has p.
-__device__ __forceinline__ bool bar_any(int id, int threads, bool p) {
-  int r;
-  asm volatile(
-      "{\n\t.reg .pred q, s;\n\t"
-      "setp.ne.s32 q, %3, 0;\n\t"
-      "bar.red.or.pred s, %1, %2, q;\n\t"
-      "selp.s32 %0, 1, 0, s;\n\t}"
-      : "=r"(r)
-      : "r"(id), "r"(threads), "r"((int)p)
-      : "memory");
-  return r != 0;
-}
-
 // 0xffff for each half that is an infinity or NaN of bfloat16.
 __device__ __forceinline__ uint32_t bf16x2_not_finite(uint32_t v) { return __vcmpeq2(v & 0x7f807f80u, 0x7f807f80u); }
 
@@ -993,11 +868,6 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
 // for 8192 causal tokens (1405).
 constexpr int PAIR_THREADS = 384;
 
-struct PairSeg {  // a CTA's part of an item: blocks kb0 .. kb1 - 1 of nb, of which tile x has the first e[x]; nb = 0: no more
-  int b, h, token0, see0, nq[2], e[2], kb0, kb1, nb, none;
-  static constexpr int RING = 4;
-};
-
 template <int HD>
 struct PairShape {
   static constexpr int ATOMS = HD / 64, QCOL = 128 * 128, Q_BYTES = ATOMS * QCOL;  // a tile of 128 rows of q
@@ -1011,34 +881,6 @@ struct PairShape {
   static int bytes(int n) { return std::max(OFF_BASE + (n + 1) * 8 + 1024, tmem_min_smem(512)); }
   static constexpr uint32_t OCOL = 256;
 };
-
-// D(tmem) (+)= A(tmem) * B(smem desc)
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t at, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(at), "l"(b), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-__device__ __forceinline__ void tmem_put_16(uint32_t taddr, const uint32_t* r) {  // completes at the next wait::st
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
-
-// One thread of a converged warp.
-__device__ __forceinline__ bool elect_one() {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "elect.sync _|p, 0xffffffff;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(r));
-  return r != 0;
-}
-__device__ __forceinline__ void tmem_st_wait_done() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 template <int HD, int MODE>
 __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int g_log, const __grid_constant__ CUtensorMap q_map,
@@ -2030,7 +1872,7 @@ __global__ void __launch_bounds__(256) k_weigh_join(ChunkAttn a, WeighTc wt, int
 // 225 / 194, 4 x 1000 over 4000 entries 87 / 81; at 0 / 10 pages of k_chunk_mma with head_dim 64: 32 single tokens over up to
 // 8192 entries 119 / 105, 32 rows of up to 16 tokens 128 / 107; at 2 / 6 pages with head_dim 128: 100 single tokens over up to
 // 500 entries 45 / 40). Without, CTAs with many short items finished up to a third later than the others.
-constexpr int PAD_PAIR = 4, PAD_MMA128 = 6, PAD_MMA = 10, PAD_SIMT = 2;
+constexpr int PAD_PAIR = 4, PAD_MMA128 = 6, PAD_MMA = 10, PAD_SIMT = 2, PAD_Q4 = 6;
 struct ChunkPath {
   bool pair;    // k_chunk_pair
   int rt;       // rows of an item
@@ -2176,7 +2018,7 @@ static cudaError_t simt_rows(const ChunkAttn& a, cudaStream_t st) {
   return cudaErrorInvalidValue;
 }
 template <typename T>
-static cudaError_t join_launch(const ChunkAttn& a, cudaStream_t st) {
+static cudaError_t join_launch(const ChunkAttn& a, cudaStream_t st) {  // of T
   const dim3 jg(a.ctas - 1, std::max(1, a.rows / 32));
   if (a.ctas <= 1) return cudaSuccess;
   return a.rows == PAIR_ROWS ? (a.c.hd == 128 ? launch_k(k_pair_join<128>, jg, dim3(256), 0, st, a) : launch_k(k_pair_join<64>, jg, dim3(256), 0, st, a))
@@ -2256,6 +2098,10 @@ static WindowPath window_path(const ChunkDev& c, int dtype, const tlf_attn_windo
     p.rt = whole.rt;
     p.ctas = whole.ctas;
     p.pad = whole.pad;
+  } else if (dtype == TLF_DTYPE_BF16 && c.G <= 16) {
+    p.rt = rows <= 8 ? 8 : 16;
+    p.ctas = chunk4_per_sm(c.hd, p.rt) * num_sms;
+    p.pad = PAD_Q4;
   } else {
     p.rt = rows <= 16 ? 16 : 64;
     p.ctas = 2 * num_sms;
@@ -2279,7 +2125,8 @@ size_t window_attn_scratch(const ChunkDev& c, int dtype, const tlf_attn_window_a
 template <typename T>
 static cudaError_t window_launch(const ChunkAttn& a, int kv_format, cudaStream_t st) {
   cudaError_t e;
-  if (kv_format == TLF_KV_4BIT) e = simt_rows<T, KEYS_4BIT>(a, st);
+  if (std::is_same<T, bf16>::value && kv_format == TLF_KV_4BIT && a.rows <= 16 && a.c.G <= 16) e = launch_chunk4(a, st);
+  else if (kv_format == TLF_KV_4BIT) e = simt_rows<T, KEYS_4BIT>(a, st);
   else if constexpr (std::is_same<T, bf16>::value) e = bf16_launch<KEYS_WINDOW>(a, st);
   else e = simt_rows<T, KEYS_WINDOW>(a, st);
   if (e) return e;
