@@ -1956,9 +1956,7 @@ static bool pool_map(CUtensorMap* m, const ChunkDev& c) {
             c.hd == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// 3-D map over q: {head_dim, Hq, tokens}, boxes of 64 elements x the heads of a kv head x 128 / G tokens, one column of a tile
-// of 128 rows; tokens past the last read as zeros.
-static bool q_map(CUtensorMap* m, const ChunkAttn& a) {
+bool chunk_q_map(CUtensorMap* m, const ChunkAttn& a) {
   const auto fn = tensor_map_encoder();
   if (!fn) return false;
   cuuint64_t dims[3] = {(cuuint64_t)a.c.hd, (cuuint64_t)a.c.Hq, (cuuint64_t)a.c.T};
@@ -1970,7 +1968,7 @@ static bool q_map(CUtensorMap* m, const ChunkAttn& a) {
 template <int HD, int MODE>
 static cudaError_t pair_launch(const ChunkAttn& a, cudaStream_t st) {
   CUtensorMap qm, pm;
-  if (!q_map(&qm, a) || !pool_map(&pm, a.c)) return cudaErrorInvalidValue;
+  if (!chunk_q_map(&qm, a) || !pool_map(&pm, a.c)) return cudaErrorInvalidValue;
   using Sh = PairShape<HD>;
   if (cudaError_t e = ensure_kernel_attrs(reinterpret_cast<const void*>(k_chunk_pair<HD, MODE>), Sh::bytes(SV_MAX_ROWS))) return e;
   return launch_k(k_chunk_pair<HD, MODE>, dim3(a.ctas), dim3(PAIR_THREADS), Sh::bytes(a.c.n), st, a, pow2_log(a.c.G), qm, pm);
@@ -1979,7 +1977,7 @@ template <int HD>
 static cudaError_t weigh_launch(ChunkAttn a, const tlf_attn_chunk_args& args, float* part, int num_sms, cudaStream_t st) {
   a.ctas = num_sms;
   CUtensorMap qm, pm;
-  if (!q_map(&qm, a) || !pool_map(&pm, a.c)) return cudaErrorInvalidValue;
+  if (!chunk_q_map(&qm, a) || !pool_map(&pm, a.c)) return cudaErrorInvalidValue;
   using Sh = WeighShape<HD>;
   if (cudaError_t e = ensure_kernel_attrs(reinterpret_cast<const void*>(k_weigh_tc<HD>), Sh::bytes(SV_MAX_ROWS))) return e;
   const WeighTc w{WeighSplit{7 - pow2_log(a.c.G), 8}, args.weight_in, args.weight_out, part};
@@ -2088,6 +2086,7 @@ static tlf_attn_chunk_args plain_args(const tlf_attn_window_args& a) {
 // tlf_attn_window. A window of 0 over a cache in the dtype is tlf_attn_chunk's case, and its kernels'.
 struct WindowPath {
   int rt, ctas, pad;  // as in ChunkPath
+  bool four;          // k_chunk4.cu's kernels
   size_t part_ml, join, werr, total;
 };
 static WindowPath window_path(const ChunkDev& c, int dtype, const tlf_attn_window_args& a, int num_sms) {
@@ -2098,7 +2097,14 @@ static WindowPath window_path(const ChunkDev& c, int dtype, const tlf_attn_windo
     p.rt = whole.rt;
     p.ctas = whole.ctas;
     p.pad = whole.pad;
+  } else if (dtype == TLF_DTYPE_BF16 && c.hd >= 64 && (c.G & (c.G - 1)) == 0 && rows > 16 && reinterpret_cast<uintptr_t>(a.q) % 16 == 0 &&
+             a.q_stride % 8 == 0) {
+    p.four = true;
+    p.rt = PAIR_ROWS;
+    p.ctas = num_sms;
+    p.pad = PAD_PAIR;
   } else if (dtype == TLF_DTYPE_BF16 && c.G <= 16) {
+    p.four = true;
     p.rt = rows <= 8 ? 8 : 16;
     p.ctas = chunk4_per_sm(c.hd, p.rt) * num_sms;
     p.pad = PAD_Q4;
@@ -2123,9 +2129,9 @@ size_t window_attn_scratch(const ChunkDev& c, int dtype, const tlf_attn_window_a
   return window_path(c, dtype, a, num_sms).total;
 }
 template <typename T>
-static cudaError_t window_launch(const ChunkAttn& a, int kv_format, cudaStream_t st) {
+static cudaError_t window_launch(const ChunkAttn& a, int kv_format, bool four, cudaStream_t st) {
   cudaError_t e;
-  if (std::is_same<T, bf16>::value && kv_format == TLF_KV_4BIT && a.rows <= 16 && a.c.G <= 16) e = launch_chunk4(a, st);
+  if (std::is_same<T, bf16>::value && kv_format == TLF_KV_4BIT && four) e = launch_chunk4(a, st);
   else if (kv_format == TLF_KV_4BIT) e = simt_rows<T, KEYS_4BIT>(a, st);
   else if constexpr (std::is_same<T, bf16>::value) e = bf16_launch<KEYS_WINDOW>(a, st);
   else e = simt_rows<T, KEYS_WINDOW>(a, st);
@@ -2154,7 +2160,7 @@ cudaError_t launch_window_attn(const ChunkDev& c, int dtype, const tlf_attn_wind
   a.join = reinterpret_cast<int4*>(s + p.join);
   a.window = args.window > 0 ? args.window : 0x7fffffff;
   a.first = args.window > 0 ? args.n_first : 0;
-  return dtype == TLF_DTYPE_BF16 ? window_launch<bf16>(a, args.kv_format, st) : window_launch<float>(a, args.kv_format, st);
+  return dtype == TLF_DTYPE_BF16 ? window_launch<bf16>(a, args.kv_format, p.four, st) : window_launch<float>(a, args.kv_format, p.four, st);
 }
 
 }  // namespace tlf

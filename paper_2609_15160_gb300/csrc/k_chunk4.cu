@@ -1,7 +1,8 @@
 // Attention of chunks of new tokens over caches in 4 bits, under a window or not (tlf_attn_window), bfloat16 calls. Items, their
 // split over the CTAs and the join are those of k_chunk.cu.
 //
-// k_chunk_q4   up to 16 query rows an item: codes straight from shared memory into mma.sync fragments.
+// k_chunk_q4     up to 16 query rows an item: codes straight from shared memory into mma.sync fragments;
+// k_chunk_pair4  more: codes turned into float16 tiles for tcgen05, pairs of 128-row tiles.
 #include <algorithm>
 
 #include <cuda_fp16.h>
@@ -505,6 +506,679 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
 }
 
 // ----------------------------------------------------------------------------
+// Many rows: tcgen05 (head_dim 64 and 128)
+// ----------------------------------------------------------------------------
+// Items, roles and tensor memory are k_chunk_pair's (k_chunk.cu): two tiles of 128 MMA rows, blocks of 64 keys, softmax with a thread a
+// row, an issuing warp a tile. What is different is where K and V come from: the producer copies a page's two blocks of codes, and four
+// warps (12-15) turn them into float16 tiles. With K' = d (n - 8), which is exact in float16 (8 bits times 3, or a power of two), scores
+// are exact but for float32's sums:
+//   q . k = sum q K' + sum over groups g of (lo_g + 8 d_g) (sum of q)_g
+// the second part as 16 more columns of the product: lo_0, lo_1, 8 d_0, 8 d_1 in K, three times beside the sums of q in three float16
+// that hold 33 bits. V' = lo + d n is rounded to float16, and so is P. Codes become numbers in one multiply-add a pair: the bits n
+// (or 16 n) of a masked word are the float16 n 2^-24. A word's eight values come out in the order 0 4 1 5 2 6 3 7; q is put into that
+// order, O is read out of it.
+//
+// Ranges: K of a block is divided by a power of two (the largest of |lo| and 16 d of the entries that some query sees gets into 2^-6 ..
+// 2^-5), q of a row multiplied by one (2^8 .. 2^9); the softmax undoes both. V is divided by 2^(e + 6), which goes into the score: M is
+// the largest s_t + e, O = sum 2^(s_t + e - M) V_t / 2^(e + 6), l = sum 2^(s_t + e - M) 2^-e, so that what has to be held in 16 bits is
+// relative to the row's largest term. e is the block's, by its largest entry; in a block with entries smaller than 2^-6 of that (as the
+// first tokens' values may be, which take most of the probability) every entry has its own: e_t - e is three more of the 16 columns,
+// beside 1 / (what the softmax multiplies by) in three float16, and 2^-e_t is read from shared memory (16 reads of 16 bytes a thread,
+// in the chain that bounds the kernel: with them in every block 721 us where it is 449 without). Where e_t - e does not fit float16
+// (scales over 2^12, keys over 2^18) entries keep the block's.
+constexpr int PAIR4_THREADS = 512;
+template <int HD>
+struct Pair4Shape {
+  using F = Kv4<HD>;
+  static constexpr int ATOMS = HD / 64, QCOL = 128 * 128, Q_BYTES = ATOMS * QCOL;  // a tile of 128 rows of q
+  static constexpr int COL = 64 * 128, T_BYTES = ATOMS * COL;                      // 64 rows of K or V
+  static constexpr int QX = 128 * 32, KX = 64 * 32, RAW = 2 * F::BLOCK;            // the 16 more columns; a page's codes and pairs
+  static constexpr int NST = HD == 128 ? 3 : 4, NRAW = HD == 128 ? 4 : 6;
+  static constexpr int OFF_K = 2 * Q_BYTES, OFF_V = OFF_K + NST * T_BYTES, OFF_QX = OFF_V + NST * T_BYTES, OFF_KX = OFF_QX + 2 * QX,
+                       OFF_RAW = OFF_KX + NST * KX, OFF_BAR = OFF_RAW + NRAW * RAW;
+  static constexpr int NBAR = 4 * NST + 3 * NRAW + 2 + 2 + 4 + 4 + 4 + 1 + 2 * PairSeg::RING;
+  static constexpr int FLAGS = 16;  // more than the blocks that the producer can be ahead of the softmax
+  static constexpr int WS = 8;      // .. that the codes' warps can
+  static constexpr int OFF_INT = OFF_BAR + NBAR * 8, OFF_INFO = (OFF_INT + (FLAGS + 4) * 4 + 15) / 16 * 16,
+                       OFF_W = OFF_INFO + FLAGS * 16, OFF_SEG = OFF_W + WS * 64 * 4;
+  static constexpr int OFF_BASE = OFF_SEG + PairSeg::RING * (int)sizeof(PairSeg);
+  static int bytes(int n) { return std::max(OFF_BASE + (n + 1) * 8 + 1024, tmem_min_smem(512)); }
+  static constexpr uint32_t OCOL = 256;
+};
+// Instruction descriptor: kind::f16, A = B = float16, D = float32, both K-major.
+constexpr uint32_t idesc_f16_f32(int M, int N) { return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24); }
+// Descriptor of a K-major tile of 16 columns: rows of 32 bytes, swizzled in atoms of 8 rows (the halves of rows 4-7 change places).
+__device__ __forceinline__ uint64_t smem_desc_x(uint32_t saddr) {
+  return (uint64_t)((saddr >> 4) & 0x3FFFu) | (uint64_t)1u << 16 | (uint64_t)(256u >> 4) << 32 | (uint64_t)1u << 46 | (uint64_t)6u << 61;
+}
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(max(-126, min(127, e)) + 127) << 23); }
+__device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  return r;
+}
+__device__ __forceinline__ uint32_t twice_f16(float x) { return pack_f16(x, x); }
+__device__ __forceinline__ void st_shared_16(uint32_t at, uint4 v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+// Eight values of a word, x -> n d + c (d24, d20: d times 2^24 and 2^20), in the order 0 4 1 5 2 6 3 7.
+__device__ __forceinline__ uint4 f16_values(uint32_t w, uint32_t d24, uint32_t d20, uint32_t c) {
+  const uint32_t x = w >> 8;
+  return make_uint4(fma_f16x2(w & 0x000f000fu, d24, c), fma_f16x2(w & 0x00f000f0u, d20, c), fma_f16x2(x & 0x000f000fu, d24, c),
+                    fma_f16x2(x & 0x00f000f0u, d20, c));
+}
+
+// Values that an asynchronous load has put into registers: no use of them moves up past this point.
+__device__ __forceinline__ void hold_32(uint32_t* r) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 8)
+    asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
+}
+
+template <int HD>
+__global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, int g_log, const __grid_constant__ CUtensorMap q_map) {
+  using Sh = Pair4Shape<HD>;
+  using F = Kv4<HD>;
+  constexpr int NST = Sh::NST, NRAW = Sh::NRAW, NG = F::NG;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ long long s_red[33];
+  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sm + Sh::OFF_BAR);
+  volatile int* s_flag = reinterpret_cast<volatile int*>(sm + Sh::OFF_INT);  // the block's page is not there
+  volatile int* abort_flag = s_flag + Sh::FLAGS;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + Sh::OFF_INT) + Sh::FLAGS + 1;
+  // of a block: what its raw scores are to be multiplied by (beside the row's power), e, 2^-e, and bits: 1 the page is not there,
+  // 2 entries have powers of their own
+  float4* s_info = reinterpret_cast<float4*>(sm + Sh::OFF_INFO);
+  float* s_w = reinterpret_cast<float*>(sm + Sh::OFF_W);  // [WS][64] 2^-e_t
+  PairSeg* s_seg = reinterpret_cast<PairSeg*>(sm + Sh::OFF_SEG);
+  long long* s_base = reinterpret_cast<long long*>(sm + Sh::OFF_BASE);
+  auto bar = [&](int i) { return smem_u32(&bars[i]); };
+  // block b of this CTA: its place in the rings, and the use's parity
+  auto k_full = [&](unsigned b) { return bar(b % NST); };
+  auto k_empty = [&](unsigned b) { return bar(NST + b % NST); };
+  auto v_full = [&](unsigned b) { return bar(2 * NST + b % NST); };
+  auto v_empty = [&](unsigned b) { return bar(3 * NST + b % NST); };
+  auto raw_full = [&](unsigned b) { return bar(4 * NST + b % NRAW); };
+  auto raw_empty = [&](unsigned b) { return bar(4 * NST + NRAW + b % NRAW); };
+  auto c_full = [&](unsigned b) { return bar(4 * NST + 2 * NRAW + b % NRAW); };
+  constexpr int B0 = 4 * NST + 3 * NRAW;
+  auto q_full = [&](int x) { return bar(B0 + x); };
+  auto q_ready = [&](int x) { return bar(B0 + 2 + x); };
+  // block n of tile x, as in k_chunk_pair: S written, P written, P V done
+  auto s_full = [&](int x, unsigned n) { return bar(B0 + 4 + 2 * x + (n & 1)); };
+  auto p_full = [&](int x, unsigned n) { return bar(B0 + 8 + 2 * x + (n & 1)); };
+  auto o_done = [&](int x, unsigned n) { return bar(B0 + 12 + 2 * x + (n & 1)); };
+  const uint32_t q_free = bar(B0 + 16);
+  auto seg_full = [&](unsigned i) { return bar(B0 + 17 + i % PairSeg::RING); };
+  auto seg_empty = [&](unsigned i) { return bar(B0 + 17 + PairSeg::RING + i % PairSeg::RING); };
+  const ChunkDev& c = a.c;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < NST; ++i) {
+      mbar_init(k_full(i), 3);
+      mbar_init(k_empty(i), 2);
+      mbar_init(v_full(i), 2);
+      mbar_init(v_empty(i), 2);
+    }
+    for (int i = 0; i < NRAW; ++i) {
+      mbar_init(raw_full(i), 1);
+      mbar_init(raw_empty(i), 5);
+      mbar_init(c_full(i), 1);
+    }
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(q_full(x), 1);
+      mbar_init(q_ready(x), 4);
+      for (unsigned n = 0; n < 2; ++n) {
+        mbar_init(s_full(x, n), 1);
+        mbar_init(p_full(x, n), 4);
+        mbar_init(o_done(x, n), 1);
+      }
+    }
+    mbar_init(q_free, 2);
+    for (unsigned i = 0; i < PairSeg::RING; ++i) {
+      mbar_init(seg_full(i), 1);
+      mbar_init(seg_empty(i), 15);  // the other warps
+    }
+    *abort_flag = 0;
+    fence_barrier_init();
+    prefetch_tensormap(&q_map);
+  }
+  if (warp == 9) {
+    tmem_alloc(smem_u32(tmem_slot), 512);
+    tmem_relinquish();
+  }
+  pdl_wait();
+  const WindowSplit sp = split_of<KEYS_4BIT>(a);
+  const int sinks = sp.sinks();
+  chunk_plan(c, sp, s_base, s_red);
+  tc_fence_before();
+  __syncthreads();  // barriers initialised, tensor memory allocated
+  tc_fence_after();
+  pdl_trigger();  // not before: a dependent CTA on this SM could take the columns that warp 9 still waits for
+  const uint32_t tmem = *tmem_slot;
+  const long long all = s_base[c.n], per = chunk_share(a, all);
+  long long pos = blockIdx.x * per;
+  const long long end = pos + per < all ? pos + per : all;
+  const int qt_log = a.sp.qt_log, QT = 1 << (qt_log - 1);  // queries of a tile
+  // a bounded wait; once any role has given up, the others skip their waits and wind down
+  auto wait = [&](uint32_t b, uint32_t parity) {
+    if (mbar_try_wait(b, parity & 1u)) return true;
+    if (*abort_flag) return false;
+    if (mbar_wait(b, parity & 1u, a.werr)) return true;
+    *abort_flag = 1;
+    return false;
+  };
+  // waits taken by the whole warp
+  auto wait_w = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, wait(b, parity)); };
+  PairSeg s;
+  unsigned segs = 0;  // read or published
+  const bool by_entry = a.scale <= 0x1p12f;
+
+  // registers of the launch: 512 x 128 = 65536; shares: 256 x 168 + 256 x 80 = 63488
+  if (warp >= 8) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+  if (warp == 8) {
+    // ---------------- producer ----------------
+    unsigned blk = 0;
+    for (bool ok = true;;) {
+      s.nb = 0;
+      ChunkItem it{};
+      if (pos < end) {
+        it = chunk_item(c, sp, s_base, pos);
+        if (segs == 0 && lane == 0) join_note(a, &it, per);
+        if (pos < it.first) pos = it.first;
+      } else if (segs == 0 && lane == 0) {
+        join_note(a, nullptr, per);
+      }
+      if (pos < end) {
+        const int q0 = it.t << qt_log, left = it.ql - q0;
+        s = PairSeg{it.b, it.h, it.t0 + q0, it.s0 + q0, {}, {}, (int)(pos - it.first), (int)(end - it.first < it.nb ? end - it.first : it.nb), it.nb, 0};
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          s.nq[x] = max(0, min(QT, left - x * QT));
+          const int last = s.see0 + x * QT + s.nq[x] - 1;  // entry of the tile's last query
+          const int nb = s.nq[x] > 0 ? (last < 0 ? 1 : last / 64 + 1 - it.skip) : 0;
+          s.e[x] = max(0, min(s.kb1, nb) - s.kb0);
+        }
+        pos = it.first + s.kb1;
+      }
+      if (lane == 0) {
+        ok = ok && (segs < PairSeg::RING || wait(seg_empty(segs), segs / PairSeg::RING - 1));
+        if (ok) {
+          s_seg[segs % PairSeg::RING] = s;
+          mbar_arrive(seg_full(segs));
+        }
+      }
+      if (s.nb == 0) break;
+      const int E = s.kb1 - s.kb0;
+      if (lane == 0) {
+        ok = ok && (segs == 0 || wait(q_free, segs - 1));
+        for (int x = 0; x < 2; ++x) {
+          if (!ok || s.e[x] == 0) continue;
+          mbar_arrive_expect_tx(q_full(x), Sh::Q_BYTES);
+#pragma unroll
+          for (int k = 0; k < Sh::ATOMS; ++k)
+            tma_load_3d(smem_u32(sm + x * Sh::Q_BYTES + k * Sh::QCOL), &q_map, k * 64, s.h << g_log, s.token0 + x * QT, q_full(x));
+        }
+      }
+      const long long k_at = ((long long)c.layer * 2 * c.Hkv + s.h) * F::BLOCK, v_at = k_at + (long long)c.Hkv * F::BLOCK;
+      for (int g0 = 0; g0 < E; g0 += 32) {
+        int mine = -1;  // the pages of 32 blocks, one a lane
+        const int at = block_at<KEYS_4BIT>(s.kb0 + g0 + lane, sinks, it.skip);
+        if (g0 + lane < E && at * 64 < it.len) mine = chunk_page(c.page_table, c.max_pages, c.n_pages, s.b, at, c.err);
+        for (int i = 0; i < min(32, E - g0); ++i, ++blk) {
+          const int page = __shfl_sync(0xffffffffu, mine, i);
+          if (lane == 0 && ok) {
+            ok = blk < NRAW || wait(raw_empty(blk), blk / NRAW - 1);
+            if (ok) {
+              s_flag[blk % Sh::FLAGS] = page < 0;
+              if (page < 0) {
+                mbar_arrive(raw_full(blk));
+              } else {
+                mbar_arrive_expect_tx(raw_full(blk), Sh::RAW);
+                const uint8_t* src = static_cast<const uint8_t*>(c.pool) + page * c.page_elems;
+                const uint32_t dst = smem_u32(sm + Sh::OFF_RAW + (blk % NRAW) * Sh::RAW);
+                bulk_g2s(dst, src + k_at, F::BLOCK, raw_full(blk));
+                bulk_g2s(dst + F::BLOCK, src + v_at, F::BLOCK, raw_full(blk));
+              }
+            }
+          }
+          __syncwarp();
+        }
+      }
+      ++segs;
+    }
+  } else if (warp == 11) {
+    // ---------------- pairs to what the codes' warps need ----------------
+    // The block's powers of two, and in the place of each pair (d, lo) two float16: 2^24 d' and 8 d' for K, 2^24 d' and lo' for V. A lane
+    // has keys 2 lane and 2 lane + 1.
+    unsigned b = 0;
+    for (bool ok = true; ok && wait_w(seg_full(segs), segs / PairSeg::RING); ++segs) {
+      s = s_seg[segs % PairSeg::RING];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(seg_empty(segs));
+      if (s.nb == 0) break;
+      // no query sees entries from `behind` on, nor, under a window, those from `first` up to gone_to: what they hold is not looked at
+      const int behind = s.see0 + s.nq[0] + s.nq[1], skip = sp.skip_at(s.see0), gone_to = hidden_to(s.see0, a.window);
+      for (int i = s.kb0; i < s.kb1; ++i, ++b) {
+        const int page0 = block_at<KEYS_4BIT>(i, sinks, skip) * 64;
+        if (!wait_w(raw_full(b), b / NRAW)) { ok = false; break; }
+        uint8_t* raw = sm + Sh::OFF_RAW + (b % NRAW) * Sh::RAW + F::CODES + lane * (8 * NG);
+        uint32_t pr[2][2 * NG];  // of K and V; key, group
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if constexpr (NG == 2) *reinterpret_cast<uint4*>(pr[x]) = *reinterpret_cast<const uint4*>(raw + x * F::BLOCK);
+          else *reinterpret_cast<uint2*>(pr[x]) = *reinterpret_cast<const uint2*>(raw + x * F::BLOCK);
+        }
+        const bool gone = s_flag[b % Sh::FLAGS] != 0;
+        bool hides[2] = {false, false};
+        if (gone || page0 + 63 >= behind || (page0 <= gone_to && page0 + 63 >= a.first)) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int e = page0 + 2 * lane + k;
+            hides[k] = gone || e >= behind || (e >= a.first && e <= gone_to);
+            if (hides[k])
+#pragma unroll
+              for (int n = 0; n < NG; ++n) pr[0][k * NG + n] = pr[1][k * NG + n] = 0;
+          }
+        }
+        // exponents, on the bits of |lo| and 16 d (0 stays small: 2^-123): halves of a word
+        auto sizes = [](uint32_t w) { return (w & 0x7fff7fffu) + 0x00000200u; };
+        auto larger = [&](const uint32_t* p) { return NG == 2 ? __vmaxu2(sizes(p[0]), sizes(p[NG - 1])) : sizes(p[0]); };
+        auto exponent = [](uint32_t w, int low) { return max(low, min(126, (int)(max(w & 0xffffu, w >> 16) >> 7) - 127)); };
+        uint32_t own_size[2];
+        int e[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          own_size[0] = larger(pr[x]);
+          own_size[1] = larger(pr[x] + NG);
+          const uint32_t v = __vmaxu2(own_size[0], own_size[1]);
+          e[x] = exponent(__reduce_max_sync(0xffffffffu, max(v & 0xffffu, v >> 16)), x == 0 ? -8 : -100);
+        }
+        // does an entry that somebody sees lie below 2^-6 of the largest?
+        const bool small = (!hides[0] && exponent(own_size[0], -100) < e[1] - 6) || (!hides[1] && exponent(own_size[1], -100) < e[1] - 6);
+        const bool own = by_entry && e[0] <= 18 && __any_sync(0xffffffffu, small);
+        uint32_t lo16[2] = {0, 0}, d16[2] = {0, 0};  // of K, for the 16 more columns
+        int et[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            if (x == 1) et[k] = own && !hides[k] ? exponent(own_size[k], -100) : e[1];
+            const int by = (x == 0 ? e[0] : et[k]) + 6;
+            const float f = pow2(-by), more = by > 126 ? pow2(126 - by) : 1.f;
+#pragma unroll
+            for (int n = 0; n < NG; ++n) {
+              float2 p = kv4_pair(pr[x][k * NG + n]);
+              p.x = p.x * f * more;
+              p.y = p.y * f * more;
+              pr[x][k * NG + n] = pack_f16(p.x * 0x1p24f, x == 0 ? 8.f * p.x : p.y);
+              if (x == 0) {
+                const uint32_t both = pack_f16(p.y, 8.f * p.x);
+                lo16[k] |= (both & 0xffffu) << (16 * n);
+                d16[k] |= (both >> 16) << (16 * n);
+              }
+            }
+          }
+          if constexpr (NG == 2) *reinterpret_cast<uint4*>(raw + x * F::BLOCK) = *reinterpret_cast<const uint4*>(pr[x]);
+          else *reinterpret_cast<uint2*>(raw + x * F::BLOCK) = *reinterpret_cast<const uint2*>(pr[x]);
+        }
+        fence_proxy_async_smem();  // (the next copy into this place comes after)
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(c_full(b));
+          mbar_arrive(raw_empty(b));
+        }
+        if (b >= NST && !wait_w(k_empty(b), b / NST - 1)) { ok = false; break; }
+        // lo, 8 d of the groups, three times; the entry's power of V, three times
+        const float down = pow2(-(e[0] + 6));
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int key = 2 * lane + k;
+          const float power = (float)(et[k] - e[1]) * down;
+          uint8_t* to = sm + Sh::OFF_KX + (b % NST) * Sh::KX + key * 32;
+          const int flip = ((key >> 2) & 1) << 4;
+          *reinterpret_cast<uint4*>(to + flip) = make_uint4(lo16[k], d16[k], lo16[k], d16[k]);
+          *reinterpret_cast<uint4*>(to + (flip ^ 16)) = make_uint4(lo16[k], d16[k], pack_f16(power, power), pack_f16(power, 0.f));
+          // (what the softmax reads with S: the issuer has seen k_full before it)
+          if (own) s_w[(b % Sh::WS) * 64 + key] = pow2(-et[k]);
+        }
+        if (lane == 0)
+          s_info[b % Sh::FLAGS] = make_float4(a.scale * pow2(e[0] + 6), (float)e[1], pow2(-e[1]), __int_as_float((gone ? 1 : 0) | (own ? 2 : 0)));
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(k_full(b));
+      }
+    }
+  } else if (warp >= 12) {
+    // ---------------- codes to float16 tiles ----------------
+    // Warps 12 and 13 make K's, 14 and 15 V's; neither waits for the other's places. A warp has 32 of the keys; a lane two of them and
+    // every other 16 bytes of their codes (8 lanes: 4 keys x 2: their writes meet no bank twice).
+    const int kv = (warp - 12) >> 1, odd = lane & 1, key0 = (warp & 1) * 32 + (lane >> 3) * 4 + ((lane >> 1) & 3);  // and key0 + 16
+    const uint32_t stage0 = smem_u32(sm) + (kv == 0 ? Sh::OFF_K : Sh::OFF_V) + key0 * 128, sign = kv == 0 ? 0x80008000u : 0u;
+    uint32_t to[4];  // the lane's 16-byte places in a row: key0 and key0 + 16 have the same
+#pragma unroll
+    for (int i = 0; i < 4; ++i) to[i] = stage0 + (((odd * 4 + i) ^ (key0 & 7)) << 4);
+    const uint8_t* from = sm + Sh::OFF_RAW + kv * F::BLOCK;
+    unsigned b = 0;
+    for (bool ok = true; ok && wait_w(seg_full(segs), segs / PairSeg::RING); ++segs) {
+      const int kb0 = s_seg[segs % PairSeg::RING].kb0, kb1 = s_seg[segs % PairSeg::RING].kb1, nb = s_seg[segs % PairSeg::RING].nb;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(seg_empty(segs));
+      if (nb == 0) break;
+      for (int i = kb0; i < kb1; ++i, ++b) {
+        if (!wait_w(raw_full(b), b / NRAW)) { ok = false; break; }
+        const uint8_t* raw = from + (b % NRAW) * Sh::RAW;
+        uint4 code[2][NG];
+        uint32_t pair[2][NG];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int n = 0; n < NG; ++n) code[x][n] = *reinterpret_cast<const uint4*>(raw + (key0 + 16 * x) * (HD / 2) + n * 32 + odd * 16);
+        if (!wait_w(c_full(b), b / NRAW)) { ok = false; break; }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int n = 0; n < NG; ++n) pair[x][n] = *reinterpret_cast<const uint32_t*>(raw + F::CODES + ((key0 + 16 * x) * NG + n) * 4);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(raw_empty(b));
+        if (b >= NST && !wait_w(kv == 0 ? k_empty(b) : v_empty(b), b / NST - 1)) { ok = false; break; }
+        const uint32_t st = (b % NST) * Sh::T_BYTES;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int n = 0; n < NG; ++n) {
+            const uint32_t d24 = __byte_perm(pair[x][n], 0, 0x1010), add = __byte_perm(pair[x][n], 0, 0x3232) ^ sign;
+            const uint32_t d20 = fma_f16x2(d24, 0x2c002c00u, 0), w[4] = {code[x][n].x, code[x][n].y, code[x][n].z, code[x][n].w};  // (a sixteenth)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) st_shared_16(to[j] + st + n * Sh::COL + x * 2048, f16_values(w[j], d24, d20, add));
+          }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(kv == 0 ? k_full(b) : v_full(b));
+      }
+    }
+  } else if (warp == 9 || warp == 10) {
+    // ---------------- MMA issuers, one a tile ----------------
+    if (elect_one()) {
+      constexpr uint32_t IDS = idesc_f16_f32(128, 64), IDO = idesc_f16_f32(128, HD) | (1u << 16);  // (V MN-major)
+      constexpr uint64_t QCOL_E = Sh::QCOL >> 4, T_E = Sh::T_BYTES >> 4, COL_E = Sh::COL >> 4, V16_E = 2048 >> 4, KX_E = Sh::KX >> 4;
+      const int x = warp - 9;
+      const uint64_t qd = smem_desc_sw128(smem_u32(sm + x * Sh::Q_BYTES)), dk = smem_desc_sw128(smem_u32(sm + Sh::OFF_K));
+      const uint64_t dv = smem_desc_sw128_mn(smem_u32(sm + Sh::OFF_V), Sh::COL);
+      const uint64_t qx = smem_desc_x(smem_u32(sm + Sh::OFF_QX + x * Sh::QX)), dkx = smem_desc_x(smem_u32(sm + Sh::OFF_KX));
+      const uint32_t t_s = tmem + 128u * x, t_o = tmem + Sh::OCOL + (uint32_t)(HD * x);
+      unsigned blk = 0, qn = 0, n = 0;  // n: blocks of the tile whose P V has been issued
+      auto issue_s = [&](unsigned b, unsigned n) {
+        const uint64_t kd = dk + (uint64_t)(b % NST) * T_E;
+#pragma unroll
+        for (int kc = 0; kc < Sh::ATOMS; ++kc)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)  // K = 16 an MMA: +32 bytes (encoded +2) inside the atom column
+            tc_mma_f16(t_s + 64u * (n & 1), qd + kc * QCOL_E + 2 * k, kd + kc * COL_E + 2 * k, IDS, (kc | k) ? 1u : 0u);
+        tc_mma_f16(t_s + 64u * (n & 1), qx, dkx + (uint64_t)(b % NST) * KX_E, IDS, 1u);
+        tc_commit(s_full(x, n));
+      };
+      bool ok = true;
+      auto next = [&] {
+        if (!wait(seg_full(segs), segs / PairSeg::RING)) return false;
+        s = s_seg[segs % PairSeg::RING];
+        mbar_arrive(seg_empty(segs));
+        ++segs;
+        return s.nb > 0;
+      };
+      while (ok && next()) {
+        const int E = s.kb1 - s.kb0, e = x ? s.e[1] : s.e[0];
+        ok = e == 0 || wait(q_ready(x), qn++);
+        for (int i = 0; i < min(2, E) && ok; ++i) {  // S of the first two blocks
+          ok = wait(k_full(blk + i), (blk + i) / NST);
+          if (!ok) break;
+          tc_fence_after();
+          if (i < e) issue_s(blk + i, n + i);
+          tc_commit(k_empty(blk + i));
+        }
+        if (ok && E <= 2) tc_commit(q_free);
+        for (int i = 0; i < E && ok; ++i) {
+          const unsigned b = blk + i;
+          const bool more = i + 2 < E;
+          // (what this tile does not use it waits for and releases all the same, in step with the other)
+          ok = wait(v_full(b), b / NST) && (!more || wait(k_full(b + 2), (b + 2) / NST)) && (i >= e || wait(p_full(x, n), n >> 1));
+          if (!ok) break;
+          if (i < e) {
+            tc_fence_after();
+            const uint64_t vd = dv + (uint64_t)(b % NST) * T_E;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)  // K = 16 keys an MMA: 8 columns of P, +2048 bytes (16 rows) of V
+              mma_ts(t_o, t_s + 64u * (n & 1) + 8u * k, vd + V16_E * k, IDO, i > 0 || k > 0 ? 1u : 0u);
+            tc_commit(o_done(x, n));
+            if (i + 2 < e) issue_s(b + 2, n + 2);
+            ++n;
+          }
+          tc_commit(v_empty(b));
+          if (more) tc_commit(k_empty(b + 2));
+          if (i + 3 == E) tc_commit(q_free);
+        }
+        blk += E;
+      }
+    }
+    __syncwarp();
+  }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    // ---------------- softmax: thread = MMA row = TMEM lane ----------------
+    const int x = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
+    const uint32_t lane_off = (uint32_t)(quad * 32) << 16;
+    const uint32_t t_s = tmem + lane_off + 128u * (uint32_t)x;
+    const uint32_t t_o = tmem + lane_off + Sh::OCOL + (uint32_t)(HD * x);
+    const int qi = row >> g_log, g = row & ((1 << g_log) - 1);
+    unsigned n = 0, blk = 0, qn = 0;  // blocks of this tile, and of the CTA; items of this tile
+    bool ok = true;
+    auto next = [&] {
+      if (!wait_w(seg_full(segs), segs / PairSeg::RING)) return false;
+      s = s_seg[segs % PairSeg::RING];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(seg_empty(segs));
+      ++segs;
+      return s.nb > 0;
+    };
+    while (ok && next()) {
+      const bool row_ok = qi < s.nq[x];
+      const int see = row_ok ? s.see0 + x * QT + qi : -1;  // a row past the tile's queries sees nothing
+      const int see0 = s.see0 + x * QT;                    // of the tile's first query
+      const int skip = sp.skip_at(s.see0), hid = hidden_to(see, a.window), edge_to = hidden_to(see0 + s.nq[x] - 1, a.window);
+      int eq = 0;  // the power of two that q of the row was multiplied by
+      if (s.e[x] > 0) {
+        // ---- this row of q: to float16, in the codes' order, with the groups' sums beside
+        if (!wait_w(q_full(x), qn++)) { ok = false; break; }
+        uint8_t* qr = sm + x * Sh::Q_BYTES + row * 128;
+        uint32_t most = 0;
+#pragma unroll
+        for (int j = 0; j < HD / 8; ++j) {
+          const uint4 v = *reinterpret_cast<const uint4*>(qr + (j / 8) * Sh::QCOL + (((j % 8) ^ (row & 7)) << 4));
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) most = max(most, max(w[k] & 0x7fff0000u, (w[k] & 0x7fffu) << 16));
+        }
+        const int e = max(-100, min(126, (int)(most >> 23) - 127));
+        eq = min(8 - e, 14 + max(-126, (int)(__float_as_uint(a.scale) >> 23) - 127));  // (what goes beside the powers of V fits, too)
+        const float up = pow2(eq);
+        float sum[NG];
+#pragma unroll
+        for (int nn = 0; nn < NG; ++nn) {
+          sum[nn] = 0.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            uint4* at = reinterpret_cast<uint4*>(qr + nn * Sh::QCOL + ((j ^ (row & 7)) << 4));
+            float f[8];
+            Vec16<bf16>::load(reinterpret_cast<const bf16*>(at), f);
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const __half2 hh = __floats2half2_rn(f[k] * up, f[k + 4] * up);
+              const float2 back = __half22float2(hh);  // (what the products will see)
+              sum[nn] += back.x + back.y;
+              w[k] = *reinterpret_cast<const uint32_t*>(&hh);
+            }
+            *at = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+        uint32_t terms[3];  // of both groups' sums
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          const __half2 hh = __floats2half2_rn(sum[0], NG == 2 ? sum[NG - 1] : 0.f);
+          const float2 back = __half22float2(hh);
+          sum[0] -= back.x;
+          if (NG == 2) sum[NG - 1] -= back.y;
+          terms[k] = *reinterpret_cast<const uint32_t*>(&hh);
+        }
+        uint8_t* xr = sm + Sh::OFF_QX + x * Sh::QX + row * 32;
+        const int flip = (row >> 2) & 1;
+        *reinterpret_cast<uint4*>(xr + (flip << 4)) = make_uint4(terms[0], terms[0], terms[1], terms[1]);
+        float c3[4], left = fminf(pow2(eq) / a.scale, 60000.f);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          c3[k] = k < 3 ? __half2float(__float2half_rn(left)) : 0.f;
+          left -= c3[k];
+        }
+        *reinterpret_cast<uint4*>(xr + ((1 ^ flip) << 4)) = make_uint4(terms[2], terms[2], pack_f16(c3[0], c3[1]), pack_f16(c3[2], c3[3]));
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_ready(x));
+      }
+      const float row_scale = pow2(-eq);
+      float m_run = -INFINITY, l_run = 0.f;  // m: of the scores in base 2 plus the power of V
+      // One block; false when a wait ran out. OWN: l from the entries' own powers of V. The whole body twice: with one body and a branch
+      // in it, the branch cost 30 us of 490 where it is not taken.
+      auto block = [&](auto own, int i, const float4 info, uint32_t (&su)[64]) {
+        const int key0 = block_at<KEYS_4BIT>(s.kb0 + i, sinks, skip) * 64;
+        const uint32_t t_sn = t_s + 64u * (n & 1);
+        const bool gone = __float_as_int(info.w) & 1;
+        const float scale = fminf(fmaxf(info.x * row_scale, 0x1p-126f), 3.4e38f), vscale = info.y;
+        if (key0 + 63 > see0 || (key0 <= edge_to && key0 + 63 >= a.first) || gone || !__all_sync(0xffffffffu, row_ok)) {
+          const int vis = gone ? -1 : see - key0;  // columns 0..vis are visible, but for past..low under a window
+          const int past = a.first - key0, low = hid - key0;
+#pragma unroll
+          for (int k = 0; k < 64; ++k)
+            if (k > vis || (k >= past && k <= low)) su[k] = 0xff800000u;  // -inf
+        }
+        float pm4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int k = 0; k < 64; ++k) pm4[k & 3] = fmaxf(pm4[k & 3], __uint_as_float(su[k]));
+        const float pm = fmaf(fmaxf(fmaxf(pm4[0], pm4[1]), fmaxf(pm4[2], pm4[3])), scale, vscale);
+        // O is rescaled only when a row's maximum grows by more than 8 in base 2, after the P V before has landed
+        const bool grow = pm - m_run > 8.f;
+        if (__any_sync(0xffffffffu, grow)) {
+          const float cr = grow ? exp2f(m_run - pm) : 1.f;  // 0 when m_run was -inf
+          if (i > 0) {
+            if (!wait_w(o_done(x, n - 1), (n - 1) >> 1)) return false;
+            tc_fence_after();
+#pragma unroll
+            for (int c0 = 0; c0 < HD; c0 += 16) {
+              float o[16];
+              tmem_ld_16(t_o + (uint32_t)c0, o);
+#pragma unroll
+              for (int k = 0; k < 16; ++k) o[k] *= cr;
+              tmem_st_16(t_o + (uint32_t)c0, o);
+            }
+          }
+          if (grow) {
+            l_run *= cr;
+            m_run = pm;
+          }
+        }
+        const float mref = m_run == -INFINITY ? 0.f : vscale - m_run;  // no visible key so far: any finite value
+        const uint64_t scale2 = f2_pack(scale, scale), mref2 = f2_pack(mref, mref);
+        uint64_t ps[2] = {0, 0};  // (two sums each)
+        const float4* w4 = reinterpret_cast<const float4*>(s_w + ((blk + i) % Sh::WS) * 64);
+#pragma unroll
+        for (int c0 = 0; c0 < 64; c0 += 32) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int k = 0; k < 32; k += 4) {
+            float w[4];
+            if constexpr (own) *reinterpret_cast<float4*>(w) = w4[(c0 + k) / 4];
+#pragma unroll
+            for (int j = 0; j < 4; j += 2) {
+              const float2 e = f2_unpack(f2_fma(f2_pack(__uint_as_float(su[c0 + k + j]), __uint_as_float(su[c0 + k + j + 1])), scale2, mref2));
+              const float p0 = ex2_fast(e.x), p1 = ex2_fast(e.y);
+              if constexpr (own) ps[j / 2] = f2_fma(f2_pack(p0, p1), f2_pack(w[j], w[j + 1]), ps[j / 2]);
+              else ps[j / 2] = f2_add(ps[j / 2], f2_pack(p0, p1));
+              pk[(k + j) / 2] = pack_f16(p0, p1);
+            }
+          }
+          tmem_put_16(t_sn + (uint32_t)(c0 / 2), pk);
+        }
+        const float2 sum = f2_unpack(f2_add(ps[0], ps[1]));
+        l_run = fmaf(sum.x + sum.y, own ? 1.f : info.z, l_run);
+        tmem_st_wait_done();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full(x, n));
+        return true;
+      };
+      for (int i = 0; i < s.e[x]; ++i, ++n) {
+        if (!wait_w(s_full(x, n), n >> 1)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t t_sn = t_s + 64u * (n & 1);
+        uint32_t su[64];
+        tmem_ld_32_issue(t_sn, su);
+        tmem_ld_32_issue(t_sn + 32, su + 32);
+        const float4 info = s_info[(blk + i) % Sh::FLAGS];
+        tmem_ld_wait();
+        hold_32(su);
+        hold_32(su + 32);
+        ok = __float_as_int(info.w) & 2 ? block(std::true_type{}, i, info, su) : block(std::false_type{}, i, info, su);
+        if (!ok) break;
+      }
+      // the last P V, then the row out: O / l, or its part
+      const bool whole = s.kb0 == 0 && s.kb1 == s.nb;
+      const long long token = s.token0 + x * QT + qi;
+      const int head = (s.h << g_log) + g;
+      const int slot = 2 * blockIdx.x + (s.kb0 == 0), prow = x * 128 + row;  // of the part
+      bf16* orow = static_cast<bf16*>(a.out) + token * a.os + (long long)head * HD;
+      const bool wide = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && a.os % 8 == 0;
+      if (ok && s.e[x] > 0) {
+        if (!wait_w(o_done(x, n - 1), (n - 1) >> 1)) break;
+        tc_fence_after();
+        const float inv = 64.f * (whole ? (l_run != 0.f ? 1.f / l_run : 0.f) : 1.f);  // (V was divided by 2^6 more)
+#pragma unroll
+        for (int c0 = 0; c0 < HD; c0 += 32) {
+          float o[32];
+          tmem_ld_32(t_o + (uint32_t)c0, o);
+          if (!row_ok) continue;
+#pragma unroll
+          for (int k = 0; k < 32; k += 8) {  // eight dims, out of the codes' order
+            const float y[8] = {o[k] * inv, o[k + 2] * inv, o[k + 4] * inv, o[k + 6] * inv, o[k + 1] * inv, o[k + 3] * inv, o[k + 5] * inv, o[k + 7] * inv};
+            if (!whole) {
+              *reinterpret_cast<float4*>(a.part_o + pair_part(slot, prow, c0 + k, HD)) = make_float4(y[0], y[1], y[2], y[3]);
+              *reinterpret_cast<float4*>(a.part_o + pair_part(slot, prow, c0 + k + 4, HD)) = make_float4(y[4], y[5], y[6], y[7]);
+            } else if (wide) {
+              *reinterpret_cast<uint4*>(orow + c0 + k) = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+            } else {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) orow[c0 + k + j] = from_f32<bf16>(y[j]);
+            }
+          }
+        }
+        tc_fence_before();
+      } else if (row_ok && !whole) {  // the tile has no block here: an empty part
+        for (int k = 0; k < HD; ++k) a.part_o[pair_part(slot, prow, k, HD)] = 0.f;
+      }
+      if (row_ok) {
+        if (!whole) a.part_ml[(size_t)slot * PAIR_ROWS + prow] = make_float2(m_run, l_run);
+        else if (a.lse) a.lse[token * c.Hq + head] = l_run != 0.f ? (m_run + log2f(l_run)) * LN2 : -INFINITY;
+      }
+      blk += s.kb1 - s.kb0;
+    }
+  }
+  if (*abort_flag) drain_copies();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) tmem_dealloc(tmem, 512);
+}
+
+// ----------------------------------------------------------------------------
 // Launches
 // ----------------------------------------------------------------------------
 template <int HD, int NT>
@@ -514,7 +1188,18 @@ static cudaError_t q4_launch(const ChunkAttn& a, cudaStream_t st) {
   return launch_k(k_chunk_q4<HD, NT>, dim3(a.ctas), dim3(Sh::THREADS), Sh::bytes(a.c.n), st, a);
 }
 int chunk4_per_sm(int hd, int rows) { return rows > 8 ? 2 : hd == 128 ? 3 : 4; }
+template <int HD>
+static cudaError_t pair4_launch(const ChunkAttn& a, cudaStream_t st) {
+  CUtensorMap qm;
+  if (!chunk_q_map(&qm, a)) return cudaErrorInvalidValue;
+  using Sh = Pair4Shape<HD>;
+  if (cudaError_t e = ensure_kernel_attrs(reinterpret_cast<const void*>(k_chunk_pair4<HD>), Sh::bytes(SV_MAX_ROWS))) return e;
+  int g_log = 0;
+  while ((2 << g_log) <= a.c.G) ++g_log;
+  return launch_k(k_chunk_pair4<HD>, dim3(a.ctas), dim3(PAIR4_THREADS), Sh::bytes(a.c.n), st, a, g_log, qm);
+}
 cudaError_t launch_chunk4(const ChunkAttn& a, cudaStream_t st) {
+  if (a.rows == PAIR_ROWS) return a.c.hd == 64 ? pair4_launch<64>(a, st) : pair4_launch<128>(a, st);
   if (a.rows == 8) return a.c.hd == 32 ? q4_launch<32, 1>(a, st) : a.c.hd == 64 ? q4_launch<64, 1>(a, st) : q4_launch<128, 1>(a, st);
   return a.c.hd == 32 ? q4_launch<32, 2>(a, st) : a.c.hd == 64 ? q4_launch<64, 2>(a, st) : q4_launch<128, 2>(a, st);
 }
