@@ -1226,12 +1226,21 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         tmem_ld_32_issue(t_sn + 32, su + 32);
         const bool gone = s_flag[(blk + i) % Sh::FLAGS] != 0;
         tmem_ld_wait();
-        if (partly_seen(key0 / 64, see0, see_last) || gone || !__all_sync(0xffffffffu, row_ok)) {
-          const int vis = gone ? -1 : see - key0;  // columns 0..vis are visible, but for past..low under a window
-          const int past = a.first - key0, low = hid - key0;
+        if constexpr (MODE == KEYS_ALL) {
+          if (key0 + 63 > see0 || gone || !__all_sync(0xffffffffu, row_ok)) {
+            const int vis = gone ? -1 : see - key0;  // columns 0..vis are visible
+#pragma unroll
+            for (int k = 0; k < 64; ++k)
+              if (k > vis) su[k] = 0xff800000u;  // -inf
+          }
+        } else if (partly_seen(key0 / 64, see0, see_last) || gone) {
+          // columns 0..see - key0 are visible, but for first - key0..hid - key0 (elsewhere a row past the tile's queries may take what
+          // its q gives: nobody reads it)
+          const uint64_t m = gone ? 0 : low_bits(see - key0 + 1) & (low_bits(a.first - key0) | ~low_bits(hid - key0 + 1));
+          const uint32_t bits[2] = {(uint32_t)m, (uint32_t)(m >> 32)};
 #pragma unroll
           for (int k = 0; k < 64; ++k)
-            if (k > vis || (MODE != KEYS_ALL && k >= past && k <= low)) su[k] = 0xff800000u;  // -inf
+            if (!(bits[k / 32] & (1u << (k % 32)))) su[k] = 0xff800000u;  // -inf
         }
         float pm4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -2097,8 +2106,11 @@ static WindowPath window_path(const ChunkDev& c, int dtype, const tlf_attn_windo
     p.rt = whole.rt;
     p.ctas = whole.ctas;
     p.pad = whole.pad;
-  } else if (dtype == TLF_DTYPE_BF16 && c.hd >= 64 && (c.G & (c.G - 1)) == 0 && rows > 16 && reinterpret_cast<uintptr_t>(a.q) % 16 == 0 &&
-             a.q_stride % 8 == 0) {
+  } else if (dtype == TLF_DTYPE_BF16 && c.hd >= 64 && (c.G & (c.G - 1)) == 0 && rows > (c.hd == 128 ? 16 : 32) &&
+             reinterpret_cast<uintptr_t>(a.q) % 16 == 0 && a.q_stride % 8 == 0) {
+    // tcgen05 where tiles of 16 rows, each with the cache again, take longer (32 rows of 16 / 32 / 64 tokens over up to 8192 entries,
+    // 16 / 8 heads x 128: 146 / 147 / 145 us against 160 / 304 / 600; 16 heads x 64, 24 / 32 / 64 tokens: 208 / 209 / 210 against
+    // 160 / 165 / 319; 4 rows of up to 100 tokens over up to 100 entries 16 / 15 against 26 / 17)
     p.four = true;
     p.rt = PAIR_ROWS;
     p.ctas = num_sms;

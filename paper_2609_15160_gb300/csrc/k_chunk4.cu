@@ -575,6 +575,79 @@ __device__ __forceinline__ void hold_32(uint32_t* r) {
     asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
 }
 
+// The softmax of a block whose entries have powers of V of their own, a row a thread: P into tensor memory, O rescaled if the row's
+// maximum grows (once the P V before has landed), l from the entries' powers. False: a wait ran out. Not inlined: a second body of the softmax in the kernel, or a branch in the one, cost 15 to 30 us of 450 where no block has any.
+struct OwnBlock {
+  uint32_t t_s, t_o;
+  float scale, vscale;
+  uint64_t seen;     // columns that the row sees
+  const float4* w;   // 2^-e_t
+  uint32_t o_done;   // barrier of the P V before, with its parity; 0: there is none
+  uint32_t parity;
+  volatile int* abort_flag;
+  uint32_t* werr;
+  float m, l;
+};
+template <int HD>
+__device__ __noinline__ bool own_block(OwnBlock& b) {
+  float pm = -INFINITY, s[16];
+#pragma unroll 1
+  for (int c0 = 0; c0 < 64; c0 += 16) {
+    tmem_ld_16(b.t_s + c0, s);
+#pragma unroll
+    for (int k = 0; k < 16; ++k)
+      if (b.seen >> (c0 + k) & 1) pm = fmaxf(pm, s[k]);
+  }
+  pm = fmaf(pm, b.scale, b.vscale);
+  const bool grow = pm - b.m > 8.f;
+  if (__any_sync(0xffffffffu, grow)) {
+    const float cr = grow ? exp2f(b.m - pm) : 1.f;
+    if (b.o_done) {
+      bool ok = *b.abort_flag == 0 && mbar_wait(b.o_done, b.parity, b.werr);
+      if (!__all_sync(0xffffffffu, ok)) {
+        *b.abort_flag = 1;
+        return false;
+      }
+      tc_fence_after();
+#pragma unroll 1
+      for (int c0 = 0; c0 < HD; c0 += 16) {
+        tmem_ld_16(b.t_o + c0, s);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) s[k] *= cr;
+        tmem_st_16(b.t_o + c0, s);
+      }
+    }
+    if (grow) {
+      b.l *= cr;
+      b.m = pm;
+    }
+  }
+  const float mref = b.m == -INFINITY ? 0.f : b.vscale - b.m;
+#pragma unroll 1
+  for (int c0 = 0; c0 < 64; c0 += 32) {
+    uint32_t pk[16];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      tmem_ld_16(b.t_s + c0 + 16 * h, s);
+#pragma unroll
+      for (int k = 0; k < 16; k += 4) {
+        const float4 w = b.w[(c0 + 16 * h + k) / 4];
+        const float wk[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          s[k + j] = b.seen >> (c0 + 16 * h + k + j) & 1 ? ex2_fast(fmaf(s[k + j], b.scale, mref)) : 0.f;
+          b.l = fmaf(s[k + j], wk[j], b.l);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) pk[8 * h + k] = pack_f16(s[2 * k], s[2 * k + 1]);
+    }
+    tmem_put_16(b.t_s + c0 / 2, pk);  // (over scores that have been read)
+    tmem_st_wait_done();
+  }
+  return true;
+}
+
 template <int HD>
 __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, int g_log, const __grid_constant__ CUtensorMap q_map) {
   using Sh = Pair4Shape<HD>;
@@ -675,9 +748,9 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
   unsigned segs = 0;  // read or published
   const bool by_entry = a.scale <= 0x1p12f;
 
-  // registers of the launch: 512 x 128 = 65536; shares: 256 x 168 + 256 x 80 = 63488
+  // registers of the launch: 512 x 128 = 65536; shares: 256 x 160 + 256 x 88 = 63488
   if (warp >= 8) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
   if (warp == 8) {
     // ---------------- producer ----------------
     unsigned blk = 0;
@@ -751,8 +824,8 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
     }
   } else if (warp == 11) {
     // ---------------- pairs to what the codes' warps need ----------------
-    // The block's powers of two, and in the place of each pair (d, lo) two float16: 2^24 d' and 8 d' for K, 2^24 d' and lo' for V. A lane
-    // has keys 2 lane and 2 lane + 1.
+    // The block's powers of two, and in the place of each pair (d, lo) two float16: 2^24 d' and 8 d' for K, 2^24 d' and lo' for V. A
+    // lane has keys 2 lane and 2 lane + 1.
     unsigned b = 0;
     for (bool ok = true; ok && wait_w(seg_full(segs), segs / PairSeg::RING); ++segs) {
       s = s_seg[segs % PairSeg::RING];
@@ -965,7 +1038,7 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
     __syncwarp();
   }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
     // ---------------- softmax: thread = MMA row = TMEM lane ----------------
     const int x = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
     const uint32_t lane_off = (uint32_t)(quad * 32) << 16;
@@ -1048,88 +1121,86 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
       }
       const float row_scale = pow2(-eq);
       float m_run = -INFINITY, l_run = 0.f;  // m: of the scores in base 2 plus the power of V
-      // One block; false when a wait ran out. OWN: l from the entries' own powers of V. The whole body twice: with one body and a branch
-      // in it, the branch cost 30 us of 490 where it is not taken.
-      auto block = [&](auto own, int i, const float4 info, uint32_t (&su)[64]) {
-        const int key0 = block_at<KEYS_4BIT>(s.kb0 + i, sinks, skip) * 64;
-        const uint32_t t_sn = t_s + 64u * (n & 1);
-        const bool gone = __float_as_int(info.w) & 1;
-        const float scale = fminf(fmaxf(info.x * row_scale, 0x1p-126f), 3.4e38f), vscale = info.y;
-        if (key0 + 63 > see0 || (key0 <= edge_to && key0 + 63 >= a.first) || gone || !__all_sync(0xffffffffu, row_ok)) {
-          const int vis = gone ? -1 : see - key0;  // columns 0..vis are visible, but for past..low under a window
-          const int past = a.first - key0, low = hid - key0;
-#pragma unroll
-          for (int k = 0; k < 64; ++k)
-            if (k > vis || (k >= past && k <= low)) su[k] = 0xff800000u;  // -inf
-        }
-        float pm4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int k = 0; k < 64; ++k) pm4[k & 3] = fmaxf(pm4[k & 3], __uint_as_float(su[k]));
-        const float pm = fmaf(fmaxf(fmaxf(pm4[0], pm4[1]), fmaxf(pm4[2], pm4[3])), scale, vscale);
-        // O is rescaled only when a row's maximum grows by more than 8 in base 2, after the P V before has landed
-        const bool grow = pm - m_run > 8.f;
-        if (__any_sync(0xffffffffu, grow)) {
-          const float cr = grow ? exp2f(m_run - pm) : 1.f;  // 0 when m_run was -inf
-          if (i > 0) {
-            if (!wait_w(o_done(x, n - 1), (n - 1) >> 1)) return false;
-            tc_fence_after();
-#pragma unroll
-            for (int c0 = 0; c0 < HD; c0 += 16) {
-              float o[16];
-              tmem_ld_16(t_o + (uint32_t)c0, o);
-#pragma unroll
-              for (int k = 0; k < 16; ++k) o[k] *= cr;
-              tmem_st_16(t_o + (uint32_t)c0, o);
-            }
-          }
-          if (grow) {
-            l_run *= cr;
-            m_run = pm;
-          }
-        }
-        const float mref = m_run == -INFINITY ? 0.f : vscale - m_run;  // no visible key so far: any finite value
-        const uint64_t scale2 = f2_pack(scale, scale), mref2 = f2_pack(mref, mref);
-        uint64_t ps[2] = {0, 0};  // (two sums each)
-        const float4* w4 = reinterpret_cast<const float4*>(s_w + ((blk + i) % Sh::WS) * 64);
-#pragma unroll
-        for (int c0 = 0; c0 < 64; c0 += 32) {
-          uint32_t pk[16];
-#pragma unroll
-          for (int k = 0; k < 32; k += 4) {
-            float w[4];
-            if constexpr (own) *reinterpret_cast<float4*>(w) = w4[(c0 + k) / 4];
-#pragma unroll
-            for (int j = 0; j < 4; j += 2) {
-              const float2 e = f2_unpack(f2_fma(f2_pack(__uint_as_float(su[c0 + k + j]), __uint_as_float(su[c0 + k + j + 1])), scale2, mref2));
-              const float p0 = ex2_fast(e.x), p1 = ex2_fast(e.y);
-              if constexpr (own) ps[j / 2] = f2_fma(f2_pack(p0, p1), f2_pack(w[j], w[j + 1]), ps[j / 2]);
-              else ps[j / 2] = f2_add(ps[j / 2], f2_pack(p0, p1));
-              pk[(k + j) / 2] = pack_f16(p0, p1);
-            }
-          }
-          tmem_put_16(t_sn + (uint32_t)(c0 / 2), pk);
-        }
-        const float2 sum = f2_unpack(f2_add(ps[0], ps[1]));
-        l_run = fmaf(sum.x + sum.y, own ? 1.f : info.z, l_run);
-        tmem_st_wait_done();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(p_full(x, n));
-        return true;
-      };
       for (int i = 0; i < s.e[x]; ++i, ++n) {
         if (!wait_w(s_full(x, n), n >> 1)) { ok = false; break; }
         tc_fence_after();
+        const int key0 = block_at<KEYS_4BIT>(s.kb0 + i, sinks, skip) * 64;
         const uint32_t t_sn = t_s + 64u * (n & 1);
-        uint32_t su[64];
-        tmem_ld_32_issue(t_sn, su);
-        tmem_ld_32_issue(t_sn + 32, su + 32);
         const float4 info = s_info[(blk + i) % Sh::FLAGS];
-        tmem_ld_wait();
-        hold_32(su);
-        hold_32(su + 32);
-        ok = __float_as_int(info.w) & 2 ? block(std::true_type{}, i, info, su) : block(std::false_type{}, i, info, su);
-        if (!ok) break;
+        const bool gone = __float_as_int(info.w) & 1;
+        const float scale = fminf(fmaxf(info.x * row_scale, 0x1p-126f), 3.4e38f), vscale = info.y;
+        const bool edge = key0 + 63 > see0 || (key0 <= edge_to && key0 + 63 >= a.first) || gone;
+        // columns 0..see - key0 are visible, but for first - key0..hid - key0 under a window (beside the edges a row past the tile's
+        // queries may take what its q gives: nobody reads it)
+        auto seen = [&] { return gone ? 0 : low_bits(see - key0 + 1) & (low_bits(a.first - key0) | ~low_bits(hid - key0 + 1)); };
+        if (__float_as_int(info.w) & 2) {
+          OwnBlock ob{t_sn, t_o, scale, vscale, edge ? seen() : ~0ull, reinterpret_cast<const float4*>(s_w + ((blk + i) % Sh::WS) * 64),
+                      i > 0 ? o_done(x, n - 1) : 0, ((n - 1) >> 1) & 1, abort_flag, a.werr, m_run, l_run};
+          ok = own_block<HD>(ob);
+          if (!ok) break;
+          m_run = ob.m;
+          l_run = ob.l;
+        } else {
+          uint32_t su[64];
+          tmem_ld_32_issue(t_sn, su);
+          tmem_ld_32_issue(t_sn + 32, su + 32);
+          tmem_ld_wait();
+          hold_32(su);
+          hold_32(su + 32);
+          if (edge) {
+            const uint64_t m = seen();
+            const uint32_t bits[2] = {(uint32_t)m, (uint32_t)(m >> 32)};
+#pragma unroll
+            for (int k = 0; k < 64; ++k)
+              if (!(bits[k / 32] & (1u << (k % 32)))) su[k] = 0xff800000u;  // -inf
+          }
+          float pm4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int k = 0; k < 64; ++k) pm4[k & 3] = fmaxf(pm4[k & 3], __uint_as_float(su[k]));
+          const float pm = fmaf(fmaxf(fmaxf(pm4[0], pm4[1]), fmaxf(pm4[2], pm4[3])), scale, vscale);
+          // O is rescaled only when a row's maximum grows by more than 8 in base 2, after the P V before has landed
+          const bool grow = pm - m_run > 8.f;
+          if (__any_sync(0xffffffffu, grow)) {
+            const float cr = grow ? exp2f(m_run - pm) : 1.f;  // 0 when m_run was -inf
+            if (i > 0) {
+              if (!wait_w(o_done(x, n - 1), (n - 1) >> 1)) { ok = false; break; }
+              tc_fence_after();
+#pragma unroll
+              for (int c0 = 0; c0 < HD; c0 += 16) {
+                float o[16];
+                tmem_ld_16(t_o + (uint32_t)c0, o);
+#pragma unroll
+                for (int k = 0; k < 16; ++k) o[k] *= cr;
+                tmem_st_16(t_o + (uint32_t)c0, o);
+              }
+            }
+            if (grow) {
+              l_run *= cr;
+              m_run = pm;
+            }
+          }
+          const float mref = m_run == -INFINITY ? 0.f : vscale - m_run;  // no visible key so far: any finite value
+          const uint64_t scale2 = f2_pack(scale, scale), mref2 = f2_pack(mref, mref);
+          uint64_t ps[2] = {0, 0};  // (two sums each)
+#pragma unroll
+          for (int c0 = 0; c0 < 64; c0 += 32) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int k = 0; k < 32; k += 2) {
+              const float2 e = f2_unpack(f2_fma(f2_pack(__uint_as_float(su[c0 + k]), __uint_as_float(su[c0 + k + 1])), scale2, mref2));
+              const float p0 = ex2_fast(e.x), p1 = ex2_fast(e.y);
+              ps[k / 2 & 1] = f2_add(ps[k / 2 & 1], f2_pack(p0, p1));
+              pk[k / 2] = pack_f16(p0, p1);
+            }
+            tmem_put_16(t_sn + (uint32_t)(c0 / 2), pk);
+          }
+          const float2 sum = f2_unpack(f2_add(ps[0], ps[1]));
+          l_run = fmaf(sum.x + sum.y, info.z, l_run);
+          tmem_st_wait_done();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full(x, n));
       }
       // the last P V, then the row out: O / l, or its part
       const bool whole = s.kb0 == 0 && s.kb1 == s.nb;

@@ -40,6 +40,9 @@ template <int MODE>
 __device__ __forceinline__ int block_at(int i, int sinks, int skip) { return MODE == KEYS_ALL || i < sinks ? i : i + skip; }
 __device__ __forceinline__ int hidden_to(int see, int window) { return see < window ? -1 : see - window; }
 
+// The n lowest bits of 64 (n may lie outside of 0..64).
+__device__ __forceinline__ uint64_t low_bits(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
+
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // base[b] = blocks of the rows before b; base[n] = all. By the whole block.
