@@ -79,14 +79,85 @@ __device__ __forceinline__ void store8(T* p, const float* x) {
   }
 }
 
+// Eight elements as they come from memory, so that several units of a lane are in flight.
+template <typename T, bool WIDE>
+struct Raw8 {
+  uint4 v[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (WIDE) {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = reinterpret_cast<const uint4*>(p)[i];
+    } else {
+      T* x = reinterpret_cast<T*>(v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = p[i];
+    }
+  }
+  __device__ __forceinline__ void get(float* x) const { load8<T, true>(reinterpret_cast<const T*>(v), x); }
+};
+
+// The eight codes of a lane's values, whose group of GL lanes the warp's lanes form; *pair: (d, lo) of the group. x: what a plain cache
+// would hold.
+//
+// The quotient (x - lo) / d of the definition, rounded once, in three instructions: with r = 1 / d rounded to nearest, q = t r, q +
+// (t - q d) r is t / d rounded to nearest (Markstein, 1990; d's significand is not all ones: it has 8 bits). Out of the range where no
+// step under- or overflows the division itself. Adding 1.5 x 2^23 rounds to an integer, ties to even, in the low bits. EXACT: lo is the
+// least value itself, as it is of bfloat16 values: t / d is in 0 .. 15 (1 + 2^-8), and needs no clamp.
+template <int GL, bool EXACT>
+__device__ __forceinline__ uint32_t quantise(float (&x)[8], uint32_t* pair, bool* bad) {
+  constexpr float LARGEST = 0x1p126f, ROUND = 12582912.f;
+  constexpr uint32_t ROUND_BITS = 0x4b400000u;
+  auto least = [&] { return fminf(fminf(fminf(x[0], x[1]), fminf(x[2], x[3])), fminf(fminf(x[4], x[5]), fminf(x[6], x[7]))); };
+  auto most = [&] { return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))); };
+  float lo = least(), hi = most(), zero = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) zero = fmaf(x[i], 0.f, zero);  // infinities and NaN: not a number
+  const bool odd = !(zero == 0.f) || !(fmaxf(-lo, hi) <= LARGEST);
+  *bad = odd;
+  if (odd) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = x[i] != x[i] ? 0.f : fmaxf(fminf(x[i], LARGEST), -LARGEST);
+    lo = least();
+    hi = most();
+  }
+#pragma unroll
+  for (int o = 1; o < GL; o *= 2) {
+    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+  }
+  const bf16 lo16 = __float2bfloat16_rn(lo);
+  lo = __bfloat162float(lo16);
+  const bf16 d16 = __float2bfloat16_rn(__fdiv_rn(fmaxf(__fsub_rn(hi, lo), 0.f), 15.f));
+  const float d = __bfloat162float(d16);
+  *pair = (uint32_t)__bfloat16_as_ushort(d16) | (uint32_t)__bfloat16_as_ushort(lo16) << 16;
+  uint32_t word = 0;
+  if (d >= 0x1p-80f && d <= 0x1p80f) {
+    const float r = __frcp_rn(d);
+    constexpr uint32_t EIGHT = (uint32_t)(0x11111111ull * ROUND_BITS);  // what the eight shifted ROUND_BITS add up to
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float t = __fsub_rn(x[i], lo), q = __fmul_rn(t, r);
+      float n = fmaf(fmaf(-q, d, t), r, q);
+      if (!EXACT) n = fminf(fmaxf(n, 0.f), 15.f);
+      word += __float_as_uint(__fadd_rn(n, ROUND)) << (4 * i);
+    }
+    word -= EIGHT;
+  } else if (d > 0.f) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) word |= (uint32_t)fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x[i], lo), d)), 0.f), 15.f) << (4 * i);
+  }
+  return word;
+}
+
 template <typename T, int HD, bool WIDE>
-__global__ void __launch_bounds__(256) k_kv4_append(ChunkDev c, Kv4Append a) {
+__global__ void __launch_bounds__(256, 3) k_kv4_append(ChunkDev c, Kv4Append a) {
   using F = Kv4<HD>;
   constexpr int L = HD / 8, HP = 32 / L, GL = F::GS / 8;  // lanes of a head, heads of a pass, lanes of a group
-  constexpr float LARGEST = 0x1p126f;
+  constexpr int U = 2;                                    // passes in flight
   pdl_wait();
-  const int lane = threadIdx.x & 31, d0 = (lane % L) * 8, half = a.rot / 2, heads = c.Hq + 2 * c.Hkv;
-  const int passes = (heads + HP - 1) / HP;
+  const int lane = threadIdx.x & 31, d0 = (lane % L) * 8, half = a.rot / 2;
+  const int pq = (c.Hq + HP - 1) / HP, pk = (c.Hkv + HP - 1) / HP;  // passes over q, and over k or v
+  const bool turns = d0 < a.rot, pairs = turns && !a.interleaved;
   const long long warps = (long long)gridDim.x * 8, all = (long long)c.T * a.parts;
   for (long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); w < all; w += warps) {
     const int t = (int)(w / a.parts), part = (int)(w % a.parts);
@@ -111,78 +182,90 @@ __global__ void __launch_bounds__(256) k_kv4_append(ChunkDev c, Kv4Append a) {
       // x_a c - x_b s, x_b c + x_a s: the sign of what the paired dim adds
       if (d < a.rot && (a.interleaved ? d % 2 == 0 : d < half)) cs[i].y = -cs[i].y;
     }
-    for (int p = part; p < passes; p += a.parts) {
-      const int h = p * HP + lane / L;
-      const bool on = h < heads, is_q = h < c.Hq, is_v = h >= c.Hq + c.Hkv;
-      const int kh = is_q ? h : is_v ? h - c.Hq - c.Hkv : h - c.Hq;
-      float x[8], y[8];
+    auto load = [&](Raw8<T, WIDE>& x, Raw8<T, WIDE>& y, const void* from, long long stride, int h, bool turned) {
+      const T* src = static_cast<const T*>(from) + t * stride + (long long)h * HD;
+      x.load(src + d0);
+      if (!turned || !pairs) return;
+      if constexpr (WIDE) {
+        y.load(src + (d0 < half ? d0 + half : d0 - half));
+      } else {
+        T* to = reinterpret_cast<T*>(y.v);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = y[i] = 0.f;
-      if (on) {
-        const T* src = is_q ? static_cast<const T*>(a.q) + t * a.qs : is_v ? static_cast<const T*>(a.v) + t * a.vs : static_cast<const T*>(a.k) + t * a.ks;
-        src += (long long)kh * HD;
-        load8<T, WIDE>(src + d0, x);
-        if (!is_v && d0 < a.rot) {
-          if (a.interleaved) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
-          } else if (WIDE) {
-            load8<T, WIDE>(src + (d0 < half ? d0 + half : d0 - half), y);
-          } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int d = d0 + i;
-              if (d < a.rot) y[i] = to_f32(src[d < half ? d + half : d - half]);
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (d0 + i < a.rot) x[i] = __fadd_rn(__fmul_rn(x[i], cs[i].x), __fmul_rn(y[i], cs[i].y));
-        }
-        if (is_q) {
-          if (!there)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = 0.f;
-          const long long to = ((long long)t * c.Hq + h) * HD + d0;
-          if (a.q_f32) store8<float, WIDE>(static_cast<float*>(a.q_out) + to, x);
-          else store8<T, WIDE>(static_cast<T*>(a.q_out) + to, x);
+        for (int i = 0; i < 8; ++i) {
+          const int d = d0 + i;
+          if (d < a.rot) to[i] = src[d < half ? d + half : d - half];
         }
       }
-      // the group: least and largest value of what a plain cache would hold
-      bool bad = false;
-      float lo = INFINITY, hi = -INFINITY;
+    };
+    auto turn = [&](float* x, const Raw8<T, WIDE>& ry) {
+      if (!turns) return;
+      float y[8];
+      if (pairs) {
+        ry.get(y);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[i] = to_f32(from_f32<T>(x[i]));
-        if (!(fabsf(x[i]) <= LARGEST)) {
-          bad = true;
-          x[i] = x[i] != x[i] ? 0.f : copysignf(LARGEST, x[i]);
+        for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (WIDE || d0 + i < a.rot) x[i] = __fadd_rn(__fmul_rn(x[i], cs[i].x), __fmul_rn(y[i], cs[i].y));
+    };
+    // passes 0 .. pq - 1 are q's, then k's, then v's; a warp's are `part`, part + parts, ..
+    int p = part;
+    for (; p < pq; p += U * a.parts) {
+      Raw8<T, WIDE> rx[U], ry[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int h = (p + u * a.parts) * HP + lane / L;
+        if (h < c.Hq) load(rx[u], ry[u], a.q, a.qs, h, true);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int h = (p + u * a.parts) * HP + lane / L;
+        if (h >= c.Hq) continue;
+        float x[8];
+        rx[u].get(x);
+        turn(x, ry[u]);
+        if (!there)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = 0.f;
+        const long long to = ((long long)t * c.Hq + h) * HD + d0;
+        if (a.q_f32) store8<float, WIDE>(static_cast<float*>(a.q_out) + to, x);
+        else store8<T, WIDE>(static_cast<T*>(a.q_out) + to, x);
+      }
+    }
+    if (e.block < 0) continue;
+    p = pq + ((part - pq) % a.parts + a.parts) % a.parts;  // the warp's first behind q's
+    for (; p < pq + 2 * pk; p += U * a.parts) {
+      Raw8<T, WIDE> rx[U], ry[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int at = p + u * a.parts - pq, is_v = at >= pk, h = (is_v ? at - pk : at) * HP + lane / L;
+        if (at < 2 * pk && h < c.Hkv) load(rx[u], ry[u], is_v ? a.v : a.k, is_v ? a.vs : a.ks, h, !is_v);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int at = p + u * a.parts - pq, is_v = at >= pk, h = (is_v ? at - pk : at) * HP + lane / L;
+        if (at >= 2 * pk) break;
+        float x[8];
+        rx[u].get(x);
+        if (h >= c.Hkv)  // (the lanes of a head that is none take part in the groups' exchanges)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = 0.f;
+        else if (!is_v) turn(x, ry[u]);
+        if (sizeof(T) == 2 && !is_v) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = to_f32(from_f32<T>(x[i]));
         }
-        lo = fminf(lo, x[i]);
-        hi = fmaxf(hi, x[i]);
+        uint32_t pair;
+        bool bad;
+        const uint32_t word = quantise<GL, sizeof(T) == 2>(x, &pair, &bad);
+        if (h >= c.Hkv) continue;
+        if (bad) sv_report(c.err, SVERR_VALUE);
+        uint8_t* block = static_cast<uint8_t*>(c.pool) + e.block + (long long)(is_v ? c.Hkv + h : h) * F::BLOCK;
+        *reinterpret_cast<uint32_t*>(block + e.off * (HD / 2) + d0 / 2) = word;
+        if (d0 % F::GS == 0) *reinterpret_cast<uint32_t*>(block + F::CODES + (e.off * F::NG + d0 / F::GS) * 4) = pair;
       }
-#pragma unroll
-      for (int o = 1; o < GL; o *= 2) {
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-      }
-      if (!on || is_q || e.block < 0) continue;
-      if (bad) sv_report(c.err, SVERR_VALUE);
-      const bf16 lo16 = __float2bfloat16_rn(lo);
-      lo = __bfloat162float(lo16);
-      const bf16 d16 = __float2bfloat16_rn(__fdiv_rn(fmaxf(__fsub_rn(hi, lo), 0.f), 15.f));
-      const float d = __bfloat162float(d16);
-      uint32_t word = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float n = d > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x[i], lo), d)), 0.f), 15.f) : 0.f;
-        word |= (uint32_t)n << (4 * i);
-      }
-      uint8_t* block = static_cast<uint8_t*>(c.pool) + e.block + (long long)(is_v ? c.Hkv + kh : kh) * F::BLOCK;
-      *reinterpret_cast<uint32_t*>(block + e.off * (HD / 2) + d0 / 2) = word;
-      if (d0 % F::GS == 0)
-        *reinterpret_cast<uint32_t*>(block + F::CODES + (e.off * F::NG + d0 / F::GS) * 4) =
-            (uint32_t)__bfloat16_as_ushort(d16) | (uint32_t)__bfloat16_as_ushort(lo16) << 16;
     }
   }
   pdl_trigger();
@@ -203,21 +286,29 @@ __global__ void __launch_bounds__(256) k_kv4_read(ChunkDev c, Kv4Read a) {
   for (long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); w < all; w += warps) {
     const int t = (int)(w / a.parts);
     const TokenEntry e = token_entry(c, t, F::BLOCK);
-    for (int p = (int)(w % a.parts); p < passes; p += a.parts) {
-      const int h = p * HP + lane / L;
-      const bool is_v = h >= c.Hkv;
-      T* to = static_cast<T*>(is_v ? a.v : a.k);
-      if (h >= 2 * c.Hkv || !to) continue;
-      float x[8];
+    constexpr int U = 4;  // passes in flight
+    for (int p = (int)(w % a.parts); p < passes; p += U * a.parts) {
+      uint32_t word[U], pair[U];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = 0.f;
-      if (e.block >= 0) {
-        const uint8_t* block = static_cast<const uint8_t*>(c.pool) + e.block + (long long)h * F::BLOCK;
-        const uint32_t word = *reinterpret_cast<const uint32_t*>(block + e.off * (HD / 2) + d0 / 2);
-        const uint32_t pair = *reinterpret_cast<const uint32_t*>(block + F::CODES + (e.off * F::NG + d0 / F::GS) * 4);
-        kv4_values(word, kv4_pair(pair), x);
+      for (int u = 0; u < U; ++u) {
+        const int h = (p + u * a.parts) * HP + lane / L;
+        word[u] = pair[u] = 0;
+        if (h < 2 * c.Hkv && e.block >= 0) {
+          const uint8_t* block = static_cast<const uint8_t*>(c.pool) + e.block + (long long)h * F::BLOCK;
+          word[u] = *reinterpret_cast<const uint32_t*>(block + e.off * (HD / 2) + d0 / 2);
+          pair[u] = *reinterpret_cast<const uint32_t*>(block + F::CODES + (e.off * F::NG + d0 / F::GS) * 4);
+        }
       }
-      store8<T, WIDE>(to + t * (is_v ? a.vs : a.ks) + (long long)(is_v ? h - c.Hkv : h) * HD + d0, x);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int h = (p + u * a.parts) * HP + lane / L;
+        const bool is_v = h >= c.Hkv;
+        T* to = static_cast<T*>(is_v ? a.v : a.k);
+        if (h >= 2 * c.Hkv || !to) continue;
+        float x[8];
+        kv4_values(word[u], kv4_pair(pair[u]), x);
+        store8<T, WIDE>(to + t * (is_v ? a.vs : a.ks) + (long long)(is_v ? h - c.Hkv : h) * HD + d0, x);
+      }
     }
   }
   pdl_trigger();
@@ -232,7 +323,7 @@ static unsigned warp_grid(long long warps, int num_sms) { return (unsigned)std::
 template <typename T, int HD>
 static cudaError_t append_launch(const ChunkDev& c, Kv4Append a, bool wide, int num_sms, cudaStream_t st) {
   constexpr int HP = 256 / HD;
-  a.parts = token_parts(c.T, (c.Hq + 2 * c.Hkv + HP - 1) / HP, num_sms);
+  a.parts = token_parts(c.T, (c.Hq + HP - 1) / HP + 2 * ((c.Hkv + HP - 1) / HP), num_sms);
   const dim3 grid(warp_grid((long long)c.T * a.parts, num_sms));
   return wide ? launch_k(k_kv4_append<T, HD, true>, grid, dim3(256), 0, st, c, a) : launch_k(k_kv4_append<T, HD, false>, grid, dim3(256), 0, st, c, a);
 }
