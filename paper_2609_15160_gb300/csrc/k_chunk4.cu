@@ -27,7 +27,8 @@ namespace tlf {
 // running maximum of s + log2(d), the largest d of the entry's groups, not of s, so that values of any magnitude fit. It is refreshed
 // when a product passes 2^15 (or p, where d is tiny, 2^100).
 //
-// CTAs of four warps, each with 16 of a page's 64 keys, and a producer warp that copies a page's two blocks.
+// CTAs of two teams of two warps, which take the pages in turn, a warp half of a page's 64 keys, 16 at a time in each step of the
+// products; and a producer warp that copies a page's two blocks.
 struct Q4Seg {  // a CTA's part of an item: blocks kb0 .. kb1 - 1 of nb; nb = 0: no more
   int b, h, token0, see0, nq, kb0, kb1, nb;
   static constexpr int RING = 4;
@@ -36,8 +37,8 @@ template <int HD, int NT>
 struct Q4Shape {
   using F = Kv4<HD>;
   static constexpr int RT = 8 * NT, WARPS = 4, THREADS = 32 * (WARPS + 1), STAGE = 2 * F::BLOCK;
-  static constexpr int PER_SM = NT == 2 ? 2 : HD == 128 ? 3 : 4;
-  static constexpr int NST = HD == 128 ? (NT == 2 ? 9 : 6) : HD == 64 ? 9 : 12;
+  static constexpr int PER_SM = HD == 128 ? (NT == 2 ? 2 : 3) : NT == 2 ? 3 : 4;
+  static constexpr int NST = HD == 128 ? (NT == 2 ? 8 : 6) : HD == 64 ? 8 : 12;  // even: a stage is always the same team's
   static constexpr int OS = HD + 4;  // floats of a merge buffer's row
   static constexpr int OFF_O = NST * STAGE, OFF_ML = OFF_O + 2 * RT * OS * 4, OFF_BAR = OFF_ML + WARPS * RT * 8;
   static constexpr int NBAR = 2 * NST + 2 * Q4Seg::RING;
@@ -86,7 +87,7 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
   if (tid == 0) {
     for (int i = 0; i < NST; ++i) {
       mbar_init(full(i), 1);
-      mbar_init(empty(i), Sh::WARPS);
+      mbar_init(empty(i), 2);
     }
     for (unsigned i = 0; i < Q4Seg::RING; ++i) {
       mbar_init(seg_full(i), 1);
@@ -173,8 +174,9 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
   const int g = lane >> 2, cl = lane & 3;
   // the key of row r of the products, of 8: two keys a lane pair up (V), and loads of neighbouring lanes meet few bank conflicts
   auto kappa = [](int r) { return HD == 128 ? (r & 1 ? 4 + ((r / 2 + 1) & 3) : r / 2) : r; };
-  const int ka = warp * 16 + kappa(g);                                        // K, pairs: keys ka, ka + 8 of the page
-  const int va = warp * 16 + kappa(2 * cl), vb = warp * 16 + kappa(2 * cl + 1);  // V: keys va, vb, va + 8, vb + 8
+  const int team = warp >> 1, half = (warp & 1) * 32;
+  const int ka = half + kappa(g);                                     // K, pairs: keys ka, ka + 8, ka + 16, ka + 24 of the page
+  const int va = half + kappa(2 * cl), vb = half + kappa(2 * cl + 1);  // V: keys va, vb, va + 8, vb + 8, ..
   for (unsigned segs = 0;; ++segs) {
     // the warps leave together or not at all: they meet at barriers below, which know no time limit
     if (bar_any(1, 32 * Sh::WARPS, !wait(seg_full(segs), segs / Q4Seg::RING))) break;
@@ -251,102 +253,110 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
       }
 
     for (int kb = it.kb0; kb < it.kb1; ++kb, ++seq) {
+      if ((int)(seq & 1u) != team) continue;
       const int st = seq % NST;
       const bool ok = __all_sync(0xffffffffu, wait(full(st), seq / NST));
-      const int page0 = block_at<KEYS_4BIT>(kb, sinks, skip) * 64, key0 = page0 + warp * 16;
-      if (ok && !s_skip[st] && key0 <= see_last && !(key0 >= a.first && key0 + 15 <= gone_to)) {
+      const int page0 = block_at<KEYS_4BIT>(kb, sinks, skip) * 64, key0 = page0 + half;
+      if (ok && !s_skip[st] && key0 <= see_last && !(key0 >= a.first && key0 + 31 <= gone_to)) {
         const uint8_t *sk = sm + st * Sh::STAGE, *sv = sk + F::BLOCK;
-        float acc[NT][NG][4];
+        uint64_t s2[NT][4];  // scores of keys ka + 8 x, both columns
+        {
+          uint64_t dn[NT][4], lo[NT][4];
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+          for (int n = 0; n < NG; ++n) {
+            float acc[NT][2][4];
 #pragma unroll
-          for (int n = 0; n < NG; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[t][n][i] = 0.f;
-#pragma unroll
-        for (int n = 0; n < NG; ++n) {
-          uint32_t wa[W], wb[W];
-          const uint8_t* p = sk + ka * (HD / 2) + n * 32 + cl * (4 * W);
-          if constexpr (W == 2) {
-            *reinterpret_cast<uint2*>(wa) = *reinterpret_cast<const uint2*>(p);
-            *reinterpret_cast<uint2*>(wb) = *reinterpret_cast<const uint2*>(p + 8 * (HD / 2));
-          } else {
-            wa[0] = *reinterpret_cast<const uint32_t*>(p);
-            wb[0] = *reinterpret_cast<const uint32_t*>(p + 8 * (HD / 2));
-          }
-#pragma unroll
-          for (int w = 0; w < W; ++w) {
-            const uint32_t xa = wa[w] >> 8, xb = wb[w] >> 8;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-              mma_f16(acc[t][n], wa[w] & LO, wb[w] & LO, wa[w] & HI, wb[w] & HI, qf[t][n][w][0], qf[t][n][w][1]);
-              mma_f16(acc[t][n], xa & LO, xb & LO, xa & HI, xb & HI, qf[t][n][w][2], qf[t][n][w][3]);
-            }
-          }
-        }
-        // the pairs of keys ka and ka + 8, of K and of V
-        uint32_t kp[2][NG], vp[2][NG];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int at = F::CODES + (ka + 8 * x) * NG * 4;
-          if constexpr (NG == 2) {
-            *reinterpret_cast<uint2*>(kp[x]) = *reinterpret_cast<const uint2*>(sk + at);
-            *reinterpret_cast<uint2*>(vp[x]) = *reinterpret_cast<const uint2*>(sv + at);
-          } else {
-            kp[x][0] = *reinterpret_cast<const uint32_t*>(sk + at);
-            vp[x][0] = *reinterpret_cast<const uint32_t*>(sv + at);
-          }
-        }
-        float s[NT][2][2];  // [key][column]
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              float dn = 0.f, lo = 0.f;
-#pragma unroll
-              for (int n = 0; n < NG; ++n) {
-                const float2 p = kv4_pair(kp[x][n]);
-                dn = fmaf(p.x, acc[t][n][2 * x + j], dn);
-                lo = fmaf(p.y, qs[t][n][j], lo);
+            for (int u = 0; u < 2; ++u) {
+              uint32_t wa[W], wb[W];
+              const uint8_t* p = sk + (ka + 16 * u) * (HD / 2) + n * 32 + cl * (4 * W);
+              if constexpr (W == 2) {
+                *reinterpret_cast<uint2*>(wa) = *reinterpret_cast<const uint2*>(p);
+                *reinterpret_cast<uint2*>(wb) = *reinterpret_cast<const uint2*>(p + 8 * (HD / 2));
+              } else {
+                wa[0] = *reinterpret_cast<const uint32_t*>(p);
+                wb[0] = *reinterpret_cast<const uint32_t*>(p + 8 * (HD / 2));
               }
-              s[t][x][j] = fmaf(dn * fa[t][j], fb, lo);
-            }
-        if (key0 + 15 > see0 || (key0 <= edge_to && key0 + 15 >= a.first)) {
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
+              for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[t][u][i] = 0.f;
+#pragma unroll
+              for (int w = 0; w < W; ++w) {
+                const uint32_t xa = wa[w] >> 8, xb = wb[w] >> 8;
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                  mma_f16(acc[t][u], wa[w] & LO, wb[w] & LO, wa[w] & HI, wb[w] & HI, qf[t][n][w][0], qf[t][n][w][1]);
+                  mma_f16(acc[t][u], xa & LO, xb & LO, xa & HI, xb & HI, qf[t][n][w][2], qf[t][n][w][3]);
+                }
+              }
+            }
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const float2 p = kv4_pair(*reinterpret_cast<const uint32_t*>(sk + F::CODES + ((ka + 8 * x) * NG + n) * 4));
+              const uint64_t d2 = f2_pack(p.x, p.x), lo2 = f2_pack(p.y, p.y);
+#pragma unroll
+              for (int t = 0; t < NT; ++t) {
+                const uint64_t ac = f2_pack(acc[t][x / 2][2 * (x & 1)], acc[t][x / 2][2 * (x & 1) + 1]), q2 = f2_pack(qs[t][n][0], qs[t][n][1]);
+                dn[t][x] = n == 0 ? f2_mul(d2, ac) : f2_fma(d2, ac, dn[t][x]);
+                lo[t][x] = n == 0 ? f2_mul(lo2, q2) : f2_fma(lo2, q2, lo[t][x]);
+              }
+            }
+          }
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            const uint64_t fa2 = f2_pack(fa[t][0], fa[t][1]), fb2 = f2_pack(fb, fb);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) s2[t][x] = f2_fma(f2_mul(dn[t][x], fa2), fb2, lo[t][x]);
+          }
+        }
+        uint32_t vp[4][NG];  // the pairs of V, of the same keys
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const uint8_t* at = sv + F::CODES + (ka + 8 * x) * NG * 4;
+          if constexpr (NG == 2) *reinterpret_cast<uint2*>(vp[x]) = *reinterpret_cast<const uint2*>(at);
+          else vp[x][0] = *reinterpret_cast<const uint32_t*>(at);
+        }
+        if (key0 + 31 > see0 || (key0 <= edge_to && key0 + 31 >= a.first)) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
             const int key = page0 + ka + 8 * x;
             const bool past = key >= a.first;
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-              for (int j = 0; j < 2; ++j)
-                if (key > see[t][j] || (past && key <= hidden_to(see[t][j], a.window))) s[t][x][j] = -INFINITY;
+            for (int t = 0; t < NT; ++t) {
+              float2 s = f2_unpack(s2[t][x]);
+              if (key > see[t][0] || (past && key <= hidden_to(see[t][0], a.window))) s.x = -INFINITY;
+              if (key > see[t][1] || (past && key <= hidden_to(see[t][1], a.window))) s.y = -INFINITY;
+              s2[t][x] = f2_pack(s.x, s.y);
+            }
             if (key > see_last || (past && key <= gone_to))  // nobody sees it: its pairs may be anything
 #pragma unroll
               for (int n = 0; n < NG; ++n) vp[x][n] = 0;
           }
         }
-        float p[NT][2][2];
-        uint32_t ph[NT][NG][2];  // p d of the two columns, keys ka and ka + 8
+        uint64_t p2[NT][4];
+        uint32_t ph[NT][4][NG];  // p d of the two columns
         auto weigh = [&] {
           bool grow = false;
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
+            const uint64_t m2 = f2_pack(-m[t][0], -m[t][1]);
             uint32_t big = 0;
+            float most = 0.f;
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-#pragma unroll
-              for (int j = 0; j < 2; ++j) p[t][x][j] = ex2_fast(s[t][x][j] - m[t][j]);
+            for (int x = 0; x < 4; ++x) {
+              const float2 e = f2_unpack(f2_add(s2[t][x], m2));
+              const float2 p = make_float2(ex2_fast(e.x), ex2_fast(e.y));
+              p2[t][x] = f2_pack(p.x, p.y);
+              most = fmaxf(most, fmaxf(p.x, p.y));
 #pragma unroll
               for (int n = 0; n < NG; ++n) {
                 const float d = kv4_pair(vp[x][n]).x;
-                ph[t][n][x] = pack_f16(p[t][x][0] * d, p[t][x][1] * d);
-                big |= ph[t][n][x] + 0x08000800u;  // the sign bit of a half from 2^15 on, infinities and NaN too
+                const float2 pd = f2_unpack(f2_mul(p2[t][x], f2_pack(d, d)));
+                ph[t][x][n] = pack_f16(pd.x, pd.y);
+                big |= ph[t][x][n] + 0x08000800u;  // the sign bit of a half from 2^15 on, infinities and NaN too
               }
             }
-            grow |= (big & 0x80008000u) != 0 || !(fmaxf(p[t][0][0], p[t][1][0]) <= 0x1p100f) || !(fmaxf(p[t][0][1], p[t][1][1]) <= 0x1p100f);
+            grow |= (big & 0x80008000u) != 0 || !(most <= 0x1p100f);
           }
           return __any_sync(0xffffffffu, grow);
         };
@@ -357,10 +367,11 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
             for (int j = 0; j < 2; ++j) {
               float top = NONE;
 #pragma unroll
-              for (int x = 0; x < 2; ++x) {
+              for (int x = 0; x < 4; ++x) {
                 float d = kv4_pair(vp[x][0]).x;
                 if constexpr (NG == 2) d = fmaxf(d, kv4_pair(vp[x][1]).x);
-                top = fmaxf(top, s[t][x][j] + log2f(fmaxf(d, 0x1p-100f)));
+                const float2 s = f2_unpack(s2[t][x]);
+                top = fmaxf(top, (j ? s.y : s.x) + log2f(fmaxf(d, 0x1p-100f)));
               }
 #pragma unroll
               for (int w = 4; w < 32; w *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
@@ -383,36 +394,46 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
+          uint64_t l2 = f2_pack(l[t][0], l[t][1]);
 #pragma unroll
-          for (int j = 0; j < 2; ++j) l[t][j] += p[t][0][j] + p[t][1][j];
+          for (int x = 0; x < 4; ++x) l2 = f2_add(l2, p2[t][x]);
+          const float2 ls = f2_unpack(l2);
+          l[t][0] = ls.x, l[t][1] = ls.y;
 #pragma unroll
           for (int n = 0; n < NG; ++n) {
-            const float la = kv4_pair(vp[0][n]).y, lb = kv4_pair(vp[1][n]).y;
+            uint64_t o2 = f2_pack(ol[t][n][0], ol[t][n][1]);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) ol[t][n][j] = fmaf(p[t][0][j], la, fmaf(p[t][1][j], lb, ol[t][n][j]));
-#pragma unroll
-            for (int x = 0; x < 2; ++x) ph[t][n][x] = transpose_8x8(ph[t][n][x]);
+            for (int x = 0; x < 4; ++x) {
+              const float lo = kv4_pair(vp[x][n]).y;
+              o2 = f2_fma(p2[t][x], f2_pack(lo, lo), o2);
+              ph[t][x][n] = transpose_8x8(ph[t][x][n]);
+            }
+            const float2 os = f2_unpack(o2);
+            ol[t][n][0] = os.x, ol[t][n][1] = os.y;
           }
         }
         // V: dims 8 g .. 8 g + 7 of a group (head_dim 32: 4 g .. 4 g + 3)
 #pragma unroll
         for (int n = 0; n < NG; ++n) {
-          uint32_t w[4];
-          const int at[4] = {va, vb, va + 8, vb + 8};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint8_t* q = sv + at[i] * (HD / 2) + n * 32 + g * (F::GS / 16);
-            if constexpr (F::GS == 64) w[i] = *reinterpret_cast<const uint32_t*>(q);
-            else w[i] = *reinterpret_cast<const uint16_t*>(q);
-          }
+          for (int u = 0; u < 2; ++u) {
+            uint32_t w[4];
+            const int at[4] = {va, vb, va + 8, vb + 8};
 #pragma unroll
-          for (int half = 0; half < MT / 2; ++half) {
-            const uint32_t sel = half ? 0x7632u : 0x5410u;
-            const uint32_t u = __byte_perm(w[0], w[1], sel), v = __byte_perm(w[2], w[3], sel), u8 = u >> 8, v8 = v >> 8;
+            for (int i = 0; i < 4; ++i) {
+              const uint8_t* q = sv + (at[i] + 16 * u) * (HD / 2) + n * 32 + g * (F::GS / 16);
+              if constexpr (F::GS == 64) w[i] = *reinterpret_cast<const uint32_t*>(q);
+              else w[i] = *reinterpret_cast<const uint16_t*>(q);
+            }
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-              mma_f16(o[t][n][2 * half], u & LO, u & HI, v & LO, v & HI, ph[t][n][0], ph[t][n][1]);
-              mma_f16(o[t][n][2 * half + 1], u8 & LO, u8 & HI, v8 & LO, v8 & HI, ph[t][n][0], ph[t][n][1]);
+            for (int h = 0; h < MT / 2; ++h) {
+              const uint32_t sel = h ? 0x7632u : 0x5410u;
+              const uint32_t x = __byte_perm(w[0], w[1], sel), y = __byte_perm(w[2], w[3], sel), x8 = x >> 8, y8 = y >> 8;
+#pragma unroll
+              for (int t = 0; t < NT; ++t) {
+                mma_f16(o[t][n][2 * h], x & LO, x & HI, y & LO, y & HI, ph[t][2 * u][n], ph[t][2 * u + 1][n]);
+                mma_f16(o[t][n][2 * h + 1], x8 & LO, x8 & HI, y8 & LO, y8 & HI, ph[t][2 * u][n], ph[t][2 * u + 1][n]);
+              }
             }
           }
         }
@@ -1258,7 +1279,7 @@ static cudaError_t q4_launch(const ChunkAttn& a, cudaStream_t st) {
   if (cudaError_t e = ensure_kernel_attrs(reinterpret_cast<const void*>(k_chunk_q4<HD, NT>), Sh::bytes(SV_MAX_ROWS))) return e;
   return launch_k(k_chunk_q4<HD, NT>, dim3(a.ctas), dim3(Sh::THREADS), Sh::bytes(a.c.n), st, a);
 }
-int chunk4_per_sm(int hd, int rows) { return rows > 8 ? 2 : hd == 128 ? 3 : 4; }
+int chunk4_per_sm(int hd, int rows) { return hd == 128 ? (rows > 8 ? 2 : 3) : rows > 8 ? 3 : 4; }
 template <int HD>
 static cudaError_t pair4_launch(const ChunkAttn& a, cudaStream_t st) {
   CUtensorMap qm;
