@@ -27,20 +27,25 @@ namespace tlf {
 // running maximum of s + log2(d), the largest d of the entry's groups, not of s, so that values of any magnitude fit. It is refreshed
 // when a product passes 2^15 (or p, where d is tiny, 2^100).
 //
-// CTAs of two teams of two warps, which take the pages in turn, a warp half of a page's 64 keys, 16 at a time in each step of the
+// CTAs of teams of two warps, which take the pages in turn, a warp half of a page's 64 keys, 16 at a time in each step of the
 // products; and a producer warp that copies a page's two blocks.
 struct Q4Seg {  // a CTA's part of an item: blocks kb0 .. kb1 - 1 of nb; nb = 0: no more
   int b, h, token0, see0, nq, kb0, kb1, nb;
   static constexpr int RING = 4;
 };
+constexpr int Q4_WARPS(int hd, int nt) { return 4; }
+constexpr int Q4_PER_SM(int hd, int nt) { return hd == 128 ? (nt == 2 ? 2 : 3) : nt == 2 ? 3 : 4; }
+constexpr int Q4_NST(int hd, int nt) { return hd == 128 ? (nt == 2 ? 8 : 6) : hd == 64 ? 8 : 12; }
 template <int HD, int NT>
 struct Q4Shape {
   using F = Kv4<HD>;
-  static constexpr int RT = 8 * NT, WARPS = 4, THREADS = 32 * (WARPS + 1), STAGE = 2 * F::BLOCK;
-  static constexpr int PER_SM = HD == 128 ? (NT == 2 ? 2 : 3) : NT == 2 ? 3 : 4;
-  static constexpr int NST = HD == 128 ? (NT == 2 ? 8 : 6) : HD == 64 ? 8 : 12;  // even: a stage is always the same team's
+  static constexpr int WARPS = Q4_WARPS(HD, NT), TEAMS = WARPS / 2;
+  static constexpr int RT = 8 * NT, THREADS = 32 * (WARPS + 1), STAGE = 2 * F::BLOCK;
+  static constexpr int PER_SM = Q4_PER_SM(HD, NT);
+  static constexpr int NST = Q4_NST(HD, NT);  // a multiple of TEAMS: a stage is always the same team's
+  static_assert(NST % TEAMS == 0, "");
   static constexpr int OS = HD + 4;  // floats of a merge buffer's row
-  static constexpr int OFF_O = NST * STAGE, OFF_ML = OFF_O + 2 * RT * OS * 4, OFF_BAR = OFF_ML + WARPS * RT * 8;
+  static constexpr int OFF_O = NST * STAGE, OFF_ML = OFF_O + TEAMS * RT * OS * 4, OFF_BAR = OFF_ML + WARPS * RT * 8;
   static constexpr int NBAR = 2 * NST + 2 * Q4Seg::RING;
   static constexpr int OFF_INT = OFF_BAR + NBAR * 8, OFF_SEG = OFF_INT + (NST + 2) / 2 * 8, OFF_BASE = OFF_SEG + Q4Seg::RING * (int)sizeof(Q4Seg);
   static int bytes(int n) { return OFF_BASE + (n + 1) * 8 + 128; }
@@ -107,6 +112,7 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
   const int G = c.G, qt = 1 << a.sp.qt_log;
   // a bounded wait; once one has run out, the others are skipped and everybody winds down
   auto wait = [&](uint32_t b, uint32_t parity) {
+    if (mbar_try_wait(b, parity & 1u)) return true;
     if (*abort_flag) return false;
     if (mbar_wait(b, parity & 1u, a.werr)) return true;
     *abort_flag = 1;
@@ -253,7 +259,7 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
       }
 
     for (int kb = it.kb0; kb < it.kb1; ++kb, ++seq) {
-      if ((int)(seq & 1u) != team) continue;
+      if ((int)(seq % Sh::TEAMS) != team) continue;
       const int st = seq % NST;
       const bool ok = __all_sync(0xffffffffu, wait(full(st), seq / NST));
       const int page0 = block_at<KEYS_4BIT>(kb, sinks, skip) * 64, key0 = page0 + half;
@@ -335,19 +341,18 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
         }
         uint64_t p2[NT][4];
         uint32_t ph[NT][4][NG];  // p d of the two columns
+        uint64_t psum[NT];
         auto weigh = [&] {
           bool grow = false;
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
             const uint64_t m2 = f2_pack(-m[t][0], -m[t][1]);
             uint32_t big = 0;
-            float most = 0.f;
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
               const float2 e = f2_unpack(f2_add(s2[t][x], m2));
               const float2 p = make_float2(ex2_fast(e.x), ex2_fast(e.y));
               p2[t][x] = f2_pack(p.x, p.y);
-              most = fmaxf(most, fmaxf(p.x, p.y));
 #pragma unroll
               for (int n = 0; n < NG; ++n) {
                 const float d = kv4_pair(vp[x][n]).x;
@@ -356,7 +361,10 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
                 big |= ph[t][x][n] + 0x08000800u;  // the sign bit of a half from 2^15 on, infinities and NaN too
               }
             }
-            grow |= (big & 0x80008000u) != 0 || !(most <= 0x1p100f);
+            const uint64_t sum2 = f2_add(f2_add(p2[t][0], p2[t][1]), f2_add(p2[t][2], p2[t][3]));
+            const float2 sum = f2_unpack(sum2);
+            grow |= (big & 0x80008000u) != 0 || !(fmaxf(sum.x, sum.y) <= 0x1p100f);
+            psum[t] = sum2;
           }
           return __any_sync(0xffffffffu, grow);
         };
@@ -394,10 +402,7 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          uint64_t l2 = f2_pack(l[t][0], l[t][1]);
-#pragma unroll
-          for (int x = 0; x < 4; ++x) l2 = f2_add(l2, p2[t][x]);
-          const float2 ls = f2_unpack(l2);
+          const float2 ls = f2_unpack(f2_add(f2_pack(l[t][0], l[t][1]), psum[t]));
           l[t][0] = ls.x, l[t][1] = ls.y;
 #pragma unroll
           for (int n = 0; n < NG; ++n) {
@@ -442,7 +447,7 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
       if (lane == 0) mbar_arrive(empty(st));
     }
 
-    // the warps' parts: each to the item's maximum, the upper two added to the lower two, then both
+    // the warps' parts: each to the item's maximum, the upper half's added to the lower's, then all
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -470,7 +475,7 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
           const float f = ex2_fast(m[t][j] - row_max(t * 8 + 2 * cl + j));
 #pragma unroll
           for (int n = 0; n < NG; ++n) {
-            float* to = s_o + ((warp & 1) * RT + t * 8 + 2 * cl + j) * OS + n * F::GS + g * (2 * MT);
+            float* to = s_o + (warp % Sh::TEAMS * RT + t * 8 + 2 * cl + j) * OS + n * F::GS + g * (2 * MT);
 #pragma unroll
             for (int i = 0; i < MT; i += 2) {  // dims in pairs: 2^24 n, and 2^24 16 n
               float4 v = make_float4(o[t][n][i][j] * 0x1p24f, o[t][n][i][2 + j] * 0x1p20f, o[t][n][i + 1][j] * 0x1p24f, o[t][n][i + 1][2 + j] * 0x1p20f);
@@ -485,16 +490,20 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
           }
         }
     };
-    if (warp >= 2) put(false);
+    if (warp >= Sh::TEAMS) put(false);
     bar_named(1, 32 * Sh::WARPS);
-    if (warp < 2) put(true);
+    if (warp < Sh::TEAMS) put(true);
     bar_named(1, 32 * Sh::WARPS);
     const bool whole = it.kb0 == 0 && it.kb1 == it.nb;
     const size_t part = (size_t)(2 * blockIdx.x + (it.kb0 == 0)) * a.rows;
     for (int i = tid; i < rows * (HD / 4); i += 32 * Sh::WARPS) {
       const int r = i / (HD / 4), d = (i % (HD / 4)) * 4;
-      const float4 u = *reinterpret_cast<const float4*>(s_o + r * OS + d), w = *reinterpret_cast<const float4*>(s_o + (RT + r) * OS + d);
-      const float4 v = make_float4(u.x + w.x, u.y + w.y, u.z + w.z, u.w + w.w);
+      float4 v = *reinterpret_cast<const float4*>(s_o + r * OS + d);
+#pragma unroll
+      for (int x = 1; x < Sh::TEAMS; ++x) {
+        const float4 u = *reinterpret_cast<const float4*>(s_o + (x * RT + r) * OS + d);
+        v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
+      }
       const float mm = row_max(r);
       float ll = 0.f;
 #pragma unroll
@@ -1279,7 +1288,7 @@ static cudaError_t q4_launch(const ChunkAttn& a, cudaStream_t st) {
   if (cudaError_t e = ensure_kernel_attrs(reinterpret_cast<const void*>(k_chunk_q4<HD, NT>), Sh::bytes(SV_MAX_ROWS))) return e;
   return launch_k(k_chunk_q4<HD, NT>, dim3(a.ctas), dim3(Sh::THREADS), Sh::bytes(a.c.n), st, a);
 }
-int chunk4_per_sm(int hd, int rows) { return hd == 128 ? (rows > 8 ? 2 : 3) : rows > 8 ? 3 : 4; }
+int chunk4_per_sm(int hd, int rows) { return Q4_PER_SM(hd, rows > 8 ? 2 : 1); }
 template <int HD>
 static cudaError_t pair4_launch(const ChunkAttn& a, cudaStream_t st) {
   CUtensorMap qm;

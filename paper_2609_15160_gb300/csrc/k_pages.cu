@@ -1,9 +1,10 @@
 // Pages of a pool and who holds them: rows that take over the pages of others (tlf_cache_fork), pages in use moved to the front
 // (tlf_cache_compact).
 //
-// Both are a plan and a copy. The plan (one cluster of eight CTAs) counts the free pages by prefix sums over the reference counts,
-// so that the k-th free page has a number without any list that outlives the call: the result depends on the inputs alone. The
-// copy runs on the whole GPU: tables, reference counts, and the entries of the pages that the plan names.
+// Both are a plan and a copy. The plan (one CTA, or a cluster of eight for large pools and many rows) counts the free pages by
+// prefix sums over the reference counts, so that the k-th free page has a number without any list that outlives the call: the result
+// depends on the inputs alone. The copy runs on the whole GPU: tables, reference counts, and the entries of the pages that the plan
+// names.
 #include <algorithm>
 
 #include <cooperative_groups.h>
@@ -14,7 +15,8 @@ namespace cg = cooperative_groups;
 
 namespace tlf {
 
-constexpr int PG_THREADS = 1024, PG_CLUSTER = 8, PG_ROWS = PG_THREADS * PG_CLUSTER;
+constexpr int PG_THREADS = 1024, PG_CLUSTER = 8, PG_WARPS = PG_THREADS / 32;
+constexpr int ONE_PAGES = 1 << 16;  // most pages of a plan by one CTA
 constexpr int COPY_THREADS = 256;
 
 // A page's blocks: (layers x K, V x heads) of two parts with `a` and `b` bytes an entry (codes and pairs in 4 bits; b = 0).
@@ -32,22 +34,60 @@ static PageShape page_shape(int layers, int hkv, int hd, int dtype, int kv_forma
   return s;
 }
 
-// Sums over the cluster: every thread gets the total and, in *before, the sum of the CTAs before its own. s_sum is the CTA's word.
-__device__ __forceinline__ int cluster_scan(int mine, int* s_sum, int* before) {
-  const cg::cluster_group cl = cg::this_cluster();
-  const int rank = blockIdx.x % PG_CLUSTER;
-  if (threadIdx.x == 0) *s_sum = mine;
-  cl.sync();
-  int total = 0, b = 0;
-  for (int i = 0; i < PG_CLUSTER; ++i) {
-    const int v = *cl.map_shared_rank(s_sum, i);
-    total += v;
-    if (i < rank) b += v;
-  }
-  cl.sync();  // nobody writes the word again, or leaves, before all have read it
-  *before = b;
-  return total;
+// Sums over the CTAs of the plan: every thread gets the total and, in *before, the sum of the CTAs before its own. s_sum is the CTA's
+// word. CS: how many CTAs, a cluster.
+template <int CS>
+__device__ __forceinline__ void plan_sync() {
+  if constexpr (CS > 1) cg::this_cluster().sync();
+  else __syncthreads();
 }
+template <int CS>
+__device__ __forceinline__ int plan_scan(int mine, int* s_sum, int* before) {
+  if constexpr (CS == 1) {
+    *before = 0;
+    return mine;
+  } else {
+    const cg::cluster_group cl = cg::this_cluster();
+    const int rank = blockIdx.x % CS;
+    if (threadIdx.x == 0) *s_sum = mine;
+    cl.sync();
+    int total = 0, b = 0;
+    for (int i = 0; i < CS; ++i) {
+      const int v = *cl.map_shared_rank(s_sum, i);
+      total += v;
+      if (i < rank) b += v;
+    }
+    cl.sync();  // nobody writes the word again, or leaves, before all have read it
+    *before = b;
+    return total;
+  }
+}
+
+// The pages in runs, one a warp of the plan: p0 .. p1 - 1 is this warp's. f(page, refs) for each, 32 at a time by all lanes (page n_pages
+// and refs -1 past the run's end).
+struct PageRun {
+  long long p0, p1;
+};
+template <int CS>
+__device__ __forceinline__ PageRun page_run(long long n_pages) {
+  const long long run = (n_pages + 32LL * PG_WARPS * CS - 1) / (32LL * PG_WARPS * CS) * 32, w = (blockIdx.x % CS) * PG_WARPS + (threadIdx.x >> 5);
+  PageRun r;
+  r.p0 = w * run < n_pages ? w * run : n_pages;
+  r.p1 = r.p0 + run < n_pages ? r.p0 + run : n_pages;
+  return r;
+}
+template <typename Fn>
+__device__ __forceinline__ void each_page(const PageRun& r, const int* refs, Fn&& f) {
+  constexpr int U = 4;
+  for (long long p = r.p0 + (threadIdx.x & 31); p - (threadIdx.x & 31) < r.p1; p += 32 * U) {
+    int v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = p + 32 * u < r.p1 ? refs[p + 32 * u] : -1;
+#pragma unroll
+    for (int u = 0; u < U; ++u) f(p + 32 * u, v[u], p + 32 * u < r.p1);
+  }
+}
+__device__ __forceinline__ int lanes_below(unsigned mask) { return __popc(mask & ((1u << (threadIdx.x & 31)) - 1)); }
 
 // ----------------------------------------------------------------------------
 // Fork
@@ -96,85 +136,97 @@ __device__ __forceinline__ int named(int page, long long n_pages, uint32_t* err)
   return -1;
 }
 
+constexpr int FORK_ONE_ROWS = 4096;  // most old rows of a plan by one CTA, which has their first new rows in shared memory
+template <int CS>
 __global__ void __launch_bounds__(PG_THREADS) k_fork_plan(ForkDev a) {
   pdl_wait();
+  extern __shared__ int s_rows[];  // CS = 1: [2 n_in]
   __shared__ int s_red[33];
   __shared__ int s_sum;
-  const cg::cluster_group cl = cg::this_cluster();
-  const int tid = threadIdx.x, rank = blockIdx.x % PG_CLUSTER, all = rank * PG_THREADS + tid;
-  for (int r = all; r < a.n_in; r += PG_ROWS) {
-    a.eldest[r] = 0x7fffffff;
-    a.children[r] = 0;
+  const int tid = threadIdx.x, lane = tid & 31, rank = blockIdx.x % CS;
+  int* eldest = CS == 1 ? s_rows : a.eldest;
+  int* children = CS == 1 ? s_rows + a.n_in : a.children;
+  for (int r = rank * PG_THREADS + tid; r < a.n_in; r += PG_THREADS * CS) {
+    eldest[r] = 0x7fffffff;
+    children[r] = 0;
   }
-  // free pages of this CTA's run, and the copy of the counts
-  const long long run = (a.n_pages + PG_CLUSTER - 1) / PG_CLUSTER, p0 = rank * run < a.n_pages ? rank * run : a.n_pages,
-                  p1 = p0 + run < a.n_pages ? p0 + run : a.n_pages;
+  // new rows in the order of their numbers: a run of them a CTA, a run of those a thread; a thread with one keeps it
+  const int rows = (a.n_out + CS - 1) / CS, b0 = min(a.n_out, rank * rows), b1 = min(a.n_out, b0 + rows);
+  const int each = (b1 - b0 + PG_THREADS - 1) / PG_THREADS, t0 = min(b1, b0 + tid * each), t1 = min(b1, t0 + each);
+  ForkRow first{-1, 0, 0, 0};
+  if (t0 < t1) first = fork_row(a, t0, true);
+  auto row_of = [&](int b) { return b == t0 ? first : fork_row(a, b, false); };
+  // free pages of this warp's run, and the copy of the counts
+  const PageRun run = page_run<CS>(a.n_pages);
   int count = 0;
-  for (long long p = p0 + tid; p < p1; p += PG_THREADS) {
-    const int v = a.refs[p];
+  each_page(run, a.refs, [&](long long p, int v, bool on) {
     count += v == 0;
-    if (a.refs_out != a.refs) a.refs_out[p] = v;
-  }
-  const int mine = block_sum(count, s_red);
-  int before;
-  const int n_free = cluster_scan(mine, &s_sum, &before);  // (its barriers order eldest's start before what follows)
-  for (int b = all; b < a.n_out; b += PG_ROWS) {
-    const ForkRow r = fork_row(a, b, true);
+    if (on && a.refs_out != a.refs) a.refs_out[p] = v;
+  });
+  count = __reduce_add_sync(0xffffffffu, count);
+  int cta_free, free_before;
+  int at_free = block_scan(lane == 0 ? count : 0, s_red, &cta_free);  // lane 0: free pages of the CTA's warps before
+  const int n_free = plan_scan<CS>(cta_free, &s_sum, &free_before);
+  at_free = __shfl_sync(0xffffffffu, at_free, 0) + free_before;
+  plan_sync<CS>();  // eldest has been started
+  for (int b = t0; b < t1; ++b) {
+    const ForkRow r = b == t0 ? first : fork_row(a, b, true);
     a.len[b] = r.len;
     if (r.parent >= 0) {
-      atomicMin(&a.eldest[r.parent], b);
-      atomicAdd(&a.children[r.parent], 1);
+      atomicMin(&eldest[r.parent], b);
+      atomicAdd(&children[r.parent], 1);
     }
   }
-  __threadfence();
-  cl.sync();
-  // does slot s >= full of row b keep the parent's page?
-  auto keeps = [&](const ForkRow& r, int b, int s) {
-    if (r.parent < 0 || __ldcg(&a.eldest[r.parent]) != b) return false;
+  if (CS > 1) __threadfence();
+  plan_sync<CS>();
+  // does slot s >= full of row b keep the parent's page? *old: that page
+  auto keeps = [&](const ForkRow& r, int b, int s, int* old) {
+    *old = -1;
+    if (r.parent < 0) return false;
     const int page = a.table_in[(size_t)r.parent * a.max_pages + s];
-    return page >= 0 && page < a.n_pages && a.refs[page] == 1;
+    if (page < 0 || page >= a.n_pages) return false;
+    *old = page;
+    return (CS == 1 ? eldest[r.parent] : __ldcg(&eldest[r.parent])) == b && a.refs[page] == 1;
   };
-  auto fresh = [&](int b) {
-    const ForkRow r = fork_row(a, b, false);
-    int n = 0;
-    for (int s = r.full; s < r.need; ++s) n += !keeps(r, b, s);
-    return n;
-  };
-  // rows in the order of their numbers: a run of them a CTA, a run of those a thread
-  const int rows = (a.n_out + PG_CLUSTER - 1) / PG_CLUSTER, b0 = min(a.n_out, rank * rows), b1 = min(a.n_out, b0 + rows);
-  const int each = (b1 - b0 + PG_THREADS - 1) / PG_THREADS, t0 = min(b1, b0 + tid * each), t1 = min(b1, t0 + each);
-  int want = 0;
-  for (int b = t0; b < t1; ++b) want += fresh(b);
+  int want = 0, old0 = -1;
+  bool keep0 = false;  // of the first row's first slot
+  for (int b = t0; b < t1; ++b) {
+    const ForkRow r = row_of(b);
+    for (int s = r.full; s < r.need; ++s) {
+      int old;
+      const bool k = keeps(r, b, s, &old);
+      want += !k;
+      if (b == t0 && s == r.full) keep0 = k, old0 = old;
+    }
+  }
   int all_mine, row_before;
   int at = block_scan(want, s_red, &all_mine);
-  const int total = cluster_scan(all_mine, &s_sum, &row_before);
+  const int total = plan_scan<CS>(all_mine, &s_sum, &row_before);
   at += row_before;
   // the first `total` free pages, in the order of their numbers
   const int taken = min(total, n_free);
-  for (long long base = p0; base < p1 && before < taken; base += PG_THREADS) {
-    const long long p = base + tid;
-    const int is = p < p1 && a.refs[p] == 0;
-    int here;
-    const int k = before + block_scan(is, s_red, &here);
-    if (is && k < taken) a.free[k] = (int)p;
-    before += here;
-  }
+  if (at_free < taken)
+    each_page(run, a.refs, [&](long long p, int v, bool) {
+      const unsigned is = __ballot_sync(0xffffffffu, v == 0);
+      const int k = at_free + lanes_below(is);
+      if (v == 0 && k < taken) a.free[k] = (int)p;
+      at_free += __popc(is);
+    });
   __threadfence();
-  cl.sync();
+  plan_sync<CS>();
   for (int b = t0; b < t1; ++b) {
-    const ForkRow r = fork_row(a, b, false);
+    const ForkRow r = row_of(b);
     int cut = r.len;
     for (int s = r.full; s < r.need; ++s) {
-      int page = -1;
-      const int old = r.parent >= 0 ? a.table_in[(size_t)r.parent * a.max_pages + s] : -1;
+      int page = -1, old = old0;
       const bool holds = s == r.full && r.len % SV_PAGE != 0;  // entries of the parent
-      if (keeps(r, b, s)) {
+      if (b == t0 && s == r.full ? keep0 : keeps(r, b, s, &old)) {
         page = old;
       } else {
         if (at < taken) page = __ldcg(&a.free[at]);
         else sv_report(a.err, SVERR_PAGES);
         ++at;
-        if (holds && (old < 0 || old >= a.n_pages)) {
+        if (holds && old < 0) {
           sv_report(a.err, DEVERR_INDEX);
           page = -1;
         }
@@ -184,7 +236,12 @@ __global__ void __launch_bounds__(PG_THREADS) k_fork_plan(ForkDev a) {
     }
     a.cut[b] = cut;
   }
-  cl.sync();
+  if constexpr (CS == 1)
+    for (int r = tid; r < a.n_in; r += PG_THREADS) {
+      a.eldest[r] = eldest[r];
+      a.children[r] = children[r];
+    }
+  if constexpr (CS > 1) cg::this_cluster().sync();
   pdl_trigger();
 }
 
@@ -295,7 +352,11 @@ cudaError_t launch_fork(const tlf_fork_args& a, void* scratch, int num_sms, cuda
                   page_shape(a.n_layers, a.n_kv_heads, a.head_dim, a.dtype, a.kv_format), static_cast<uint8_t*>(a.pool), a.page_table,
                   a.lens, a.parents, a.refs, a.table_out, a.lens_out, a.refs_out, a.entry_pos, a.entry_weight, a.err,
                   at(s.eldest), at(s.children), at(s.len), at(s.cut), at(s.free)};
-  if (cudaError_t e = launch_cluster(k_fork_plan, dim3(PG_CLUSTER), dim3(PG_THREADS), PG_CLUSTER, 0, st, d)) return e;
+  // (1000 pages, 64 rows: see below; a CTA's threads have the pages 32 K at a time)
+  const bool one = a.n_in <= FORK_ONE_ROWS && a.n_out <= FORK_ONE_ROWS && a.n_pages <= ONE_PAGES;
+  if (cudaError_t e = one ? launch_k(k_fork_plan<1>, dim3(1), dim3(PG_THREADS), (size_t)a.n_in * 8, st, d)
+                          : launch_cluster(k_fork_plan<PG_CLUSTER>, dim3(PG_CLUSTER), dim3(PG_THREADS), PG_CLUSTER, 0, st, d))
+    return e;
   const int units = std::max(1, (d.shape.blocks + COPY_THREADS / 32 - 1) / (COPY_THREADS / 32));
   const long long jobs = (long long)a.n_out * units + a.n_in;
   return launch_k(k_fork_apply, dim3((unsigned)std::min<long long>(jobs, 8LL * num_sms)), dim3(COPY_THREADS), 0, st, d, units);
@@ -317,34 +378,45 @@ struct CompactDev {
   int *hole, *mover, *rank, *count;  // scratch: [n_pages] target and source of the k-th move, [n_pages] k of a page that moves, moves
 };
 
+template <int CS>
 __global__ void __launch_bounds__(PG_THREADS) k_compact_plan(CompactDev a) {
   pdl_wait();
   __shared__ int s_red[33];
   __shared__ int s_sum;
-  const int tid = threadIdx.x, rank = blockIdx.x % PG_CLUSTER;
-  const long long run = (a.n_pages + PG_CLUSTER - 1) / PG_CLUSTER, p0 = rank * run < a.n_pages ? rank * run : a.n_pages,
-                  p1 = p0 + run < a.n_pages ? p0 + run : a.n_pages;
-  int count = 0, before, below_before;
-  for (long long p = p0 + tid; p < p1; p += PG_THREADS) count += a.refs[p] > 0;
-  const int live = cluster_scan(block_sum(count, s_red), &s_sum, &before);
-  count = 0;
-  for (long long p = p0 + tid; p < p1 && p < live; p += PG_THREADS) count += a.refs[p] > 0;
-  const int below = cluster_scan(block_sum(count, s_red), &s_sum, &below_before);  // pages in use that stay
-  for (long long base = p0; base < p1; base += PG_THREADS) {
-    const long long p = base + tid;
-    const int used = p < p1 && a.refs[p] > 0;
-    int here;
-    const int k = before + block_scan(used, s_red, &here);  // pages in use before p
-    if (p < p1) {
-      if (p < live && !used) a.hole[p - k] = (int)p;
-      if (p >= live && used) {
+  const int lane = threadIdx.x & 31;
+  const PageRun run = page_run<CS>(a.n_pages);
+  int count = 0, cta, before;
+  each_page(run, a.refs, [&](long long, int v, bool) { count += v > 0; });
+  count = __reduce_add_sync(0xffffffffu, count);
+  int at = block_scan(lane == 0 ? count : 0, s_red, &cta);  // lane 0: pages in use of the CTA's warps before
+  const int live = plan_scan<CS>(cta, &s_sum, &before);
+  at = __shfl_sync(0xffffffffu, at, 0) + before;
+  // pages in use that stay: those before page `live`, whose run knows how many they are
+  int below = -1;
+  {
+    int n = at;
+    if (run.p0 <= live && live < run.p1) {
+      each_page(run, a.refs, [&](long long p, int v, bool) { n += __popc(__ballot_sync(0xffffffffu, v > 0 && p < live)); });
+      below = n;
+    }
+  }
+  if (live >= a.n_pages) below = live;
+  int any;
+  below = plan_scan<CS>(block_sum(lane == 0 && below >= 0 && live < a.n_pages ? below : 0, s_red), &s_sum, &any);
+  if (live >= a.n_pages) below = live;
+  each_page(run, a.refs, [&](long long p, int v, bool on) {
+    const unsigned used = __ballot_sync(0xffffffffu, v > 0);
+    const int k = at + lanes_below(used);  // pages in use before p
+    if (on) {
+      if (p < live && v <= 0) a.hole[p - k] = (int)p;
+      if (p >= live && v > 0) {
         a.mover[k - below] = (int)p;
         a.rank[p] = k - below;
       }
     }
-    before += here;
-  }
-  if (rank == 0 && tid == 0) {
+    at += __popc(used);
+  });
+  if (blockIdx.x % CS == 0 && threadIdx.x == 0) {
     *a.n_live = live;
     *a.count = live - below;
   }
@@ -411,7 +483,9 @@ cudaError_t launch_compact(const tlf_compact_args& a, void* scratch, int num_sms
   const CompactDev d{a.n, a.max_pages, a.n_pages, page_shape(a.n_layers, a.n_kv_heads, a.head_dim, a.dtype, a.kv_format),
                      static_cast<uint8_t*>(a.pool), a.page_table, a.refs, a.table_out, a.refs_out, a.n_live, a.entry_pos,
                      a.entry_weight, a.err, at(s.hole), at(s.mover), at(s.rank), at(s.count)};
-  if (cudaError_t e = launch_cluster(k_compact_plan, dim3(PG_CLUSTER), dim3(PG_THREADS), PG_CLUSTER, 0, st, d)) return e;
+  if (cudaError_t e = a.n_pages <= ONE_PAGES ? launch_k(k_compact_plan<1>, dim3(1), dim3(PG_THREADS), 0, st, d)
+                                             : launch_cluster(k_compact_plan<PG_CLUSTER>, dim3(PG_CLUSTER), dim3(PG_THREADS), PG_CLUSTER, 0, st, d))
+    return e;
   const int units = std::max(1, (d.shape.blocks + COPY_THREADS / 32 - 1) / (COPY_THREADS / 32));
   return launch_k(k_compact_apply, dim3(8 * num_sms), dim3(COPY_THREADS), 0, st, d, units);
 }
