@@ -213,9 +213,10 @@ def _addr(buf) -> Optional[int]:
 def _stream(stream) -> Optional[int]:
     if stream is None:
         return None
-    if hasattr(stream, "cuda_stream"):
+    try:
         return stream.cuda_stream
-    return int(stream)
+    except AttributeError:
+        return int(stream)
 
 
 # ----------------------------------------------------------------------------
@@ -419,8 +420,8 @@ def _format(c: TlfChunk, four_bits: bool):
 
 
 def _pair(c: TlfChunk, a):
-    """The arguments' tensors are large enough for the batch (looked at once for the same numbers: a program may change them)."""
-    batch = (c.n_tokens, c.n_heads, c.n_kv_heads, c.head_dim, c.dtype, c.n_pages)
+    """The arguments' tensors are large enough for the batch (looked at once for the same batch: a program may change it)."""
+    batch = bytes(c)  # (one copy instead of six fields, each call)
     if getattr(a, "batch", None) == batch:
         return
     rows, hq, kh, hd, dt, pages = a.fits
