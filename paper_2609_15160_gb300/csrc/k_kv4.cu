@@ -109,10 +109,12 @@ __device__ __forceinline__ uint32_t quantise(float (&x)[8], uint32_t* pair, bool
   constexpr uint32_t ROUND_BITS = 0x4b400000u;
   auto least = [&] { return fminf(fminf(fminf(x[0], x[1]), fminf(x[2], x[3])), fminf(fminf(x[4], x[5]), fminf(x[6], x[7]))); };
   auto most = [&] { return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))); };
-  float lo = least(), hi = most(), zero = 0.f;
+  float lo = least(), hi = most();
+  uint64_t zero2 = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) zero = fmaf(x[i], 0.f, zero);  // infinities and NaN: not a number
-  const bool odd = !(zero == 0.f) || !(fmaxf(-lo, hi) <= LARGEST);
+  for (int i = 0; i < 8; i += 2) zero2 = f2_fma(f2_pack(x[i], x[i + 1]), 0, zero2);  // infinities and NaN: not a number
+  const float2 zero = f2_unpack(zero2);
+  const bool odd = !(zero.x + zero.y == 0.f) || !(fmaxf(-lo, hi) <= LARGEST);
   *bad = odd;
   if (odd) {
 #pragma unroll
@@ -134,12 +136,17 @@ __device__ __forceinline__ uint32_t quantise(float (&x)[8], uint32_t* pair, bool
   if (d >= 0x1p-80f && d <= 0x1p80f) {
     const float r = __frcp_rn(d);
     constexpr uint32_t EIGHT = (uint32_t)(0x11111111ull * ROUND_BITS);  // what the eight shifted ROUND_BITS add up to
+    const uint64_t lo2 = f2_pack(-lo, -lo), r2 = f2_pack(r, r), d2 = f2_pack(-d, -d), round2 = f2_pack(ROUND, ROUND);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float t = __fsub_rn(x[i], lo), q = __fmul_rn(t, r);
-      float n = fmaf(fmaf(-q, d, t), r, q);
-      if (!EXACT) n = fminf(fmaxf(n, 0.f), 15.f);
-      word += __float_as_uint(__fadd_rn(n, ROUND)) << (4 * i);
+    for (int i = 0; i < 8; i += 2) {  // (two at a time, each step rounded as it would be alone)
+      const uint64_t t = f2_add(f2_pack(x[i], x[i + 1]), lo2), q = f2_mul(t, r2);
+      uint64_t n = f2_fma(f2_fma(q, d2, t), r2, q);
+      if (!EXACT) {
+        const float2 c = f2_unpack(n);
+        n = f2_pack(fminf(fmaxf(c.x, 0.f), 15.f), fminf(fmaxf(c.y, 0.f), 15.f));
+      }
+      const float2 b = f2_unpack(f2_add(n, round2));
+      word += (__float_as_uint(b.x) << (4 * i)) + (__float_as_uint(b.y) << (4 * i + 4));
     }
     word -= EIGHT;
   } else if (d > 0.f) {
@@ -153,41 +160,25 @@ template <typename T, int HD, bool WIDE>
 __global__ void __launch_bounds__(256, 3) k_kv4_append(ChunkDev c, Kv4Append a) {
   using F = Kv4<HD>;
   constexpr int L = HD / 8, HP = 32 / L, GL = F::GS / 8;  // lanes of a head, heads of a pass, lanes of a group
-  constexpr int U = 2;                                    // passes in flight
   pdl_wait();
   const int lane = threadIdx.x & 31, d0 = (lane % L) * 8, half = a.rot / 2;
-  const int pq = (c.Hq + HP - 1) / HP, pk = (c.Hkv + HP - 1) / HP;  // passes over q, and over k or v
+  const int pq = (c.Hq + HP - 1) / HP, pk = (c.Hkv + HP - 1) / HP, passes = pq + 2 * pk;  // q's passes, then k's, then v's
   const bool turns = d0 < a.rot, pairs = turns && !a.interleaved;
+  const int partner = d0 < half ? half : -half;
   const long long warps = (long long)gridDim.x * 8, all = (long long)c.T * a.parts;
   for (long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); w < all; w += warps) {
     const int t = (int)(w / a.parts), part = (int)(w % a.parts);
-    int pos = a.positions[t];
-    const bool there = pos >= 0 && pos < a.max_pos;
-    if (!there) {
-      if (lane == 0) sv_report(c.err, DEVERR_INDEX);
-      pos = 0;
-    }
-    TokenEntry e = token_entry(c, t, F::BLOCK);
-    if (!there) e.block = -1;
-    if (part == 0 && lane == 0 && e.block >= 0) {
-      if (a.entry_pos) a.entry_pos[e.slot] = pos;
-      if (a.entry_weight) a.entry_weight[e.slot] = 0.f;
-    }
-    float2 cs[8];  // of each of the lane's dims; (1, 0): not turned
-    const float2* row = a.table + (long long)pos * half;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int d = d0 + i;
-      cs[i] = d >= a.rot ? make_float2(1.f, 0.f) : a.interleaved ? row[d / 2] : row[d < half ? d : d - half];
-      // x_a c - x_b s, x_b c + x_a s: the sign of what the paired dim adds
-      if (d < a.rot && (a.interleaved ? d % 2 == 0 : d < half)) cs[i].y = -cs[i].y;
-    }
-    auto load = [&](Raw8<T, WIDE>& x, Raw8<T, WIDE>& y, const void* from, long long stride, int h, bool turned) {
-      const T* src = static_cast<const T*>(from) + t * stride + (long long)h * HD;
+    const T *q_row = static_cast<const T*>(a.q) + t * a.qs, *k_row = static_cast<const T*>(a.k) + t * a.ks, *v_row = static_cast<const T*>(a.v) + t * a.vs;
+    // the lane's eight dims of pass p, and those that they are paired with; the next pass is in flight while one is worked on
+    auto load = [&](Raw8<T, WIDE>& x, Raw8<T, WIDE>& y, int p) {
+      const bool is_q = p < pq, is_v = p >= pq + pk;
+      const int h = (is_q ? p : is_v ? p - pq - pk : p - pq) * HP + lane / L;
+      if (h >= (is_q ? c.Hq : c.Hkv)) return;
+      const T* src = (is_q ? q_row : is_v ? v_row : k_row) + (unsigned)h * HD;
       x.load(src + d0);
-      if (!turned || !pairs) return;
+      if (is_v || !pairs) return;
       if constexpr (WIDE) {
-        y.load(src + (d0 < half ? d0 + half : d0 - half));
+        y.load(src + (d0 + partner));
       } else {
         T* to = reinterpret_cast<T*>(y.v);
 #pragma unroll
@@ -197,75 +188,90 @@ __global__ void __launch_bounds__(256, 3) k_kv4_append(ChunkDev c, Kv4Append a) 
         }
       }
     };
-    auto turn = [&](float* x, const Raw8<T, WIDE>& ry) {
-      if (!turns) return;
-      float y[8];
-      if (pairs) {
-        ry.get(y);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (WIDE || d0 + i < a.rot) x[i] = __fadd_rn(__fmul_rn(x[i], cs[i].x), __fmul_rn(y[i], cs[i].y));
-    };
-    // passes 0 .. pq - 1 are q's, then k's, then v's; a warp's are `part`, part + parts, ..
-    int p = part;
-    for (; p < pq; p += U * a.parts) {
-      Raw8<T, WIDE> rx[U], ry[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = (p + u * a.parts) * HP + lane / L;
-        if (h < c.Hq) load(rx[u], ry[u], a.q, a.qs, h, true);
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = (p + u * a.parts) * HP + lane / L;
-        if (h >= c.Hq) continue;
-        float x[8];
-        rx[u].get(x);
-        turn(x, ry[u]);
-        if (!there)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = 0.f;
-        const long long to = ((long long)t * c.Hq + h) * HD + d0;
-        if (a.q_f32) store8<float, WIDE>(static_cast<float*>(a.q_out) + to, x);
-        else store8<T, WIDE>(static_cast<T*>(a.q_out) + to, x);
-      }
+    Raw8<T, WIDE> rx{}, ry{};
+    if (part < passes) load(rx, ry, part);
+    int pos = a.positions[t];
+    const bool there = pos >= 0 && pos < a.max_pos;
+    if (!there) {
+      if (lane == 0) sv_report(c.err, DEVERR_INDEX);
+      pos = 0;
     }
-    if (e.block < 0) continue;
-    p = pq + ((part - pq) % a.parts + a.parts) % a.parts;  // the warp's first behind q's
-    for (; p < pq + 2 * pk; p += U * a.parts) {
-      Raw8<T, WIDE> rx[U], ry[U];
+    uint64_t c2[4], s2[4];  // cosines and sines of each of the lane's dims, two together
+    const float2* row = a.table + (long long)pos * half;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int at = p + u * a.parts - pq, is_v = at >= pk, h = (is_v ? at - pk : at) * HP + lane / L;
-        if (at < 2 * pk && h < c.Hkv) load(rx[u], ry[u], is_v ? a.v : a.k, is_v ? a.vs : a.ks, h, !is_v);
+    for (int i = 0; i < 8; i += 2) {
+      float2 cs[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int d = d0 + i + k;
+        cs[k] = d >= a.rot ? make_float2(1.f, 0.f) : a.interleaved ? row[d / 2] : row[d < half ? d : d - half];
+        // x_a c - x_b s, x_b c + x_a s: the sign of what the paired dim adds
+        if (d < a.rot && (a.interleaved ? d % 2 == 0 : d < half)) cs[k].y = -cs[k].y;
       }
+      c2[i / 2] = f2_pack(cs[0].x, cs[1].x);
+      s2[i / 2] = f2_pack(cs[0].y, cs[1].y);
+    }
+    TokenEntry e = token_entry(c, t, F::BLOCK);
+    if (!there) e.block = -1;
+    if (part == 0 && lane == 0 && e.block >= 0) {
+      if (a.entry_pos) a.entry_pos[e.slot] = pos;
+      if (a.entry_weight) a.entry_weight[e.slot] = 0.f;
+    }
+    uint8_t* blocks = static_cast<uint8_t*>(c.pool) + e.block;
+    const unsigned code_at = e.off * (HD / 2) + d0 / 2, pair_at = F::CODES + (e.off * F::NG + d0 / F::GS) * 4;
+    const long long out0 = (long long)t * c.Hq * HD;
+    const int end = e.block >= 0 ? passes : pq;  // without an entry: the query alone
+    for (int p = part; p < end; p += a.parts) {
+      Raw8<T, WIDE> nx{}, ny{};
+      if (p + a.parts < end) load(nx, ny, p + a.parts);
+      const bool is_q = p < pq, is_v = p >= pq + pk;
+      const int h = (is_q ? p : is_v ? p - pq - pk : p - pq) * HP + lane / L;
+      const bool on = h < (is_q ? c.Hq : c.Hkv);
+      float x[8];
+      rx.get(x);
+      if (!is_v && turns) {
+        float y[8];
+        if (pairs) {
+          ry.get(y);
+        } else {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int at = p + u * a.parts - pq, is_v = at >= pk, h = (is_v ? at - pk : at) * HP + lane / L;
-        if (at >= 2 * pk) break;
-        float x[8];
-        rx[u].get(x);
-        if (h >= c.Hkv)  // (the lanes of a head that is none take part in the groups' exchanges)
+          for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
+        }
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = 0.f;
-        else if (!is_v) turn(x, ry[u]);
+        for (int i = 0; i < 8; i += 2) {  // (products and sums rounded one by one)
+          const float2 v = f2_unpack(f2_add(f2_mul(f2_pack(x[i], x[i + 1]), c2[i / 2]), f2_mul(f2_pack(y[i], y[i + 1]), s2[i / 2])));
+          if (WIDE || d0 + i < a.rot) x[i] = v.x, x[i + 1] = v.y;
+        }
+      }
+      if (is_q) {
+        if (on) {
+          if (!there)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = 0.f;
+          const unsigned to = (unsigned)h * HD + d0;
+          if (a.q_f32) store8<float, WIDE>(static_cast<float*>(a.q_out) + out0 + to, x);
+          else store8<T, WIDE>(static_cast<T*>(a.q_out) + out0 + to, x);
+        }
+      } else {
         if (sizeof(T) == 2 && !is_v) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[i] = to_f32(from_f32<T>(x[i]));
         }
+        if (!on)  // (the lanes of a head that is none take part in the groups' exchanges)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = 0.f;
         uint32_t pair;
         bool bad;
         const uint32_t word = quantise<GL, sizeof(T) == 2>(x, &pair, &bad);
-        if (h >= c.Hkv) continue;
-        if (bad) sv_report(c.err, SVERR_VALUE);
-        uint8_t* block = static_cast<uint8_t*>(c.pool) + e.block + (long long)(is_v ? c.Hkv + h : h) * F::BLOCK;
-        *reinterpret_cast<uint32_t*>(block + e.off * (HD / 2) + d0 / 2) = word;
-        if (d0 % F::GS == 0) *reinterpret_cast<uint32_t*>(block + F::CODES + (e.off * F::NG + d0 / F::GS) * 4) = pair;
+        if (on) {
+          if (bad) sv_report(c.err, SVERR_VALUE);
+          uint8_t* block = blocks + (size_t)(is_v ? c.Hkv + h : h) * F::BLOCK;
+          *reinterpret_cast<uint32_t*>(block + code_at) = word;
+          if (d0 % F::GS == 0) *reinterpret_cast<uint32_t*>(block + pair_at) = pair;
+        }
       }
+      rx = nx;
+      ry = ny;
     }
   }
   pdl_trigger();
