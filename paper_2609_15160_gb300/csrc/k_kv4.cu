@@ -196,20 +196,14 @@ __global__ void __launch_bounds__(256, 3) k_kv4_append(ChunkDev c, Kv4Append a) 
       if (lane == 0) sv_report(c.err, DEVERR_INDEX);
       pos = 0;
     }
-    uint64_t c2[4], s2[4];  // cosines and sines of each of the lane's dims, two together
+    float2 cs[8];  // cosine and sine of each of the lane's dims
     const float2* row = a.table + (long long)pos * half;
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      float2 cs[2];
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int d = d0 + i + k;
-        cs[k] = d >= a.rot ? make_float2(1.f, 0.f) : a.interleaved ? row[d / 2] : row[d < half ? d : d - half];
-        // x_a c - x_b s, x_b c + x_a s: the sign of what the paired dim adds
-        if (d < a.rot && (a.interleaved ? d % 2 == 0 : d < half)) cs[k].y = -cs[k].y;
-      }
-      c2[i / 2] = f2_pack(cs[0].x, cs[1].x);
-      s2[i / 2] = f2_pack(cs[0].y, cs[1].y);
+    for (int i = 0; i < 8; ++i) {
+      const int d = d0 + i;
+      cs[i] = d >= a.rot ? make_float2(1.f, 0.f) : a.interleaved ? row[d / 2] : row[d < half ? d : d - half];
+      // x_a c - x_b s, x_b c + x_a s: the sign of what the paired dim adds
+      if (d < a.rot && (a.interleaved ? d % 2 == 0 : d < half)) cs[i].y = -cs[i].y;
     }
     TokenEntry e = token_entry(c, t, F::BLOCK);
     if (!there) e.block = -1;
@@ -238,10 +232,8 @@ __global__ void __launch_bounds__(256, 3) k_kv4_append(ChunkDev c, Kv4Append a) 
           for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
         }
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {  // (products and sums rounded one by one)
-          const float2 v = f2_unpack(f2_add(f2_mul(f2_pack(x[i], x[i + 1]), c2[i / 2]), f2_mul(f2_pack(y[i], y[i + 1]), s2[i / 2])));
-          if (WIDE || d0 + i < a.rot) x[i] = v.x, x[i + 1] = v.y;
-        }
+        for (int i = 0; i < 8; ++i)  // (products and sums rounded one by one; two an instruction, the compiler fuses them)
+          if (WIDE || d0 + i < a.rot) x[i] = __fadd_rn(__fmul_rn(x[i], cs[i].x), __fmul_rn(y[i], cs[i].y));
       }
       if (is_q) {
         if (on) {

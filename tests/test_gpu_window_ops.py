@@ -272,6 +272,8 @@ PACK = {
     "half-128": ([5, 64], [3, 130], 2, 1, 128, "bf16", 128, "half"),
     "inter-64": ([0, 7], [9, 1], 6, 2, 64, "bf16", 32, "interleaved"),
     "inter-128": ([0], [300], 8, 8, 128, "bf16", 128, "interleaved"),
+    "half-many": ([0, 7], [2500, 1200], 4, 4, 64, "bf16", 64, "half"),
+    "f32-many": ([3, 0], [1500, 900], 4, 2, 64, "f32", 64, "interleaved"),
     "odd-rot": ([3, 60], [5, 8], 3, 1, 64, "bf16", 10, "half"),
     "odd-rot-inter": ([3, 60], [5, 8], 3, 3, 32, "bf16", 6, "interleaved"),
     "32": ([0, 50], [20, 30], 4, 2, 32, "bf16", 32, "half"),
