@@ -866,6 +866,9 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
 // 4 x 1000 tokens with weights) has 16 keys in flight (four: 139). With the join: 327 us for the case above in single calls (1455
 // TFLOP/s, 0.76 of the measured bf16 rate; 371 to 386 in a long loop, where the clock falls), 284 us with 16 heads x 64 (838), 195 us
 // for 8192 causal tokens (1405).
+//
+// Under a window (MODE) the same on a band: 4 x 2048 tokens, window 1024, 16 / 8 heads x 128: 89 us (740 TFLOP/s): an
+// item has 20 blocks, so that its ends, which the loop does not hide, weigh more than in a whole cache.
 constexpr int PAIR_THREADS = 384;
 
 template <int HD>
@@ -2106,11 +2109,12 @@ static WindowPath window_path(const ChunkDev& c, int dtype, const tlf_attn_windo
     p.rt = whole.rt;
     p.ctas = whole.ctas;
     p.pad = whole.pad;
-  } else if (dtype == TLF_DTYPE_BF16 && c.hd >= 64 && (c.G & (c.G - 1)) == 0 && rows > (c.hd == 128 ? 16 : 32) &&
+  } else if (dtype == TLF_DTYPE_BF16 && c.hd >= 64 && (c.G & (c.G - 1)) == 0 && (rows > (c.hd == 128 ? 16 : 48) || c.G > 16) &&
              reinterpret_cast<uintptr_t>(a.q) % 16 == 0 && a.q_stride % 8 == 0) {
-    // tcgen05 where tiles of 16 rows, each with the cache again, take longer (32 rows of 16 / 32 / 64 tokens over up to 8192 entries,
-    // 16 / 8 heads x 128: 146 / 147 / 145 us against 160 / 304 / 600; 16 heads x 64, 24 / 32 / 64 tokens: 208 / 209 / 210 against
-    // 160 / 165 / 319; 4 rows of up to 100 tokens over up to 100 entries 16 / 15 against 26 / 17)
+    // tcgen05 where tiles of 16 rows, each with the cache again, take longer. 32 rows over up to 8192 entries, 16 / 8 heads x 128, of
+    // 8 / 12 / 16 / 32 tokens: 146 / 147 / 145 / 146 us, in tiles of 16 rows 85 / 145 / 148 / 282; 16 heads x 64, of 16 / 32 / 48 / 64
+    // tokens: 207 / 208 / 208 / 210, in tiles 78 / 140 / 204 / 267; under a window of 1024, 4 rows of 40 / 64 tokens: 22.1 / 22.5 and
+    // 21.3 / 23.8
     p.four = true;
     p.rt = PAIR_ROWS;
     p.ctas = num_sms;

@@ -29,6 +29,11 @@ namespace tlf {
 //
 // CTAs of teams of two warps, which take the pages in turn, a warp half of a page's 64 keys, 16 at a time in each step of the
 // products; and a producer warp that copies a page's two blocks.
+//
+// Bound by the latency of dependent instructions: the twelve warps that 128 registers a thread leave room for issue in 53 % of the
+// cycles. 16 single tokens over 32k entries, 16 / 8 heads x 128: 122 us with the join, 4.9 TB/s; 32 over up to 8192 entries, 16 heads x
+// 64: 53 us; 32 rows of up to 16 tokens under a window of 4096, 16 heads x 64: 59 us. The first of them with one team and 16 keys a step
+// 153 us, with more warps a CTA 163, with four CTAs an SM 153 and with two 132.
 struct Q4Seg {  // a CTA's part of an item: blocks kb0 .. kb1 - 1 of nb; nb = 0: no more
   int b, h, token0, see0, nq, kb0, kb1, nb;
   static constexpr int RING = 4;
@@ -553,9 +558,15 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
 // the largest s_t + e, O = sum 2^(s_t + e - M) V_t / 2^(e + 6), l = sum 2^(s_t + e - M) 2^-e, so that what has to be held in 16 bits is
 // relative to the row's largest term. e is the block's, by its largest entry; in a block with entries smaller than 2^-6 of that (as the
 // first tokens' values may be, which take most of the probability) every entry has its own: e_t - e is three more of the 16 columns,
-// beside 1 / (what the softmax multiplies by) in three float16, and 2^-e_t is read from shared memory (16 reads of 16 bytes a thread,
-// in the chain that bounds the kernel: with them in every block 721 us where it is 449 without). Where e_t - e does not fit float16
-// (scales over 2^12, keys over 2^18) entries keep the block's.
+// beside 1 / (what the softmax multiplies by) in three float16, and 2^-e_t is read from shared memory (own_block, which is
+// slow: all blocks by it take 1151 us where it is 449). Where e_t - e does not fit float16 (scales over 2^12, keys over 2^18) entries
+// keep the block's.
+//
+// Bound by the softmax warps' chain, as k_chunk_pair is, which the codes' warps make longer: their instructions and accesses of
+// shared memory meet its own and the MMAs' reads. A block of 64 keys and two tiles takes 2240 cycles at head_dim 128, of which the
+// tensor pipe works half. 4 x 2048 tokens over up to 10240 entries, 16 / 8 heads x 128: 446 us with the join, 1090 TFLOP/s (395 with
+// nothing converted, k_chunk_pair over bfloat16 371); 16 heads x 64: 396 us. Tried and slower: other splits of the registers (168 / 80,
+// 152 / 96), waits that sleep, the softmax's two halves in a loop (492).
 constexpr int PAIR4_THREADS = 512;
 template <int HD>
 struct Pair4Shape {

@@ -6,6 +6,10 @@
 // warp goes over a token's heads, 256 / head_dim at a time, so that a lane's dims, and with them its row of the rotary table, stay
 // the same for all of them. Sums and products are rounded one by one: a code next to a border does not depend on how they are
 // fused.
+//
+// Bound by instructions (69 % of the issue slots) and the latency of a token's passes, two waves of warps: 7157 tokens, 16 / 8 heads
+// x 128, 64 dims turned: 33 us; reading them back 12 us. With the compiler's divisions 79 us. 64 tokens, 16 heads x 64: 6.3 us with
+// their read, in a graph.
 #include <algorithm>
 
 #include "k_kv4.cuh"
@@ -32,7 +36,7 @@ __device__ __forceinline__ int token_row(const ChunkDev& c, int t) {
   return b;
 }
 
-// The entry of token t: byte offset of K's block of head 0 and place in the page; -1 without one (reported if `must`).
+// The entry of token t: byte offset of K's block of head 0 and place in the page; -1 (reported) without one.
 struct TokenEntry {
   long long block, slot;  // bytes from the pool's start; page * 64 + place
   int off;
@@ -312,7 +316,8 @@ __global__ void __launch_bounds__(256) k_kv4_read(ChunkDev c, Kv4Read a) {
   pdl_trigger();
 }
 
-// Warps that share a token: one each where the tokens fill the GPU, else as many as it has passes.
+// Warps that share a token: one each where the tokens fill the GPU, else as many as it has passes (append and read, 16 / 8 heads x 128:
+// 7157 tokens 44.9 us, with two 49.1; 1600 tokens 16.1, with one 17.9; 512 tokens 11.0, with one 14.2).
 static int token_parts(int T, int passes, int num_sms) {
   return (int)std::min<long long>(passes, std::max<long long>(1, (long long)num_sms * 32 / std::max(1, T)));
 }

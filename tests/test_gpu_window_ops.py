@@ -83,6 +83,9 @@ SHAPES = {
     "none-new": ([10, 0, 64, 130], [0, 4, 0, 2], 4, 2, 32, "bf16"),
     "mqa": ([0, 77], [5, 11], 24, 1, 64, "bf16"),
     "g64": ([3, 150], [2, 1], 64, 1, 64, "bf16"),
+    "g32-ones": ([200, 0, 63], [1, 1, 1], 32, 1, 64, "bf16"),
+    "few-48": ([0, 300], [48, 40], 2, 2, 64, "bf16"),
+    "many-49": ([0, 300], [49, 40], 2, 2, 64, "bf16"),
     "many": ([0, 64, 100], [130, 257, 64], 4, 2, 128, "bf16"),
     "many-mha": ([0, 1, 500], [300, 127, 128], 2, 2, 64, "bf16"),
     "many-g5": ([17, 200], [140, 33], 5, 1, 64, "bf16"),
