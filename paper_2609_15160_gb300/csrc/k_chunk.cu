@@ -2109,7 +2109,7 @@ static WindowPath window_path(const ChunkDev& c, int dtype, const tlf_attn_windo
     p.rt = whole.rt;
     p.ctas = whole.ctas;
     p.pad = whole.pad;
-  } else if (dtype == TLF_DTYPE_BF16 && c.hd >= 64 && (c.G & (c.G - 1)) == 0 && (rows > (c.hd == 128 ? 16 : 48) || c.G > 16) &&
+  } else if (dtype == TLF_DTYPE_BF16 && c.hd >= 64 && (c.G & (c.G - 1)) == 0 && (rows > (c.hd == 128 ? 16 : 48) || (c.G > 16 && rows > 0)) &&
              reinterpret_cast<uintptr_t>(a.q) % 16 == 0 && a.q_stride % 8 == 0) {
     // tcgen05 where tiles of 16 rows, each with the cache again, take longer. 32 rows over up to 8192 entries, 16 / 8 heads x 128, of
     // 8 / 12 / 16 / 32 tokens: 146 / 147 / 145 / 146 us, in tiles of 16 rows 85 / 145 / 148 / 282; 16 heads x 64, of 16 / 32 / 48 / 64

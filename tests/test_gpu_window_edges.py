@@ -98,6 +98,21 @@ def test_rows_behind_the_last_token_and_past_max_chunk_stay_as_they_were(T, kind
         assert (lse[:c.T] == 7).sum() == 3 * c.hq
 
 
+@pytest.mark.parametrize("kind", ["plain", "4bit"])
+@pytest.mark.parametrize("hq,hd,dtype", [(4, 64, "bf16"), (64, 64, "bf16"), (64, 128, "bf16"), (4, 64, "f32")])
+def test_a_batch_without_tokens_writes_nothing(T, kind, hq, hd, dtype):
+    import torch
+    c = _cache(kind, [70, 0, 300], [0, 0, 0], hq, 2, hd, dtype, seed=1)
+    d = c.device()
+    q = torch.ones(3, hq, hd, dtype=getattr(torch, {"bf16": "bfloat16", "f32": "float32"}[dtype]), device="cuda")
+    out, lse = torch.full_like(q, 7), torch.full((3, hq), 7.0, device="cuda")
+    b, a = _batch(T, c, d), T.attn_window_args(q, out, lse=lse, window=30, n_first=1, kv4=kind == "4bit")
+    n = T.tlf_attn_window_scratch_bytes(b, a)
+    T.tlf_attn_window(b, a, torch.empty(n, dtype=torch.uint8, device="cuda"), n)
+    torch.cuda.synchronize()
+    assert (out == 7).all() and (lse == 7).all() and int(d["err"][0].item()) == 0
+
+
 def test_calls_on_two_streams_at_once(T):
     """Attention of two batches, a fork and a compaction of two pools, each with its own scratch, at the same time."""
     import torch
