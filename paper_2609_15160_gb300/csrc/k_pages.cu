@@ -8,7 +8,7 @@
 //
 // Small calls are bound by the plan's latency and the host's call (forks of 64 rows over 1000 pages: 9.7 us in a graph; compaction of 16
 // rows: 7.1 us), large ones by HBM (a compaction that reads and writes 2.7 GB: 411 us, 6.7 TB/s; the copies of 512 rows forked off 32,
-// 388 MB written: 84 us, 4.6 TB/s).
+// 388 MB written: 75 us, 5.2 TB/s).
 #include <algorithm>
 
 #include <cooperative_groups.h>
@@ -275,7 +275,9 @@ __device__ __forceinline__ void copy_entries(const PageShape& sh, const uint8_t*
 
 // Work units of eight blocks a row (a warp a block); the first unit of a row also writes its table row, counts its references, and
 // so on. What k_fork_plan has put into table_out, slots full .. need - 1, is only read here.
-__global__ void __launch_bounds__(COPY_THREADS) k_fork_apply(ForkDev a, int units) {
+// Units differ (rows without a copy have nearly nothing to do): many small CTAs, four on an SM. 512 rows forked off 32: 75 us the call; with
+// three on an SM and 1216 CTAs, as registers would have it, 85, with five (spills) 117.
+__global__ void __launch_bounds__(COPY_THREADS, 4) k_fork_apply(ForkDev a, int units) {
   pdl_trigger();
   pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -364,7 +366,7 @@ cudaError_t launch_fork(const tlf_fork_args& a, void* scratch, int num_sms, cuda
     return e;
   const int units = std::max(1, (d.shape.blocks + COPY_THREADS / 32 - 1) / (COPY_THREADS / 32));
   const long long jobs = (long long)a.n_out * units + a.n_in;
-  return launch_k(k_fork_apply, dim3((unsigned)std::min<long long>(jobs, 8LL * num_sms)), dim3(COPY_THREADS), 0, st, d, units);
+  return launch_k(k_fork_apply, dim3((unsigned)std::min<long long>(jobs, 32LL * num_sms)), dim3(COPY_THREADS), 0, st, d, units);
 }
 
 // ----------------------------------------------------------------------------
