@@ -867,7 +867,7 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
 // TFLOP/s, 0.76 of the measured bf16 rate; 371 to 386 in a long loop, where the clock falls), 284 us with 16 heads x 64 (838), 195 us
 // for 8192 causal tokens (1405).
 //
-// Under a window (MODE) the same on a band: 4 x 2048 tokens, window 1024, 16 / 8 heads x 128: 89 us (740 TFLOP/s): an
+// Under a window (MODE) the same on a band: 4 x 2048 tokens, window 1024, 16 / 8 heads x 128: 88 us (740 TFLOP/s): an
 // item has 20 blocks, so that its ends, which the loop does not hide, weigh more than in a whole cache.
 constexpr int PAIR_THREADS = 384;
 
