@@ -23,9 +23,11 @@ namespace tlf {
 // A lane's word of K has codes i and i + 4 in one register, which q's fragment follows; words of V of two neighbouring keys are
 // paired by byte permutations. q is scaled by a power of two a row into float16's range.
 //
-// p_t d_t,g is rounded to float16, an operand's type, as the other kernels round p. What float16 has to hold is 2^(s - M) d: M is the
-// running maximum of s + log2(d), the largest d of the entry's groups, not of s, so that values of any magnitude fit. It is refreshed
-// when a product passes 2^15 (or p, where d is tiny, 2^100).
+// p_t d_t,g is rounded to float16, an operand's type, as the other kernels round p. What float16 has to hold is 2^(s - M) d: M + 8 is
+// the running maximum of s + log2(z), not of s, so that values of any magnitude fit. z, the size of an entry's values, is the largest of
+// its groups' d and of 2^-64 |lo| + 2^-60: groups that hold one value, or nothing, have no d. M is refreshed when a p d passes 2^15, a
+// lane's sum of p 2^80 or one of p lo 2^110: p is at most 2^68 then and p lo 2^72, so that float32 holds the sums over 2^31 entries.
+// Digits go where values are below 2^-80, and, where they are of 2^100 and more, with what weighs less than 2^-26.
 //
 // CTAs of teams of two warps, which take the pages in turn, a warp half of a page's 64 keys, 16 at a time in each step of the
 // products; and a producer warp that copies a page's two blocks.
@@ -344,34 +346,40 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
               for (int n = 0; n < NG; ++n) vp[x][n] = 0;
           }
         }
-        uint64_t p2[NT][4];
         uint32_t ph[NT][4][NG];  // p d of the two columns
-        uint64_t psum[NT];
+        uint64_t psum[NT], lsum[NT][NG];  // sum of p; ol with this step's
         auto weigh = [&] {
-          bool grow = false;
+          uint32_t big = 0;
+          float sums = 0.f, lows = 0.f;
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
             const uint64_t m2 = f2_pack(-m[t][0], -m[t][1]);
-            uint32_t big = 0;
+            uint64_t p2[4];
+#pragma unroll
+            for (int n = 0; n < NG; ++n) lsum[t][n] = f2_pack(ol[t][n][0], ol[t][n][1]);
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
               const float2 e = f2_unpack(f2_add(s2[t][x], m2));
               const float2 p = make_float2(ex2_fast(e.x), ex2_fast(e.y));
-              p2[t][x] = f2_pack(p.x, p.y);
+              p2[x] = f2_pack(p.x, p.y);
 #pragma unroll
               for (int n = 0; n < NG; ++n) {
-                const float d = kv4_pair(vp[x][n]).x;
-                const float2 pd = f2_unpack(f2_mul(p2[t][x], f2_pack(d, d)));
+                const float2 v = kv4_pair(vp[x][n]), pd = f2_unpack(f2_mul(p2[x], f2_pack(v.x, v.x)));
                 ph[t][x][n] = pack_f16(pd.x, pd.y);
                 big |= ph[t][x][n] + 0x08000800u;  // the sign bit of a half from 2^15 on, infinities and NaN too
+                lsum[t][n] = f2_fma(p2[x], f2_pack(v.y, v.y), lsum[t][n]);
               }
             }
-            const uint64_t sum2 = f2_add(f2_add(p2[t][0], p2[t][1]), f2_add(p2[t][2], p2[t][3]));
-            const float2 sum = f2_unpack(sum2);
-            grow |= (big & 0x80008000u) != 0 || !(fmaxf(sum.x, sum.y) <= 0x1p100f);
-            psum[t] = sum2;
+            psum[t] = f2_add(f2_add(p2[0], p2[1]), f2_add(p2[2], p2[3]));
+            const float2 sum = f2_unpack(psum[t]);
+            sums = fmaxf(sums, fmaxf(sum.x, sum.y));
+#pragma unroll
+            for (int n = 0; n < NG; ++n) {
+              const float2 low = f2_unpack(lsum[t][n]);
+              lows = fmaxf(lows, fmaxf(fabsf(low.x), fabsf(low.y)));
+            }
           }
-          return __any_sync(0xffffffffu, grow);
+          return __any_sync(0xffffffffu, (big & 0x80008000u) != 0 || sums > 0x1p80f || lows > 0x1p110f);
         };
         if (weigh()) {
 #pragma unroll
@@ -381,10 +389,13 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
               float top = NONE;
 #pragma unroll
               for (int x = 0; x < 4; ++x) {
-                float d = kv4_pair(vp[x][0]).x;
-                if constexpr (NG == 2) d = fmaxf(d, kv4_pair(vp[x][1]).x);
+                float2 p = kv4_pair(vp[x][0]);
+                if constexpr (NG == 2) {
+                  const float2 r = kv4_pair(vp[x][1]);
+                  p = make_float2(fmaxf(p.x, r.x), fmaxf(fabsf(p.y), fabsf(r.y)));
+                }
                 const float2 s = f2_unpack(s2[t][x]);
-                top = fmaxf(top, (j ? s.y : s.x) + log2f(fmaxf(d, 0x1p-100f)));
+                top = fmaxf(top, (j ? s.y : s.x) + (log2f(fmaxf(p.x, fmaf(fabsf(p.y), 0x1p-64f, 0x1p-60f))) - 8.f));
               }
 #pragma unroll
               for (int w = 4; w < 32; w *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
@@ -411,15 +422,10 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
           l[t][0] = ls.x, l[t][1] = ls.y;
 #pragma unroll
           for (int n = 0; n < NG; ++n) {
-            uint64_t o2 = f2_pack(ol[t][n][0], ol[t][n][1]);
+            const float2 low = f2_unpack(lsum[t][n]);
+            ol[t][n][0] = low.x, ol[t][n][1] = low.y;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const float lo = kv4_pair(vp[x][n]).y;
-              o2 = f2_fma(p2[t][x], f2_pack(lo, lo), o2);
-              ph[t][x][n] = transpose_8x8(ph[t][x][n]);
-            }
-            const float2 os = f2_unpack(o2);
-            ol[t][n][0] = os.x, ol[t][n][1] = os.y;
+            for (int x = 0; x < 4; ++x) ph[t][x][n] = transpose_8x8(ph[t][x][n]);
           }
         }
         // V: dims 8 g .. 8 g + 7 of a group (head_dim 32: 4 g .. 4 g + 3)
@@ -463,7 +469,13 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
 #pragma unroll
           for (int n = 0; n < NG; ++n) ol[t][n][j] += __shfl_xor_sync(0xffffffffu, ol[t][n][j], w);
         }
-        if (g == 0) s_ml[warp * RT + t * 8 + 2 * cl + j] = make_float2(m[t][j], l[t][j]);
+        // (M goes up by the power of two in l where that is positive: parts whose values differ by more than 2^126 meet at one M)
+        float2 ml = make_float2(m[t][j], l[t][j]);
+        if (ml.y > 0x1p20f) {
+          ml.x += (float)((int)(__float_as_uint(ml.y) >> 23) - 127);
+          ml.y *= ex2_fast(m[t][j] - ml.x);
+        }
+        if (g == 0) s_ml[warp * RT + t * 8 + 2 * cl + j] = ml;
       }
     bar_named(1, 32 * Sh::WARPS);
     auto row_max = [&](int r) {

@@ -1,0 +1,76 @@
+"""Attention over 4-bit caches at the ends of what they hold: values, keys, queries and scales of any magnitude.
+
+Bounds as in test_gpu_window_ops, with a little more for the statistics: they are kept relative to powers of two of up to 126 to
+either side, so that sums and differences of numbers below 256 are rounded to half a step of 2^-16 up to four times, each a
+relative error of 2^-17 ln 2 of a probability: 2^-15 in all, in lse and, beside the rounding to bfloat16, in out.
+"""
+import numpy as np
+import pytest
+
+import _serve_ref as R
+import _window_ref as W
+from test_gpu_window_ops import RB, T, U, _attend  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+STAT = 2.0 ** -15
+
+
+def _hold_far(c, d, got, ref, tokens=None):
+    out, lse, spread, terms = (x if tokens is None else x[tokens] for x in ref)
+    D = 2 * (c.hd + 8) * U * terms
+    o, l = (x[:c.T].float().cpu().numpy().astype(np.float64) for x in got)
+    if tokens is not None:
+        o, l = o[tokens], l[tokens]
+    bound = (2 * D + STAT + RB)[..., None] * spread + (RB + 4 * U) * np.abs(out) * (1 + RB)
+    assert np.isfinite(o).all() and (np.abs(o - out) <= bound).all(), np.nanmax(np.abs(o - out) / np.maximum(bound, 1e-300))
+    lb = D + STAT + 2 * U * np.abs(lse)
+    assert (np.abs(l - lse) <= lb).all(), np.max(np.abs(l - lse) / lb)
+    assert int(d["err"][0].item()) == 0
+
+
+def _filled(c, what, size, seed=0):
+    """Values of about `size`: each entry's all the same, the same behind 150 entries of zeros, or at random."""
+    rng = np.random.default_rng(seed)
+    v = c.pool[:, :, 1]
+    if what == "random":
+        v *= np.float32(size / 16)  # (heads off centre and entries four times the others: up to 2^4)
+        np.clip(v, -size, size, out=v)
+    else:
+        v[:] = (size * rng.choice([-1.0, 1.0], v.shape[:-1] + (1,)) * rng.uniform(0.5, 1, v.shape[:-1] + (1,))).astype(np.float32)
+    if what == "zeros":
+        for b in range(c.n):
+            p, o = c.at(b, np.arange(min(150, c.lens[b])))
+            c.pool[p, c.layer, 1, :, o] = 0
+    c.pool4 = W.blocks(*W.quantise(c.round(c.pool)))
+
+
+@pytest.mark.parametrize("what", ["one value", "zeros", "random"])
+@pytest.mark.parametrize("old,new,hq,hkv,hd", [
+    ([0, 0, 40], [1, 1, 1], 4, 2, 64), ([5000, 300], [1, 1], 4, 2, 128), ([600, 150], [1, 1], 4, 4, 32), ([3000, 0], [3, 1], 8, 2, 128),
+    ([5000, 300], [9, 16], 2, 2, 64)], ids=["one", "ones", "ones-32", "few", "few-64"])
+@pytest.mark.parametrize("size", [2.0 ** -70, 2.0 ** -40, 2.0 ** 13, 2.0 ** 28, 2.0 ** 70, 2.0 ** 126])
+def test_values_of_any_magnitude_few_tokens(T, what, old, new, hq, hkv, hd, size):
+    """32768 entries of 8192, or one of 2^28, in all dims once passed float32's range in the sums."""
+    c = W.Cache4(old, new, hq, hkv, hd, "bf16", seed=hd)
+    _filled(c, what, min(size, 2.0 ** 100) if what == "random" else size)
+    d = c.device()
+    for window, first in ((0, 0), (70, 3)):
+        _hold_far(c, d, _attend(T, c, d, window, first, max_chunk=max(new)), W.attention(c, window, first))
+
+
+@pytest.mark.parametrize("new", [[1, 1], [4, 7]], ids=["one", "few"])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_magnitudes_beside_each_other_few_tokens(T, new, hd):
+    """Entries from 2^-70 to 2^90, some with all values alike, some with large scores. What a small term adds is rounded to the row's
+    largest."""
+    c = W.Cache4([700, 200], new, 4, 2, hd, "bf16", seed=hd + 1)
+    rng = np.random.default_rng(5)
+    c.pool[:, :, 1] *= (2.0 ** rng.uniform(-70, 90, c.pool[:, :, 1].shape[:-1] + (1,))).astype(np.float32)
+    c.pool[:, :, 1, :, 5::7] = c.pool[:, :, 1, :, 5::7, :1]
+    c.pool[:, :, 0, :, 3::50] *= 20
+    c.pool4 = W.blocks(*W.quantise(c.round(c.pool)))
+    d = c.device()
+    for window, first in ((0, 0), (33, 5)):
+        ref = W.attention(c, window, first)
+        top = ref[2].max(-1, keepdims=True)
+        _hold_far(c, d, _attend(T, c, d, window, first, max_chunk=max(new)), (ref[0], ref[1], np.maximum(ref[2], top), ref[3]))
