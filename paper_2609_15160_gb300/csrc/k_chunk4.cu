@@ -197,6 +197,8 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
     if (it.nb == 0) break;
     const int nq = it.nq, rows = nq * G, see0 = it.see0, see_last = see0 + nq - 1;
     const int skip = sp.skip_at(see0), gone_to = hidden_to(see0, a.window), edge_to = hidden_to(see_last, a.window);
+    // 2^24 and the scale together may pass float32's range; where they could, q of finite scores is small, and the power goes to q's
+    const bool vast = a.scale > 0x1p64f;
     // q of row g of every tile: dims 64 grp + 8 w + i, words w = 2 cl, 2 cl + 1 (head_dim 32: w = cl)
     uint32_t qf[NT][NG][W][4];
     float fa[NT][2], qs[NT][NG][2];  // of this lane's columns 2 cl, 2 cl + 1: what the scaled q counts, scale times the sums of q
@@ -228,7 +230,7 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
       // a power of two that puts the largest into 2^14 .. 2^15
-      const int e = max(-100, min(126, (int)(__float_as_uint(mx) >> 23) - 127));
+      const int e = max(-112, min(126, (int)(__float_as_uint(mx) >> 23) - 127));
       const float up = __uint_as_float((uint32_t)(14 - e + 127) << 23), down = __uint_as_float((uint32_t)(max(e - 14, -126) + 127) << 23);
 #pragma unroll
       for (int n = 0; n < NG; ++n)
@@ -242,14 +244,14 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int from = 4 * (2 * cl + j), rj = t * 8 + 2 * cl + j;
-        fa[t][j] = __shfl_sync(0xffffffffu, down, from);
+        fa[t][j] = __shfl_sync(0xffffffffu, down, from) * (vast ? 0x1p64f : 1.f);
 #pragma unroll
         for (int n = 0; n < NG; ++n) qs[t][n][j] = __shfl_sync(0xffffffffu, sum[n], from) * a.scale;
         // rows past the tile's see what its first query sees, with q = 0; nobody reads them
         see[t][j] = see0 + (rj < rows ? rj / G : 0);
       }
     }
-    const float fb = a.scale * 0x1p24f;
+    const float fb = a.scale * (vast ? 0x1p-40f : 0x1p24f);
     float m[NT][2], l[NT][2], ol[NT][NG][2], o[NT][NG][MT][4];
 #pragma unroll
     for (int t = 0; t < NT; ++t)

@@ -74,3 +74,36 @@ def test_magnitudes_beside_each_other_few_tokens(T, new, hd):
         ref = W.attention(c, window, first)
         top = ref[2].max(-1, keepdims=True)
         _hold_far(c, d, _attend(T, c, d, window, first, max_chunk=max(new)), (ref[0], ref[1], np.maximum(ref[2], top), ref[3]))
+
+
+def _scaled(c, q, every):
+    """Queries times q, every third one zero, every other third (the one behind it) as `every` says."""
+    c.q = R.bf16(c.q * np.float32(q))
+    c.q[::3] = 0
+    c.q[1::3] = R.bf16(c.q[1::3] * np.float32(every))
+
+
+@pytest.mark.parametrize("scale,q", [(1e19, 2.0 ** -63), (1e31, 2.0 ** -103), (1e31, 1.0), (1e35, 2.0 ** -116), (1e35, 1.0), (2e38, 2.0 ** -122)])
+@pytest.mark.parametrize("new,hq,hkv,hd", [([1, 1], 4, 2, 64), ([2, 3], 8, 2, 128), ([9, 12], 2, 2, 64), ([3, 1], 4, 4, 32)],
+                         ids=["one", "few", "few-64", "few-32"])
+def test_the_largest_scales_few_tokens(T, new, hq, hkv, hd, scale, q):
+    """With queries as small as the scale is large, and with ordinary ones, of which the largest score takes all; queries of zeros see
+    every entry alike."""
+    c = W.Cache4([100, 300], new, hq, hkv, hd, "bf16", seed=hd)
+    _scaled(c, q, 2.0 ** -4)
+    d = c.device()
+    for window, first in ((0, 0), (64, 5)):
+        _hold_far(c, d, _attend(T, c, d, window, first, scale, max_chunk=max(new)), W.attention(c, window, first, scale))
+
+
+@pytest.mark.parametrize("q", [2.0 ** -120, 2.0 ** -40, 2.0 ** 40, 2.0 ** 115])
+@pytest.mark.parametrize("new,hq,hkv,hd", [([1, 1], 4, 2, 64), ([2, 3], 8, 2, 128)], ids=["one", "few"])
+def test_queries_and_keys_of_any_magnitude_few_tokens(T, new, hq, hkv, hd, q):
+    """Keys as small as the queries are large."""
+    c = W.Cache4([100, 300], new, hq, hkv, hd, "bf16", seed=hd + 2)
+    c.pool[:, :, 0] *= np.float32(1 / q)
+    c.pool4 = W.blocks(*W.quantise(c.round(c.pool)))
+    _scaled(c, q, 0.5)
+    d = c.device()
+    for window, first in ((0, 0), (64, 5)):
+        _hold_far(c, d, _attend(T, c, d, window, first, max_chunk=max(new)), W.attention(c, window, first))
