@@ -631,12 +631,14 @@ __device__ __forceinline__ void hold_32(uint32_t* r) {
 }
 
 // The softmax of a block whose entries have powers of V of their own, a row a thread: P into tensor memory, O rescaled if the row's
-// maximum grows (once the P V before has landed), l from the entries' powers. False: a wait ran out. Not inlined: a second body of the softmax in the kernel, or a branch in the one, cost 15 to 30 us of 450 where no block has any.
+// maximum grows (once the P V before has landed), l from the entries' powers; also of blocks whose scores may be so large that their
+// differences to the maximum have to be exact. False: a wait ran out. Not inlined: a second body of the softmax in the kernel, or a branch in the one, cost 15 to 30 us of 450 where no block has any.
 struct OwnBlock {
   uint32_t t_s, t_o;
   float scale, vscale;
   uint64_t seen;     // columns that the row sees
-  const float4* w;   // 2^-e_t
+  const float4* w;   // 2^-e_t; NULL: that of the block, w0
+  float w0;
   uint32_t o_done;   // barrier of the P V before, with its parity; 0: there is none
   uint32_t parity;
   volatile int* abort_flag;
@@ -677,7 +679,7 @@ __device__ __noinline__ bool own_block(OwnBlock& b) {
       b.m = pm;
     }
   }
-  const float mref = b.m == -INFINITY ? 0.f : b.vscale - b.m;
+  const float mref = b.m == -INFINITY ? 0.f : b.m;
 #pragma unroll 1
   for (int c0 = 0; c0 < 64; c0 += 32) {
     uint32_t pk[16];
@@ -686,11 +688,11 @@ __device__ __noinline__ bool own_block(OwnBlock& b) {
       tmem_ld_16(b.t_s + c0 + 16 * h, s);
 #pragma unroll
       for (int k = 0; k < 16; k += 4) {
-        const float4 w = b.w[(c0 + 16 * h + k) / 4];
+        const float4 w = b.w ? b.w[(c0 + 16 * h + k) / 4] : make_float4(b.w0, b.w0, b.w0, b.w0);
         const float wk[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          s[k + j] = b.seen >> (c0 + 16 * h + k + j) & 1 ? ex2_fast(fmaf(s[k + j], b.scale, mref)) : 0.f;
+          s[k + j] = b.seen >> (c0 + 16 * h + k + j) & 1 ? ex2_fast(fmaf(s[k + j], b.scale, b.vscale) - mref) : 0.f;
           b.l = fmaf(s[k + j], wk[j], b.l);
         }
       }
@@ -715,8 +717,8 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
   volatile int* s_flag = reinterpret_cast<volatile int*>(sm + Sh::OFF_INT);  // the block's page is not there
   volatile int* abort_flag = s_flag + Sh::FLAGS;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + Sh::OFF_INT) + Sh::FLAGS + 1;
-  // of a block: what its raw scores are to be multiplied by (beside the row's power), e, 2^-e, and bits: 1 the page is not there,
-  // 2 entries have powers of their own
+  // of a block: the power of two that its raw scores are to be multiplied by (beside the scale and the row's power), e, 2^-e, and bits:
+  // 1 the page is not there, 2 entries have powers of their own
   float4* s_info = reinterpret_cast<float4*>(sm + Sh::OFF_INFO);
   float* s_w = reinterpret_cast<float*>(sm + Sh::OFF_W);  // [WS][64] 2^-e_t
   PairSeg* s_seg = reinterpret_cast<PairSeg*>(sm + Sh::OFF_SEG);
@@ -973,7 +975,7 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
           if (own) s_w[(b % Sh::WS) * 64 + key] = pow2(-et[k]);
         }
         if (lane == 0)
-          s_info[b % Sh::FLAGS] = make_float4(a.scale * pow2(e[0] + 6), (float)e[1], pow2(-e[1]), __int_as_float((gone ? 1 : 0) | (own ? 2 : 0)));
+          s_info[b % Sh::FLAGS] = make_float4(__int_as_float(e[0] + 6), (float)e[1], pow2(-e[1]), __int_as_float((gone ? 1 : 0) | (own ? 2 : 0)));
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(k_full(b));
@@ -1174,7 +1176,6 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
         __syncwarp();
         if (lane == 0) mbar_arrive(q_ready(x));
       }
-      const float row_scale = pow2(-eq);
       float m_run = -INFINITY, l_run = 0.f;  // m: of the scores in base 2 plus the power of V
       for (int i = 0; i < s.e[x]; ++i, ++n) {
         if (!wait_w(s_full(x, n), n >> 1)) { ok = false; break; }
@@ -1183,13 +1184,17 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
         const uint32_t t_sn = t_s + 64u * (n & 1);
         const float4 info = s_info[(blk + i) % Sh::FLAGS];
         const bool gone = __float_as_int(info.w) & 1;
-        const float scale = fminf(fmaxf(info.x * row_scale, 0x1p-126f), 3.4e38f), vscale = info.y;
+        // (in two steps: the powers of the keys and of q may each pass float32's range where their product does not)
+        const int ex = __float_as_int(info.x) - eq;
+        const float scale = fminf(fmaxf(a.scale * pow2(ex >> 1) * pow2(ex - (ex >> 1)), 0x1p-126f), 3.4e38f), vscale = info.y;
         const bool edge = key0 + 63 > see0 || (key0 <= edge_to && key0 + 63 >= a.first) || gone;
         // columns 0..see - key0 are visible, but for first - key0..hid - key0 under a window (beside the edges a row past the tile's
         // queries may take what its q gives: nobody reads it)
         auto seen = [&] { return gone ? 0 : low_bits(see - key0 + 1) & (low_bits(a.first - key0) | ~low_bits(hid - key0 + 1)); };
-        if (__float_as_int(info.w) & 2) {
-          OwnBlock ob{t_sn, t_o, scale, vscale, edge ? seen() : ~0ull, reinterpret_cast<const float4*>(s_w + ((blk + i) % Sh::WS) * 64),
+        // raw scores are below 2^13: past 2^26 in all, the maximum and the scores have to be rounded alike, which own_block does
+        const bool own = __float_as_int(info.w) & 2;
+        if (__any_sync(0xffffffffu, own || scale > 0x1p13f)) {
+          OwnBlock ob{t_sn, t_o, scale, vscale, edge ? seen() : ~0ull, own ? reinterpret_cast<const float4*>(s_w + ((blk + i) % Sh::WS) * 64) : nullptr, info.z,
                       i > 0 ? o_done(x, n - 1) : 0, ((n - 1) >> 1) & 1, abort_flag, a.werr, m_run, l_run};
           ok = own_block<HD>(ob);
           if (!ok) break;

@@ -107,3 +107,36 @@ def test_queries_and_keys_of_any_magnitude_few_tokens(T, new, hq, hkv, hd, q):
     d = c.device()
     for window, first in ((0, 0), (64, 5)):
         _hold_far(c, d, _attend(T, c, d, window, first, max_chunk=max(new)), W.attention(c, window, first))
+
+
+@pytest.mark.parametrize("scale,q", [(1e8, 1.0), (1e12, 2.0 ** -40), (1e31, 2.0 ** -103), (1e31, 1.0), (1e35, 2.0 ** -116), (1e35, 1.0), (2e38, 2.0 ** -118)])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_the_largest_scales_many_tokens(T, hd, scale, q):
+    c = W.Cache4([100, 300], [60, 90], 4, 2, hd, "bf16", seed=hd)
+    _scaled(c, q, 2.0 ** -4)
+    d = c.device()
+    for window, first in ((0, 0), (64, 5)):
+        _hold_far(c, d, _attend(T, c, d, window, first, scale), W.attention(c, window, first, scale))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("to", [2.0 ** 30, 2.0 ** 60])
+def test_one_score_beyond_all_others_many_tokens(T, hd, to):
+    """Scores of up to `to`: the entry with the largest takes all, whatever rounds beside it. Keys, queries and values are powers of two
+    and zeros, so that the largest score is exact and some distance ahead."""
+    c = W.Cache4([100, 300], [60, 90], 4, 2, hd, "bf16", seed=hd)
+    c.pool[:, :, 0] = 0
+    c.q[:] = 0
+    c.q[:, :, 3] = 2.0 ** 20
+    for b in range(c.n):
+        for e, k in ((7, to / 2.0 ** 21), (33, to / 2.0 ** 20), (99, to / 2.0 ** 22)):
+            p, o = c.at(b, np.array([e]))
+            c.pool[p, c.layer, 0, :, o, 3] = k
+    c.pool4 = W.blocks(*W.quantise(c.round(c.pool)))
+    d = c.device()
+    out, _ = _attend(T, c, d, 0, 0, 1.0)
+    o = out.float().cpu().numpy()
+    for b in range(c.n):
+        vl, vn = c.two(b, 1)
+        want = np.repeat((vl + vn)[33], 2, 0)
+        assert (np.abs(o[c.cu[b]:c.cu[b + 1]] - want) <= (RB + 2.0 ** -11) * (np.abs(vl) + np.abs(vn))[33].repeat(2, 0)).all()
