@@ -563,18 +563,19 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
 // are exact but for float32's sums:
 //   q . k = sum q K' + sum over groups g of (lo_g + 8 d_g) (sum of q)_g
 // the second part as 16 more columns of the product: lo_0, lo_1, 8 d_0, 8 d_1 in K, three times beside the sums of q in three float16
-// that hold 33 bits. V' = lo + d n is rounded to float16, and so is P. Codes become numbers in one multiply-add a pair: the bits n
+// that hold 33 bits (lo and 8 d: three columns of each; 12 of 16 with two groups). V' = lo + d n is rounded to float16, and so is P. Codes become numbers in one multiply-add a pair: the bits n
 // (or 16 n) of a masked word are the float16 n 2^-24. A word's eight values come out in the order 0 4 1 5 2 6 3 7; q is put into that
 // order, O is read out of it.
 //
 // Ranges: K of a block is divided by a power of two (the largest of |lo| and 16 d of the entries that some query sees gets into 2^-6 ..
-// 2^-5), q of a row multiplied by one (2^8 .. 2^9); the softmax undoes both. V is divided by 2^(e + 6), which goes into the score: M is
-// the largest s_t + e, O = sum 2^(s_t + e - M) V_t / 2^(e + 6), l = sum 2^(s_t + e - M) 2^-e, so that what has to be held in 16 bits is
-// relative to the row's largest term. e is the block's, by its largest entry; in a block with entries smaller than 2^-6 of that (as the
-// first tokens' values may be, which take most of the probability) every entry has its own: e_t - e is three more of the 16 columns,
-// beside 1 / (what the softmax multiplies by) in three float16, and 2^-e_t is read from shared memory (own_block, which is
-// slow: all blocks by it take 1151 us where it is 449). Where e_t - e does not fit float16 (scales over 2^12, keys over 2^18) entries
-// keep the block's.
+// 2^-5: what an entry has below 2^-18 of that is rounded), q of a row multiplied by one (2^8 .. 2^9); the softmax undoes both. V is
+// divided by 2^(e + 6), which goes into the score: M is the largest s_t + e, O = sum 2^(s_t + e - M) V_t / 2^(e + 6),
+// l = sum 2^(s_t + e - M) 2^-e, so that what has to be held in 16 bits is relative to the row's largest term. e is the block's, by its
+// largest entry; in a block with entries smaller than 2^-6 of that (as the first tokens' values may be, which take most of the
+// probability), or with none above 2^-40, every entry has its own, e_t, by 2^-e_t in shared memory, and l adds up 2^(s_t - M) where
+// the term of O is too small for float32 (own_block, which is slow: all blocks by it take 1300 us where it is 455).
+// e is at least -88: 2^8 2^88 times 2^31 entries stay in float32. Values of a row's blocks that lie further than 2^100 apart lose the
+// weights of the small ones.
 //
 // Bound by the softmax warps' chain, as k_chunk_pair is, which the codes' warps make longer: their instructions and accesses of
 // shared memory meet its own and the MMAs' reads. A block of 64 keys and two tiles takes 2240 cycles at head_dim 128, of which the
@@ -630,14 +631,20 @@ __device__ __forceinline__ void hold_32(uint32_t* r) {
     asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
 }
 
+__device__ __forceinline__ void tmem_put_8(uint32_t taddr, const uint32_t* r) {  // completes at the next wait::st
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+               "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+
 // The softmax of a block whose entries have powers of V of their own, a row a thread: P into tensor memory, O rescaled if the row's
 // maximum grows (once the P V before has landed), l from the entries' powers; also of blocks whose scores may be so large that their
 // differences to the maximum have to be exact. False: a wait ran out. Not inlined: a second body of the softmax in the kernel, or a branch in the one, cost 15 to 30 us of 450 where no block has any.
 struct OwnBlock {
   uint32_t t_s, t_o;
-  float scale, vscale;
+  float scale;
   uint64_t seen;     // columns that the row sees
-  const float4* w;   // 2^-e_t; NULL: that of the block, w0
+  const float* w;    // 2^-e_t; NULL: that of the block, w0
   float w0;
   uint32_t o_done;   // barrier of the P V before, with its parity; 0: there is none
   uint32_t parity;
@@ -647,15 +654,28 @@ struct OwnBlock {
 };
 template <int HD>
 __device__ __noinline__ bool own_block(OwnBlock& b) {
+  const uint32_t t_s = b.t_s;
+  const float scale = b.scale, w0 = b.w0;
+  const float4* w4 = reinterpret_cast<const float4*>(b.w);
   float pm = -INFINITY, s[16];
+  auto weights = [&](int k, float (&w)[4]) {  // 2^-e_t of entries k .. k + 3
+    const float4 v = w4 ? w4[k / 4] : make_float4(w0, w0, w0, w0);
+    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+  };
+  // e_t: 127 less the exponent's bits, which 2^23 takes in as they are
+  auto power = [](float w) { return (0x1p23f + 127.f) - __uint_as_float(0x4b000000u | __float_as_uint(w) >> 23); };
 #pragma unroll 1
   for (int c0 = 0; c0 < 64; c0 += 16) {
-    tmem_ld_16(b.t_s + c0, s);
+    const uint32_t seen = (uint32_t)(b.seen >> c0);
+    tmem_ld_16(t_s + c0, s);
 #pragma unroll
-    for (int k = 0; k < 16; ++k)
-      if (b.seen >> (c0 + k) & 1) pm = fmaxf(pm, s[k]);
+    for (int k = 0; k < 16; k += 4) {
+      float w[4];
+      weights(c0 + k, w);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) pm = fmaxf(pm, seen >> (k + j) & 1 ? fmaf(s[k + j], scale, power(w[j])) : -INFINITY);
+    }
   }
-  pm = fmaf(pm, b.scale, b.vscale);
   const bool grow = pm - b.m > 8.f;
   if (__any_sync(0xffffffffu, grow)) {
     const float cr = grow ? exp2f(b.m - pm) : 1.f;
@@ -680,28 +700,36 @@ __device__ __noinline__ bool own_block(OwnBlock& b) {
     }
   }
   const float mref = b.m == -INFINITY ? 0.f : b.m;
+  float l = b.l;
 #pragma unroll 1
-  for (int c0 = 0; c0 < 64; c0 += 32) {
-    uint32_t pk[16];
+  for (int c0 = 0; c0 < 64; c0 += 16) {
+    const uint32_t seen = (uint32_t)(b.seen >> c0);
+    uint32_t pk[8];
+    float p[16];
+    bool none = false;  // a term of O too small for float32
+    tmem_ld_16(t_s + c0, s);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      tmem_ld_16(b.t_s + c0 + 16 * h, s);
+    for (int k = 0; k < 16; k += 4) {
+      float w[4];
+      weights(c0 + k, w);
 #pragma unroll
-      for (int k = 0; k < 16; k += 4) {
-        const float4 w = b.w ? b.w[(c0 + 16 * h + k) / 4] : make_float4(b.w0, b.w0, b.w0, b.w0);
-        const float wk[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          s[k + j] = b.seen >> (c0 + 16 * h + k + j) & 1 ? ex2_fast(fmaf(s[k + j], b.scale, b.vscale) - mref) : 0.f;
-          b.l = fmaf(s[k + j], wk[j], b.l);
-        }
+      for (int j = 0; j < 4; ++j) {
+        p[k + j] = seen >> (k + j) & 1 ? ex2_fast(fmaf(s[k + j], scale, power(w[j])) - mref) : 0.f;
+        l = fmaf(p[k + j], w[j], l);
+        none |= p[k + j] == 0.f && (seen >> (k + j) & 1);
       }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) pk[8 * h + k] = pack_f16(s[2 * k], s[2 * k + 1]);
     }
-    tmem_put_16(b.t_s + c0 / 2, pk);  // (over scores that have been read)
+    if (__any_sync(0xffffffffu, none)) {
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+        if (p[k] == 0.f && (seen >> k & 1)) l += ex2_fast(fmaf(s[k], scale, -mref));
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) pk[k] = pack_f16(p[2 * k], p[2 * k + 1]);
+    tmem_put_8(t_s + c0 / 2, pk);  // (over scores that have been read)
     tmem_st_wait_done();
   }
+  b.l = l;
   return true;
 }
 
@@ -803,7 +831,6 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
   auto wait_w = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, wait(b, parity)); };
   PairSeg s;
   unsigned segs = 0;  // read or published
-  const bool by_entry = a.scale <= 0x1p12f;
 
   // registers of the launch: 512 x 128 = 65536; shares: 256 x 160 + 256 x 88 = 63488
   if (warp >= 8) {
@@ -924,18 +951,18 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
           own_size[0] = larger(pr[x]);
           own_size[1] = larger(pr[x] + NG);
           const uint32_t v = __vmaxu2(own_size[0], own_size[1]);
-          e[x] = exponent(__reduce_max_sync(0xffffffffu, max(v & 0xffffu, v >> 16)), x == 0 ? -8 : -100);
+          e[x] = exponent(__reduce_max_sync(0xffffffffu, max(v & 0xffffu, v >> 16)), x == 0 ? -118 : -88);
         }
         // does an entry that somebody sees lie below 2^-6 of the largest?
-        const bool small = (!hides[0] && exponent(own_size[0], -100) < e[1] - 6) || (!hides[1] && exponent(own_size[1], -100) < e[1] - 6);
-        const bool own = by_entry && e[0] <= 18 && __any_sync(0xffffffffu, small);
+        const bool small = (!hides[0] && exponent(own_size[0], -88) < e[1] - 6) || (!hides[1] && exponent(own_size[1], -88) < e[1] - 6);
+        const bool own = e[1] < -40 || __any_sync(0xffffffffu, small);
         uint32_t lo16[2] = {0, 0}, d16[2] = {0, 0};  // of K, for the 16 more columns
         int et[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            if (x == 1) et[k] = own && !hides[k] ? exponent(own_size[k], -100) : e[1];
+            if (x == 1) et[k] = own && !hides[k] ? exponent(own_size[k], -88) : e[1];
             const int by = (x == 0 ? e[0] : et[k]) + 6;
             const float f = pow2(-by), more = by > 126 ? pow2(126 - by) : 1.f;
 #pragma unroll
@@ -961,16 +988,14 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
           mbar_arrive(raw_empty(b));
         }
         if (b >= NST && !wait_w(k_empty(b), b / NST - 1)) { ok = false; break; }
-        // lo, 8 d of the groups, three times; the entry's power of V, three times
-        const float down = pow2(-(e[0] + 6));
+        // lo, 8 d of the groups, three times
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           const int key = 2 * lane + k;
-          const float power = (float)(et[k] - e[1]) * down;
           uint8_t* to = sm + Sh::OFF_KX + (b % NST) * Sh::KX + key * 32;
           const int flip = ((key >> 2) & 1) << 4;
           *reinterpret_cast<uint4*>(to + flip) = make_uint4(lo16[k], d16[k], lo16[k], d16[k]);
-          *reinterpret_cast<uint4*>(to + (flip ^ 16)) = make_uint4(lo16[k], d16[k], pack_f16(power, power), pack_f16(power, 0.f));
+          *reinterpret_cast<uint4*>(to + (flip ^ 16)) = make_uint4(lo16[k], d16[k], 0, 0);
           // (what the softmax reads with S: the issuer has seen k_full before it)
           if (own) s_w[(b % Sh::WS) * 64 + key] = pow2(-et[k]);
         }
@@ -1130,8 +1155,7 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
 #pragma unroll
           for (int k = 0; k < 4; ++k) most = max(most, max(w[k] & 0x7fff0000u, (w[k] & 0x7fffu) << 16));
         }
-        const int e = max(-100, min(126, (int)(most >> 23) - 127));
-        eq = min(8 - e, 14 + max(-126, (int)(__float_as_uint(a.scale) >> 23) - 127));  // (what goes beside the powers of V fits, too)
+        eq = 8 - max(-112, min(126, (int)(most >> 23) - 127));
         const float up = pow2(eq);
         float sum[NG];
 #pragma unroll
@@ -1165,13 +1189,7 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
         uint8_t* xr = sm + Sh::OFF_QX + x * Sh::QX + row * 32;
         const int flip = (row >> 2) & 1;
         *reinterpret_cast<uint4*>(xr + (flip << 4)) = make_uint4(terms[0], terms[0], terms[1], terms[1]);
-        float c3[4], left = fminf(pow2(eq) / a.scale, 60000.f);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          c3[k] = k < 3 ? __half2float(__float2half_rn(left)) : 0.f;
-          left -= c3[k];
-        }
-        *reinterpret_cast<uint4*>(xr + ((1 ^ flip) << 4)) = make_uint4(terms[2], terms[2], pack_f16(c3[0], c3[1]), pack_f16(c3[2], c3[3]));
+        *reinterpret_cast<uint4*>(xr + ((1 ^ flip) << 4)) = make_uint4(terms[2], terms[2], 0, 0);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(q_ready(x));
@@ -1194,7 +1212,7 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
         // raw scores are below 2^13: past 2^26 in all, the maximum and the scores have to be rounded alike, which own_block does
         const bool own = __float_as_int(info.w) & 2;
         if (__any_sync(0xffffffffu, own || scale > 0x1p13f)) {
-          OwnBlock ob{t_sn, t_o, scale, vscale, edge ? seen() : ~0ull, own ? reinterpret_cast<const float4*>(s_w + ((blk + i) % Sh::WS) * 64) : nullptr, info.z,
+          OwnBlock ob{t_sn, t_o, scale, edge ? seen() : ~0ull, own ? s_w + ((blk + i) % Sh::WS) * 64 : nullptr, info.z,
                       i > 0 ? o_done(x, n - 1) : 0, ((n - 1) >> 1) & 1, abort_flag, a.werr, m_run, l_run};
           ok = own_block<HD>(ob);
           if (!ok) break;
@@ -1272,7 +1290,14 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
       if (ok && s.e[x] > 0) {
         if (!wait_w(o_done(x, n - 1), (n - 1) >> 1)) break;
         tc_fence_after();
-        const float inv = 64.f * (whole ? (l_run != 0.f ? 1.f / l_run : 0.f) : 1.f);  // (V was divided by 2^6 more)
+        float inv = whole ? (l_run != 0.f ? 1.f / l_run : 0.f) : 1.f;
+        if (!whole && l_run > 0x1p20f) {  // (as in k_chunk_q4)
+          const float up = m_run + (float)((int)(__float_as_uint(l_run) >> 23) - 127);
+          inv = ex2_fast(m_run - up);
+          l_run *= inv;
+          m_run = up;
+        }
+        inv *= 64.f;  // (V was divided by 2^6 more)
 #pragma unroll
         for (int c0 = 0; c0 < HD; c0 += 32) {
           float o[32];

@@ -140,3 +140,38 @@ def test_one_score_beyond_all_others_many_tokens(T, hd, to):
         vl, vn = c.two(b, 1)
         want = np.repeat((vl + vn)[33], 2, 0)
         assert (np.abs(o[c.cu[b]:c.cu[b + 1]] - want) <= (RB + 2.0 ** -11) * (np.abs(vl) + np.abs(vn))[33].repeat(2, 0)).all()
+
+
+@pytest.mark.parametrize("values", ["alike", "apart", "zeros"])
+@pytest.mark.parametrize("k,q,scale", [(2.0 ** -14, 2.0 ** 14, 0), (2.0 ** -20, 2.0 ** 20, 0), (2.0 ** -28, 1.0, 2.0 ** 25), (2.0 ** -100, 2.0 ** 100, 0),
+                                       (2.0 ** -35, 2.0 ** 35, 0), (2.0 ** 20, 2.0 ** -20, 0), (2.0 ** 60, 1.0, 2.0 ** -63), (2.0 ** 115, 2.0 ** -115, 0),
+                                       (1.0, 2.0 ** -60, 2.0 ** 57), (2.0 ** -118, 2.0 ** 115, 1.0)])
+@pytest.mark.parametrize("new,hd", [([60, 90], 64), ([60, 90], 128), ([2, 3], 64), ([2, 3], 128)], ids=["many-64", "many-128", "few-64", "few-128"])
+def test_keys_queries_and_scales_of_any_magnitude(T, new, hd, k, q, scale, values):
+    """Small keys under large queries and the other way round, or under scales of any size: the same scores as ever; beside values that are
+    alike, 2^-30 to 2^30 and 2^-12 zeros."""
+    c = W.Cache4([100, 300], new, 4, 2, hd, "bf16", seed=hd + 3)
+    rng = np.random.default_rng(7)
+    c.pool[:, :, 0] *= np.float32(k)
+    if values == "apart":
+        c.pool[:, :, 1] *= (2.0 ** rng.uniform(-30, 30, c.pool[:, :, 1].shape[:-1] + (1,))).astype(np.float32)
+    if values == "zeros":
+        c.pool[:, :, 1] *= 2.0 ** -12 * rng.integers(0, 2, c.pool[:, :, 1].shape[:-1] + (1,)).astype(np.float32)
+    c.pool4 = W.blocks(*W.quantise(c.round(c.pool)))
+    _scaled(c, q, 0.5)
+    d = c.device()
+    for window, first in ((0, 0), (64, 5)):
+        ref = W.attention(c, window, first, scale)
+        top = ref[2].max(-1, keepdims=True)  # (a small term is rounded to the row's largest)
+        _hold_far(c, d, _attend(T, c, d, window, first, scale, max_chunk=max(new)), (ref[0], ref[1], np.maximum(ref[2], top), ref[3]))
+
+
+@pytest.mark.parametrize("what", ["one value", "zeros", "random"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("size", [2.0 ** -70, 2.0 ** -40, 2.0 ** 28, 2.0 ** 90])
+def test_values_of_any_magnitude_many_tokens(T, what, hd, size):
+    c = W.Cache4([1000, 150], [60, 90], 4, 2, hd, "bf16", seed=hd)
+    _filled(c, what, size)
+    d = c.device()
+    for window, first in ((0, 0), (70, 3)):
+        _hold_far(c, d, _attend(T, c, d, window, first), W.attention(c, window, first))
