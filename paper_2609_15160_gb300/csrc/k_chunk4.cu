@@ -1297,7 +1297,6 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
           l_run *= inv;
           m_run = up;
         }
-        inv *= 64.f;  // (V was divided by 2^6 more)
 #pragma unroll
         for (int c0 = 0; c0 < HD; c0 += 32) {
           float o[32];
@@ -1305,7 +1304,9 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
           if (!row_ok) continue;
 #pragma unroll
           for (int k = 0; k < 32; k += 8) {  // eight dims, out of the codes' order
-            const float y[8] = {o[k] * inv, o[k + 2] * inv, o[k + 4] * inv, o[k + 6] * inv, o[k + 1] * inv, o[k + 3] * inv, o[k + 5] * inv, o[k + 7] * inv};
+            float y[8] = {o[k], o[k + 2], o[k + 4], o[k + 6], o[k + 1], o[k + 3], o[k + 5], o[k + 7]};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = y[j] * 64.f * inv;  // (V was divided by 2^6 more, which 1 / l may have no room for)
             if (!whole) {
               *reinterpret_cast<float4*>(a.part_o + pair_part(slot, prow, c0 + k, HD)) = make_float4(y[0], y[1], y[2], y[3]);
               *reinterpret_cast<float4*>(a.part_o + pair_part(slot, prow, c0 + k + 4, HD)) = make_float4(y[4], y[5], y[6], y[7]);

@@ -175,3 +175,15 @@ def test_values_of_any_magnitude_many_tokens(T, what, hd, size):
     d = c.device()
     for window, first in ((0, 0), (70, 3)):
         _hold_far(c, d, _attend(T, c, d, window, first), W.attention(c, window, first))
+
+
+@pytest.mark.parametrize("what", ["one value", "random"])
+@pytest.mark.parametrize("new", [[60, 90], [300, 40]], ids=["parts", "whole"])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_the_largest_values_many_tokens(T, what, new, hd):
+    """1 / l is 2^126 with values of 2^126."""
+    c = W.Cache4([1000, 150] if new[0] < 100 else [0, 20], new, 8, 4, hd, "bf16", seed=hd)
+    _filled(c, what, 2.0 ** 126)
+    d = c.device()
+    for window, first in ((0, 0), (70, 3)):
+        _hold_far(c, d, _attend(T, c, d, window, first), W.attention(c, window, first))
