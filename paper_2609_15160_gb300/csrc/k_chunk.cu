@@ -1202,7 +1202,6 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
     const uint32_t t_s = tmem + lane_off + 128u * (uint32_t)x;
     const uint32_t t_o = tmem + lane_off + Sh::OCOL + (uint32_t)(HD * x);
     const int qi = row >> g_log, g = row & ((1 << g_log) - 1);
-    const float scale = a.scale;
     unsigned n = 0, blk = 0;  // blocks of this tile, and of the CTA
     bool ok = true;
     // waits taken by the whole warp: the TMEM accesses after them are warp-collective
@@ -1218,7 +1217,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
       const int see = row_ok ? s.see0 + x * QT + qi : -1;  // a row past the tile's queries sees nothing
       const int see0 = s.see0 + x * QT;                    // of the tile's first query
       const int skip = skip_of(s.see0), see_last = see0 + s.nq[x] - 1, hid = MODE == KEYS_ALL ? -1 : hidden_to(see, a.window);
-      float m_run = -INFINITY, l_run = 0.f;                // m in units of the raw scores
+      float m_run = -INFINITY, l_run = 0.f, scale = a.scale;  // m in units of the raw scores; scale: smaller where m is large
       for (int i = 0; i < s.e[x]; ++i, ++n) {
         if (!wait_w(s_full(x, n), n >> 1)) { ok = false; break; }
         tc_fence_after();
@@ -1269,6 +1268,9 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
           if (grow) {
             l_run *= cr;
             m_run = pm;
+            // s scale - m scale, rounded once, keeps what rounding m scale left, half a step. A score that it matters for, of 2^28, has
+            // no neighbour in float32 that is not 16 away, so that a smaller scale leaves the same keys with the probability.
+            scale = fminf(a.scale, 0x1p28f / fabsf(pm));
           }
         }
         const float mref = m_run == -INFINITY ? 0.f : m_run * scale;  // no visible key so far: any finite value
@@ -1329,8 +1331,8 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_chunk_pair(ChunkAttn a, int
         for (int k = 0; k < HD; ++k) a.part_o[pair_part(slot, prow, k, HD)] = 0.f;
       }
       if (row_ok) {
-        if (!whole) a.part_ml[(size_t)slot * PAIR_ROWS + prow] = make_float2(m_run == -INFINITY ? -INFINITY : m_run * scale, l_run);
-        else if (a.lse) a.lse[token * c.Hq + head] = l_run != 0.f ? (m_run * scale + log2f(l_run)) * LN2 : -INFINITY;
+        if (!whole) a.part_ml[(size_t)slot * PAIR_ROWS + prow] = make_float2(m_run == -INFINITY ? -INFINITY : m_run * a.scale, l_run);
+        else if (a.lse) a.lse[token * c.Hq + head] = l_run != 0.f ? (m_run * a.scale + log2f(l_run)) * LN2 : -INFINITY;
       }
       if (ok && s_left[(segs - 1) % PairSeg::RING] == segs - 1) {  // (written before the last P V that it concerns)
         __syncwarp();  // the rows are written

@@ -187,3 +187,14 @@ def test_the_largest_values_many_tokens(T, what, new, hd):
     d = c.device()
     for window, first in ((0, 0), (70, 3)):
         _hold_far(c, d, _attend(T, c, d, window, first), W.attention(c, window, first))
+
+
+@pytest.mark.parametrize("scale,q", [(1e8, 1.0), (1e31, 2.0 ** -103), (1e31, 1.0), (1e35, 1.0), (2e38, 2.0 ** -118)])
+@pytest.mark.parametrize("new", [[1, 1], [5, 8], [60, 90]], ids=["one", "few", "many"])
+@pytest.mark.parametrize("dtype,hd", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+def test_the_largest_scales_over_plain_caches(T, dtype, hd, new, scale, q):
+    c = R.Cache([100, 300], new, 4, 2, hd, dtype, seed=3)
+    _scaled(c, q, 2.0 ** -4)
+    d = c.device()
+    for window, first in ((0, 0), (64, 5)):
+        _hold_far(c, d, _attend(T, c, d, window, first, scale, max_chunk=max(new)), W.attention(c, window, first, scale))
