@@ -614,7 +614,8 @@ int tlf_cache_fork(const tlf_fork_args* a, void* scratch, size_t scratch_bytes, 
 /* The pages in use to the front of the pool. With L pages of refs > 0, the k-th page in use at or past L moves (all layers, K
  * and V, positions and weights) to the k-th free page below L; table_out names the pages' new places, refs_out counts them, and
  * n_live gets L: pages from L on hold nothing any more and may be given back. The tables must be all that name pages of the
- * pool. table_out and refs_out may be the inputs' own buffers. */
+ * pool; a page that a table names and refs does not count gets -1 and sets err bit 2. table_out and refs_out may be the inputs' own
+ * buffers. */
 typedef struct tlf_compact_args {
   int32_t n;            /* rows, 1..65535 */
   int32_t n_kv_heads, head_dim, n_layers;

@@ -382,7 +382,7 @@ struct CompactDev {
   int* pos;
   float* weight;
   uint32_t* err;
-  int *hole, *mover, *rank, *count;  // scratch: [n_pages] target and source of the k-th move, [n_pages] k of a page that moves, moves
+  int *hole, *mover, *rank, *count;  // scratch: [n_pages] target and source of the k-th move, [n_pages] k of a page that moves (-1: nobody counts the page), moves
 };
 
 template <int CS>
@@ -416,10 +416,8 @@ __global__ void __launch_bounds__(PG_THREADS) k_compact_plan(CompactDev a) {
     const int k = at + lanes_below(used);  // pages in use before p
     if (on) {
       if (p < live && v <= 0) a.hole[p - k] = (int)p;
-      if (p >= live && v > 0) {
-        a.mover[k - below] = (int)p;
-        a.rank[p] = k - below;
-      }
+      if (p >= live && v > 0) a.mover[k - below] = (int)p;
+      a.rank[p] = v <= 0 ? -1 : p < live ? 0 : k - below;
     }
     at += __popc(used);
   });
@@ -439,9 +437,10 @@ __global__ void __launch_bounds__(COPY_THREADS) k_compact_apply(CompactDev a, in
   for (long long i = me; i < (long long)a.n * a.max_pages; i += threads) {
     const int page = named(a.table_in[i], a.n_pages, a.err);
     int to = page;
-    if (page >= live) {  // (a page that nobody counts has no new place)
-      const int k = a.rank[page];
-      to = k >= 0 && k < moves && a.mover[k] == page ? a.hole[k] : -1;
+    if (page >= 0) {
+      const int k = a.rank[page];  // (refs may be changing)
+      if (k < 0) to = -1;
+      else if (page >= live) to = a.hole[k];
       if (to < 0) sv_report(a.err, DEVERR_INDEX);
     }
     a.table_out[i] = to;
