@@ -24,17 +24,18 @@ namespace tlf {
 // paired by byte permutations. q is scaled by a power of two a row into float16's range.
 //
 // p_t d_t,g is rounded to float16, an operand's type, as the other kernels round p. What float16 has to hold is 2^(s - M) d: M + 8 is
-// the running maximum of s + log2(z), not of s, so that values of any magnitude fit. z, the size of an entry's values, is the largest of
-// its groups' d and of 2^-64 |lo| + 2^-60: groups that hold one value, or nothing, have no d. M is refreshed when a p d passes 2^15, a
-// lane's sum of p 2^80 or one of p lo 2^110: p is at most 2^68 then and p lo 2^72, so that float32 holds the sums over 2^31 entries.
-// Digits go where values are below 2^-80, and, where they are of 2^100 and more, with what weighs less than 2^-26.
+// the running maximum of s + log2(d), the largest d of the entry's groups, not of s, so that values of any magnitude fit. It is refreshed
+// when a p d passes 2^15, or a lane's sum of p 2^80. d counts as at least 2^-64 |lo| in all of this: a group that holds one value has
+// none (and codes of 0, or 15 2^-64 of the value too much), and p lo then is below 2^79; and as at least 2^-60 in M: p is at most 2^68.
+// So float32 holds the sums over 2^31 entries. Digits go where values are below 2^-80, and, where they are of 2^100 and more, with what
+// weighs less than 2^-26.
 //
 // CTAs of teams of two warps, which take the pages in turn, a warp half of a page's 64 keys, 16 at a time in each step of the
 // products; and a producer warp that copies a page's two blocks.
 //
 // Bound by the latency of dependent instructions: the twelve warps that 128 registers a thread leave room for issue in 53 % of the
-// cycles. 16 single tokens over 32k entries, 16 / 8 heads x 128: 122 us with the join, 4.9 TB/s; 32 over up to 8192 entries, 16 heads x
-// 64: 53 us; 32 rows of up to 16 tokens under a window of 4096, 16 heads x 64: 59 us. The first of them with one team and 16 keys a step
+// cycles. 16 single tokens over 32k entries, 16 / 8 heads x 128: 125 us with the join, 4.7 TB/s; 32 over up to 8192 entries, 16 heads x
+// 64: 55 us; 32 rows of up to 16 tokens under a window of 4096, 16 heads x 64: 60 us. The first of them with one team and 16 keys a step
 // 153 us, with more warps a CTA 163, with four CTAs an SM 153 and with two 132.
 struct Q4Seg {  // a CTA's part of an item: blocks kb0 .. kb1 - 1 of nb; nb = 0: no more
   int b, h, token0, see0, nq, kb0, kb1, nb;
@@ -348,40 +349,36 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
               for (int n = 0; n < NG; ++n) vp[x][n] = 0;
           }
         }
+        uint64_t p2[NT][4];
         uint32_t ph[NT][4][NG];  // p d of the two columns
-        uint64_t psum[NT], lsum[NT][NG];  // sum of p; ol with this step's
+        uint64_t psum[NT];
+        // d of a pair, or 2^-64 |lo| (on the bits: a float's exponent less 64)
+        auto step_of = [](uint32_t w) { return __uint_as_float((uint32_t)max(max((int)(w << 16), (int)(w & 0x7fff0000u) - (64 << 23)), 0)); };
         auto weigh = [&] {
-          uint32_t big = 0;
-          float sums = 0.f, lows = 0.f;
+          bool grow = false;
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
             const uint64_t m2 = f2_pack(-m[t][0], -m[t][1]);
-            uint64_t p2[4];
-#pragma unroll
-            for (int n = 0; n < NG; ++n) lsum[t][n] = f2_pack(ol[t][n][0], ol[t][n][1]);
+            uint32_t big = 0;
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
               const float2 e = f2_unpack(f2_add(s2[t][x], m2));
               const float2 p = make_float2(ex2_fast(e.x), ex2_fast(e.y));
-              p2[x] = f2_pack(p.x, p.y);
+              p2[t][x] = f2_pack(p.x, p.y);
 #pragma unroll
               for (int n = 0; n < NG; ++n) {
-                const float2 v = kv4_pair(vp[x][n]), pd = f2_unpack(f2_mul(p2[x], f2_pack(v.x, v.x)));
+                const float d = step_of(vp[x][n]);
+                const float2 pd = f2_unpack(f2_mul(p2[t][x], f2_pack(d, d)));
                 ph[t][x][n] = pack_f16(pd.x, pd.y);
                 big |= ph[t][x][n] + 0x08000800u;  // the sign bit of a half from 2^15 on, infinities and NaN too
-                lsum[t][n] = f2_fma(p2[x], f2_pack(v.y, v.y), lsum[t][n]);
               }
             }
-            psum[t] = f2_add(f2_add(p2[0], p2[1]), f2_add(p2[2], p2[3]));
-            const float2 sum = f2_unpack(psum[t]);
-            sums = fmaxf(sums, fmaxf(sum.x, sum.y));
-#pragma unroll
-            for (int n = 0; n < NG; ++n) {
-              const float2 low = f2_unpack(lsum[t][n]);
-              lows = fmaxf(lows, fmaxf(fabsf(low.x), fabsf(low.y)));
-            }
+            const uint64_t sum2 = f2_add(f2_add(p2[t][0], p2[t][1]), f2_add(p2[t][2], p2[t][3]));
+            const float2 sum = f2_unpack(sum2);
+            grow |= (big & 0x80008000u) != 0 || !(fmaxf(sum.x, sum.y) <= 0x1p80f);
+            psum[t] = sum2;
           }
-          return __any_sync(0xffffffffu, (big & 0x80008000u) != 0 || sums > 0x1p80f || lows > 0x1p110f);
+          return __any_sync(0xffffffffu, grow);
         };
         if (weigh()) {
 #pragma unroll
@@ -391,13 +388,10 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
               float top = NONE;
 #pragma unroll
               for (int x = 0; x < 4; ++x) {
-                float2 p = kv4_pair(vp[x][0]);
-                if constexpr (NG == 2) {
-                  const float2 r = kv4_pair(vp[x][1]);
-                  p = make_float2(fmaxf(p.x, r.x), fmaxf(fabsf(p.y), fabsf(r.y)));
-                }
+                float d = fmaxf(step_of(vp[x][0]), 0x1p-60f);
+                if constexpr (NG == 2) d = fmaxf(d, step_of(vp[x][1]));
                 const float2 s = f2_unpack(s2[t][x]);
-                top = fmaxf(top, (j ? s.y : s.x) + (log2f(fmaxf(p.x, fmaf(fabsf(p.y), 0x1p-64f, 0x1p-60f))) - 8.f));
+                top = fmaxf(top, (j ? s.y : s.x) + (log2f(d) - 8.f));
               }
 #pragma unroll
               for (int w = 4; w < 32; w *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
@@ -424,10 +418,15 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
           l[t][0] = ls.x, l[t][1] = ls.y;
 #pragma unroll
           for (int n = 0; n < NG; ++n) {
-            const float2 low = f2_unpack(lsum[t][n]);
-            ol[t][n][0] = low.x, ol[t][n][1] = low.y;
+            uint64_t o2 = f2_pack(ol[t][n][0], ol[t][n][1]);
 #pragma unroll
-            for (int x = 0; x < 4; ++x) ph[t][x][n] = transpose_8x8(ph[t][x][n]);
+            for (int x = 0; x < 4; ++x) {
+              const float lo = kv4_pair(vp[x][n]).y;
+              o2 = f2_fma(p2[t][x], f2_pack(lo, lo), o2);
+              ph[t][x][n] = transpose_8x8(ph[t][x][n]);
+            }
+            const float2 os = f2_unpack(o2);
+            ol[t][n][0] = os.x, ol[t][n][1] = os.y;
           }
         }
         // V: dims 8 g .. 8 g + 7 of a group (head_dim 32: 4 g .. 4 g + 3)
@@ -563,24 +562,24 @@ __global__ void __launch_bounds__(Q4Shape<HD, NT>::THREADS, Q4Shape<HD, NT>::PER
 // are exact but for float32's sums:
 //   q . k = sum q K' + sum over groups g of (lo_g + 8 d_g) (sum of q)_g
 // the second part as 16 more columns of the product: lo_0, lo_1, 8 d_0, 8 d_1 in K, three times beside the sums of q in three float16
-// that hold 33 bits (lo and 8 d: three columns of each; 12 of 16 with two groups). V' = lo + d n is rounded to float16, and so is P. Codes become numbers in one multiply-add a pair: the bits n
-// (or 16 n) of a masked word are the float16 n 2^-24. A word's eight values come out in the order 0 4 1 5 2 6 3 7; q is put into that
-// order, O is read out of it.
+// that hold 33 bits (12 columns with two groups; the last four are zeros). V' = lo + d n is rounded to float16, and so is P. Codes
+// become numbers in one multiply-add a pair: the bits n (or 16 n) of a masked word are the float16 n 2^-24. A word's eight values come
+// out in the order 0 4 1 5 2 6 3 7; q is put into that order, O is read out of it.
 //
 // Ranges: K of a block is divided by a power of two (the largest of |lo| and 16 d of the entries that some query sees gets into 2^-6 ..
 // 2^-5: what an entry has below 2^-18 of that is rounded), q of a row multiplied by one (2^8 .. 2^9); the softmax undoes both. V is
-// divided by 2^(e + 6), which goes into the score: M is the largest s_t + e, O = sum 2^(s_t + e - M) V_t / 2^(e + 6),
+// divided by 2^(e + 6), which goes into the score: M + 6 is the largest s_t + e, O = sum 2^(s_t + e - M) V_t / 2^(e + 6),
 // l = sum 2^(s_t + e - M) 2^-e, so that what has to be held in 16 bits is relative to the row's largest term. e is the block's, by its
 // largest entry; in a block with entries smaller than 2^-6 of that (as the first tokens' values may be, which take most of the
 // probability), or with none above 2^-40, every entry has its own, e_t, by 2^-e_t in shared memory, and l adds up 2^(s_t - M) where
-// the term of O is too small for float32 (own_block, which is slow: all blocks by it take 1300 us where it is 455).
-// e is at least -88: 2^8 2^88 times 2^31 entries stay in float32. Values of a row's blocks that lie further than 2^100 apart lose the
-// weights of the small ones.
+// the term of O is too small for float32 (own_block, which is slow: all blocks by it take 1310 us where it is 448).
+// e is at least -88, so that 2^14 2^88 times 2^26 entries of a part stay in float32, as 64 / l does with values of 2^126. Where values of
+// a row's blocks lie further than 2^100 apart, the weights of the small ones are lost.
 //
 // Bound by the softmax warps' chain, as k_chunk_pair is, which the codes' warps make longer: their instructions and accesses of
 // shared memory meet its own and the MMAs' reads. A block of 64 keys and two tiles takes 2240 cycles at head_dim 128, of which the
-// tensor pipe works half. 4 x 2048 tokens over up to 10240 entries, 16 / 8 heads x 128: 446 us with the join, 1090 TFLOP/s (395 with
-// nothing converted, k_chunk_pair over bfloat16 371); 16 heads x 64: 396 us. Tried and slower: other splits of the registers (168 / 80,
+// tensor pipe works half. 4 x 2048 tokens over up to 10240 entries, 16 / 8 heads x 128: 448 us with the join, 1090 TFLOP/s (395 with
+// nothing converted, k_chunk_pair over bfloat16 371); 16 heads x 64: 398 us. Tried and slower: other splits of the registers (168 / 80,
 // 152 / 96), waits that sleep, the softmax's two halves in a loop (492).
 constexpr int PAIR4_THREADS = 512;
 template <int HD>
@@ -676,9 +675,9 @@ __device__ __noinline__ bool own_block(OwnBlock& b) {
       for (int j = 0; j < 4; ++j) pm = fmaxf(pm, seen >> (k + j) & 1 ? fmaf(s[k + j], scale, power(w[j])) : -INFINITY);
     }
   }
-  const bool grow = pm - b.m > 8.f;
+  const bool grow = pm - b.m > 14.f;
   if (__any_sync(0xffffffffu, grow)) {
-    const float cr = grow ? exp2f(b.m - pm) : 1.f;
+    const float m_new = pm - 6.f, cr = grow ? exp2f(b.m - m_new) : 1.f;
     if (b.o_done) {
       bool ok = *b.abort_flag == 0 && mbar_wait(b.o_done, b.parity, b.werr);
       if (!__all_sync(0xffffffffu, ok)) {
@@ -696,7 +695,7 @@ __device__ __noinline__ bool own_block(OwnBlock& b) {
     }
     if (grow) {
       b.l *= cr;
-      b.m = pm;
+      b.m = m_new;
     }
   }
   const float mref = b.m == -INFINITY ? 0.f : b.m;
@@ -1128,6 +1127,8 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
     const uint32_t t_o = tmem + lane_off + Sh::OCOL + (uint32_t)(HD * x);
     const int qi = row >> g_log, g = row & ((1 << g_log) - 1);
     unsigned n = 0, blk = 0, qn = 0;  // blocks of this tile, and of the CTA; items of this tile
+    const uint32_t scale_bits = __float_as_uint(a.scale < 0x1p-100f ? a.scale * 0x1p64f : a.scale), scale_frac = scale_bits & 0x7fffffu;
+    const int scale_exp = (int)(scale_bits >> 23) - (a.scale < 0x1p-100f ? 64 : 0);
     bool ok = true;
     auto next = [&] {
       if (!wait_w(seg_full(segs), segs / PairSeg::RING)) return false;
@@ -1194,24 +1195,29 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
         __syncwarp();
         if (lane == 0) mbar_arrive(q_ready(x));
       }
+      const int row_exp = scale_exp - eq;
       float m_run = -INFINITY, l_run = 0.f;  // m: of the scores in base 2 plus the power of V
       for (int i = 0; i < s.e[x]; ++i, ++n) {
         if (!wait_w(s_full(x, n), n >> 1)) { ok = false; break; }
         tc_fence_after();
         const int key0 = block_at<KEYS_4BIT>(s.kb0 + i, sinks, skip) * 64;
         const uint32_t t_sn = t_s + 64u * (n & 1);
+        uint32_t su[64];
+        tmem_ld_32_issue(t_sn, su);
+        tmem_ld_32_issue(t_sn + 32, su + 32);
         const float4 info = s_info[(blk + i) % Sh::FLAGS];
         const bool gone = __float_as_int(info.w) & 1;
-        // (in two steps: the powers of the keys and of q may each pass float32's range where their product does not)
-        const int ex = __float_as_int(info.x) - eq;
-        const float scale = fminf(fmaxf(a.scale * pow2(ex >> 1) * pow2(ex - (ex >> 1)), 0x1p-126f), 3.4e38f), vscale = info.y;
+        // (on the exponents: the powers of the keys and of q may each pass float32's range where their product does not)
+        const int ex = max(1, min(254, row_exp + __float_as_int(info.x)));
+        const float scale = __uint_as_float(scale_frac | (uint32_t)ex << 23), vscale = info.y;
         const bool edge = key0 + 63 > see0 || (key0 <= edge_to && key0 + 63 >= a.first) || gone;
         // columns 0..see - key0 are visible, but for first - key0..hid - key0 under a window (beside the edges a row past the tile's
         // queries may take what its q gives: nobody reads it)
         auto seen = [&] { return gone ? 0 : low_bits(see - key0 + 1) & (low_bits(a.first - key0) | ~low_bits(hid - key0 + 1)); };
         // raw scores are below 2^13: past 2^26 in all, the maximum and the scores have to be rounded alike, which own_block does
         const bool own = __float_as_int(info.w) & 2;
-        if (__any_sync(0xffffffffu, own || scale > 0x1p13f)) {
+        if (__any_sync(0xffffffffu, own || ex > 127 + 13)) {
+          tmem_ld_wait();
           OwnBlock ob{t_sn, t_o, scale, edge ? seen() : ~0ull, own ? s_w + ((blk + i) % Sh::WS) * 64 : nullptr, info.z,
                       i > 0 ? o_done(x, n - 1) : 0, ((n - 1) >> 1) & 1, abort_flag, a.werr, m_run, l_run};
           ok = own_block<HD>(ob);
@@ -1219,9 +1225,6 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
           m_run = ob.m;
           l_run = ob.l;
         } else {
-          uint32_t su[64];
-          tmem_ld_32_issue(t_sn, su);
-          tmem_ld_32_issue(t_sn + 32, su + 32);
           tmem_ld_wait();
           hold_32(su);
           hold_32(su + 32);
@@ -1236,10 +1239,10 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
 #pragma unroll
           for (int k = 0; k < 64; ++k) pm4[k & 3] = fmaxf(pm4[k & 3], __uint_as_float(su[k]));
           const float pm = fmaf(fmaxf(fmaxf(pm4[0], pm4[1]), fmaxf(pm4[2], pm4[3])), scale, vscale);
-          // O is rescaled only when a row's maximum grows by more than 8 in base 2, after the P V before has landed
-          const bool grow = pm - m_run > 8.f;
+          // O is rescaled only when a row's maximum grows by more than 8 in base 2, after the P V before has landed; P is 2^6 then
+          const bool grow = pm - m_run > 14.f;
           if (__any_sync(0xffffffffu, grow)) {
-            const float cr = grow ? exp2f(m_run - pm) : 1.f;  // 0 when m_run was -inf
+            const float m_new = pm - 6.f, cr = grow ? exp2f(m_run - m_new) : 1.f;  // 0 when m_run was -inf
             if (i > 0) {
               if (!wait_w(o_done(x, n - 1), (n - 1) >> 1)) { ok = false; break; }
               tc_fence_after();
@@ -1254,7 +1257,7 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
             }
             if (grow) {
               l_run *= cr;
-              m_run = pm;
+              m_run = m_new;
             }
           }
           const float mref = m_run == -INFINITY ? 0.f : vscale - m_run;  // no visible key so far: any finite value
@@ -1290,11 +1293,11 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
       if (ok && s.e[x] > 0) {
         if (!wait_w(o_done(x, n - 1), (n - 1) >> 1)) break;
         tc_fence_after();
-        float inv = whole ? (l_run != 0.f ? 1.f / l_run : 0.f) : 1.f;
+        float inv = 64.f * (whole ? (l_run != 0.f ? 1.f / l_run : 0.f) : 1.f);  // (V was divided by 2^6 more)
         if (!whole && l_run > 0x1p20f) {  // (as in k_chunk_q4)
-          const float up = m_run + (float)((int)(__float_as_uint(l_run) >> 23) - 127);
-          inv = ex2_fast(m_run - up);
-          l_run *= inv;
+          const float up = m_run + (float)((int)(__float_as_uint(l_run) >> 23) - 127), by = ex2_fast(m_run - up);
+          inv *= by;
+          l_run *= by;
           m_run = up;
         }
 #pragma unroll
@@ -1304,9 +1307,7 @@ __global__ void __launch_bounds__(PAIR4_THREADS, 1) k_chunk_pair4(ChunkAttn a, i
           if (!row_ok) continue;
 #pragma unroll
           for (int k = 0; k < 32; k += 8) {  // eight dims, out of the codes' order
-            float y[8] = {o[k], o[k + 2], o[k + 4], o[k + 6], o[k + 1], o[k + 3], o[k + 5], o[k + 7]};
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = y[j] * 64.f * inv;  // (V was divided by 2^6 more, which 1 / l may have no room for)
+            const float y[8] = {o[k] * inv, o[k + 2] * inv, o[k + 4] * inv, o[k + 6] * inv, o[k + 1] * inv, o[k + 3] * inv, o[k + 5] * inv, o[k + 7] * inv};
             if (!whole) {
               *reinterpret_cast<float4*>(a.part_o + pair_part(slot, prow, c0 + k, HD)) = make_float4(y[0], y[1], y[2], y[3]);
               *reinterpret_cast<float4*>(a.part_o + pair_part(slot, prow, c0 + k + 4, HD)) = make_float4(y[4], y[5], y[6], y[7]);
