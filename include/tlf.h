@@ -549,8 +549,14 @@ int tlf_kv4_read(const tlf_chunk* c, const tlf_kv4_read_args* a, void* stream);
  * tlf_attn_chunk, but a query at entry E sees the entries e <= E of its row with e > E - window or e < n_first (window 0: all).
  * Entries are counted, not positions: a cache that tokens left entries out of has a window of so many entries. Pages whose
  * entries no query of the call sees are not looked up: their places in the page table may hold anything.
- * The cache is in the dtype, or in 4 bits (kv_format), which is read as the values that it stands for, unrounded in the scores;
- * float32 softmax statistics and sums as in tlf_attn_chunk. */
+ * The cache is in the dtype, or in 4 bits (kv_format), which is read as the values that it stands for; float32 softmax statistics
+ * and sums as in tlf_attn_chunk. In a bfloat16 call over a cache in 4 bits:
+ * - what the keys of a page have below 2^-18 of the page's largest (visible, of the head) may be rounded off; else the scores are
+ *   those of the values, but for float32 sums;
+ * - values of any magnitude up to 2^126 are taken, beside each other too as long as those of a row are within 2^100; of values past
+ *   2^100, what weighs less than 2^-26 may be left out; groups of query heads that are over 16 and not a power of two, and float32
+ *   calls, add values up as they are, so that their sum over the visible entries has to be float32's.
+ * The scale times a query is to be float32's as well. */
 typedef struct tlf_attn_window_args {
   const void* q;        /* as in tlf_attn_chunk_args */
   int64_t q_stride;
@@ -581,7 +587,9 @@ int tlf_attn_window(const tlf_chunk* c, const tlf_attn_window_args* a, void* scr
  * New pages are the free ones, lowest first, in the order of (b, s). Where none is left (or the parent's page with the entries
  * to copy is not there) the slot gets -1, err bit 16 (or 2) is set, and lens_out[b] is cut to the entries before the slot if the
  * row had any there. refs_out = refs less the old rows' entries, plus the new rows': what no new row goes on from is freed.
- * To free rows, leave them out of parents; to grow rows, parents[b] = b; to admit a row, -1.
+ * To free rows, leave them out of parents; to grow rows, parents[b] = b; to admit a row, -1. reserve is one number for all rows:
+ * a prompt that is admitted beside rows that grow by a token is a call of its own. The plan's time grows with it (64 rows: 10 us
+ * up to 200 tokens, 90 at 8192, 280 at 32768).
  * Copies go into free pages alone: the old rows' entries stay as they are until somebody writes to the pages. table_out may not
  * overlap page_table; lens_out and refs_out may be the inputs' own buffers. */
 typedef struct tlf_fork_args {

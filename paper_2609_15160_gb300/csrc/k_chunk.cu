@@ -867,7 +867,7 @@ __global__ void __launch_bounds__(288, MmaShape<HD, MT>::PER_SM) k_chunk_mma(Chu
 // TFLOP/s, 0.76 of the measured bf16 rate; 371 to 386 in a long loop, where the clock falls), 284 us with 16 heads x 64 (838), 195 us
 // for 8192 causal tokens (1405).
 //
-// Under a window (MODE) the same on a band: 4 x 2048 tokens, window 1024, 16 / 8 heads x 128: 88 us (740 TFLOP/s): an
+// Under a window (MODE) the same on a band: 4 x 2048 tokens, window 1024, 16 / 8 heads x 128: 89 us (730 TFLOP/s): an
 // item has 20 blocks, so that its ends, which the loop does not hide, weigh more than in a whole cache.
 constexpr int PAIR_THREADS = 384;
 
@@ -2116,7 +2116,9 @@ static WindowPath window_path(const ChunkDev& c, int dtype, const tlf_attn_windo
     // tcgen05 where tiles of 16 rows, each with the cache again, take longer. 32 rows over up to 8192 entries, 16 / 8 heads x 128, of
     // 8 / 12 / 16 / 32 tokens: 146 / 147 / 145 / 146 us, in tiles of 16 rows 85 / 145 / 148 / 282; 16 heads x 64, of 16 / 32 / 48 / 64
     // tokens: 207 / 208 / 208 / 210, in tiles 78 / 140 / 204 / 267; under a window of 1024, 4 rows of 40 / 64 tokens: 22.1 / 22.5 and
-    // 21.3 / 23.8
+    // 21.3 / 23.8. The tiles of 128 rows hold whole groups of a power of two heads alone: other groups of up to 16 are in tiles of 16
+    // rows at any length (4 x 2048 tokens over up to 10240 entries, 24 / 8 and 28 / 4 heads x 128: 5.8 ms, 16 / 8 heads 0.45), larger
+    // ones on the CUDA cores (64 single tokens over up to 4096 entries, 24 / 1 heads x 128: 395 us, 32 / 1 heads 39).
     p.four = true;
     p.rt = PAIR_ROWS;
     p.ctas = num_sms;
